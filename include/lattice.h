@@ -47,7 +47,7 @@
 extern "C" {
 #endif
 
-#define LATTICE_ABI_VERSION 10
+#define LATTICE_ABI_VERSION 11
 #define LATTICE_MAX_LAYERS 8
 
 typedef enum {
@@ -419,6 +419,161 @@ lattice_status lattice_linear_fp8_fwd(const uint8_t* qA, int64_t lda, const floa
                                       const float* bias, int32_t M, int32_t N, int32_t K,
                                       int32_t relu, int32_t fast_accum, void* Y,
                                       lattice_dtype y_dtype, int64_t ldy, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Event sequences (Sections 3.3.1, 3.3.2, 3.3.4)                           */
+/* ------------------------------------------------------------------------ */
+
+/* The sequence feature processor's attention event models: rotary positions
+ * and attention over a user's events, queries and keys normalised per head
+ * (QK-norm, Section 3.3.4).  A batch is jagged, as the categorical one is:
+ * the events of S users packed in rows, sequence s in rows offsets[s] ..
+ * offsets[s+1]-1 of every tensor.  Rows behind the last sequence (padding of
+ * a fixed-size batch) are never read and stay as they were in every output.
+ *
+ * Tensors of event heads are [rows, heads, head_dim] with the heads of a row
+ * contiguous and a row stride in elements, so slices of one projection's
+ * output (q, k and v side by side) need no copy.  Row strides are multiples
+ * of 8 elements up to 2^22 and pointers 16-byte aligned (else INVALID_ARG).  head_dim is
+ * a multiple of 8, at most 128; query head h reads key/value head
+ * h / (heads / kv_heads). */
+typedef struct {
+  int64_t rows;            /* rows of every tensor, < 2^30 */
+  int32_t num_seqs;        /* S >= 0 */
+  const int32_t* offsets;  /* device [S+1], offsets[0] = 0, non-decreasing, offsets[S] <= rows */
+  const int32_t* span;     /* device [rows, 2], 8-byte aligned: written by lattice_seq_plan, read by
+                              every other call */
+  int64_t max_len;         /* no sequence is longer; 0: unknown (rows is used).  With a bound that a
+                              sequence exceeds, lattice_seq_attn_bwd drops gradients of its sinks. */
+} lattice_seqs;
+
+/* Span of every row: the first row of its sequence and the row behind its
+ * last one ({2^31 - 1, 0} for rows behind the last sequence).  Depends on the
+ * offsets alone: one call per batch serves every layer and direction.  span
+ * is seqs->span's memory.  Offsets that break the rules above give undefined
+ * results but no access outside the rows.  Errors: INVALID_ARG, HIP. */
+lattice_status lattice_seq_plan(const lattice_seqs* seqs, int32_t* span, void* stream);
+
+/* Per-head RMSNorm of queries and keys and the rotary position rotation in
+ * one pass: for a head vector x of a row at position p,
+ *   z = gain * x / sqrt(mean(x^2) + eps),
+ *   (z_u, z_v) -> (z_u cos a - z_v sin a, z_u sin a + z_v cos a),
+ *   a = p theta^(-2 m / rotary_dim), m = 0 .. rotary_dim / 2 - 1,
+ * with (u, v) = (m, m + rotary_dim / 2), or (2m, 2m + 1) when interleaved;
+ * dimensions >= rotary_dim are not rotated.  Angles are reduced in 64 bits,
+ * so positions may be any int32 (event times, not only indexes).  Arithmetic
+ * is fp32, rounded once to the storage type. */
+typedef struct {
+  lattice_dtype dtype;
+  int32_t heads, kv_heads, head_dim;  /* heads, kv_heads 1 .. 1024 */
+  int32_t rotary_dim;       /* multiple of 8, 0 .. head_dim */
+  int32_t interleaved;      /* 1: neighbouring dimensions are a pair; 0: the two halves */
+  double theta;             /* > 0 */
+  float eps;                /* >= 0 */
+  const float* gain_q;      /* device [head_dim] fp32, or NULL: ones */
+  const float* gain_k;
+  const int32_t* positions; /* device [rows], or NULL: a row's index in its sequence */
+} lattice_qk_rope_desc;
+
+/* seqs->span may be NULL when desc->positions is given: every row is then
+ * taken.  q_out / k_out may be q / k (same strides).  Errors: INVALID_ARG,
+ * UNSUPPORTED (head_dim, rotary_dim), HIP. */
+lattice_status lattice_qk_rope_fwd(const lattice_qk_rope_desc* desc, const lattice_seqs* seqs,
+                                   const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                                   void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride,
+                                   void* stream);
+
+/* Gradient of lattice_qk_rope_fwd: q and k are its inputs, d_q_out and d_k_out
+ * the gradients of its outputs; writes dq and dk (storage dtype; may be
+ * d_q_out and d_k_out, same strides) and, where not NULL, dgain_q and dgain_k
+ * [head_dim] (fp32, overwritten, summed over rows and heads in a fixed
+ * order).  Errors: as lattice_qk_rope_fwd, WORKSPACE. */
+size_t lattice_qk_rope_bwd_workspace(const lattice_qk_rope_desc* desc, int64_t rows);
+lattice_status lattice_qk_rope_bwd(const lattice_qk_rope_desc* desc, const lattice_seqs* seqs,
+                                   const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                                   const void* d_q_out, int64_t d_q_out_stride, const void* d_k_out,
+                                   int64_t d_k_out_stride, void* dq, int64_t dq_stride, void* dk,
+                                   int64_t dk_stride, float* dgain_q, float* dgain_k, void* ws,
+                                   size_t ws_bytes, void* stream);
+
+/* Windowed attention over the events of each sequence.  Row i sees row j of
+ * its own sequence when j <= i and either i - j < window or j is one of the
+ * sequence's first `sinks` rows, and key_mask[j] != 0 (events hidden from
+ * every reader; their k and v are never used).
+ *   out_i = sum_j P_ij v_j,  P_ij = exp(scale <q_i, k_j> - lse_i).
+ * A row that sees nothing gets out = 0 and lse = -inf, and passes no
+ * gradient.  A non-finite value reaches only rows that see it. */
+#define LATTICE_SEQ_MAX_SINKS 64
+typedef struct {
+  lattice_dtype dtype;
+  int32_t heads, kv_heads, head_dim;  /* heads a multiple of kv_heads, 1 .. 1024 */
+  int32_t window;           /* >= 1 (the longest sequence's length or more: every earlier row) */
+  int32_t sinks;            /* 0 .. LATTICE_SEQ_MAX_SINKS */
+  float scale;              /* of the scores, > 0 and finite (usually 1 / sqrt(head_dim)) */
+  const uint8_t* key_mask;  /* device [rows] or NULL: every row is seen */
+} lattice_seq_attn_desc;
+
+/* lse: device [heads, rows] fp32 (natural logarithm), or NULL when no backward
+ * follows.  Probabilities enter the second product in the storage type,
+ * relative to a running maximum; sums and statistics are fp32.  Errors:
+ * INVALID_ARG, UNSUPPORTED (head_dim), HIP. */
+lattice_status lattice_seq_attn_fwd(const lattice_seq_attn_desc* desc, const lattice_seqs* seqs,
+                                    const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                                    const void* v, int64_t v_stride, void* out, int64_t out_stride,
+                                    float* lse, void* stream);
+
+/* Gradients of lattice_seq_attn_fwd from its inputs, out and lse: dq [rows,
+ * heads, head_dim], dk and dv [rows, kv_heads, head_dim] (storage dtype,
+ * overwritten; a shared head's gradient is summed over its query heads in a
+ * fixed order).  Errors: as lattice_seq_attn_fwd, WORKSPACE. */
+size_t lattice_seq_attn_bwd_workspace(const lattice_seq_attn_desc* desc, const lattice_seqs* seqs);
+lattice_status lattice_seq_attn_bwd(const lattice_seq_attn_desc* desc, const lattice_seqs* seqs,
+                                    const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                                    const void* v, int64_t v_stride, const void* out, int64_t out_stride,
+                                    const float* lse, const void* d_out, int64_t d_out_stride,
+                                    void* dq, int64_t dq_stride, void* dk, int64_t dk_stride,
+                                    void* dv, int64_t dv_stride, void* ws, size_t ws_bytes, void* stream);
+
+/* Serving keeps each user's rotated keys and values in a ring of sinks +
+ * window slots: position p in slot p when p < sinks, else in slot sinks +
+ * (p - sinks) % window.  Once position p is written, the rows that the query at
+ * p sees are exactly slots 0 .. min(p + 1, sinks + window) - 1, so a user's
+ * memory and the work of an event are bounded however long the history. */
+typedef struct {
+  void* k;                  /* device [num_caches, kv_heads, sinks + window, head_dim], storage dtype */
+  void* v;
+  int32_t num_caches;
+} lattice_seq_cache;
+
+/* Lays processed histories into their caches: row t of sequence s, at position
+ * first[s] + (its index in the sequence), goes to cache cache_index[s] unless
+ * a later row of the call takes its slot.  k is as lattice_qk_rope_fwd gives it.
+ * Other slots stay as they were.  cache_index: device [S] or NULL (s); a
+ * sequence whose index is outside 0 .. num_caches - 1 is skipped; indexes
+ * must differ.  first: device [S] (>= 0) or NULL (0).  desc: dtype, kv_heads,
+ * head_dim, window and sinks are read.  Errors: INVALID_ARG, UNSUPPORTED, HIP. */
+lattice_status lattice_seq_cache_fill(const lattice_seq_attn_desc* desc, const lattice_seqs* seqs,
+                                      const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                                      const int32_t* first, const int32_t* cache_index,
+                                      const lattice_seq_cache* cache, void* stream);
+
+/* One event for each of `batch` users, in one call: q and k are normalised and
+ * rotated (rope, which may be NULL: taken as they are), k and v written to the
+ * slot of position lens[b], and out_b is the attention of the query over
+ * the cache's visible slots: what lattice_qk_rope_fwd and lattice_seq_attn_fwd
+ * give for the last row of the whole history.  lens: device [batch], events that
+ * the user already has (int32 positions in the sequence; the caller advances
+ * them); rope->positions, if given, is [batch].  cache_index as above
+ * ([batch]); a user with an index out of range or lens < 0 is skipped: nothing
+ * of it is read or written.  key_mask must be NULL (hidden events are not
+ * appended); dtype, heads, kv_heads and head_dim of rope and desc agree.
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP. */
+size_t lattice_seq_step_workspace(const lattice_seq_attn_desc* desc, int32_t batch);
+lattice_status lattice_seq_step(const lattice_seq_attn_desc* desc, const lattice_qk_rope_desc* rope,
+                                int32_t batch, const void* q, int64_t q_stride, const void* k,
+                                int64_t k_stride, const void* v, int64_t v_stride, const int32_t* lens,
+                                const int32_t* cache_index, const lattice_seq_cache* cache, void* out,
+                                int64_t out_stride, void* ws, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Whole training step                                                      */

@@ -6,7 +6,7 @@ loading fails loudly otherwise.
 """
 import ctypes
 import os
-from ctypes import POINTER, Structure, c_char_p, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import POINTER, Structure, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "liblattice.so")
@@ -113,6 +113,31 @@ class lattice_step_layout(Structure):
                                           "fp8_bytes")])
 
 
+SEQ_MAX_SINKS = 64
+
+
+class lattice_seqs(Structure):
+    _fields_ = [("rows", c_int64), ("num_seqs", c_int32), ("offsets", c_void_p), ("span", c_void_p),
+                ("max_len", c_int64)]
+
+
+class lattice_qk_rope_desc(Structure):
+    _fields_ = [("dtype", c_int), ("heads", c_int32), ("kv_heads", c_int32), ("head_dim", c_int32),
+                ("rotary_dim", c_int32), ("interleaved", c_int32), ("theta", c_double), ("eps", c_float),
+                ("gain_q", c_void_p), ("gain_k", c_void_p), ("positions", c_void_p)]
+
+
+class lattice_seq_attn_desc(Structure):
+    _fields_ = [("dtype", c_int), ("heads", c_int32), ("kv_heads", c_int32), ("head_dim", c_int32),
+                ("window", c_int32), ("sinks", c_int32), ("scale", c_float), ("key_mask", c_void_p)]
+
+
+class lattice_seq_cache(Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("num_caches", c_int32)]
+
+
+_ROWS = [c_void_p, c_int64]          # a tensor of event rows and its row stride
+
 # (name, restype, argtypes)
 _SIGS = [
     ("lattice_embbag_fwd", c_int, [POINTER(lattice_tables), POINTER(lattice_jagged), c_int, c_void_p,
@@ -151,6 +176,21 @@ _SIGS = [
                              POINTER(lattice_step_opts), c_void_p, c_size_t, c_void_p]),
     ("lattice_forward", c_int, [POINTER(lattice_model_desc), POINTER(lattice_batch_desc),
                                 POINTER(lattice_step_opts), c_void_p, c_size_t, c_void_p]),
+    ("lattice_seq_plan", c_int, [POINTER(lattice_seqs), c_void_p, c_void_p]),
+    ("lattice_qk_rope_fwd", c_int, [POINTER(lattice_qk_rope_desc), POINTER(lattice_seqs)] + 4 * _ROWS + [c_void_p]),
+    ("lattice_qk_rope_bwd_workspace", c_size_t, [POINTER(lattice_qk_rope_desc), c_int64]),
+    ("lattice_qk_rope_bwd", c_int, [POINTER(lattice_qk_rope_desc), POINTER(lattice_seqs)] + 6 * _ROWS
+     + [c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    ("lattice_seq_attn_fwd", c_int, [POINTER(lattice_seq_attn_desc), POINTER(lattice_seqs)] + 4 * _ROWS
+     + [c_void_p, c_void_p]),
+    ("lattice_seq_attn_bwd_workspace", c_size_t, [POINTER(lattice_seq_attn_desc), POINTER(lattice_seqs)]),
+    ("lattice_seq_attn_bwd", c_int, [POINTER(lattice_seq_attn_desc), POINTER(lattice_seqs)] + 4 * _ROWS
+     + [c_void_p] + 4 * _ROWS + [c_void_p, c_size_t, c_void_p]),
+    ("lattice_seq_cache_fill", c_int, [POINTER(lattice_seq_attn_desc), POINTER(lattice_seqs)] + 2 * _ROWS
+     + [c_void_p, c_void_p, POINTER(lattice_seq_cache), c_void_p]),
+    ("lattice_seq_step_workspace", c_size_t, [POINTER(lattice_seq_attn_desc), c_int32]),
+    ("lattice_seq_step", c_int, [POINTER(lattice_seq_attn_desc), POINTER(lattice_qk_rope_desc), c_int32]
+     + 3 * _ROWS + [c_void_p, c_void_p, POINTER(lattice_seq_cache)] + _ROWS + [c_void_p, c_size_t, c_void_p]),
     ("lattice_status_string", c_char_p, [c_int]),
     ("lattice_last_error", c_char_p, []),
     ("lattice_abi_version", c_int, []),

@@ -8,7 +8,7 @@
 #include <cstring>
 #include <mutex>
 
-#include "../../include/lattice.h"
+#include "abi_check.h"
 #include "common.h"
 #include "kernels.h"
 #include "swishrn.h"
@@ -25,31 +25,12 @@ void set_error(const char* fmt, ...) {
 
 using namespace lat;
 
-#define FAIL(code, ...)         \
-  do {                          \
-    ::lat::set_error(__VA_ARGS__); \
-    return code;                \
-  } while (0)
-#define REQUIRE(cond, ...) \
-  do {                     \
-    if (!(cond)) FAIL(LATTICE_ERR_INVALID_ARG, __VA_ARGS__); \
-  } while (0)
-#define HIPRET(expr)                                  \
-  do {                                                \
-    hipError_t e__ = (expr);                          \
-    if (e__ != hipSuccess) return LATTICE_ERR_HIP;    \
-  } while (0)
 // inside helpers that return a hipError_t
 #define HIP_TRY(expr)                                 \
   do {                                                \
     hipError_t e__ = (expr);                          \
     if (e__ != hipSuccess) return e__;                \
   } while (0)
-
-static inline DType dt_of(lattice_dtype d) { return d == LATTICE_BF16 ? DT_BF16 : DT_F32; }
-static inline size_t esize(lattice_dtype d) { return d == LATTICE_BF16 ? 2 : 4; }
-static inline hipStream_t strm(void* s) { return reinterpret_cast<hipStream_t>(s); }
-static inline size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 static lattice_status check_dim(int dim, lattice_dtype dt) {
   if (dim <= 0 || dim > 256) FAIL(LATTICE_ERR_UNSUPPORTED, "dim %d outside 1..256", dim);

@@ -1,0 +1,903 @@
+// Windowed attention over packed event sequences, forward and backward.
+//
+//   V(i) = { j : start(i) <= j <= i, i - j < W or j < start(i) + N, shown(j) }
+//   s_ij = scale <q_i, k_j>, P_ij = exp(s_ij - lse_i), o_i = sum_j P_ij v_j
+//   delta_i = <do_i, o_i>, dS_ij = P_ij (<do_i, v_j> - delta_i)
+//   dq_i = scale sum_j dS_ij k_j, dk_j = scale sum_i dS_ij q_i, dv_j = sum_i P_ij do_i
+//
+// Tiles lie on the packed row axis, whatever the sequence boundaries: many
+// short sequences fill a tile as one long sequence does, and no list of tiles
+// is needed.  The keys of a tile of rows are one contiguous range (from the
+// first row's window to the last row) and the sinks of the first row's
+// sequence, where they lie before it: later sequences start inside the range.
+// Which of them a row sees is a comparison with the row's own bounds, made
+// only in key tiles that some row of the wave sees in part.
+//
+// Forward and dQ: a block is 4 waves of 32 rows of one head each; query heads
+// that share a key head share the block (as many of 4, 2 or 1 as divide the
+// group) so that a block's rows span a short range.  The product is taken
+// transposed, S^T = K Q^T: a lane holds one row's scores, its maximum and sum
+// need one exchange between lane halves, and the probabilities are the
+// next product's operand (O^T = V^T P^T) where they are.  K and V tiles go from
+// memory straight to LDS one tile ahead.
+//
+// dK and dV: a block is 4 waves of 32 keys, over the rows that see them and
+// the group's heads, S = Q K^T with the keys in registers.  Rows that see a
+// sink after its window has passed are spread over blocks of their own
+// (seq_sink_kernel: a long sequence's sinks would otherwise be one block's work),
+// whose partial sums the main kernel adds in a fixed order.  No atomics.
+//
+// A masked pair has P = 0, but 0 * (a non-finite value) is not 0: where a
+// wave's result is not finite, the block repeats its sweep with the non-finite
+// values of the second operand replaced by zeros, and those pairs that see
+// them poisoned, and takes the elements that this finds finite.
+#include "kernels.h"
+#include "seq_tile.h"
+
+namespace lat {
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+struct AttnK {                     // kernel arguments
+  int rows, dim, heads, kv_heads, group, window, sinks;
+  int hb, row_tiles;               // heads of a block (forward, dQ), its row tiles
+  int ns;                          // splits of a sequence's late rows (sinks' gradients)
+  int num_seqs;
+  float scale;
+  const int32_t* offsets;
+  const SeqSpan* span;
+  const uint8_t* mask;
+  SeqTensor q, k, v, o, go, gq, gk, gv;
+  float* lse;                      // [heads, rows]
+  float* lse2;                     // workspace [heads, rows]: lse log2 e, +inf where nothing is seen
+  float* delta;                    // workspace [heads, rows]
+  float* part;                     // workspace [seqs][kv_heads][ns][2][sinks][dim]
+};
+
+// What a lane's row sees, and its wave's and block's key ranges.
+struct RowView {
+  int i, start, lo;                // lo: first row of its window
+  unsigned wlim, nsk;              // sees j - lo <= wlim, or j - start < nsk
+  bool valid;
+};
+
+__device__ inline RowView row_view(const AttnK& A, int i) {
+  RowView v;
+  v.i = i;
+  SeqSpan sp{SEQ_NO_ROW, 0};
+  if (i < A.rows) sp = A.span[i];
+  v.valid = sp.start != SEQ_NO_ROW;
+  v.start = sp.start;
+  v.lo = v.valid ? max(sp.start, i - A.window + 1) : SEQ_NO_ROW;
+  v.wlim = v.valid ? (unsigned)(i - v.lo) : 0u;
+  v.nsk = v.valid ? (unsigned)min(A.sinks, i - sp.start + 1) : 0u;
+  return v;
+}
+
+// Key tiles of a block of rows: `ts` tiles of the sinks before its range
+// [lo, hi], then the range's.
+struct KeyTiles {
+  int s0, nsink, ts, lo, hi, n;
+  template <int BK>
+  __device__ inline void init(const AttnK& A, int r0, int nrows) {
+    const int lane = threadIdx.x & 63;
+    int last = -1;
+    for (int b = 0; b < nrows; b += 64) {
+      const int i = r0 + b + lane;
+      const bool ok = b + lane < nrows && i < A.rows && A.span[i].start != SEQ_NO_ROW;
+      const uint64_t m = __ballot(ok);
+      if (m) last = r0 + b + 63 - __builtin_clzll(m);
+    }
+    hi = last;
+    n = ts = nsink = s0 = lo = 0;
+    if (last < 0) return;
+    // the first row that belongs to a sequence is r0 unless the offsets are malformed
+    int st = A.span[r0].start;
+    if (st == SEQ_NO_ROW) st = r0;
+    s0 = __builtin_amdgcn_readfirstlane(st);
+    lo = max(s0, r0 - A.window + 1);
+    nsink = min(A.sinks, lo - s0);
+    ts = (nsink + BK - 1) / BK;
+    n = ts + (hi - lo + BK) / BK;
+  }
+  template <int BK>
+  __device__ inline void at(int t, int& kt, int& nk) const {
+    kt = t < ts ? s0 + t * BK : lo + (t - ts) * BK;
+    nk = min(BK, (t < ts ? s0 + nsink : hi + 1) - kt);
+  }
+};
+
+// Bits of the tile's keys that exist and are shown
+template <int BK>
+__device__ inline uint64_t key_bits(const uint8_t* mask, int kt, int nk) {
+  const uint64_t all = nk >= 64 ? ~0ull : (1ull << nk) - 1;
+  if (!mask) return all;
+  const int lane = threadIdx.x & 63;
+  return __ballot(mask[kt + min(lane, nk - 1)] != 0) & all;
+}
+
+// Block -> (row tile, key head, heads of the group).
+struct BlockAt { int tile, kv, h0; };
+__device__ inline BlockAt block_at(const AttnK& A) {
+  const int hg = A.group / A.hb, per = A.kv_heads * hg;
+  const int b = blockIdx.x;
+  BlockAt r;
+  const int x = b % per;
+  r.tile = b / per;
+  r.kv = x / hg;
+  r.h0 = r.kv * A.group + (x % hg) * A.hb;
+  return r;
+}
+
+// ---------------------------------------------------------------------------
+template <typename T, int DP> struct AttnCfg {
+  static constexpr int BK = sizeof(T) == 4 && DP == 128 ? 32 : 64;   // keys of a tile
+  static constexpr size_t LDS = (size_t)2 * 2 * BK * DP * sizeof(T); // two stages of K and V
+};
+
+// Scores of 32 keys (row0 in the tile) against the wave's 32 rows
+template <typename T, int DP>
+__device__ inline f32x16 scores(const char* S, uint32_t rl, int row0, const Frag<T>* q) {
+  using TL = Tile<T, DP>;
+  f32x16 c;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) c[r] = 0.f;
+#pragma unroll
+  for (int s = 0; s < TL::KS; ++s) mma32(TL::rowfrag(S, rl, row0, s), q[s], c);
+  return c;
+}
+
+__device__ inline int frag_off(int r) { return 8 * (r >> 2) + (r & 3); }   // + 4 (lane / 32)
+
+// whether the lane's row sees key j0 + frag_off(r), j0 with the lane half's 4 in it
+__device__ inline bool sees(const RowView& v, int j, uint32_t bits, int r) {
+  const bool in = (unsigned)(j - v.lo) <= v.wlim || (unsigned)(j - v.start) < v.nsk;
+  return in && ((bits >> frag_off(r)) & 1);
+}
+
+// whether it may see one of the keys kt .. kt + nk - 1
+__device__ inline bool reaches(const RowView& v, int kt, int nk) {
+  return v.valid && ((kt <= v.i && v.lo < kt + nk) || (v.start < kt + nk && v.start + (int)v.nsk > kt));
+}
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256, 2) void seq_fwd_kernel(AttnK A) {
+  using TL = Tile<T, DP>;
+  constexpr int BK = AttnCfg<T, DP>::BK, TB = BK * TL::RB;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int half = lane >> 5;
+  const BlockAt B = block_at(A);
+  const int brows = 128 / A.hb, r0 = B.tile * brows;
+  const int head = B.h0 + w % A.hb;
+  KeyTiles kt_;
+  kt_.init<BK>(A, r0, brows);
+  if (kt_.n == 0) return;
+  const RowView V = row_view(A, r0 + (w / A.hb) * 32 + (lane & 31));
+  const T* kb = (const T*)A.k.p + (int64_t)B.kv * A.dim;
+  const T* vb = (const T*)A.v.p + (int64_t)B.kv * A.dim;
+
+  TileLoad<T, DP, BK, 4> lk, lv;
+  lk.init(w, A.dim, A.k.ld);
+  lv.init(w, A.dim, A.v.ld);
+  auto issue = [&](int t, uint64_t& bits) {
+    int kt, nk;
+    kt_.at<BK>(t, kt, nk);
+    bits = key_bits<BK>(A.mask, kt, nk);
+    char* S = smem + (t & 1) * 2 * TB;
+    lk.issue(S, w, kb + (int64_t)kt * A.k.ld, nk, bits);
+    lv.issue(S + TB, w, vb + (int64_t)kt * A.v.ld, nk, bits);
+  };
+
+  Frag<T> q[TL::KS];
+  {
+    const T* qp = (const T*)A.q.p + (int64_t)(V.valid ? V.i : r0) * A.q.ld + head * A.dim;
+#pragma unroll
+    for (int s = 0; s < TL::KS; ++s) {
+      const int d = 16 * s + 8 * half;
+      load_frag(qp + (d < A.dim ? d : 0), V.valid && d < A.dim, q[s]);
+    }
+  }
+  const uint32_t rl = TL::row_lane(), cl = TL::col_lane();
+  const float c = A.scale * LOG2E;
+  f32x16 o[TL::DB];
+  float m, l;
+
+  // One pass over the block's keys.  strict: see the head of this file.
+  auto sweep = [&](bool strict) {
+#pragma unroll
+    for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[db][r] = 0.f;
+    m = -INFINITY;
+    l = 0.f;
+    uint64_t bits, next = 0;
+    issue(0, bits);
+#pragma unroll 1
+    for (int t = 0; t < kt_.n; ++t) {
+      // this wave's loads of tile t have landed and its reads of tile t - 1
+      // returned; past the barrier everybody's have
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (t + 1 < kt_.n) issue(t + 1, next);
+      int kt, nk;
+      kt_.at<BK>(t, kt, nk);
+      if (wave_any(reaches(V, kt, nk))) {
+        const char *SK = smem + (t & 1) * 2 * TB, *SV = SK + TB;
+        const bool full = nk == BK && bits == (BK == 64 ? ~0ull : 0xffffffffull) &&
+                          wave_all(!V.valid || (V.lo <= kt && V.i >= kt + BK - 1));
+        f32x16 s[BK / 32];
+#pragma unroll
+        for (int b = 0; b < BK / 32; ++b) s[b] = scores<T, DP>(SK, rl, 32 * b, q);
+        if (!full || strict) {
+#pragma unroll
+          for (int b = 0; b < BK / 32; ++b) {
+            const uint32_t kb32 = (uint32_t)(bits >> (32 * b)) >> (4 * half);
+            const int j0 = kt + 32 * b + 4 * half;
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              s[b][r] = sees(V, j0 + frag_off(r), kb32, r) ? s[b][r] : -INFINITY;
+          }
+        }
+        float tm = s[0][0];
+#pragma unroll
+        for (int b = 0; b < BK / 32; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) tm = fmaxf(tm, s[b][r]);
+        tm = max32(tm);
+        // The maximum moves only when it grew by more than 8 octaves: until
+        // then probabilities are up to 2^8, exact in both types' ranges, and
+        // the accumulators need no rescaling.
+        const bool up = (tm - m) * c > 8.f;                   // also from -inf
+        if (wave_any(up)) {
+          const float mn = up ? tm : m;
+          const float f = up ? __builtin_amdgcn_exp2f((m - mn) * c) : 1.f;
+          l *= f;
+#pragma unroll
+          for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[db][r] *= f;
+          m = mn;
+        }
+        const float mc = m == -INFINITY ? 0.f : m * c;
+#pragma unroll
+        for (int b = 0; b < BK / 32; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            s[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], c, -mc));
+            l += s[b][r];
+          }
+        if (strict) {
+#pragma unroll
+          for (int b = 0; b < BK / 32; ++b) {
+            const f32x16 bad = TL::count_nonfinite(SV, rl, 32 * b);
+            const uint32_t kb32 = (uint32_t)(bits >> (32 * b)) >> (4 * half);
+            const int j0 = kt + 32 * b + 4 * half;
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if (bad[r] > 0.f && sees(V, j0 + frag_off(r), kb32, r)) s[b][r] = NAN;
+          }
+        }
+#pragma unroll
+        for (int b = 0; b < BK / 32; ++b)
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            Frag<T> p;
+            pack_frag(s[b], hf, p);
+#pragma unroll
+            for (int db = 0; db < TL::DB; ++db) {
+              Frag<T> f = TL::colfrag(SV, cl, 32 * b + 16 * hf, db);
+              if (strict) f = finite_part(f);
+              mma32(f, p, o[db]);
+            }
+          }
+      }
+      bits = next;
+    }
+    l = add32(l);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[db][r] *= inv;
+  };
+
+  T* op = (T*)A.o.p + (int64_t)V.i * A.o.ld + head * A.dim;
+  auto store = [&](bool patch) {
+    if (!V.valid) return;
+#pragma unroll
+    for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int d = 32 * db + 8 * g + 4 * half;
+        if (d >= A.dim) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (patch && nonfinite(o[db][4 * g + e])) o[db][4 * g + e] = ld(op + d + e);
+        if constexpr (sizeof(T) == 2)
+          *reinterpret_cast<u32x2*>(op + d) = u32x2{pack_bf2(o[db][4 * g], o[db][4 * g + 1]),
+                                                    pack_bf2(o[db][4 * g + 2], o[db][4 * g + 3])};
+        else
+          *reinterpret_cast<f32x4*>(op + d) = f32x4{o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]};
+      }
+  };
+  sweep(false);
+  if (A.lse && V.valid && half == 0)
+    A.lse[(int64_t)head * A.rows + V.i] = l == 0.f ? -INFINITY : (m * c + __builtin_amdgcn_logf(l)) * LN2;
+  float z = 0.f;
+#pragma unroll
+  for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) z = __builtin_fmaf(o[db][r], 0.f, z);
+  store(false);
+  if (__syncthreads_or(V.valid && z != 0.f)) {
+    sweep(true);
+    store(true);
+  }
+}
+
+// ---------------------------------------------------------------------------
+template <typename T, int DP>
+__global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_dq_kernel(AttnK A) {
+  using TL = Tile<T, DP>;
+  constexpr int BK = AttnCfg<T, DP>::BK, TB = BK * TL::RB;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int half = lane >> 5;
+  const BlockAt B = block_at(A);
+  const int brows = 128 / A.hb, r0 = B.tile * brows;
+  const int head = B.h0 + w % A.hb;
+  KeyTiles kt_;
+  kt_.init<BK>(A, r0, brows);
+  if (kt_.n == 0) return;
+  const RowView V = row_view(A, r0 + (w / A.hb) * 32 + (lane & 31));
+  const T* kb = (const T*)A.k.p + (int64_t)B.kv * A.dim;
+  const T* vb = (const T*)A.v.p + (int64_t)B.kv * A.dim;
+
+  TileLoad<T, DP, BK, 4> lk, lv;
+  lk.init(w, A.dim, A.k.ld);
+  lv.init(w, A.dim, A.v.ld);
+  auto issue = [&](int t, uint64_t& bits) {
+    int kt, nk;
+    kt_.at<BK>(t, kt, nk);
+    bits = key_bits<BK>(A.mask, kt, nk);
+    char* S = smem + (t & 1) * 2 * TB;
+    lk.issue(S, w, kb + (int64_t)kt * A.k.ld, nk, bits);
+    lv.issue(S + TB, w, vb + (int64_t)kt * A.v.ld, nk, bits);
+  };
+
+  Frag<T> q[TL::KS], go[TL::KS];
+  float delta = 0.f;
+  {
+    const int64_t i = V.valid ? V.i : r0;
+    const T* qp = (const T*)A.q.p + i * A.q.ld + head * A.dim;
+    const T* gp = (const T*)A.go.p + i * A.go.ld + head * A.dim;
+    const T* op = (const T*)A.o.p + i * A.o.ld + head * A.dim;
+#pragma unroll
+    for (int s = 0; s < TL::KS; ++s) {
+      const int d = 16 * s + 8 * half;
+      const bool ok = V.valid && d < A.dim;
+      const int dd = d < A.dim ? d : 0;
+      Frag<T> ov;
+      load_frag(qp + dd, ok, q[s]);
+      load_frag(gp + dd, ok, go[s]);
+      load_frag(op + dd, ok, ov);
+      delta += dot_frag(go[s], ov);
+    }
+  }
+  delta = add32(delta);
+  float lse2 = INFINITY;
+  if (V.valid) {
+    const float x = A.lse[(int64_t)head * A.rows + V.i];
+    lse2 = x == -INFINITY ? INFINITY : x * LOG2E;
+    if (x == -INFINITY) delta = 0.f;
+  }
+  if (V.valid && half == 0) {
+    A.lse2[(int64_t)head * A.rows + V.i] = lse2;
+    A.delta[(int64_t)head * A.rows + V.i] = delta;
+  }
+  const uint32_t rl = TL::row_lane(), cl = TL::col_lane();
+  const float c = A.scale * LOG2E;
+  f32x16 dq[TL::DB];
+
+  auto sweep = [&](bool strict) {
+#pragma unroll
+    for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dq[db][r] = 0.f;
+    uint64_t bits, next = 0;
+    issue(0, bits);
+#pragma unroll 1
+    for (int t = 0; t < kt_.n; ++t) {
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (t + 1 < kt_.n) issue(t + 1, next);
+      int kt, nk;
+      kt_.at<BK>(t, kt, nk);
+      if (wave_any(reaches(V, kt, nk))) {
+        const char *SK = smem + (t & 1) * 2 * TB, *SV = SK + TB;
+        const bool full = nk == BK && bits == (BK == 64 ? ~0ull : 0xffffffffull) &&
+                          wave_all(!V.valid || (V.lo <= kt && V.i >= kt + BK - 1));
+#pragma unroll
+        for (int b = 0; b < BK / 32; ++b) {
+          f32x16 p = scores<T, DP>(SK, rl, 32 * b, q);
+          const f32x16 dp = scores<T, DP>(SV, rl, 32 * b, go);
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c, -lse2)) * (dp[r] - delta);
+          if (!full || strict) {
+            const uint32_t kb32 = (uint32_t)(bits >> (32 * b)) >> (4 * half);
+            const int j0 = kt + 32 * b + 4 * half;
+            f32x16 bad;
+            if (strict) bad = TL::count_nonfinite(SK, rl, 32 * b);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const bool see = sees(V, j0 + frag_off(r), kb32, r);
+              p[r] = see ? p[r] : 0.f;
+              if (strict && see && bad[r] > 0.f) p[r] = NAN;
+            }
+          }
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            Frag<T> f;
+            pack_frag(p, hf, f);
+#pragma unroll
+            for (int db = 0; db < TL::DB; ++db) {
+              Frag<T> kf = TL::colfrag(SK, cl, 32 * b + 16 * hf, db);
+              if (strict) kf = finite_part(kf);
+              mma32(kf, f, dq[db]);
+            }
+          }
+        }
+      }
+      bits = next;
+    }
+#pragma unroll
+    for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dq[db][r] *= A.scale;
+  };
+
+  T* op = (T*)A.gq.p + (int64_t)V.i * A.gq.ld + head * A.dim;
+  auto store = [&](bool patch) {
+    if (!V.valid) return;
+#pragma unroll
+    for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int d = 32 * db + 8 * g + 4 * half;
+        if (d >= A.dim) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (patch && nonfinite(dq[db][4 * g + e])) dq[db][4 * g + e] = ld(op + d + e);
+        if constexpr (sizeof(T) == 2)
+          *reinterpret_cast<u32x2*>(op + d) = u32x2{pack_bf2(dq[db][4 * g], dq[db][4 * g + 1]),
+                                                    pack_bf2(dq[db][4 * g + 2], dq[db][4 * g + 3])};
+        else
+          *reinterpret_cast<f32x4*>(op + d) =
+              f32x4{dq[db][4 * g], dq[db][4 * g + 1], dq[db][4 * g + 2], dq[db][4 * g + 3]};
+      }
+  };
+  sweep(false);
+  float z = 0.f;
+#pragma unroll
+  for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) z = __builtin_fmaf(dq[db][r], 0.f, z);
+  store(false);
+  if (__syncthreads_or(V.valid && z != 0.f)) {
+    sweep(true);
+    store(true);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Late rows of a sequence: those behind the window of every sink.
+__device__ inline int late_row(const AttnK& A, int start) {
+  return (int)min((int64_t)start + A.sinks + A.window - 1, (int64_t)SEQ_NO_ROW);
+}
+// rows of a split of n late rows
+__device__ inline int late_chunk(const AttnK& A, int n) { return ((n + A.ns - 1) / A.ns + 31) & ~31; }
+
+// One 32-row subtile against the wave's 32 keys: accumulates dv and dk.
+// SQ / SG: the rows' q and d_out in LDS (row0 the subtile's first row there),
+// L / E: their lse2 and delta.  d: the subtile's first row minus the lane's
+// key; rows with d + offset < lim see it.
+template <typename T, int DP>
+__device__ inline void dkv_subtile(const char* SQ, const char* SG, const float* L, const float* E, int row0,
+                                   uint32_t rl, uint32_t cl, const Frag<T>* kf, const Frag<T>* vf, float c, int d,
+                                   unsigned lim, bool full, bool strict, f32x16* dk, f32x16* dv) {
+  using TL = Tile<T, DP>;
+  const int half = (threadIdx.x & 63) >> 5;
+  f32x16 p = scores<T, DP>(SQ, rl, row0, kf);
+  f32x16 ds = scores<T, DP>(SG, rl, row0, vf);
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const f32x4 l4 = *reinterpret_cast<const f32x4*>(L + row0 + 8 * g + 4 * half);
+    const f32x4 e4 = *reinterpret_cast<const f32x4*>(E + row0 + 8 * g + 4 * half);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int r = 4 * g + e;
+      p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c, -l4[e]));
+      ds[r] = p[r] * (ds[r] - e4[e]);
+    }
+  }
+  if (!full || strict) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const bool see = (unsigned)(d + frag_off(r) + 4 * half) < lim;
+      p[r] = see ? p[r] : 0.f;
+      ds[r] = see ? ds[r] : 0.f;
+    }
+    if (strict) {
+      const f32x16 bq = TL::count_nonfinite(SQ, rl, row0), bg = TL::count_nonfinite(SG, rl, row0);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const bool see = (unsigned)(d + frag_off(r) + 4 * half) < lim;
+        if (see && bg[r] > 0.f) p[r] = NAN;
+        if (see && bq[r] > 0.f) ds[r] = NAN;
+      }
+    }
+  }
+#pragma unroll
+  for (int hf = 0; hf < 2; ++hf) {
+    Frag<T> pf, df;
+    pack_frag(p, hf, pf);
+    pack_frag(ds, hf, df);
+#pragma unroll
+    for (int db = 0; db < TL::DB; ++db) {
+      Frag<T> g = TL::colfrag(SG, cl, row0 + 16 * hf, db), q = TL::colfrag(SQ, cl, row0 + 16 * hf, db);
+      if (strict) {
+        g = finite_part(g);
+        q = finite_part(q);
+      }
+      mma32(g, pf, dv[db]);
+      mma32(q, df, dk[db]);
+    }
+  }
+}
+
+template <typename T, int DP>
+__device__ inline void load_keys(const AttnK& A, int j, bool ok, int kv, Frag<T>* kf, Frag<T>* vf) {
+  const int half = (threadIdx.x & 63) >> 5;
+  const T* kp = (const T*)A.k.p + (int64_t)j * A.k.ld + kv * A.dim;
+  const T* vp = (const T*)A.v.p + (int64_t)j * A.v.ld + kv * A.dim;
+#pragma unroll
+  for (int s = 0; s < Tile<T, DP>::KS; ++s) {
+    const int d = 16 * s + 8 * half, dd = d < A.dim ? d : 0;
+    load_frag(kp + dd, ok && d < A.dim, kf[s]);
+    load_frag(vp + dd, ok && d < A.dim, vf[s]);
+  }
+}
+
+typedef __attribute__((address_space(3))) float seq_lds_f32;
+// `rows` values (zeros past them) straight to LDS, one per lane
+__device__ inline void issue_stats(char* S, const float* p, int rows) {
+  const int lane = threadIdx.x & 63;
+  const __amdgpu_buffer_rsrc_t rs =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(p), (short)0, (int)0x7fffffff, BUF_RSRC_WORD3);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (seq_lds_void*)S, 4, (int)(lane < rows ? lane * 4u : 0x80000000u), 0,
+                                           0, 0);
+}
+
+template <typename T, int DP> struct DkvCfg {
+  static constexpr int BQ = sizeof(T) == 4 && DP == 128 ? 32 : 64;    // rows of a tile
+  static constexpr int STAGE = 2 * BQ * DP * (int)sizeof(T) + 512;    // q, d_out, lse2, delta (64 floats each)
+  static constexpr size_t LDS = (size_t)2 * STAGE;
+  static constexpr int SINK_STAGE = 2 * 32 * DP * (int)sizeof(T) + 512;   // a wave's 32 rows
+  static constexpr size_t SINK_LDS = (size_t)4 * SINK_STAGE;
+};
+
+template <typename T, int DP>
+__global__ __launch_bounds__(256, 1) void seq_dkv_kernel(AttnK A) {
+  using TL = Tile<T, DP>;
+  using Cfg = DkvCfg<T, DP>;
+  constexpr int BQ = Cfg::BQ, TB = BQ * TL::RB;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int half = lane >> 5;
+  const int kv = blockIdx.x % A.kv_heads, k0 = (blockIdx.x / A.kv_heads) * 128;
+  // a lane's key, and how many rows from it on see it here
+  const int j = k0 + 32 * w + (lane & 31);
+  SeqSpan sp{SEQ_NO_ROW, 0};
+  if (j < A.rows) sp = A.span[j];
+  const bool valid = sp.start != SEQ_NO_ROW;
+  const bool shown = valid && (!A.mask || A.mask[j]);
+  const bool sink = valid && j - sp.start < A.sinks;
+  int end = 0;
+  if (valid) end = sink ? min(sp.end, late_row(A, sp.start)) : (int)min((int64_t)sp.end, (int64_t)j + A.window);
+  const unsigned lim = shown ? (unsigned)(end - j) : 0u;
+  // rows [k0, bend) of the block, [.., wend) of the wave
+  int wend = end;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) wend = max(wend, __shfl_xor(wend, o, 64));
+  wend = __builtin_amdgcn_readfirstlane(wend);
+  __shared__ int ends[4];
+  if (lane == 0) ends[w] = wend;
+  __syncthreads();
+  const int bend = max(max(ends[0], ends[1]), max(ends[2], ends[3]));
+  if (bend <= k0) return;                      // no row of a sequence here
+  const int per_head = (bend - k0 + BQ - 1) / BQ, n = per_head * A.group;
+
+  TileLoad<T, DP, BQ, 4> lq, lg;
+  lq.init(w, A.dim, A.q.ld);
+  lg.init(w, A.dim, A.go.ld);
+  auto issue = [&](int t) {
+    const int g = t / per_head, i0 = k0 + (t - g * per_head) * BQ, h = kv * A.group + g;
+    const int nr = min(BQ, bend - i0);
+    char* S = smem + (t & 1) * Cfg::STAGE;
+    lq.issue(S, w, (const T*)A.q.p + (int64_t)i0 * A.q.ld + h * A.dim, nr, ~0ull);
+    lg.issue(S + TB, w, (const T*)A.go.p + (int64_t)i0 * A.go.ld + h * A.dim, nr, ~0ull);
+    const int64_t at = (int64_t)h * A.rows + i0;
+    if (w == 0) issue_stats(S + 2 * TB, A.lse2 + at, nr);
+    if (w == 1) issue_stats(S + 2 * TB + 256, A.delta + at, nr);
+  };
+  Frag<T> kf[TL::KS], vf[TL::KS];
+  load_keys<T, DP>(A, valid ? j : k0, shown, kv, kf, vf);
+  const uint32_t rl = TL::row_lane(), cl = TL::col_lane();
+  const float c = A.scale * LOG2E;
+  f32x16 dk[TL::DB], dv[TL::DB];
+
+  auto sweep = [&](bool strict) {
+#pragma unroll
+    for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dk[db][r] = dv[db][r] = 0.f;
+    issue(0);
+#pragma unroll 1
+    for (int t = 0; t < n; ++t) {
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (t + 1 < n) issue(t + 1);
+      const int i0 = k0 + (t % per_head) * BQ;
+      const char* S = smem + (t & 1) * Cfg::STAGE;
+#pragma unroll
+      for (int b = 0; b < BQ / 32; ++b) {
+        const int ib = i0 + 32 * b;
+        // rows ib .. ib+31 reach the wave's keys k0 + 32 w .. + 31
+        if (ib + 31 < k0 + 32 * w || ib >= wend) continue;
+        const bool full = wave_all((unsigned)(ib - j) < lim && (unsigned)(ib + 31 - j) < lim);
+        dkv_subtile<T, DP>(S, S + TB, (const float*)(S + 2 * TB), (const float*)(S + 2 * TB + 256), 32 * b, rl, cl, kf,
+                           vf, c, ib - j, lim, full, strict, dk, dv);
+      }
+    }
+    // sinks: the late rows' partial sums, in split order (a hidden sink has no
+    // gradient; its sums are zeros times what may not be finite)
+    if (A.ns > 0 && sink && shown && sp.end > late_row(A, sp.start)) {
+      const int late = sp.end - late_row(A, sp.start), used = (late + late_chunk(A, late) - 1) / late_chunk(A, late);
+      int lo = 0, hi = A.num_seqs;               // the sequence: the last that starts at sp.start or before
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (A.offsets[mid] <= sp.start) lo = mid; else hi = mid;
+      }
+      for (int u = 0; u < used; ++u) {
+        const float* P = A.part + ((((int64_t)lo * A.kv_heads + kv) * A.ns + u) * 2 * A.sinks + (j - sp.start)) * A.dim;
+#pragma unroll
+        for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int dd = 32 * db + 8 * g + 4 * half;
+            if (dd >= A.dim) continue;
+            const f32x4 a = *reinterpret_cast<const f32x4*>(P + dd);
+            const f32x4 b = *reinterpret_cast<const f32x4*>(P + (int64_t)A.sinks * A.dim + dd);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              dk[db][4 * g + e] += a[e];
+              dv[db][4 * g + e] += b[e];
+            }
+          }
+      }
+    }
+#pragma unroll
+    for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dk[db][r] *= A.scale;
+  };
+  auto store1 = [&](T* op, f32x16* x, bool patch) {
+#pragma unroll
+    for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int d = 32 * db + 8 * g + 4 * half;
+        if (d >= A.dim) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (patch && nonfinite(x[db][4 * g + e])) x[db][4 * g + e] = ld(op + d + e);
+        if constexpr (sizeof(T) == 2)
+          *reinterpret_cast<u32x2*>(op + d) =
+              u32x2{pack_bf2(x[db][4 * g], x[db][4 * g + 1]), pack_bf2(x[db][4 * g + 2], x[db][4 * g + 3])};
+        else
+          *reinterpret_cast<f32x4*>(op + d) = f32x4{x[db][4 * g], x[db][4 * g + 1], x[db][4 * g + 2], x[db][4 * g + 3]};
+      }
+  };
+  auto store = [&](bool patch) {
+    if (!valid) return;
+    store1((T*)A.gk.p + (int64_t)j * A.gk.ld + kv * A.dim, dk, patch);
+    store1((T*)A.gv.p + (int64_t)j * A.gv.ld + kv * A.dim, dv, patch);
+  };
+  sweep(false);
+  float z = 0.f;
+#pragma unroll
+  for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) z = __builtin_fmaf(dk[db][r], 0.f, __builtin_fmaf(dv[db][r], 0.f, z));
+  store(false);
+  if (__syncthreads_or(valid && z != 0.f)) {
+    sweep(true);
+    store(true);
+  }
+}
+
+// Partial dk and dv of a sequence's sinks over a split of its late rows, every
+// one of which sees every sink.  A block: 32 sinks of one key head; its waves
+// take every fourth subtile of rows, their sums are added in wave order.
+template <typename T, int DP>
+__global__ __launch_bounds__(256, 1) void seq_sink_kernel(AttnK A, int parts) {
+  using TL = Tile<T, DP>;
+  using Cfg = DkvCfg<T, DP>;
+  constexpr int TB = 32 * TL::RB;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int half = lane >> 5;
+  int b = blockIdx.x;
+  const int part = b % parts; b /= parts;
+  const int u = b % A.ns; b /= A.ns;
+  const int kv = b % A.kv_heads, seq = b / A.kv_heads;
+  const int s0 = A.offsets[seq], e0 = min(A.offsets[seq + 1], A.rows);
+  if (s0 < 0 || s0 >= e0) return;
+  const int x0 = late_row(A, s0), late = e0 - x0;
+  if (late <= 0) return;
+  const int chunk = late_chunk(A, late), a0 = x0 + u * chunk, a1 = (int)min((int64_t)e0, (int64_t)a0 + chunk);
+  if (u * (int64_t)chunk >= late) return;
+  const int a = part * 32 + (lane & 31), j = s0 + a;   // late rows exist: the sequence has all its sinks
+  const bool shown = a < A.sinks && (!A.mask || A.mask[j]);
+  const int per_head = (a1 - a0 + 31) / 32, n = per_head * A.group;
+
+  TileLoad<T, DP, 32, 1> lq, lg;
+  lq.init(0, A.dim, A.q.ld);
+  lg.init(0, A.dim, A.go.ld);
+  char* S = smem + w * Cfg::SINK_STAGE;
+  Frag<T> kf[TL::KS], vf[TL::KS];
+  load_keys<T, DP>(A, a < A.sinks ? j : s0, shown, kv, kf, vf);
+  const uint32_t rl = TL::row_lane(), cl = TL::col_lane();
+  const float c = A.scale * LOG2E;
+  f32x16 dk[TL::DB], dv[TL::DB];
+#pragma unroll
+  for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dk[db][r] = dv[db][r] = 0.f;
+#pragma unroll 1
+  for (int t = w; t < n; t += 4) {
+    const int g = t / per_head, i0 = a0 + (t - g * per_head) * 32, h = kv * A.group + g, nr = min(32, a1 - i0);
+    const int64_t at = (int64_t)h * A.rows + i0;
+    // the wave's own stage: its reads of the subtile before have returned
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    lq.issue(S, 0, (const T*)A.q.p + (int64_t)i0 * A.q.ld + h * A.dim, nr, ~0ull);
+    lg.issue(S + TB, 0, (const T*)A.go.p + (int64_t)i0 * A.go.ld + h * A.dim, nr, ~0ull);
+    issue_stats(S + 2 * TB, A.lse2 + at, nr);
+    issue_stats(S + 2 * TB + 256, A.delta + at, nr);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    dkv_subtile<T, DP>(S, S + TB, (const float*)(S + 2 * TB), (const float*)(S + 2 * TB + 256), 0, rl, cl, kf, vf, c, 0,
+                       shown ? (unsigned)nr : 0u, nr == 32 && wave_all(shown), false, dk, dv);
+  }
+  // waves' sums, one after the other, in LDS [2][DP][33]
+  float* R = reinterpret_cast<float*>(smem);
+  for (int v = 0; v < 4; ++v) {
+    __syncthreads();
+    if (w != v) continue;
+#pragma unroll
+    for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int d = 32 * db + frag_off(r) + 4 * half, x = d * 33 + (lane & 31);
+        R[x] = dk[db][r] + (v ? R[x] : 0.f);
+        R[DP * 33 + x] = dv[db][r] + (v ? R[DP * 33 + x] : 0.f);
+      }
+  }
+  __syncthreads();
+  float* P = A.part + (((int64_t)seq * A.kv_heads + kv) * A.ns + u) * 2 * A.sinks * A.dim;
+  const int na = min(32, A.sinks - part * 32);
+  for (int x = threadIdx.x; x < 2 * na * A.dim; x += 256) {
+    const int m = x / (na * A.dim), y = x - m * na * A.dim, r = y / A.dim, d = y - r * A.dim;
+    P[((int64_t)m * A.sinks + part * 32 + r) * A.dim + d] = R[m * DP * 33 + d * 33 + r];
+  }
+}
+
+// ---------------------------------------------------------------------------
+static AttnK attn_args(const SeqAttnArgs& a) {
+  AttnK A{};
+  A.rows = (int)a.rows;
+  A.dim = a.dim;
+  A.heads = a.heads;
+  A.kv_heads = a.kv_heads;
+  A.group = a.heads / a.kv_heads;
+  A.window = a.window < a.rows ? a.window : (int)a.rows;
+  A.sinks = a.sinks;
+  A.hb = A.group % 4 == 0 ? 4 : A.group % 2 == 0 ? 2 : 1;
+  A.row_tiles = cdiv(a.rows, 128 / A.hb);
+  A.num_seqs = a.num_seqs;
+  A.scale = a.scale;
+  A.offsets = a.offsets;
+  A.span = a.span;
+  A.mask = a.key_mask;
+  A.q = a.q; A.k = a.k; A.v = a.v; A.o = a.o; A.go = a.go; A.gq = a.gq; A.gk = a.gk; A.gv = a.gv;
+  A.lse = a.lse;
+  return A;
+}
+
+// Splits of a sequence's late rows: about 256 rows each, no more than give
+// every compute unit a few blocks; 0 where no sequence has late rows.
+static int late_splits(const SeqAttnArgs& a) {
+  const int64_t late = a.max_len - ((int64_t)a.sinks + a.window - 1);
+  if (a.sinks == 0 || late <= 0 || a.num_seqs == 0) return 0;
+  int64_t n = cdiv(late, 256);
+  const int64_t most = cdiv(2048, (int64_t)a.num_seqs * a.kv_heads);
+  if (n > most) n = most;
+  return (int)(n > 64 ? 64 : n < 1 ? 1 : n);
+}
+
+static size_t stats_bytes(const SeqAttnArgs& a) {
+  return ((size_t)a.heads * a.rows * sizeof(float) + 255) & ~(size_t)255;
+}
+
+size_t seq_attn_bwd_workspace(const SeqAttnArgs& a) {
+  return 2 * stats_bytes(a) + (size_t)a.num_seqs * a.kv_heads * late_splits(a) * 2 * a.sinks * a.dim * sizeof(float);
+}
+
+template <typename T, int DP>
+static hipError_t fwd_launch(const AttnK& A, hipStream_t s) {
+  static LdsLimit lim;
+  LAT_HIP_CHECK(lds_limit(seq_fwd_kernel<T, DP>, AttnCfg<T, DP>::LDS, lim));
+  seq_fwd_kernel<T, DP><<<A.row_tiles * (A.heads / A.hb), 256, AttnCfg<T, DP>::LDS, s>>>(A);
+  LAT_LAUNCH_CHECK();
+  return hipSuccess;
+}
+
+template <typename T, int DP>
+static hipError_t bwd_launch(const AttnK& A, hipStream_t s) {
+  static LdsLimit l0, l1, l2;
+  LAT_HIP_CHECK(lds_limit(seq_dq_kernel<T, DP>, AttnCfg<T, DP>::LDS, l0));
+  LAT_HIP_CHECK(lds_limit(seq_dkv_kernel<T, DP>, DkvCfg<T, DP>::LDS, l1));
+  LAT_HIP_CHECK(lds_limit(seq_sink_kernel<T, DP>, DkvCfg<T, DP>::SINK_LDS, l2));
+  // dQ also writes the rows' statistics that the other two read
+  seq_dq_kernel<T, DP><<<A.row_tiles * (A.heads / A.hb), 256, AttnCfg<T, DP>::LDS, s>>>(A);
+  LAT_LAUNCH_CHECK();
+  if (A.ns > 0) {
+    const int parts = (A.sinks + 31) / 32;
+    seq_sink_kernel<T, DP><<<A.num_seqs * A.kv_heads * A.ns * parts, 256, DkvCfg<T, DP>::SINK_LDS, s>>>(A, parts);
+    LAT_LAUNCH_CHECK();
+  }
+  seq_dkv_kernel<T, DP><<<cdiv(A.rows, 128) * A.kv_heads, 256, DkvCfg<T, DP>::LDS, s>>>(A);
+  LAT_LAUNCH_CHECK();
+  return hipSuccess;
+}
+
+hipError_t seq_attn_fwd(const SeqAttnArgs& a, hipStream_t s) {
+  if (a.rows == 0 || a.num_seqs == 0) return hipSuccess;
+  const AttnK A = attn_args(a);
+  if (a.dt == DT_BF16)
+    return a.dim <= 32 ? fwd_launch<bf16_t, 32>(A, s) : a.dim <= 64 ? fwd_launch<bf16_t, 64>(A, s)
+                                                                  : fwd_launch<bf16_t, 128>(A, s);
+  return a.dim <= 32 ? fwd_launch<float, 32>(A, s) : a.dim <= 64 ? fwd_launch<float, 64>(A, s)
+                                                               : fwd_launch<float, 128>(A, s);
+}
+
+hipError_t seq_attn_bwd(const SeqAttnArgs& a, void* ws, hipStream_t s) {
+  if (a.rows == 0 || a.num_seqs == 0) return hipSuccess;
+  AttnK A = attn_args(a);
+  const size_t stats = stats_bytes(a);
+  A.lse2 = (float*)ws;
+  A.delta = (float*)((char*)ws + stats);
+  A.part = (float*)((char*)ws + 2 * stats);
+  A.ns = late_splits(a);
+  if (a.dt == DT_BF16)
+    return a.dim <= 32 ? bwd_launch<bf16_t, 32>(A, s) : a.dim <= 64 ? bwd_launch<bf16_t, 64>(A, s)
+                                                                  : bwd_launch<bf16_t, 128>(A, s);
+  return a.dim <= 32 ? bwd_launch<float, 32>(A, s) : a.dim <= 64 ? bwd_launch<float, 64>(A, s)
+                                                               : bwd_launch<float, 128>(A, s);
+}
+
+}  // namespace lat

@@ -1,0 +1,483 @@
+"""Event-sequence operators on the GPU against the float64 oracle: every row,
+head and gradient element within the bound that follows from the roundings a
+correct evaluation makes (oracle/seqattn.py)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import seqattn as o
+
+DEV = "cuda"
+TT = {"bf16": torch.bfloat16, "f32": torch.float32}
+pytestmark = pytest.mark.gpu
+
+
+def randn(rng, *shape):
+    return torch.from_numpy(rng.standard_normal(shape).astype(np.float32))
+
+
+def f64(t):
+    return t.detach().float().cpu().double().numpy()
+
+
+def offs(lens):
+    return np.concatenate([[0], np.cumsum(lens)]).astype(np.int64)
+
+
+def within(got, want, bound, what):
+    g = f64(got)
+    assert np.isfinite(g).all(), f"{what}: not finite"
+    over = np.abs(g - want) - bound
+    i = np.unravel_index(np.argmax(over), over.shape)
+    assert over[i] <= 1e-30, f"{what} at {i}: {g[i]} against {want[i]}, bound {bound[i]}"
+
+
+# ---------------------------------------------------------------------------
+LENS = {"one": [1], "two": [2], "empty": [0, 5, 0, 0, 3, 0], "edges": [63, 64, 65, 1, 127, 128, 129],
+        "ones": [1] * 70, "short": [20, 3, 31, 8, 1, 60, 17] * 9, "long": [700], "mixed": [300, 1, 0, 129, 400]}
+
+
+def plan(lens, pad=0, max_len=0):
+    from paper_2512_09200_amd import api
+    off = offs(lens)
+    rows = int(off[-1]) + pad
+    return off, rows, api.lattice_seq_plan(torch.from_numpy(off.astype(np.int32)).to(DEV), rows, max_len=max_len,
+                                           padded=pad > 0)
+
+
+@pytest.mark.parametrize("lens", list(LENS))
+@pytest.mark.parametrize("pad", [0, 37])
+def test_plan(lens, pad):
+    off, rows, s = plan(LENS[lens], pad)
+    want = np.full((rows, 2), 0)
+    want[:, 0] = 2 ** 31 - 1
+    for a, e in zip(off[:-1], off[1:]):
+        want[a:e] = a, e
+    assert np.array_equal(s.span.cpu().numpy(), want)
+
+
+# ---------------------------------------------------------------------------
+ROPE = [("bf16", 4, 2, 64, 64, False), ("f32", 2, 1, 32, 32, True), ("bf16", 3, 3, 96, 64, True),
+        ("f32", 5, 1, 40, 24, False), ("bf16", 1, 1, 8, 8, False), ("f32", 2, 2, 128, 0, False),
+        ("bf16", 8, 1, 128, 128, False), ("bf16", 2, 1, 24, 8, True), ("f32", 4, 4, 16, 16, False)]
+
+
+@pytest.mark.parametrize("dt,H,J,D,R,inter", ROPE)
+@pytest.mark.parametrize("far", [False, True])
+def test_qk_rope(dt, H, J, D, R, inter, far):
+    from paper_2512_09200_amd import api
+    rng = np.random.default_rng(D * 100 + H)
+    lens = [37, 1, 90, 0, 5]
+    off, rows, s = plan(lens, pad=3)
+    n = int(off[-1])
+    # q and k side by side in one projection's rows
+    qk = randn(rng, rows, H + J, D).to(TT[dt]).to(DEV)
+    q, k = qk[:, :H], qk[:, H:]
+    gq, gk = (1 + 0.2 * randn(rng, D)).to(DEV), (1 + 0.2 * randn(rng, D)).to(DEV)
+    pos = rng.integers(-2 ** 31, 2 ** 31, rows) if far else o.positions_of(off, rows)
+    kw = dict(gain_q=gq, gain_k=gk, theta=10000.0, rotary=R, interleaved=inter, eps=1e-5,
+              positions=torch.from_numpy(pos.astype(np.int32)).to(DEV) if far else None)
+    buf = torch.full((rows, H + J, D), 7.0, dtype=TT[dt], device=DEV)
+    yq, yk = api.lattice_qk_rope_fwd(s, q, k, q_out=buf[:, :H], k_out=buf[:, H:], **kw)
+    dq_, dk_ = randn(rng, rows, H, D).to(TT[dt]).to(DEV), randn(rng, rows, J, D).to(TT[dt]).to(DEV)
+    gbuf = torch.full((rows, H + J, D), 7.0, dtype=TT[dt], device=DEV)
+    dq, dk, dgq, dgk = api.lattice_qk_rope_bwd(s, q, k, dq_, dk_, dq=gbuf[:, :H], dk=gbuf[:, H:], **kw)
+    u = o.HALF_STEP[dt]
+    for x, g, y, dy, dx, dg, name in ((q, gq, yq, dq_, dq, dgq, "q"), (k, gk, yk, dk_, dk, dgk, "k")):
+        X, G, DY = f64(x)[:n], f64(g), f64(dy)[:n]
+        want, z = o.qk_rope(X, G, pos[:n], R, 10000.0, 1e-5, inter)
+        # norm (D squares summed, square root, division, two products), angle
+        # (reduced to 2^-24 turns or better) and its sine, two products and a sum
+        size = np.abs(z).copy()
+        a, b = o.pair_index(R, inter)
+        both = np.hypot(z[..., a], z[..., b])
+        size[..., a], size[..., b] = both, both
+        within(y[:n], want, u * np.abs(want) + (D + 40) * o.U32 * size, "y" + name)
+        wdx, wdg, terms = o.qk_rope_bwd(X, G, pos[:n], R, 10000.0, 1e-5, inter, DY)
+        r = 1 / np.sqrt((X ** 2).mean(-1, keepdims=True) + 1e-5)
+        h = np.abs(G) * (np.abs(DY).max(-1, keepdims=True) * 1.5)
+        bound = u * np.abs(wdx) + (2 * D + 64) * o.U32 * r * (h + np.abs(X * r) * (h * np.abs(X * r)).mean(-1, keepdims=True))
+        within(dx[:n], wdx, bound, "d" + name)
+        # (terms' size before the rotation mixes pairs: at most sqrt(2) times)
+        big = (np.abs(X * r) * np.abs(DY).max(-1, keepdims=True) * 1.5).sum((0, 1))
+        within(dg, wdg, o.U32 * ((D + 64) * big + 300 * terms), "dgain_" + name)
+    assert (buf[n:] == 7).all() and (gbuf[n:] == 7).all()          # rows behind the last sequence
+
+
+def test_qk_rope_in_place_without_plan_or_gains():
+    from paper_2512_09200_amd import api
+    rng = np.random.default_rng(3)
+    x = randn(rng, 50, 3, 32).to(DEV)
+    pos = torch.arange(50, dtype=torch.int32, device=DEV)
+    ref = api.lattice_qk_rope_fwd(None, x[:, :2], x[:, 2:], positions=pos)
+    dref = api.lattice_qk_rope_bwd(None, x[:, :2], x[:, 2:], *ref, positions=pos)
+    assert dref[2] is None and dref[3] is None
+    want, _ = o.qk_rope(f64(x[:, :2]), 1.0, np.arange(50), 32, 1e4, 1e-6, False)
+    assert np.abs(f64(ref[0]) - want).max() < 1e-5
+    d = [t.clone() for t in ref]
+    api.lattice_qk_rope_bwd(None, x[:, :2], x[:, 2:], *d, positions=pos, dq=d[0], dk=d[1])
+    y = x.clone()
+    api.lattice_qk_rope_fwd(None, y[:, :2], y[:, 2:], positions=pos, q_out=y[:, :2], k_out=y[:, 2:])
+    assert torch.equal(y, torch.cat(ref, 1)) and torch.equal(d[0], dref[0]) and torch.equal(d[1], dref[1])
+
+
+# ---------------------------------------------------------------------------
+def attn_case(dt, H, J, D, lens, W, N, hidden=0.0, pad=0, max_len=0, seed=0, all_hidden=False):
+    from paper_2512_09200_amd import api
+    rng = np.random.default_rng(seed + D + H)
+    off, rows, s = plan(lens, pad, max_len)
+    qkv = randn(rng, rows, H + 2 * J, D).to(TT[dt]).to(DEV)
+    q, k, v = qkv[:, :H], qkv[:, H:H + J], qkv[:, H + J:]
+    do = randn(rng, rows, H, D).to(TT[dt]).to(DEV)
+    shown = rng.random(rows) >= hidden
+    if all_hidden:
+        shown[:] = False
+    mask = torch.from_numpy(shown.astype(np.uint8)).to(DEV) if hidden or all_hidden else None
+    kw = dict(window=W, sinks=N, key_mask=mask)
+    out, lse = api.lattice_seq_attn_fwd(s, q, k, v, **kw)
+    dq, dk, dv = api.lattice_seq_attn_bwd(s, q, k, v, out, lse, do, **kw)
+    return dict(off=off, rows=rows, s=s, q=q, k=k, v=v, do=do, shown=shown, kw=kw, out=out, lse=lse, dq=dq, dk=dk, dv=dv)
+
+
+def check_attn(c, dt, W, N):
+    n, D = int(c["off"][-1]), c["q"].shape[2]
+    a = [f64(c[m])[:n] for m in ("q", "k", "v")]
+    W = min(W, n + 1)
+    f = o.attn(*a, c["off"], W, N, D ** -0.5, c["shown"][:n], dt)
+    within(c["out"][:n], f["o"], f["o_bound"], "out")
+    L = f64(c["lse"])[:, :n]
+    empty = np.isneginf(f["lse"])
+    assert np.array_equal(np.isneginf(L), empty)
+    assert np.abs(np.where(empty, 0, L - np.where(empty, 0, f["lse"]))).max(initial=0) < 1e-4
+    g, b = o.attn_bwd(*a, c["off"], W, N, D ** -0.5, c["shown"][:n], f64(c["do"])[:n], dt)
+    for m in ("dq", "dk", "dv"):
+        within(c[m][:n], g[m], b[m], m)
+
+
+SHAPES = [("bf16", 4, 2, 64), ("bf16", 1, 1, 32), ("f32", 2, 2, 32), ("bf16", 8, 2, 128), ("f32", 3, 1, 128),
+          ("bf16", 6, 2, 96), ("f32", 4, 1, 40), ("bf16", 3, 3, 8), ("f32", 8, 1, 64), ("bf16", 16, 1, 16)]
+
+
+@pytest.mark.parametrize("lens", list(LENS))
+@pytest.mark.parametrize("dt,H,J,D", SHAPES[:5])
+def test_attention_lengths(dt, H, J, D, lens):
+    check_attn(attn_case(dt, H, J, D, LENS[lens], 48, 3, pad=5), dt, 48, 3)
+
+
+@pytest.mark.parametrize("W,N", [(1, 0), (1, 1), (2, 7), (16, 5), (16, 40), (31, 64), (64, 0), (100, 33), (129, 1),
+                                 (300, 4), (701, 4), (2 ** 31 - 1, 0), (2 ** 31 - 1, 64)])
+@pytest.mark.parametrize("dt,H,J,D", [SHAPES[0], SHAPES[4]])
+def test_attention_windows(dt, H, J, D, W, N):
+    check_attn(attn_case(dt, H, J, D, [700, 90, 1], W, N, max_len=700), dt, W, N)
+
+
+@pytest.mark.parametrize("dt,H,J,D", SHAPES)
+def test_attention_shapes_with_hidden_events(dt, H, J, D):
+    check_attn(attn_case(dt, H, J, D, LENS["mixed"], 37, 6, hidden=0.4, pad=3), dt, 37, 6)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_attention_rows_that_see_nothing(dt):
+    c = attn_case(dt, 4, 2, 64, [90, 40], 20, 2, all_hidden=True)
+    for m in ("out", "dq", "dk", "dv"):
+        assert (c[m] == 0).all(), m
+    assert torch.isneginf(c["lse"]).all()
+    check_attn(attn_case(dt, 4, 2, 64, [90, 40], 3, 1, hidden=0.8), dt, 3, 1)
+
+
+def test_sinks_of_very_long_sequences_in_many_splits():
+    # 64 splits of late rows; the oracle's own work bounds the length
+    check_attn(attn_case("bf16", 2, 1, 32, [3, 2600, 10], 8, 35), "bf16", 8, 35)
+
+
+@pytest.mark.parametrize("dt,D", [("bf16", 64), ("f32", 128)])
+def test_rows_behind_the_last_sequence_stay(dt, D):
+    from paper_2512_09200_amd import api
+    c = attn_case(dt, 4, 2, D, [70, 60], 40, 2, pad=130)
+    n = 130
+    qn, kn, vn, don = (c[m].clone() for m in ("q", "k", "v", "do"))
+    for t in (qn, kn, vn, don):
+        t[n:] = float("nan")
+    mk = lambda t: torch.full_like(t, 3.0)  # noqa: E731
+    out, lse = api.lattice_seq_attn_fwd(c["s"], qn, kn, vn, out=mk(c["out"]), **c["kw"])
+    g = api.lattice_seq_attn_bwd(c["s"], qn, kn, vn, out, lse, don, dq=mk(c["dq"]), dk=mk(c["dk"]), dv=mk(c["dv"]),
+                                 **c["kw"])
+    for got, m in zip((out,) + tuple(g), ("out", "dq", "dk", "dv")):
+        assert torch.equal(got[:n], c[m][:n]), m
+        assert (got[n:] == 3).all(), m
+        assert (c[m][n:] == 0).all(), m                # allocated by the call: zeros
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("dt,D", [("bf16", 64), ("f32", 32), ("bf16", 128)])
+def test_nonfinite_values_reach_only_rows_that_see_them(dt, D, bad):
+    from paper_2512_09200_amd import api
+    lens, W, N = [90, 70, 140], 24, 2
+    c = attn_case(dt, 4, 2, D, lens, W, N, hidden=0.2)
+    n = sum(lens)
+    see = np.zeros((n, n), bool)
+    for a, e in zip(c["off"][:-1], c["off"][1:]):
+        see[a:e, a:e] = o.visible(e - a, W, N, c["shown"][a:e])
+    hidden = int(np.flatnonzero(~c["shown"])[3])
+    shown = int(np.flatnonzero(c["shown"][100:])[5]) + 100
+    # (which, row): rows of out / dq that may change, keys of dk / dv that may
+    for which, at in (("k", hidden), ("v", hidden), ("k", shown), ("v", shown), ("q", 33), ("do", 200)):
+        x = {m: c[m].clone() for m in ("q", "k", "v", "do")}
+        x[which][at, :, 3] = bad
+        out, lse = api.lattice_seq_attn_fwd(c["s"], x["q"], x["k"], x["v"], **c["kw"])
+        dq, dk, dv = api.lattice_seq_attn_bwd(c["s"], x["q"], x["k"], x["v"], out, lse, x["do"], **c["kw"])
+        if which in "kv":
+            rows = see[:, at].copy()                   # rows that see it
+            keys = see[rows].any(0)
+            if which == "v":
+                assert not np.isfinite(f64(out)[rows, :, 3]).any(), which
+                rest = np.delete(f64(out), 3, axis=2)
+                assert np.isfinite(rest).all()         # other dimensions of v are as they were
+        else:
+            rows = np.zeros(n, bool)
+            rows[at] = True
+            keys = see[at]
+            if which == "do":
+                assert torch.equal(out, c["out"])
+        for m, touched in (("out", rows), ("dq", rows), ("dk", keys), ("dv", keys)):
+            g = f64({"out": out, "dq": dq, "dk": dk, "dv": dv}[m])
+            w = f64(c[m])
+            assert np.isfinite(g[~touched]).all(), (which, at, m)
+            assert np.allclose(g[~touched], w[~touched], rtol=2e-2, atol=1e-2 if dt == "bf16" else 1e-5), (which, at, m)
+
+
+def test_attention_twice_on_side_streams_and_in_a_graph_gives_the_same_bits():
+    from paper_2512_09200_amd import api
+    c = attn_case("bf16", 8, 2, 64, LENS["mixed"], 60, 4, hidden=0.1)
+    names = ("out", "lse", "dq", "dk", "dv")
+
+    def go():
+        s = api.lattice_seq_plan(c["s"].offsets, c["rows"], max_len=400)
+        out, lse = api.lattice_seq_attn_fwd(s, c["q"], c["k"], c["v"], **c["kw"])
+        return (out, lse) + tuple(api.lattice_seq_attn_bwd(s, c["q"], c["k"], c["v"], out, lse, c["do"], **c["kw"]))
+
+    def same(r):
+        for x, m in zip(r, names):
+            assert torch.equal(x, c[m]), m
+
+    same(go())
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s1):
+        r1 = go()
+    with torch.cuda.stream(s2):
+        r2 = go()
+    torch.cuda.synchronize()
+    same(r1)
+    same(r2)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        rg = go()
+    for _ in range(3):
+        for x in rg:
+            x.zero_()
+        g.replay()
+        same(go())                                     # eager work between the replays
+        torch.cuda.synchronize()
+        same(rg)
+
+
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dt,J,D,W,N", [("bf16", 2, 64, 30, 3), ("f32", 1, 8, 1, 0), ("bf16", 3, 40, 7, 64),
+                                        ("f32", 2, 128, 200, 1), ("bf16", 40, 128, 20, 2)])
+@pytest.mark.parametrize("first", [False, True])
+def test_cache_fill(dt, J, D, W, N, first):
+    from paper_2512_09200_amd import api
+    rng = np.random.default_rng(W + D)
+    lens = [3, 0, 300, 29, 1, 77]
+    off, rows, s = plan(lens, pad=4)
+    k, v = randn(rng, rows, J, D).to(TT[dt]).to(DEV), randn(rng, rows, J, D).to(TT[dt]).to(DEV)
+    kc, vc = (randn(rng, 9, J, W + N, D).to(TT[dt]).to(DEV) for _ in "kv")
+    index = np.array([4, 0, 8, 9, -1, 2])                  # the fourth and fifth are out of range
+    f = np.array([0, 7, 5, 0, 3, 1000]) if first else np.zeros(6, int)
+    want = o.cache_fill(f64(kc), f64(vc), f64(k), f64(v), off, W, N, index, f)
+    i32 = lambda a: torch.from_numpy(a.astype(np.int32)).to(DEV)  # noqa: E731
+    api.lattice_seq_cache_fill(s, k, v, kc, vc, W, N, cache_index=i32(index), first=i32(f) if first else None)
+    assert np.array_equal(f64(kc), want[0]) and np.array_equal(f64(vc), want[1])
+
+
+STEP = [("bf16", 4, 2, 64, 30, 3), ("f32", 2, 1, 32, 5, 0), ("bf16", 8, 1, 128, 700, 4), ("f32", 3, 3, 96, 129, 1),
+        ("bf16", 20, 1, 40, 64, 64), ("f32", 17, 1, 128, 333, 7), ("bf16", 2, 2, 8, 1, 0), ("bf16", 32, 2, 128, 5000, 2)]
+
+
+@pytest.mark.parametrize("dt,H,J,D,W,N", STEP)
+@pytest.mark.parametrize("rope", [True, False])
+def test_step_against_the_definition(dt, H, J, D, W, N, rope):
+    from paper_2512_09200_amd import api
+    rng = np.random.default_rng(H + D + W)
+    cap = W + N
+    lens = np.array([0, 1, N, cap - 1, cap, 3 * cap + 1, -1, min(cap, 200) // 2, 5])
+    B = len(lens)
+    index = rng.permutation(B + 2)[:B]
+    index[8] = B + 2                                       # out of range
+    q, k, v = (randn(rng, B, h, D).to(TT[dt]).to(DEV) for h in (H, J, J))
+    kc, vc = (randn(rng, B + 2, J, cap, D).to(TT[dt]).to(DEV) for _ in "kv")
+    for b in range(B):                                     # slots nothing was written to yet
+        if 0 <= lens[b] < cap and index[b] < B + 2:
+            kc[index[b], :, lens[b]:] = float("nan")
+            vc[index[b], :, lens[b]:] = float("nan")
+    pos = rng.integers(0, 2 ** 30, B)
+    gq, gk = 1 + 0.1 * randn(rng, D), 1 + 0.1 * randn(rng, D)
+    R = D // 16 * 8
+    i32 = lambda a: torch.from_numpy(a.astype(np.int32)).to(DEV)  # noqa: E731
+    kc0, vc0 = f64(kc), f64(vc)
+    out = torch.full((B, H, D), 5.0, dtype=TT[dt], device=DEV)
+    kw = dict(gain_q=gq.to(DEV), gain_k=gk.to(DEV), rotary=R, positions=i32(pos)) if rope else dict(rope=False)
+    api.lattice_seq_step(q, k, v, i32(lens), kc, vc, W, N, cache_index=i32(index), out=out, **kw)
+    Q, K, V = f64(q), f64(k), f64(v)
+    u = o.HALF_STEP[dt]
+    eq = np.zeros(B)
+    if rope:
+        Qr, _ = o.qk_rope(Q, f64(gq), pos, R, 1e4, 1e-6, False)
+        Kr, _ = o.qk_rope(K, f64(gk), pos, R, 1e4, 1e-6, False)
+    else:
+        Qr, Kr = Q, K
+    KC, VC = f64(kc), f64(vc)
+    for b in range(B):
+        at = index[b]
+        if lens[b] < 0 or at >= B + 2:
+            assert (out[b] == 5).all()
+            if at < B + 2:
+                assert np.array_equal(KC[at], kc0[at], equal_nan=True)
+            continue
+        slot, n = o.slot_of(int(lens[b]), W, N), min(lens[b] + 1, cap)
+        kc0[at, :, slot], vc0[at, :, slot] = Kr[b], V[b]
+        e = (u if rope else 0) * np.abs(Kr[b]) + (D + 40) * o.U32 * np.abs(Kr[b]).max() * 1.5
+        assert (np.abs(KC[at, :, slot] - Kr[b]) <= e).all()
+        assert np.array_equal(VC[at, :, slot], V[b])
+        kc0[at, :, slot] = KC[at, :, slot]                 # the attention reads the stored key
+        assert np.array_equal(KC[at], kc0[at], equal_nan=True) and np.array_equal(VC[at], vc0[at], equal_nan=True)
+        for h in range(H):
+            j = h // (H // J)
+            kk, vv = KC[at, j, :n], VC[at, j, :n]
+            s = kk @ Qr[b, h] / np.sqrt(D)
+            size = (np.abs(kk) @ np.abs(Qr[b, h])).max() / np.sqrt(D)
+            p = np.exp(s - s.max())
+            P = p / p.sum()
+            # the rotated query is rounded to the storage type (u per element of
+            # each product), then as the batch's attention
+            es = (u if rope else 0) * size + (2 * D + 48) * o.U32 * size * 1.5 + (n + 16) * o.U32
+            r = u if dt == "bf16" else 0
+            # P's error: exp(es) - 1 up, its normalisation the same
+            bound = (r + 2 * np.expm1(es)) * (P @ np.abs(vv)) + u * np.abs(P @ vv) * (1 + r)
+            within(out[b, h], P @ vv, bound, f"out {b} {h}")
+    _ = eq
+
+
+@pytest.mark.parametrize("dt,H,J,D,W,N", [("bf16", 4, 2, 64, 16, 2), ("f32", 4, 1, 32, 40, 0)])
+def test_histories_trained_and_served_alike(dt, H, J, D, W, N):
+    """Norm and rotation, attention, cache fill, then event by event: the
+    served outputs are the batch's last rows, and the caches those that a
+    fill with the whole history gives."""
+    from paper_2512_09200_amd import api
+    rng = np.random.default_rng(1)
+    lens, more = np.array([5, 0, 33, 90]), 20
+    full = lens + more
+    off = offs(full)
+    q, k, v = (randn(rng, int(off[-1]), h, D).to(TT[dt]).to(DEV) for h in (H, J, J))
+    gq, gk = (1 + 0.1 * randn(rng, D)).to(DEV), (1 + 0.1 * randn(rng, D)).to(DEV)
+    kw = dict(gain_q=gq, gain_k=gk, theta=500.0)
+    i32 = lambda a: torch.from_numpy(np.asarray(a).astype(np.int32)).to(DEV)  # noqa: E731
+    s = api.lattice_seq_plan(i32(off), int(off[-1]))
+    qr, kr = api.lattice_qk_rope_fwd(s, q, k, **kw)
+    ref, lse = api.lattice_seq_attn_fwd(s, qr, kr, v, W, N)
+    # training: the chain's gradient against the oracle's chain
+    do = randn(rng, *q.shape).to(TT[dt]).to(DEV)
+    dqr, dkr, dv = api.lattice_seq_attn_bwd(s, qr, kr, v, ref, lse, do, W, N)
+    dq, dk, dgq, dgk = api.lattice_qk_rope_bwd(s, q, k, dqr, dkr, **kw)
+    pos = o.positions_of(off, int(off[-1]))
+    Q, _ = o.qk_rope(f64(q), f64(gq), pos, D, 500.0, 1e-6, False)
+    K, _ = o.qk_rope(f64(k), f64(gk), pos, D, 500.0, 1e-6, False)
+    shown = np.ones(len(Q), bool)
+    g, _ = o.attn_bwd(Q, K, f64(v), off, W, N, D ** -0.5, shown, f64(do))
+    tol = 3e-2 if dt == "bf16" else 1e-5
+    for x, gain, dy, dx, dg in ((q, gq, g["dq"], dq, dgq), (k, gk, g["dk"], dk, dgk)):
+        wdx, wdg, _ = o.qk_rope_bwd(f64(x), f64(gain), pos, D, 500.0, 1e-6, False, dy)
+        assert np.linalg.norm(f64(dx) - wdx) <= tol * np.linalg.norm(wdx)
+        assert np.linalg.norm(f64(dg) - wdg) <= tol * np.linalg.norm(wdg)
+    assert np.linalg.norm(f64(dv) - g["dv"]) <= tol * np.linalg.norm(g["dv"])
+    # serving
+    idx = i32([2, 0, 3, 1])
+    kc = torch.zeros(4, J, W + N, D, dtype=TT[dt], device=DEV)
+    vc = torch.zeros_like(kc)
+    past = np.concatenate([np.arange(a, a + n) for a, n in zip(off[:-1], lens)])
+    s0 = api.lattice_seq_plan(i32(offs(lens)), int(lens.sum()))
+    api.lattice_seq_cache_fill(s0, kr[past], v[past], kc, vc, W, N, cache_index=idx)
+    have = i32(lens)
+    for t in range(more):
+        rows = off[:-1] + lens + t
+        out = api.lattice_seq_step(q[rows], k[rows], v[rows], have, kc, vc, W, N, cache_index=idx, **kw)
+        # two correct evaluations of one row, each off by P's and its own rounding
+        err = np.linalg.norm(f64(out) - f64(ref[rows]), axis=-1) / np.linalg.norm(f64(ref[rows]), axis=-1)
+        assert err.max() <= (4 * 2.0 ** -8 * np.sqrt(W + N) if dt == "bf16" else 1e-5), t
+        have += 1
+    kc2, vc2 = torch.zeros_like(kc), torch.zeros_like(vc)
+    api.lattice_seq_cache_fill(s, kr, v, kc2, vc2, W, N, cache_index=idx)
+    assert torch.equal(vc, vc2)
+    assert (kc.float() - kc2.float()).abs().max() <= (2 ** -5 if dt == "bf16" else 1e-5)
+
+
+def test_step_in_a_graph_that_advances_by_itself():
+    from paper_2512_09200_amd import api
+    rng = np.random.default_rng(5)
+    B, H, J, D, W, N = 3, 4, 2, 64, 900, 2
+    q, k, v = (randn(rng, B, h, D).to(torch.bfloat16).to(DEV) for h in (H, J, J))
+    kc, vc = (torch.zeros(B, J, W + N, D, dtype=torch.bfloat16, device=DEV) for _ in "kv")
+    lens = torch.zeros(B, dtype=torch.int32, device=DEV)
+    k2, v2, l2 = kc.clone(), vc.clone(), lens.clone()
+
+    def go(kc, vc, lens):
+        out = api.lattice_seq_step(q, k, v, lens, kc, vc, W, N)
+        lens += 1
+        return out
+    go(k2, v2, l2)                                          # the library is loaded, kernels too
+    k2.zero_(), v2.zero_(), l2.zero_()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        rg = go(kc, vc, lens)
+    for t in range(5):
+        q.copy_(randn(rng, B, H, D).to(DEV))
+        k.copy_(randn(rng, B, J, D).to(DEV))
+        g.replay()
+        ref = go(k2, v2, l2)
+        torch.cuda.synchronize()
+        assert torch.equal(rg, ref), t
+    assert torch.equal(kc, k2) and torch.equal(lens, l2)
+
+
+def test_binding_refusals():
+    from paper_2512_09200_amd import api
+    from paper_2512_09200_amd._abi import LatticeError
+    off, rows, s = plan([10, 6])
+    q = torch.zeros(16, 4, 64, device=DEV)
+    k = torch.zeros(16, 2, 64, device=DEV)
+    with pytest.raises(ValueError):
+        api.lattice_seq_attn_fwd(s, q[:15], k[:15], k[:15], 4)
+    with pytest.raises(ValueError):
+        api.lattice_seq_attn_fwd(s, q, k, k.bfloat16(), 4)
+    with pytest.raises(ValueError):
+        api.lattice_seq_attn_fwd(s, q, k, k.cpu(), 4)
+    with pytest.raises(ValueError):
+        api.lattice_qk_rope_fwd(None, q, k)
+    with pytest.raises(LatticeError, match="INVALID_ARG"):
+        api.lattice_seq_attn_fwd(s, q, k, k, 0)
+    with pytest.raises(LatticeError, match="INVALID_ARG"):          # 4-byte aligned
+        x = torch.zeros(16 * 256 + 1, device=DEV)[1:].view(16, 4, 64)
+        api.lattice_seq_attn_fwd(s, x, k, k, 4)
+    with pytest.raises(LatticeError, match="UNSUPPORTED"):
+        api.lattice_seq_attn_fwd(s, torch.zeros(16, 1, 136, device=DEV), torch.zeros(16, 1, 136, device=DEV),
+                                 torch.zeros(16, 1, 136, device=DEV), 4)
+    with pytest.raises(TypeError):
+        api.lattice_seq_attn_fwd(s, q.half(), k.half(), k.half(), 4)
+    # no rows, no sequences
+    none = api.lattice_seq_plan(torch.zeros(1, dtype=torch.int32, device=DEV), 0)
+    out, lse = api.lattice_seq_attn_fwd(none, q[:0], k[:0], k[:0], 4)
+    assert out.shape == (0, 4, 64) and lse.shape == (4, 0)
+    dq, dk, dgq, dgk = api.lattice_qk_rope_bwd(none, q[:0], k[:0], q[:0], k[:0], gain_q=torch.ones(64, device=DEV))
+    assert (dgq == 0).all() and dgk is None
+    api.lattice_seq_attn_bwd(none, q[:0], k[:0], k[:0], out, lse, q[:0], 4)
