@@ -68,11 +68,12 @@ def visible(n, window, sinks, shown):
 
 
 def attn(q, k, v, offsets, window, sinks, scale, shown, storage="f32"):
-    """Returns dict(o, lse, o_bound)."""
+    """Returns dict(o, lse, o_bound, o_wide): o_wide bounds the output before
+    its rounding to the storage type, with 2^-16 for the pair (out, out_lo)."""
     rows, H, D = q.shape
     J = k.shape[1]
     u = HALF_STEP[storage]
-    o, ob = np.zeros(q.shape), np.zeros(q.shape)
+    o, ob, ow = np.zeros(q.shape), np.zeros(q.shape), np.zeros(q.shape)
     lse = np.full((H, rows), -np.inf)
     for a, e in zip(offsets[:-1], offsets[1:]):
         n = e - a
@@ -83,8 +84,10 @@ def attn(q, k, v, offsets, window, sinks, scale, shown, storage="f32"):
             P, L, es = _probabilities(q[a:e, h], kk[:, j], see, scale)
             lse[h, a:e] = L
             o[a:e, h] = P @ vv[:, j]
-            ob[a:e, h] = ((u if storage != "f32" else 0) + 2 * es[:, None] + (n + 4) * U32) * (P @ np.abs(vv[:, j])) + u * np.abs(o[a:e, h])
-    return dict(o=o, lse=lse, o_bound=ob)
+            ow[a:e, h] = ((u if storage != "f32" else 0) + 2 * es[:, None] + (n + 4) * U32) * (P @ np.abs(vv[:, j]))
+            ob[a:e, h] = ow[a:e, h] * (1 + u) + u * np.abs(o[a:e, h])
+            ow[a:e, h] += min(u, 2.0 ** -16) * np.abs(o[a:e, h]) * (1 + u)
+    return dict(o=o, lse=lse, o_bound=ob, o_wide=ow)
 
 
 def _probabilities(q, k, see, scale):
@@ -122,8 +125,8 @@ def attn_bwd(q, k, v, offsets, window, sinks, scale, shown, do, storage="f32"):
             dP = G @ V.T
             delta = (G * f["o"][a:e, h]).sum(1, keepdims=True)
             dS = P * (dP - delta)
-            # errors of dP, of delta (from the stored output) and of P
-            e_delta = (np.abs(G) * f["o_bound"][a:e, h]).sum(1, keepdims=True) + (D + 2) * U32 * (
+            # errors of dP, of delta (from out and out_lo) and of P
+            e_delta = (np.abs(G) * f["o_wide"][a:e, h]).sum(1, keepdims=True) + (D + 2) * U32 * (
                 np.abs(G) * np.abs(f["o"][a:e, h])).sum(1, keepdims=True)
             e_dP = (D + 2) * U32 * (np.abs(G) @ np.abs(V).T)
             e_dS = P * (e_dP + e_delta) + 2 * es[:, None] * np.abs(dS) + r * np.abs(dS) + 4 * U32 * np.abs(P) * (

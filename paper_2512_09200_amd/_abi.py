@@ -182,10 +182,10 @@ _SIGS = [
     ("lattice_qk_rope_bwd", c_int, [POINTER(lattice_qk_rope_desc), POINTER(lattice_seqs)] + 6 * _ROWS
      + [c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
     ("lattice_seq_attn_fwd", c_int, [POINTER(lattice_seq_attn_desc), POINTER(lattice_seqs)] + 4 * _ROWS
-     + [c_void_p, c_void_p]),
+     + [c_void_p, c_void_p, c_void_p]),
     ("lattice_seq_attn_bwd_workspace", c_size_t, [POINTER(lattice_seq_attn_desc), POINTER(lattice_seqs)]),
     ("lattice_seq_attn_bwd", c_int, [POINTER(lattice_seq_attn_desc), POINTER(lattice_seqs)] + 4 * _ROWS
-     + [c_void_p] + 4 * _ROWS + [c_void_p, c_size_t, c_void_p]),
+     + [c_void_p, c_void_p] + 4 * _ROWS + [c_void_p, c_size_t, c_void_p]),
     ("lattice_seq_cache_fill", c_int, [POINTER(lattice_seq_attn_desc), POINTER(lattice_seqs)] + 2 * _ROWS
      + [c_void_p, c_void_p, POINTER(lattice_seq_cache), c_void_p]),
     ("lattice_seq_step_workspace", c_size_t, [POINTER(lattice_seq_attn_desc), c_int32]),

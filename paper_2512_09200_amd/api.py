@@ -698,9 +698,18 @@ def _attn_desc(q, kv_heads, window, sinks, scale, key_mask):
                                    key_mask=_vec(key_mask, torch.uint8, q.shape[0], "key_mask"))
 
 
+class SeqAttnSaved:
+    """What lattice_seq_attn_fwd keeps for lattice_seq_attn_bwd: lse [heads,
+    rows] fp32 and, for bf16, out_lo (what rounding took from out)."""
+    __slots__ = ("lse", "out_lo")
+
+    def __init__(self, lse, out_lo):
+        self.lse, self.out_lo = lse, out_lo
+
+
 def lattice_seq_attn_fwd(seqs, q, k, v, window, sinks=0, scale=None, key_mask=None, lse=True, out=None, stream=None):
-    """Windowed attention over packed event sequences; returns (out, lse), lse
-    [heads, rows] fp32 for the backward (None when lse is False).  scale None:
+    """Windowed attention over packed event sequences; returns (out, saved),
+    saved a SeqAttnSaved for the backward (None when lse is False).  scale None:
     1 / sqrt(head_dim); key_mask: uint8 [rows], 0 hides an event from every
     reader."""
     with _on_device(q):
@@ -710,16 +719,20 @@ def lattice_seq_attn_fwd(seqs, q, k, v, window, sinks=0, scale=None, key_mask=No
         if out.shape != q.shape or v.shape != k.shape:
             raise ValueError("out must have q's shape, v k's")
         _same(q, k, v, out, key_mask, seqs.offsets)
-        L = torch.empty((q.shape[1], rows), dtype=torch.float32, device=q.device) if lse else None
+        saved = None
+        if lse:
+            saved = SeqAttnSaved(torch.empty((q.shape[1], rows), dtype=torch.float32, device=q.device),
+                                 torch.empty(q.shape, dtype=q.dtype, device=q.device) if desc.dtype == A.BF16 else None)
         check(load().lattice_seq_attn_fwd(byref(desc), byref(seqs.desc), *_heads(q, q, rows, "q"),
                                           *_heads(k, q, rows, "k"), *_heads(v, q, rows, "v"),
-                                          *_heads(out, q, rows, "out"), _p(L), _stream(stream)))
-    return out, L
+                                          *_heads(out, q, rows, "out"), _p(saved.lse) if lse else None,
+                                          _p(saved.out_lo) if lse else None, _stream(stream)))
+    return out, saved
 
 
-def lattice_seq_attn_bwd(seqs, q, k, v, out, lse, d_out, window, sinks=0, scale=None, key_mask=None, dq=None,
+def lattice_seq_attn_bwd(seqs, q, k, v, out, saved, d_out, window, sinks=0, scale=None, key_mask=None, dq=None,
                          dk=None, dv=None, stream=None):
-    """Gradients (dq, dk, dv) of lattice_seq_attn_fwd, from its out and lse."""
+    """Gradients (dq, dk, dv) of lattice_seq_attn_fwd, from its out and saved."""
     with _on_device(q):
         rows = seqs.rows
         desc = _attn_desc(q, k.shape[1], window, sinks, scale, key_mask)
@@ -728,13 +741,14 @@ def lattice_seq_attn_bwd(seqs, q, k, v, out, lse, d_out, window, sinks=0, scale=
         dv = _new_heads(v, v.shape[1], seqs) if dv is None else dv
         if not (out.shape == d_out.shape == dq.shape == q.shape and v.shape == dk.shape == dv.shape == k.shape):
             raise ValueError("out, d_out and dq must have q's shape, v, dk and dv k's")
-        _same(q, k, v, out, lse, d_out, dq, dk, dv, key_mask, seqs.offsets)
+        _same(q, k, v, out, saved.lse, saved.out_lo, d_out, dq, dk, dv, key_mask, seqs.offsets)
         lib = load()
         wsb = lib.lattice_seq_attn_bwd_workspace(byref(desc), byref(seqs.desc))
         ws = torch.empty(max(wsb, 1), dtype=torch.uint8, device=q.device)
         check(lib.lattice_seq_attn_bwd(byref(desc), byref(seqs.desc), *_heads(q, q, rows, "q"),
                                        *_heads(k, q, rows, "k"), *_heads(v, q, rows, "v"), *_heads(out, q, rows, "out"),
-                                       _vec(lse, torch.float32, q.shape[1] * rows, "lse"),
+                                       _vec(saved.lse, torch.float32, q.shape[1] * rows, "lse"),
+                                       _vec(saved.out_lo, q.dtype, out.numel(), "out_lo"),
                                        *_heads(d_out, q, rows, "d_out"), *_heads(dq, q, rows, "dq"),
                                        *_heads(dk, q, rows, "dk"), *_heads(dv, q, rows, "dv"), _p(ws), wsb,
                                        _stream(stream)))

@@ -53,6 +53,7 @@ struct SeqAttnArgs {
   float scale = 0.f;
   SeqTensor q, k, v, o;
   float* lse = nullptr;                // [heads, rows]
+  void* out_lo = nullptr;              // [rows, heads, dim], bf16 only
   SeqTensor go, gq, gk, gv;            // backward
 };
 hipError_t seq_attn_fwd(const SeqAttnArgs& a, hipStream_t s);

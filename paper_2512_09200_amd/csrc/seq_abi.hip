@@ -206,7 +206,8 @@ lattice_status lattice_qk_rope_bwd(const lattice_qk_rope_desc* d, const lattice_
 
 lattice_status lattice_seq_attn_fwd(const lattice_seq_attn_desc* d, const lattice_seqs* seqs, const void* q,
                                     int64_t q_stride, const void* k, int64_t k_stride, const void* v,
-                                    int64_t v_stride, void* out, int64_t out_stride, float* lse, void* stream) {
+                                    int64_t v_stride, void* out, int64_t out_stride, float* lse, void* out_lo,
+                                    void* stream) {
   TRY(check_attn(d));
   TRY(check_seqs(seqs));
   if (seqs->rows == 0 || seqs->num_seqs == 0) return LATTICE_OK;
@@ -215,6 +216,7 @@ lattice_status lattice_seq_attn_fwd(const lattice_seq_attn_desc* d, const lattic
   TRY(check_tensor("k", k, k_stride, d->kv_heads, d->head_dim));
   TRY(check_tensor("v", v, v_stride, d->kv_heads, d->head_dim));
   TRY(check_tensor("out", out, out_stride, d->heads, d->head_dim));
+  REQUIRE((uintptr_t)out_lo % 16 == 0, "out_lo is not 16-byte aligned");
   TRY(check_attn_size(d, seqs));
   SeqAttnArgs a = attn_args(d, seqs);
   a.q = tensor(q, q_stride);
@@ -222,6 +224,7 @@ lattice_status lattice_seq_attn_fwd(const lattice_seq_attn_desc* d, const lattic
   a.v = tensor(v, v_stride);
   a.o = tensor(out, out_stride);
   a.lse = lse;
+  a.out_lo = out_lo;
   HIPRET(seq_attn_fwd(a, strm(stream)));
   return LATTICE_OK;
 }
@@ -234,9 +237,9 @@ size_t lattice_seq_attn_bwd_workspace(const lattice_seq_attn_desc* d, const latt
 lattice_status lattice_seq_attn_bwd(const lattice_seq_attn_desc* d, const lattice_seqs* seqs, const void* q,
                                     int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                                     int64_t v_stride, const void* out, int64_t out_stride, const float* lse,
-                                    const void* d_out, int64_t d_out_stride, void* dq, int64_t dq_stride, void* dk,
-                                    int64_t dk_stride, void* dv, int64_t dv_stride, void* ws, size_t ws_bytes,
-                                    void* stream) {
+                                    const void* out_lo, const void* d_out, int64_t d_out_stride, void* dq,
+                                    int64_t dq_stride, void* dk, int64_t dk_stride, void* dv, int64_t dv_stride,
+                                    void* ws, size_t ws_bytes, void* stream) {
   TRY(check_attn(d));
   TRY(check_seqs(seqs));
   if (seqs->rows == 0 || seqs->num_seqs == 0) return LATTICE_OK;
@@ -250,6 +253,7 @@ lattice_status lattice_seq_attn_bwd(const lattice_seq_attn_desc* d, const lattic
   TRY(check_tensor("dq", dq, dq_stride, d->heads, d->head_dim));
   TRY(check_tensor("dk", dk, dk_stride, d->kv_heads, d->head_dim));
   TRY(check_tensor("dv", dv, dv_stride, d->kv_heads, d->head_dim));
+  REQUIRE((uintptr_t)out_lo % 16 == 0, "out_lo is not 16-byte aligned");
   TRY(check_attn_size(d, seqs));
   SeqAttnArgs a = attn_args(d, seqs);
   const size_t need = seq_attn_bwd_workspace(a);
@@ -260,6 +264,7 @@ lattice_status lattice_seq_attn_bwd(const lattice_seq_attn_desc* d, const lattic
   a.v = tensor(v, v_stride);
   a.o = tensor(out, out_stride);
   a.lse = const_cast<float*>(lse);
+  a.out_lo = const_cast<void*>(out_lo);
   a.go = tensor(d_out, d_out_stride);
   a.gq = tensor(dq, dq_stride);
   a.gk = tensor(dk, dk_stride);

@@ -31,6 +31,8 @@
 // wave's result is not finite, the block repeats its sweep with the non-finite
 // values of the second operand replaced by zeros, and those pairs that see
 // them poisoned, and takes the elements that this finds finite.
+#include <type_traits>
+
 #include "kernels.h"
 #include "seq_tile.h"
 
@@ -49,6 +51,7 @@ struct AttnK {                     // kernel arguments
   const uint8_t* mask;
   SeqTensor q, k, v, o, go, gq, gk, gv;
   float* lse;                      // [heads, rows]
+  void* out_lo;                    // [rows, heads, dim] or null: what rounding took from o (bf16)
   float* lse2;                     // workspace [heads, rows]: lse log2 e, +inf where nothing is seen
   float* delta;                    // workspace [heads, rows]
   float* part;                     // workspace [seqs][kv_heads][ns][2][sinks][dim]
@@ -56,8 +59,8 @@ struct AttnK {                     // kernel arguments
 
 // What a lane's row sees, and its wave's and block's key ranges.
 struct RowView {
-  int i, start, lo;                // lo: first row of its window
-  unsigned wlim, nsk;              // sees j - lo <= wlim, or j - start < nsk
+  int i, start, lo;                // sees lo .. i (its window) and the nsk rows from start
+  unsigned nsk;
   bool valid;
 };
 
@@ -69,7 +72,6 @@ __device__ inline RowView row_view(const AttnK& A, int i) {
   v.valid = sp.start != SEQ_NO_ROW;
   v.start = sp.start;
   v.lo = v.valid ? max(sp.start, i - A.window + 1) : SEQ_NO_ROW;
-  v.wlim = v.valid ? (unsigned)(i - v.lo) : 0u;
   v.nsk = v.valid ? (unsigned)min(A.sinks, i - sp.start + 1) : 0u;
   return v;
 }
@@ -149,10 +151,22 @@ __device__ inline f32x16 scores(const char* S, uint32_t rl, int row0, const Frag
 
 __device__ inline int frag_off(int r) { return 8 * (r >> 2) + (r & 3); }   // + 4 (lane / 32)
 
-// whether the lane's row sees key j0 + frag_off(r), j0 with the lane half's 4 in it
-__device__ inline bool sees(const RowView& v, int j, uint32_t bits, int r) {
-  const bool in = (unsigned)(j - v.lo) <= v.wlim || (unsigned)(j - v.start) < v.nsk;
-  return in && ((bits >> frag_off(r)) & 1);
+// Bits lo .. hi of a word (none where they miss 0 .. 31)
+__device__ inline uint32_t bit_range(int lo, int hi) {
+  const uint32_t m = (0xffffffffu << (max(lo, 0) & 31)) & (0xffffffffu >> ((31 - min(hi, 31)) & 31));
+  return lo > 31 || hi < 0 || lo > hi ? 0u : m;
+}
+// Which of the keys jb .. jb+31 the lane's row sees, shifted so that element r
+// of a product is bit frag_off(r): one word per 32 keys, and two operations
+// an element to apply it.
+__device__ inline uint32_t row_bits(const RowView& v, int jb, uint32_t keys) {
+  const uint32_t m = bit_range(v.lo - jb, v.i - jb) | bit_range(v.start - jb, v.start - jb + (int)v.nsk - 1);
+  return v.valid ? (m & keys) >> (4 * ((threadIdx.x & 63) >> 5)) : 0u;
+}
+// all ones where bit frag_off(r) of a word is set, else zero
+__device__ inline uint32_t bit_mask(uint32_t w, int r) { return (uint32_t)__builtin_amdgcn_sbfe((int)w, frag_off(r), 1); }
+__device__ inline float keep_or(float x, uint32_t m, uint32_t other) {
+  return __uint_as_float((__float_as_uint(x) & m) | (other & ~m));
 }
 
 // whether it may see one of the keys kt .. kt + nk - 1
@@ -160,27 +174,74 @@ __device__ inline bool reaches(const RowView& v, int kt, int nk) {
   return v.valid && ((kt <= v.i && v.lo < kt + nk) || (v.start < kt + nk && v.start + (int)v.nsk > kt));
 }
 
+// The row of a lane and its fragments of q (or d_out, ...): loads that depend
+// on nothing but the row's number, made before the tile's bounds are known.
+template <typename T, int DP>
+__device__ __forceinline__ void load_rows(const SeqTensor& t, int i, int head, int dim, Frag<T> (&f)[Tile<T, DP>::KS]) {
+  const int half = (threadIdx.x & 63) >> 5;
+  const T* p = (const T*)t.p + (int64_t)i * t.ld + head * dim;
+#pragma unroll
+  for (int s = 0; s < Tile<T, DP>::KS; ++s) {
+    const int d = 16 * s + 8 * half;
+    load_frag(p + (d < dim ? d : 0), d < dim, f[s]);
+  }
+}
+
+// Elements of O^T-shaped accumulators (lane: one row, element r of block db is
+// column 32 db + frag_off(r) + 4 (lane / 32)) to a row of memory.  PATCH:
+// non-finite elements keep what memory holds.  lo: what the rounding to bf16
+// took, rounded to bf16.
+template <typename T, int DP, bool PATCH>
+__device__ __forceinline__ void store_row(T* op, T* lo, int dim, f32x16 (&x)[Tile<T, DP>::DB]) {
+  const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int db = 0; db < Tile<T, DP>::DB; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int d = 32 * db + 8 * g + 4 * half;
+      if (d >= dim) continue;
+      float y[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        y[e] = x[db][4 * g + e];
+        if (PATCH && nonfinite(y[e])) y[e] = ld(op + d + e);
+      }
+      if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<u32x2*>(op + d) = u32x2{pack_bf2(y[0], y[1]), pack_bf2(y[2], y[3])};
+        if (lo) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] -= bf2f(f2bf(y[e]));
+          *reinterpret_cast<u32x2*>(lo + d) = u32x2{pack_bf2(y[0], y[1]), pack_bf2(y[2], y[3])};
+        }
+      } else {
+        *reinterpret_cast<f32x4*>(op + d) = f32x4{y[0], y[1], y[2], y[3]};
+      }
+    }
+}
+
 template <typename T, int DP>
 __global__ __launch_bounds__(256, 2) void seq_fwd_kernel(AttnK A) {
   using TL = Tile<T, DP>;
-  constexpr int BK = AttnCfg<T, DP>::BK, TB = BK * TL::RB;
+  constexpr int BK = AttnCfg<T, DP>::BK, TB = BK * TL::RB, NB = BK / 32;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5;
   const BlockAt B = block_at(A);
   const int brows = 128 / A.hb, r0 = B.tile * brows;
-  const int head = B.h0 + w % A.hb;
+  const int head = B.h0 + w % A.hb, row = r0 + (w / A.hb) * 32 + (lane & 31);
+  Frag<T> q[TL::KS];
+  load_rows<T, DP>(A.q, min(row, A.rows - 1), head, A.dim, q);
+  const RowView V = row_view(A, row);
   KeyTiles kt_;
   kt_.init<BK>(A, r0, brows);
   if (kt_.n == 0) return;
-  const RowView V = row_view(A, r0 + (w / A.hb) * 32 + (lane & 31));
   const T* kb = (const T*)A.k.p + (int64_t)B.kv * A.dim;
   const T* vb = (const T*)A.v.p + (int64_t)B.kv * A.dim;
 
   TileLoad<T, DP, BK, 4> lk, lv;
   lk.init(w, A.dim, A.k.ld);
   lv.init(w, A.dim, A.v.ld);
-  auto issue = [&](int t, uint64_t& bits) {
+  auto issue = [&](int t, uint64_t& bits) __attribute__((always_inline)) {
     int kt, nk;
     kt_.at<BK>(t, kt, nk);
     bits = key_bits<BK>(A.mask, kt, nk);
@@ -188,23 +249,84 @@ __global__ __launch_bounds__(256, 2) void seq_fwd_kernel(AttnK A) {
     lk.issue(S, w, kb + (int64_t)kt * A.k.ld, nk, bits);
     lv.issue(S + TB, w, vb + (int64_t)kt * A.v.ld, nk, bits);
   };
-
-  Frag<T> q[TL::KS];
-  {
-    const T* qp = (const T*)A.q.p + (int64_t)(V.valid ? V.i : r0) * A.q.ld + head * A.dim;
-#pragma unroll
-    for (int s = 0; s < TL::KS; ++s) {
-      const int d = 16 * s + 8 * half;
-      load_frag(qp + (d < A.dim ? d : 0), V.valid && d < A.dim, q[s]);
-    }
-  }
   const uint32_t rl = TL::row_lane(), cl = TL::col_lane();
   const float c = A.scale * LOG2E;
   f32x16 o[TL::DB];
   float m, l;
 
+  // N subtiles of 32 keys from subtile b0 of the tile at kt
+  auto attend = [&](auto strict_, auto n_, int b0, const char* SK, const char* SV, int kt, uint64_t bits)
+      __attribute__((always_inline)) {
+    constexpr bool strict = decltype(strict_)::value;
+    constexpr int N = decltype(n_)::value;
+    const bool full = (uint32_t)(bits >> (32 * b0)) == 0xffffffffu && (N == 1 || (bits >> 32) == 0xffffffffu) &&
+                      wave_all(!V.valid || (V.lo <= kt + 32 * b0 && V.i >= kt + 32 * (b0 + N) - 1));
+    f32x16 s[N];
+#pragma unroll
+    for (int b = 0; b < N; ++b) s[b] = scores<T, DP>(SK, rl, 32 * (b0 + b), q);
+    uint32_t see[N];
+    if (!full || strict) {
+#pragma unroll
+      for (int b = 0; b < N; ++b) {
+        see[b] = row_bits(V, kt + 32 * (b0 + b), (uint32_t)(bits >> (32 * (b0 + b))));
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[b][r] = keep_or(s[b][r], bit_mask(see[b], r), 0xff800000u);
+      }
+    }
+    float tm = s[0][0];
+#pragma unroll
+    for (int b = 0; b < N; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) tm = fmaxf(tm, s[b][r]);
+    tm = max32(tm);
+    // The maximum moves only when it grew by more than 8 octaves: until
+    // then probabilities are up to 2^8, exact in both types' ranges, and
+    // the accumulators need no rescaling.
+    const bool up = (tm - m) * c > 8.f;                       // also from -inf
+    if (wave_any(up)) {
+      const float mn = up ? tm : m;
+      const float f = up ? __builtin_amdgcn_exp2f((m - mn) * c) : 1.f;
+      l *= f;
+#pragma unroll
+      for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[db][r] *= f;
+      m = mn;
+    }
+    const float mc = m == -INFINITY ? 0.f : m * c;
+#pragma unroll
+    for (int b = 0; b < N; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], c, -mc));
+        l += s[b][r];
+      }
+    if constexpr (strict) {
+#pragma unroll
+      for (int b = 0; b < N; ++b) {
+        const f32x16 bad = TL::count_nonfinite(SV, rl, 32 * (b0 + b));
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (bad[r] > 0.f && bit_mask(see[b], r)) s[b][r] = NAN;
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < N; ++b)
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        Frag<T> p;
+        pack_frag(s[b], hf, p);
+#pragma unroll
+        for (int db = 0; db < TL::DB; ++db) {
+          Frag<T> f = TL::colfrag(SV, cl, 32 * (b0 + b) + 16 * hf, db);
+          if (strict) f = finite_part(f);
+          mma32(f, p, o[db]);
+        }
+      }
+  };
   // One pass over the block's keys.  strict: see the head of this file.
-  auto sweep = [&](bool strict) {
+  auto sweep = [&](auto strict_) __attribute__((always_inline)) {
+    constexpr bool strict = decltype(strict_)::value;
 #pragma unroll
     for (int db = 0; db < TL::DB; ++db)
 #pragma unroll
@@ -223,75 +345,19 @@ __global__ __launch_bounds__(256, 2) void seq_fwd_kernel(AttnK A) {
       if (t + 1 < kt_.n) issue(t + 1, next);
       int kt, nk;
       kt_.at<BK>(t, kt, nk);
-      if (wave_any(reaches(V, kt, nk))) {
-        const char *SK = smem + (t & 1) * 2 * TB, *SV = SK + TB;
-        const bool full = nk == BK && bits == (BK == 64 ? ~0ull : 0xffffffffull) &&
-                          wave_all(!V.valid || (V.lo <= kt && V.i >= kt + BK - 1));
-        f32x16 s[BK / 32];
-#pragma unroll
-        for (int b = 0; b < BK / 32; ++b) s[b] = scores<T, DP>(SK, rl, 32 * b, q);
-        if (!full || strict) {
-#pragma unroll
-          for (int b = 0; b < BK / 32; ++b) {
-            const uint32_t kb32 = (uint32_t)(bits >> (32 * b)) >> (4 * half);
-            const int j0 = kt + 32 * b + 4 * half;
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              s[b][r] = sees(V, j0 + frag_off(r), kb32, r) ? s[b][r] : -INFINITY;
-          }
+      const char *SK = smem + (t & 1) * 2 * TB, *SV = SK + TB;
+      // subtiles of 32 keys that no row of the wave reaches are left out
+      const bool in0 = wave_any(reaches(V, kt, min(nk, 32)));
+      if constexpr (NB == 1) {
+        if (in0) attend(strict_, std::integral_constant<int, 1>{}, 0, SK, SV, kt, bits);
+      } else {
+        const bool in1 = nk > 32 && wave_any(reaches(V, kt + 32, nk - 32));
+        if (!strict && in0 && in1) {
+          attend(strict_, std::integral_constant<int, 2>{}, 0, SK, SV, kt, bits);
+        } else {
+          if (in0) attend(strict_, std::integral_constant<int, 1>{}, 0, SK, SV, kt, bits);
+          if (in1) attend(strict_, std::integral_constant<int, 1>{}, 1, SK, SV, kt, bits);
         }
-        float tm = s[0][0];
-#pragma unroll
-        for (int b = 0; b < BK / 32; ++b)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) tm = fmaxf(tm, s[b][r]);
-        tm = max32(tm);
-        // The maximum moves only when it grew by more than 8 octaves: until
-        // then probabilities are up to 2^8, exact in both types' ranges, and
-        // the accumulators need no rescaling.
-        const bool up = (tm - m) * c > 8.f;                   // also from -inf
-        if (wave_any(up)) {
-          const float mn = up ? tm : m;
-          const float f = up ? __builtin_amdgcn_exp2f((m - mn) * c) : 1.f;
-          l *= f;
-#pragma unroll
-          for (int db = 0; db < TL::DB; ++db)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[db][r] *= f;
-          m = mn;
-        }
-        const float mc = m == -INFINITY ? 0.f : m * c;
-#pragma unroll
-        for (int b = 0; b < BK / 32; ++b)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            s[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], c, -mc));
-            l += s[b][r];
-          }
-        if (strict) {
-#pragma unroll
-          for (int b = 0; b < BK / 32; ++b) {
-            const f32x16 bad = TL::count_nonfinite(SV, rl, 32 * b);
-            const uint32_t kb32 = (uint32_t)(bits >> (32 * b)) >> (4 * half);
-            const int j0 = kt + 32 * b + 4 * half;
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              if (bad[r] > 0.f && sees(V, j0 + frag_off(r), kb32, r)) s[b][r] = NAN;
-          }
-        }
-#pragma unroll
-        for (int b = 0; b < BK / 32; ++b)
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            Frag<T> p;
-            pack_frag(s[b], hf, p);
-#pragma unroll
-            for (int db = 0; db < TL::DB; ++db) {
-              Frag<T> f = TL::colfrag(SV, cl, 32 * b + 16 * hf, db);
-              if (strict) f = finite_part(f);
-              mma32(f, p, o[db]);
-            }
-          }
       }
       bits = next;
     }
@@ -303,26 +369,9 @@ __global__ __launch_bounds__(256, 2) void seq_fwd_kernel(AttnK A) {
       for (int r = 0; r < 16; ++r) o[db][r] *= inv;
   };
 
-  T* op = (T*)A.o.p + (int64_t)V.i * A.o.ld + head * A.dim;
-  auto store = [&](bool patch) {
-    if (!V.valid) return;
-#pragma unroll
-    for (int db = 0; db < TL::DB; ++db)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int d = 32 * db + 8 * g + 4 * half;
-        if (d >= A.dim) continue;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (patch && nonfinite(o[db][4 * g + e])) o[db][4 * g + e] = ld(op + d + e);
-        if constexpr (sizeof(T) == 2)
-          *reinterpret_cast<u32x2*>(op + d) = u32x2{pack_bf2(o[db][4 * g], o[db][4 * g + 1]),
-                                                    pack_bf2(o[db][4 * g + 2], o[db][4 * g + 3])};
-        else
-          *reinterpret_cast<f32x4*>(op + d) = f32x4{o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]};
-      }
-  };
-  sweep(false);
+  T* const op = (T*)A.o.p + (int64_t)V.i * A.o.ld + head * A.dim;
+  T* const lo = A.out_lo ? (T*)A.out_lo + ((int64_t)V.i * A.heads + head) * A.dim : nullptr;
+  sweep(std::false_type{});
   if (A.lse && V.valid && half == 0)
     A.lse[(int64_t)head * A.rows + V.i] = l == 0.f ? -INFINITY : (m * c + __builtin_amdgcn_logf(l)) * LN2;
   float z = 0.f;
@@ -330,10 +379,10 @@ __global__ __launch_bounds__(256, 2) void seq_fwd_kernel(AttnK A) {
   for (int db = 0; db < TL::DB; ++db)
 #pragma unroll
     for (int r = 0; r < 16; ++r) z = __builtin_fmaf(o[db][r], 0.f, z);
-  store(false);
+  if (V.valid) store_row<T, DP, false>(op, lo, A.dim, o);
   if (__syncthreads_or(V.valid && z != 0.f)) {
-    sweep(true);
-    store(true);
+    sweep(std::true_type{});
+    if (V.valid) store_row<T, DP, true>(op, lo, A.dim, o);
   }
 }
 
@@ -347,18 +396,34 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
   const int half = lane >> 5;
   const BlockAt B = block_at(A);
   const int brows = 128 / A.hb, r0 = B.tile * brows;
-  const int head = B.h0 + w % A.hb;
+  const int head = B.h0 + w % A.hb, row = r0 + (w / A.hb) * 32 + (lane & 31);
+  Frag<T> q[TL::KS], go[TL::KS];
+  float delta = 0.f;
+  {
+    const int i = min(row, A.rows - 1);
+    Frag<T> ov[TL::KS];
+    load_rows<T, DP>(A.go, i, head, A.dim, go);
+    load_rows<T, DP>(A.o, i, head, A.dim, ov);
+    load_rows<T, DP>(A.q, i, head, A.dim, q);
+#pragma unroll
+    for (int s = 0; s < TL::KS; ++s) delta += dot_frag(go[s], ov[s]);
+    if (A.out_lo) {
+      load_rows<T, DP>(SeqTensor{A.out_lo, (int64_t)A.heads * A.dim}, i, head, A.dim, ov);
+#pragma unroll
+      for (int s = 0; s < TL::KS; ++s) delta += dot_frag(go[s], ov[s]);
+    }
+  }
+  const RowView V = row_view(A, row);
   KeyTiles kt_;
   kt_.init<BK>(A, r0, brows);
   if (kt_.n == 0) return;
-  const RowView V = row_view(A, r0 + (w / A.hb) * 32 + (lane & 31));
   const T* kb = (const T*)A.k.p + (int64_t)B.kv * A.dim;
   const T* vb = (const T*)A.v.p + (int64_t)B.kv * A.dim;
 
   TileLoad<T, DP, BK, 4> lk, lv;
   lk.init(w, A.dim, A.k.ld);
   lv.init(w, A.dim, A.v.ld);
-  auto issue = [&](int t, uint64_t& bits) {
+  auto issue = [&](int t, uint64_t& bits) __attribute__((always_inline)) {
     int kt, nk;
     kt_.at<BK>(t, kt, nk);
     bits = key_bits<BK>(A.mask, kt, nk);
@@ -366,26 +431,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
     lk.issue(S, w, kb + (int64_t)kt * A.k.ld, nk, bits);
     lv.issue(S + TB, w, vb + (int64_t)kt * A.v.ld, nk, bits);
   };
-
-  Frag<T> q[TL::KS], go[TL::KS];
-  float delta = 0.f;
-  {
-    const int64_t i = V.valid ? V.i : r0;
-    const T* qp = (const T*)A.q.p + i * A.q.ld + head * A.dim;
-    const T* gp = (const T*)A.go.p + i * A.go.ld + head * A.dim;
-    const T* op = (const T*)A.o.p + i * A.o.ld + head * A.dim;
-#pragma unroll
-    for (int s = 0; s < TL::KS; ++s) {
-      const int d = 16 * s + 8 * half;
-      const bool ok = V.valid && d < A.dim;
-      const int dd = d < A.dim ? d : 0;
-      Frag<T> ov;
-      load_frag(qp + dd, ok, q[s]);
-      load_frag(gp + dd, ok, go[s]);
-      load_frag(op + dd, ok, ov);
-      delta += dot_frag(go[s], ov);
-    }
-  }
   delta = add32(delta);
   float lse2 = INFINITY;
   if (V.valid) {
@@ -401,7 +446,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
   const float c = A.scale * LOG2E;
   f32x16 dq[TL::DB];
 
-  auto sweep = [&](bool strict) {
+  auto sweep = [&](auto strict_) __attribute__((always_inline)) {
+    constexpr bool strict = decltype(strict_)::value;
 #pragma unroll
     for (int db = 0; db < TL::DB; ++db)
 #pragma unroll
@@ -416,39 +462,37 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
       if (t + 1 < kt_.n) issue(t + 1, next);
       int kt, nk;
       kt_.at<BK>(t, kt, nk);
-      if (wave_any(reaches(V, kt, nk))) {
-        const char *SK = smem + (t & 1) * 2 * TB, *SV = SK + TB;
-        const bool full = nk == BK && bits == (BK == 64 ? ~0ull : 0xffffffffull) &&
-                          wave_all(!V.valid || (V.lo <= kt && V.i >= kt + BK - 1));
+      const char *SK = smem + (t & 1) * 2 * TB, *SV = SK + TB;
 #pragma unroll
-        for (int b = 0; b < BK / 32; ++b) {
-          f32x16 p = scores<T, DP>(SK, rl, 32 * b, q);
-          const f32x16 dp = scores<T, DP>(SV, rl, 32 * b, go);
+      for (int b = 0; b < BK / 32; ++b) {
+        if (nk <= 32 * b || !wave_any(reaches(V, kt + 32 * b, min(32, nk - 32 * b)))) continue;
+        const bool full = (uint32_t)(bits >> (32 * b)) == 0xffffffffu &&
+                          wave_all(!V.valid || (V.lo <= kt + 32 * b && V.i >= kt + 32 * b + 31));
+        f32x16 p = scores<T, DP>(SK, rl, 32 * b, q);
+        const f32x16 dp = scores<T, DP>(SV, rl, 32 * b, go);
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c, -lse2)) * (dp[r] - delta);
-          if (!full || strict) {
-            const uint32_t kb32 = (uint32_t)(bits >> (32 * b)) >> (4 * half);
-            const int j0 = kt + 32 * b + 4 * half;
-            f32x16 bad;
-            if (strict) bad = TL::count_nonfinite(SK, rl, 32 * b);
+        for (int r = 0; r < 16; ++r)
+          p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c, -lse2)) * (dp[r] - delta);
+        if (!full || strict) {
+          const uint32_t see = row_bits(V, kt + 32 * b, (uint32_t)(bits >> (32 * b)));
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const bool see = sees(V, j0 + frag_off(r), kb32, r);
-              p[r] = see ? p[r] : 0.f;
-              if (strict && see && bad[r] > 0.f) p[r] = NAN;
-            }
+          for (int r = 0; r < 16; ++r) p[r] = keep_or(p[r], bit_mask(see, r), 0u);
+          if constexpr (strict) {
+            const f32x16 bad = TL::count_nonfinite(SK, rl, 32 * b);
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if (bad[r] > 0.f && bit_mask(see, r)) p[r] = NAN;
           }
+        }
 #pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            Frag<T> f;
-            pack_frag(p, hf, f);
+        for (int hf = 0; hf < 2; ++hf) {
+          Frag<T> f;
+          pack_frag(p, hf, f);
 #pragma unroll
-            for (int db = 0; db < TL::DB; ++db) {
-              Frag<T> kf = TL::colfrag(SK, cl, 32 * b + 16 * hf, db);
-              if (strict) kf = finite_part(kf);
-              mma32(kf, f, dq[db]);
-            }
+          for (int db = 0; db < TL::DB; ++db) {
+            Frag<T> kf = TL::colfrag(SK, cl, 32 * b + 16 * hf, db);
+            if (strict) kf = finite_part(kf);
+            mma32(kf, f, dq[db]);
           }
         }
       }
@@ -460,36 +504,17 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
       for (int r = 0; r < 16; ++r) dq[db][r] *= A.scale;
   };
 
-  T* op = (T*)A.gq.p + (int64_t)V.i * A.gq.ld + head * A.dim;
-  auto store = [&](bool patch) {
-    if (!V.valid) return;
-#pragma unroll
-    for (int db = 0; db < TL::DB; ++db)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int d = 32 * db + 8 * g + 4 * half;
-        if (d >= A.dim) continue;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (patch && nonfinite(dq[db][4 * g + e])) dq[db][4 * g + e] = ld(op + d + e);
-        if constexpr (sizeof(T) == 2)
-          *reinterpret_cast<u32x2*>(op + d) = u32x2{pack_bf2(dq[db][4 * g], dq[db][4 * g + 1]),
-                                                    pack_bf2(dq[db][4 * g + 2], dq[db][4 * g + 3])};
-        else
-          *reinterpret_cast<f32x4*>(op + d) =
-              f32x4{dq[db][4 * g], dq[db][4 * g + 1], dq[db][4 * g + 2], dq[db][4 * g + 3]};
-      }
-  };
-  sweep(false);
+  T* const op = (T*)A.gq.p + (int64_t)V.i * A.gq.ld + head * A.dim;
+  sweep(std::false_type{});
   float z = 0.f;
 #pragma unroll
   for (int db = 0; db < TL::DB; ++db)
 #pragma unroll
     for (int r = 0; r < 16; ++r) z = __builtin_fmaf(dq[db][r], 0.f, z);
-  store(false);
+  if (V.valid) store_row<T, DP, false>(op, nullptr, A.dim, dq);
   if (__syncthreads_or(V.valid && z != 0.f)) {
-    sweep(true);
-    store(true);
+    sweep(std::true_type{});
+    if (V.valid) store_row<T, DP, true>(op, nullptr, A.dim, dq);
   }
 }
 
@@ -505,10 +530,11 @@ __device__ inline int late_chunk(const AttnK& A, int n) { return ((n + A.ns - 1)
 // SQ / SG: the rows' q and d_out in LDS (row0 the subtile's first row there),
 // L / E: their lse2 and delta.  d: the subtile's first row minus the lane's
 // key; rows with d + offset < lim see it.
-template <typename T, int DP>
-__device__ inline void dkv_subtile(const char* SQ, const char* SG, const float* L, const float* E, int row0,
-                                   uint32_t rl, uint32_t cl, const Frag<T>* kf, const Frag<T>* vf, float c, int d,
-                                   unsigned lim, bool full, bool strict, f32x16* dk, f32x16* dv) {
+template <typename T, int DP, bool strict>
+__device__ __forceinline__ void dkv_subtile(const char* SQ, const char* SG, const float* L, const float* E, int row0,
+                                   uint32_t rl, uint32_t cl, const Frag<T> (&kf)[Tile<T, DP>::KS],
+                                   const Frag<T> (&vf)[Tile<T, DP>::KS], float c, int d, unsigned lim, bool full,
+                                   f32x16 (&dk)[Tile<T, DP>::DB], f32x16 (&dv)[Tile<T, DP>::DB]) {
   using TL = Tile<T, DP>;
   const int half = (threadIdx.x & 63) >> 5;
   f32x16 p = scores<T, DP>(SQ, rl, row0, kf);
@@ -525,19 +551,18 @@ __device__ inline void dkv_subtile(const char* SQ, const char* SG, const float* 
     }
   }
   if (!full || strict) {
+    const uint32_t see = bit_range(-d, (int)lim - 1 - d) >> (4 * half);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const bool see = (unsigned)(d + frag_off(r) + 4 * half) < lim;
-      p[r] = see ? p[r] : 0.f;
-      ds[r] = see ? ds[r] : 0.f;
+      p[r] = keep_or(p[r], bit_mask(see, r), 0u);
+      ds[r] = keep_or(ds[r], bit_mask(see, r), 0u);
     }
-    if (strict) {
+    if constexpr (strict) {
       const f32x16 bq = TL::count_nonfinite(SQ, rl, row0), bg = TL::count_nonfinite(SG, rl, row0);
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const bool see = (unsigned)(d + frag_off(r) + 4 * half) < lim;
-        if (see && bg[r] > 0.f) p[r] = NAN;
-        if (see && bq[r] > 0.f) ds[r] = NAN;
+        if (bg[r] > 0.f && bit_mask(see, r)) p[r] = NAN;
+        if (bq[r] > 0.f && bit_mask(see, r)) ds[r] = NAN;
       }
     }
   }
@@ -640,7 +665,8 @@ __global__ __launch_bounds__(256, 1) void seq_dkv_kernel(AttnK A) {
   const float c = A.scale * LOG2E;
   f32x16 dk[TL::DB], dv[TL::DB];
 
-  auto sweep = [&](bool strict) {
+  auto sweep = [&](auto strict_) __attribute__((always_inline)) {
+    constexpr bool strict = decltype(strict_)::value;
 #pragma unroll
     for (int db = 0; db < TL::DB; ++db)
 #pragma unroll
@@ -660,8 +686,8 @@ __global__ __launch_bounds__(256, 1) void seq_dkv_kernel(AttnK A) {
         // rows ib .. ib+31 reach the wave's keys k0 + 32 w .. + 31
         if (ib + 31 < k0 + 32 * w || ib >= wend) continue;
         const bool full = wave_all((unsigned)(ib - j) < lim && (unsigned)(ib + 31 - j) < lim);
-        dkv_subtile<T, DP>(S, S + TB, (const float*)(S + 2 * TB), (const float*)(S + 2 * TB + 256), 32 * b, rl, cl, kf,
-                           vf, c, ib - j, lim, full, strict, dk, dv);
+        dkv_subtile<T, DP, strict>(S, S + TB, (const float*)(S + 2 * TB), (const float*)(S + 2 * TB + 256), 32 * b, rl,
+                                   cl, kf, vf, c, ib - j, lim, full, dk, dv);
       }
     }
     // sinks: the late rows' partial sums, in split order (a hidden sink has no
@@ -696,38 +722,24 @@ __global__ __launch_bounds__(256, 1) void seq_dkv_kernel(AttnK A) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) dk[db][r] *= A.scale;
   };
-  auto store1 = [&](T* op, f32x16* x, bool patch) {
-#pragma unroll
-    for (int db = 0; db < TL::DB; ++db)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int d = 32 * db + 8 * g + 4 * half;
-        if (d >= A.dim) continue;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (patch && nonfinite(x[db][4 * g + e])) x[db][4 * g + e] = ld(op + d + e);
-        if constexpr (sizeof(T) == 2)
-          *reinterpret_cast<u32x2*>(op + d) =
-              u32x2{pack_bf2(x[db][4 * g], x[db][4 * g + 1]), pack_bf2(x[db][4 * g + 2], x[db][4 * g + 3])};
-        else
-          *reinterpret_cast<f32x4*>(op + d) = f32x4{x[db][4 * g], x[db][4 * g + 1], x[db][4 * g + 2], x[db][4 * g + 3]};
-      }
-  };
-  auto store = [&](bool patch) {
-    if (!valid) return;
-    store1((T*)A.gk.p + (int64_t)j * A.gk.ld + kv * A.dim, dk, patch);
-    store1((T*)A.gv.p + (int64_t)j * A.gv.ld + kv * A.dim, dv, patch);
-  };
-  sweep(false);
+  T* const kp = (T*)A.gk.p + (int64_t)j * A.gk.ld + kv * A.dim;
+  T* const vp = (T*)A.gv.p + (int64_t)j * A.gv.ld + kv * A.dim;
+  sweep(std::false_type{});
   float z = 0.f;
 #pragma unroll
   for (int db = 0; db < TL::DB; ++db)
 #pragma unroll
     for (int r = 0; r < 16; ++r) z = __builtin_fmaf(dk[db][r], 0.f, __builtin_fmaf(dv[db][r], 0.f, z));
-  store(false);
+  if (valid) {
+    store_row<T, DP, false>(kp, nullptr, A.dim, dk);
+    store_row<T, DP, false>(vp, nullptr, A.dim, dv);
+  }
   if (__syncthreads_or(valid && z != 0.f)) {
-    sweep(true);
-    store(true);
+    sweep(std::true_type{});
+    if (valid) {
+      store_row<T, DP, true>(kp, nullptr, A.dim, dk);
+      store_row<T, DP, true>(vp, nullptr, A.dim, dv);
+    }
   }
 }
 
@@ -735,7 +747,7 @@ __global__ __launch_bounds__(256, 1) void seq_dkv_kernel(AttnK A) {
 // one of which sees every sink.  A block: 32 sinks of one key head; its waves
 // take every fourth subtile of rows, their sums are added in wave order.
 template <typename T, int DP>
-__global__ __launch_bounds__(256, 1) void seq_sink_kernel(AttnK A, int parts) {
+__global__ __launch_bounds__(256, 1) void seq_sink_kernel(AttnK A, int parts, int per_block) {
   using TL = Tile<T, DP>;
   using Cfg = DkvCfg<T, DP>;
   constexpr int TB = 32 * TL::RB;
@@ -745,13 +757,19 @@ __global__ __launch_bounds__(256, 1) void seq_sink_kernel(AttnK A, int parts) {
   int b = blockIdx.x;
   const int part = b % parts; b /= parts;
   const int u = b % A.ns; b /= A.ns;
-  const int kv = b % A.kv_heads, seq = b / A.kv_heads;
+  const int kv = b % A.kv_heads, first = b / A.kv_heads * per_block;
+  // which of the block's sequences have late rows in this split
+  bool any = false;
+  if (lane < per_block && first + lane < A.num_seqs) {
+    const int s0 = A.offsets[first + lane], e0 = min(A.offsets[first + lane + 1], A.rows);
+    const int late = e0 - late_row(A, max(s0, 0));
+    any = s0 >= 0 && s0 < e0 && late > 0 && (int64_t)u * late_chunk(A, late) < late;
+  }
+  for (uint64_t todo = __ballot(any); todo; todo &= todo - 1) {
+  const int seq = first + __builtin_ctzll(todo);
   const int s0 = A.offsets[seq], e0 = min(A.offsets[seq + 1], A.rows);
-  if (s0 < 0 || s0 >= e0) return;
   const int x0 = late_row(A, s0), late = e0 - x0;
-  if (late <= 0) return;
   const int chunk = late_chunk(A, late), a0 = x0 + u * chunk, a1 = (int)min((int64_t)e0, (int64_t)a0 + chunk);
-  if (u * (int64_t)chunk >= late) return;
   const int a = part * 32 + (lane & 31), j = s0 + a;   // late rows exist: the sequence has all its sinks
   const bool shown = a < A.sinks && (!A.mask || A.mask[j]);
   const int per_head = (a1 - a0 + 31) / 32, n = per_head * A.group;
@@ -780,8 +798,8 @@ __global__ __launch_bounds__(256, 1) void seq_sink_kernel(AttnK A, int parts) {
     issue_stats(S + 2 * TB, A.lse2 + at, nr);
     issue_stats(S + 2 * TB + 256, A.delta + at, nr);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    dkv_subtile<T, DP>(S, S + TB, (const float*)(S + 2 * TB), (const float*)(S + 2 * TB + 256), 0, rl, cl, kf, vf, c, 0,
-                       shown ? (unsigned)nr : 0u, nr == 32 && wave_all(shown), false, dk, dv);
+    dkv_subtile<T, DP, false>(S, S + TB, (const float*)(S + 2 * TB), (const float*)(S + 2 * TB + 256), 0, rl, cl, kf,
+                              vf, c, 0, shown ? (unsigned)nr : 0u, nr == 32 && wave_all(shown), dk, dv);
   }
   // waves' sums, one after the other, in LDS [2][DP][33]
   float* R = reinterpret_cast<float*>(smem);
@@ -804,6 +822,8 @@ __global__ __launch_bounds__(256, 1) void seq_sink_kernel(AttnK A, int parts) {
     const int m = x / (na * A.dim), y = x - m * na * A.dim, r = y / A.dim, d = y - r * A.dim;
     P[((int64_t)m * A.sinks + part * 32 + r) * A.dim + d] = R[m * DP * 33 + d * 33 + r];
   }
+  __syncthreads();                           // R is read; the stages may be loaded again
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -825,6 +845,7 @@ static AttnK attn_args(const SeqAttnArgs& a) {
   A.mask = a.key_mask;
   A.q = a.q; A.k = a.k; A.v = a.v; A.o = a.o; A.go = a.go; A.gq = a.gq; A.gk = a.gk; A.gv = a.gv;
   A.lse = a.lse;
+  A.out_lo = a.dt == DT_BF16 ? a.out_lo : nullptr;
   return A;
 }
 
@@ -867,7 +888,12 @@ static hipError_t bwd_launch(const AttnK& A, hipStream_t s) {
   LAT_LAUNCH_CHECK();
   if (A.ns > 0) {
     const int parts = (A.sinks + 31) / 32;
-    seq_sink_kernel<T, DP><<<A.num_seqs * A.kv_heads * A.ns * parts, 256, DkvCfg<T, DP>::SINK_LDS, s>>>(A, parts);
+    // a block looks at several sequences where there are many: most of many
+    // are short and have no late rows
+    const int64_t all = (int64_t)A.num_seqs * A.kv_heads * A.ns * parts;
+    const int pb = (int)(all < 2048 ? 1 : all / 2048 > 64 ? 64 : all / 2048);
+    seq_sink_kernel<T, DP><<<cdiv(A.num_seqs, pb) * A.kv_heads * A.ns * parts, 256, DkvCfg<T, DP>::SINK_LDS, s>>>(
+        A, parts, pb);
     LAT_LAUNCH_CHECK();
   }
   seq_dkv_kernel<T, DP><<<cdiv(A.rows, 128) * A.kv_heads, 256, DkvCfg<T, DP>::LDS, s>>>(A);

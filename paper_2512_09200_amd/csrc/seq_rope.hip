@@ -54,7 +54,7 @@ void rope_turns(double theta, int rotary, RopeTurns* t) {
 }
 
 struct RopeK {                               // kernel arguments
-  int rows, heads, hk, dim, rotary, inter, tb, lp, chunks, groups;   // hk = heads + kv_heads
+  int rows, heads, hk, dim, rotary, tb, lp, chunks, groups;   // hk = heads + kv_heads
   float eps, inv_dim;
   const SeqSpan* span;
   const int32_t* pos;
@@ -99,8 +99,9 @@ __device__ inline float group_sum(float v, int lp) {
   return v;
 }
 
-// T storage type, E elements of a run; blocks go over groups of tb rows.
-template <typename T, int E, bool BWD>
+// T storage type, E elements of a run, INTER pairs of neighbours; blocks go
+// over groups of tb rows.
+template <typename T, int E, bool BWD, bool INTER>
 __global__ __launch_bounds__(256) void rope_kernel(RopeK A, RopeTurns turns) {
   extern __shared__ float2 cs[];             // [tb][rotary / 2]; backward's end: dgain partials
   const int tid = threadIdx.x, np = A.rotary >> 1;
@@ -110,7 +111,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeK A, RopeTurns turns) {
   int lo, hi;
   bool rot;
   const int m0 = c * E;
-  if (A.inter) {
+  if (INTER) {
     lo = c * 2 * E;
     hi = lo + E;
     rot = lo < A.rotary;
@@ -133,9 +134,32 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeK A, RopeTurns turns) {
 #pragma unroll
     for (int e = 0; e < 2 * E; ++e) dg[0][e] = dg[1][e] = 0.f;
 
-  for (int64_t t0 = (int64_t)blockIdx.x * A.tb; t0 < A.rows; t0 += (int64_t)gridDim.x * A.tb) {
+  // an item's loads: head h of row t0 + t
+  auto fetch = [&](int64_t t0, int it, float (&v)[2 * E], float (&d)[2 * E], int& start) __attribute__((always_inline)) {
+    const int t = it / A.hk, h = it - t * A.hk;
+    const int64_t row = t0 + t;
+    const bool isk = h >= A.heads;
+    const int hh = isk ? h - A.heads : h;
+    const SeqTensor X = isk ? A.xk : A.xq;
+    const T* x = (const T*)X.p + row * X.ld + hh * A.dim;
+    ldE<T, E>(x + lo, v);
+    ldE<T, E>(x + hi, v + E);
+    if constexpr (BWD) {
+      const SeqTensor Y = isk ? A.dyk : A.dyq;
+      const T* y = (const T*)Y.p + row * Y.ld + hh * A.dim;
+      ldE<T, E>(y + lo, d);
+      ldE<T, E>(y + hi, d + E);
+    }
+    start = A.span ? A.span[row].start : 0;
+  };
+  const int64_t step = (int64_t)gridDim.x * A.tb;
+  for (int64_t t0 = (int64_t)blockIdx.x * A.tb; t0 < A.rows; t0 += step) {
+    const int tn = (int)min((int64_t)A.tb, A.rows - t0), items = tn * A.hk;
+    // the first item's loads are in flight while the angles are made
+    float v[2 * E], d[2 * E];
+    int start = SEQ_NO_ROW;
+    if (group < items) fetch(t0, group, v, d, start);
     if (t0 != (int64_t)blockIdx.x * A.tb) __syncthreads();           // the rows before read cs
-    const int tn = (int)min((int64_t)A.tb, A.rows - t0);
     for (int u = tid; u < tn * np; u += 256) {
       const int t = u / np, m = u - t * np;
       int p;
@@ -144,78 +168,74 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeK A, RopeTurns turns) {
       cs[u] = rope_cs(p, turns.f[m]);
     }
     __syncthreads();
-    const int items = tn * A.hk;
     for (int it = group; it < items; it += A.groups) {
-      const int t = it / A.hk, h = it - t * A.hk;
-      const int64_t row = t0 + t;
-      if (A.span && A.span[row].start == SEQ_NO_ROW) continue;       // uniform over the head's lanes
-      const bool isk = h >= A.heads;
-      const int hh = isk ? h - A.heads : h;
-      const SeqTensor X = isk ? A.xk : A.xq, O = isk ? A.ok : A.oq;
-      const T* x = (const T*)X.p + row * X.ld + hh * A.dim;
-      T* o = (T*)O.p + row * O.ld + hh * A.dim;
-      float v[2 * E];
-      ldE<T, E>(x + lo, v);
-      ldE<T, E>(x + hi, v + E);
-      float d[2 * E];
-      if constexpr (BWD) {
-        const SeqTensor Y = isk ? A.dyk : A.dyq;
-        const T* y = (const T*)Y.p + row * Y.ld + hh * A.dim;
-        ldE<T, E>(y + lo, d);
-        ldE<T, E>(y + hi, d + E);
-      }
-      float ss = 0.f;
+      float vn[2 * E], dn[2 * E];
+      int sn = SEQ_NO_ROW;
+      if (it + A.groups < items) fetch(t0, it + A.groups, vn, dn, sn);
+      if (start != SEQ_NO_ROW) {                                     // uniform over the head's lanes
+        const int t = it / A.hk, h = it - t * A.hk;
+        const bool isk = h >= A.heads;
+        const SeqTensor O = isk ? A.ok : A.oq;
+        T* o = (T*)O.p + (t0 + t) * O.ld + (isk ? h - A.heads : h) * A.dim;
+        float ss = 0.f;
 #pragma unroll
-      for (int e = 0; e < 2 * E; ++e) ss += v[e] * v[e];
-      if (!lane_on) ss = 0.f;
-      ss = group_sum(ss, A.lp);
-      const float r = 1.f / sqrtf(ss * A.inv_dim + A.eps);
-      const float2* w = cs + t * np + m0;
-      if constexpr (!BWD) {
-        float z[2 * E];
+        for (int e = 0; e < 2 * E; ++e) ss += v[e] * v[e];
+        if (!lane_on) ss = 0.f;
+        ss = group_sum(ss, A.lp);
+        const float r = 1.f / sqrtf(ss * A.inv_dim + A.eps);
+        const float2* w = cs + t * np + m0;
+        if constexpr (!BWD) {
+          float z[2 * E];
 #pragma unroll
-        for (int e = 0; e < 2 * E; ++e) z[e] = v[e] * r * (isk ? gain[1][e] : gain[0][e]);
-        if (rot) {
+          for (int e = 0; e < 2 * E; ++e) z[e] = v[e] * r * (isk ? gain[1][e] : gain[0][e]);
+          if (rot) {
 #pragma unroll
-          for (int m = 0; m < E; ++m) {
-            const int a = A.inter ? 2 * m : m, b = A.inter ? 2 * m + 1 : E + m;
-            const float za = z[a], zb = z[b];
-            z[a] = za * w[m].x - zb * w[m].y;
-            z[b] = za * w[m].y + zb * w[m].x;
+            for (int m = 0; m < E; ++m) {
+              const int a = INTER ? 2 * m : m, b = INTER ? 2 * m + 1 : E + m;
+              const float za = z[a], zb = z[b];
+              z[a] = za * w[m].x - zb * w[m].y;
+              z[b] = za * w[m].y + zb * w[m].x;
+            }
+          }
+          if (lane_on) {
+            stE<T, E>(o + lo, z);
+            stE<T, E>(o + hi, z + E);
+          }
+        } else {
+          if (rot) {
+#pragma unroll
+            for (int m = 0; m < E; ++m) {
+              const int a = INTER ? 2 * m : m, b = INTER ? 2 * m + 1 : E + m;
+              const float da = d[a], db = d[b];
+              d[a] = da * w[m].x + db * w[m].y;
+              d[b] = db * w[m].x - da * w[m].y;
+            }
+          }
+          float hx = 0.f;
+#pragma unroll
+          for (int e = 0; e < 2 * E; ++e) {
+            const float n = v[e] * r;
+            dg[0][e] += isk ? 0.f : d[e] * n;
+            dg[1][e] += isk ? d[e] * n : 0.f;
+            d[e] *= isk ? gain[1][e] : gain[0][e];
+            hx += d[e] * n;
+          }
+          if (!lane_on) hx = 0.f;
+          hx = group_sum(hx, A.lp) * A.inv_dim;
+#pragma unroll
+          for (int e = 0; e < 2 * E; ++e) d[e] = r * (d[e] - v[e] * r * hx);
+          if (lane_on) {
+            stE<T, E>(o + lo, d);
+            stE<T, E>(o + hi, d + E);
           }
         }
-        if (lane_on) {
-          stE<T, E>(o + lo, z);
-          stE<T, E>(o + hi, z + E);
-        }
-      } else {
-        if (rot) {
-#pragma unroll
-          for (int m = 0; m < E; ++m) {
-            const int a = A.inter ? 2 * m : m, b = A.inter ? 2 * m + 1 : E + m;
-            const float da = d[a], db = d[b];
-            d[a] = da * w[m].x + db * w[m].y;
-            d[b] = db * w[m].x - da * w[m].y;
-          }
-        }
-        float hx = 0.f;
-#pragma unroll
-        for (int e = 0; e < 2 * E; ++e) {
-          const float n = v[e] * r;
-          dg[0][e] += isk ? 0.f : d[e] * n;
-          dg[1][e] += isk ? d[e] * n : 0.f;
-          d[e] *= isk ? gain[1][e] : gain[0][e];
-          hx += d[e] * n;
-        }
-        if (!lane_on) hx = 0.f;
-        hx = group_sum(hx, A.lp) * A.inv_dim;
-#pragma unroll
-        for (int e = 0; e < 2 * E; ++e) d[e] = r * (d[e] - v[e] * r * hx);
-        if (lane_on) {
-          stE<T, E>(o + lo, d);
-          stE<T, E>(o + hi, d + E);
-        }
       }
+#pragma unroll
+      for (int e = 0; e < 2 * E; ++e) {
+        v[e] = vn[e];
+        if constexpr (BWD) d[e] = dn[e];
+      }
+      start = sn;
     }
   }
   if constexpr (BWD) {
@@ -288,7 +308,6 @@ static hipError_t rope_launch(const RopeArgs& a, const RopeTurns& t, float* part
   A.hk = a.heads + a.kv_heads;
   A.dim = a.dim;
   A.rotary = a.rotary;
-  A.inter = a.interleaved;
   A.tb = rope_tb(a.rows);
   A.chunks = a.dim / (2 * E);
   A.lp = 1;
@@ -308,13 +327,15 @@ static hipError_t rope_launch(const RopeArgs& a, const RopeTurns& t, float* part
     lds = lds > need ? lds : need;
   }
   const int grid = rope_blocks(a.rows, BWD);
+  auto launch = [&](auto kern) { kern<<<grid, 256, lds, s>>>(A, t); };
+#define ROPE_PICK(T, E_) \
+  (a.interleaved ? launch(rope_kernel<T, E_, BWD, true>) : launch(rope_kernel<T, E_, BWD, false>))
   if (a.dt == DT_BF16) {
-    if (E == 8) rope_kernel<bf16_t, 8, BWD><<<grid, 256, lds, s>>>(A, t);
-    else rope_kernel<bf16_t, 4, BWD><<<grid, 256, lds, s>>>(A, t);
+    if (E == 8) ROPE_PICK(bf16_t, 8); else ROPE_PICK(bf16_t, 4);
   } else {
-    if (E == 8) rope_kernel<float, 8, BWD><<<grid, 256, lds, s>>>(A, t);
-    else rope_kernel<float, 4, BWD><<<grid, 256, lds, s>>>(A, t);
+    if (E == 8) ROPE_PICK(float, 8); else ROPE_PICK(float, 4);
   }
+#undef ROPE_PICK
   LAT_LAUNCH_CHECK();
   return hipSuccess;
 }

@@ -25,6 +25,7 @@ namespace lat {
 constexpr float STEP_LOG2E = 1.4426950408889634f;
 constexpr int STEP_HEADS = 16;               // head columns of a block
 constexpr int STEP_TILE = 32;                // slots of a wave's tile
+constexpr int STEP_MAX_SPLITS = 1024;
 
 struct StepK {
   SeqCacheArgs c;
@@ -44,15 +45,21 @@ __device__ inline void mma16(const Frag<float>& a, const Frag<float>& b, f32x4& 
 #pragma unroll
   for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[e], b.v[e], c, 0, 0, 0);
 }
-template <typename T> __device__ inline Frag<T> frag_of(const float* x);
-template <> __device__ inline Frag<bf16_t> frag_of<bf16_t>(const float* x) {
-  return {__builtin_bit_cast(bf16x8, Vec16<bf16_t>::pack(x))};
-}
-template <> __device__ inline Frag<float> frag_of<float>(const float* x) {
-  Frag<float> f;
+// Operands that the step itself computes (the rotated query, probabilities) go
+// into the matrix instructions as two bf16 parts, value and remainder: the
+// matrix cores have the time, and the result is then rounded once, at the
+// end.  fp32 operands are taken as they are.
+template <typename T> struct Parts { static constexpr int N = sizeof(T) == 2 ? 2 : 1; Frag<T> p[N]; };
+__device__ inline void split(const float* x, Parts<bf16_t>& f) {
+  float r[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) f.v[e] = x[e];
-  return f;
+  for (int e = 0; e < 8; ++e) r[e] = x[e] - bf2f(f2bf(x[e]));
+  f.p[0].v = __builtin_bit_cast(bf16x8, Vec16<bf16_t>::pack(x));
+  f.p[1].v = __builtin_bit_cast(bf16x8, Vec16<bf16_t>::pack(r));
+}
+__device__ inline void split(const float* x, Parts<float>& f) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f.p[0].v[e] = x[e];
 }
 __device__ inline float wave_sum(float v) {
 #pragma unroll
@@ -63,7 +70,7 @@ __device__ inline float wave_sum(float v) {
 template <typename T, int DP> struct StepCfg {
   using TL = Tile<T, DP>;
   static constexpr int VT = STEP_TILE * TL::RB;                       // a wave's V stage
-  static constexpr int NEW = (STEP_HEADS + 2) * DP * (int)sizeof(T);  // q rows, new k, new v
+  static constexpr int NEW = STEP_HEADS * DP * 4 + 2 * DP * (int)sizeof(T);   // q rows (fp32), new k, new v
   static constexpr size_t LOOP = (size_t)8 * VT + NEW;
   static constexpr size_t JOIN = (size_t)4 * STEP_HEADS * (DP + 4) * sizeof(float);
   static constexpr size_t LDS = LOOP > JOIN ? LOOP : JOIN;
@@ -91,8 +98,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
   const int64_t base = ((int64_t)ci * A.c.kv_heads + kv) * A.cap;
   T* const kc = (T*)A.c.kc + base * D;
   T* const vc = (T*)A.c.vc + base * D;
-  T* const qn = reinterpret_cast<T*>(smem + 8 * Cfg::VT);             // [16][DP]
-  T* const kn = qn + STEP_HEADS * DP;
+  float* const qn = reinterpret_cast<float*>(smem + 8 * Cfg::VT);     // [16][DP]
+  T* const kn = reinterpret_cast<T*>(qn + STEP_HEADS * DP);
   T* const vn = kn + DP;
 
   TileLoad<T, DP, STEP_TILE, 1> lv;
@@ -123,7 +130,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
     float2 cs{1.f, 0.f};
     if (A.rope && rot) cs = rope_cs(A.pos ? A.pos[b] : p, turns.f[lane]);
     for (int r = w; r < STEP_HEADS + 2; r += 4) {
-      T* dst = qn + r * DP;
       const bool isq = r < STEP_HEADS, live = !isq || r < nh;
       const T* src = isq ? (const T*)A.q.p + (int64_t)b * A.q.ld + (h0 + min(r, nh - 1)) * D
                    : r == STEP_HEADS ? (const T*)A.k.p + (int64_t)b * A.k.ld + kv * D
@@ -138,9 +144,17 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
         zx = tx;
         zy = ty;
       }
+      zx = live && on ? zx : 0.f;
+      zy = live && on ? zy : 0.f;
       if (x < DP) {
-        st(dst + x, live && on ? zx : 0.f);
-        st(dst + y, live && on ? zy : 0.f);
+        if (isq) {
+          qn[r * DP + x] = zx;
+          qn[r * DP + y] = zy;
+        } else {
+          T* dst = kn + (r - STEP_HEADS) * DP;
+          st(dst + x, zx);
+          st(dst + y, zy);
+        }
       }
     }
   }
@@ -154,9 +168,13 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
           *reinterpret_cast<const u32x4*>((m ? vn : kn) + d);
     }
   }
-  Frag<T> qf[KS];
+  Parts<T> qf[KS];
 #pragma unroll
-  for (int s = 0; s < KS; ++s) load_frag(qn + l16 * DP + 32 * s + 8 * g16, true, qf[s]);
+  for (int s = 0; s < KS; ++s) {
+    Frag<float> f;
+    load_frag(qn + l16 * DP + 32 * s + 8 * g16, true, f);
+    split(f.v, qf[s]);
+  }
 
   const float c = A.scale * STEP_LOG2E;
   f32x4 o[OB];
@@ -209,7 +227,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
           load_frag(kn + 32 * i + 8 * g16, true, fn);
           if (at == 16 * r + l16) f = fn;
         }
-        mma16(f, qf[i], s[r]);
+#pragma unroll
+        for (int x = Parts<T>::N - 1; x >= 0; --x) mma16(f, qf[i].p[x], s[r]);
       }
     }
     float x[8], tm = -INFINITY;
@@ -236,9 +255,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
       x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], c, -mc));
       l += x[e];
     }
-    const Frag<T> pf = frag_of<T>(x);
+    Parts<T> pf;
+    split(x, pf);
 #pragma unroll
-    for (int i = 0; i < OB; ++i) mma16(vfrag(S, i), pf, o[i]);
+    for (int i = 0; i < OB; ++i) {
+      const Frag<T> f = vfrag(S, i);
+#pragma unroll
+      for (int y = Parts<T>::N - 1; y >= 0; --y) mma16(f, pf.p[y], o[i]);
+    }
   };
 #pragma unroll 1
   for (int t = w; t < tiles; t += 8) {
@@ -294,27 +318,46 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
   }
 }
 
-// out of a user's head from its splits, in split order
-template <typename T>
-__global__ __launch_bounds__(256) void seq_step_join_kernel(StepK A, int batch) {
-  const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int D = A.c.dim;
-  const int64_t bh = x / D;
-  if (bh >= (int64_t)batch * A.heads) return;
-  const int d = (int)(x - bh * D), b = (int)(bh / A.heads), h = (int)(bh - (int64_t)b * A.heads);
+// out of a user's head from its splits.  A block a head: the splits' weights
+// go to LDS, then 256 / DP strands of threads add every so many splits, and
+// the strands' sums are added in strand order.
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void seq_step_join_kernel(StepK A) {
+  constexpr int ST = 256 / DP;
+  __shared__ float wt[STEP_MAX_SPLITS], sum[256], red[8];
+  const int bh = blockIdx.x, b = bh / A.heads, h = bh - b * A.heads, tid = threadIdx.x, D = A.c.dim;
   const int p = A.lens[b], ci = A.c.index ? A.c.index[b] : b;
   if (p < 0 || ci < 0 || ci >= A.c.num_caches) return;
   const float c = A.scale * STEP_LOG2E;
-  const float* P = A.part + bh * A.ns * (D + 2);
+  const float* P = A.part + (int64_t)bh * A.ns * (D + 2);
   float M = -INFINITY, L = 0.f, O = 0.f;
-  for (int u = 0; u < A.ns; ++u) M = fmaxf(M, P[u * (D + 2) + D]);
-  for (int u = 0; u < A.ns; ++u) {
-    const float* Q = P + u * (D + 2);
-    const float f = Q[D] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((Q[D] - M) * c);
-    L += Q[D + 1] * f;
-    O += Q[d] * f;
+  for (int u = tid; u < A.ns; u += 256) M = fmaxf(M, P[u * (D + 2) + D]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+  if ((tid & 63) == 0) red[tid >> 6] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  for (int u = tid; u < A.ns; u += 256) {
+    const float m = P[u * (D + 2) + D], f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - M) * c);
+    wt[u] = f;
+    L += P[u * (D + 2) + D + 1] * f;
   }
-  st((T*)A.out.p + (int64_t)b * A.out.ld + h * D + d, O / L);
+  L = wave_sum(L);
+  if ((tid & 63) == 0) red[4 + (tid >> 6)] = L;
+  __syncthreads();
+  L = (red[4] + red[5]) + (red[6] + red[7]);
+  const int d = tid % DP, strand = tid / DP;
+  if (d < D) {
+#pragma unroll 8
+    for (int u = strand; u < A.ns; u += ST) O += wt[u] * P[u * (D + 2) + d];
+  }
+  sum[tid] = O;
+  __syncthreads();
+  if (strand == 0 && d < D) {
+#pragma unroll
+    for (int i = 1; i < ST; ++i) O += sum[i * DP + d];
+    st((T*)A.out.p + (int64_t)b * A.out.ld + h * D + d, O / L);
+  }
 }
 
 // Splits of the slots: enough blocks for four a compute unit, at least 256 slots
@@ -322,7 +365,7 @@ __global__ __launch_bounds__(256) void seq_step_join_kernel(StepK A, int batch) 
 static int step_splits(int batch, int heads, int kv_heads, int cap) {
   const int hg = cdiv(heads / kv_heads, STEP_HEADS);
   const int64_t blocks = (int64_t)batch * kv_heads * hg;
-  int64_t n = cdiv(1024, blocks);
+  int64_t n = cdiv(STEP_MAX_SPLITS, blocks);
   if (n > cdiv(cap, 256)) n = cdiv(cap, 256);
   return (int)n;
 }
@@ -340,7 +383,7 @@ static hipError_t step_launch(const StepK& A, const RopeTurns& t, int batch, hip
   seq_step_kernel<T, DP><<<batch * A.c.kv_heads * A.hg * A.ns, 256, StepCfg<T, DP>::LDS, s>>>(A, t);
   LAT_LAUNCH_CHECK();
   if (A.ns > 1) {
-    seq_step_join_kernel<T><<<cdiv((int64_t)batch * A.heads * A.c.dim, 256), 256, 0, s>>>(A, batch);
+    seq_step_join_kernel<T, DP><<<batch * A.heads, 256, 0, s>>>(A);
     LAT_LAUNCH_CHECK();
   }
   return hipSuccess;

@@ -145,7 +145,7 @@ def check_attn(c, dt, W, N):
     W = min(W, n + 1)
     f = o.attn(*a, c["off"], W, N, D ** -0.5, c["shown"][:n], dt)
     within(c["out"][:n], f["o"], f["o_bound"], "out")
-    L = f64(c["lse"])[:, :n]
+    L = f64(c["lse"].lse)[:, :n]
     empty = np.isneginf(f["lse"])
     assert np.array_equal(np.isneginf(L), empty)
     assert np.abs(np.where(empty, 0, L - np.where(empty, 0, f["lse"]))).max(initial=0) < 1e-4
@@ -181,7 +181,7 @@ def test_attention_rows_that_see_nothing(dt):
     c = attn_case(dt, 4, 2, 64, [90, 40], 20, 2, all_hidden=True)
     for m in ("out", "dq", "dk", "dv"):
         assert (c[m] == 0).all(), m
-    assert torch.isneginf(c["lse"]).all()
+    assert torch.isneginf(c["lse"].lse).all()
     check_attn(attn_case(dt, 4, 2, 64, [90, 40], 3, 1, hidden=0.8), dt, 3, 1)
 
 
@@ -249,12 +249,14 @@ def test_nonfinite_values_reach_only_rows_that_see_them(dt, D, bad):
 def test_attention_twice_on_side_streams_and_in_a_graph_gives_the_same_bits():
     from paper_2512_09200_amd import api
     c = attn_case("bf16", 8, 2, 64, LENS["mixed"], 60, 4, hidden=0.1)
-    names = ("out", "lse", "dq", "dk", "dv")
+    names = ("out", "lse", "lo", "dq", "dk", "dv")
+    c.update(lo=c["lse"].out_lo, lse=c["lse"].lse)
 
     def go():
         s = api.lattice_seq_plan(c["s"].offsets, c["rows"], max_len=400)
         out, lse = api.lattice_seq_attn_fwd(s, c["q"], c["k"], c["v"], **c["kw"])
-        return (out, lse) + tuple(api.lattice_seq_attn_bwd(s, c["q"], c["k"], c["v"], out, lse, c["do"], **c["kw"]))
+        return (out, lse.lse, lse.out_lo) + tuple(api.lattice_seq_attn_bwd(s, c["q"], c["k"], c["v"], out, lse, c["do"],
+                                                                           **c["kw"]))
 
     def same(r):
         for x, m in zip(r, names):
@@ -477,7 +479,7 @@ def test_binding_refusals():
     # no rows, no sequences
     none = api.lattice_seq_plan(torch.zeros(1, dtype=torch.int32, device=DEV), 0)
     out, lse = api.lattice_seq_attn_fwd(none, q[:0], k[:0], k[:0], 4)
-    assert out.shape == (0, 4, 64) and lse.shape == (4, 0)
+    assert out.shape == (0, 4, 64) and lse.lse.shape == (4, 0)
     dq, dk, dgq, dgk = api.lattice_qk_rope_bwd(none, q[:0], k[:0], q[:0], k[:0], gain_q=torch.ones(64, device=DEV))
     assert (dgq == 0).all() and dgk is None
     api.lattice_seq_attn_bwd(none, q[:0], k[:0], k[:0], out, lse, q[:0], 4)

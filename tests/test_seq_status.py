@@ -99,7 +99,7 @@ def test_rope_tensors(lib):
 
 
 def _fwd(lib, d, s, q=P, ldq=QS, k=P, ldk=KS, v=P, ldv=KS, o=P, ldo=QS):
-    return lib.lattice_seq_attn_fwd(byref(d), byref(s), q, ldq, k, ldk, v, ldv, o, ldo, None, None)
+    return lib.lattice_seq_attn_fwd(byref(d), byref(s), q, ldq, k, ldk, v, ldv, o, ldo, None, None, None)
 
 
 @pytest.mark.parametrize("bad,status", BAD_HEADS + [
@@ -109,8 +109,8 @@ def _fwd(lib, d, s, q=P, ldq=QS, k=P, ldk=KS, v=P, ldv=KS, o=P, ldo=QS):
 def test_attn_descriptor(lib, bad, status):
     d, s, c = attn(**bad), seqs(), cache()
     assert _fwd(lib, d, s) == status
-    assert lib.lattice_seq_attn_bwd(byref(d), byref(s), P, QS, P, KS, P, KS, P, QS, P, P, QS, P, QS, P, KS, P, KS, P,
-                                    1 << 40, None) == status
+    assert lib.lattice_seq_attn_bwd(byref(d), byref(s), P, QS, P, KS, P, KS, P, QS, P, None, P, QS, P, QS, P, KS, P,
+                                    KS, P, 1 << 40, None) == status
     assert lib.lattice_seq_cache_fill(byref(d), byref(s), P, KS, P, KS, None, None, byref(c), None) == status
     assert lib.lattice_seq_step(byref(d), None, 2, P, QS, P, KS, P, KS, P, None, byref(c), P, QS, P, 1 << 40,
                                 None) == status
@@ -132,9 +132,10 @@ def test_attn_tensors(lib):
     need = lib.lattice_seq_attn_bwd_workspace(byref(d), byref(s))
     assert need > 0
 
-    def bwd(lse=P, ws=P, n=need, s=s, go=P):
-        return lib.lattice_seq_attn_bwd(byref(d), byref(s), P, QS, P, KS, P, KS, P, QS, lse, go, QS, P, QS, P, KS, P,
-                                        KS, ws, n, None)
+    def bwd(lse=P, ws=P, n=need, s=s, go=P, lo=None):
+        return lib.lattice_seq_attn_bwd(byref(d), byref(s), P, QS, P, KS, P, KS, P, QS, lse, lo, go, QS, P, QS, P, KS,
+                                        P, KS, ws, n, None)
+    assert bwd(lo=P + 8) == INVALID_ARG
     assert bwd(lse=None) == INVALID_ARG
     assert bwd(go=None) == INVALID_ARG
     assert bwd(s=seqs(offsets=None)) == INVALID_ARG
