@@ -2,7 +2,6 @@
 include/lattice.h, taking torch tensors that live on the GPU.  Argument
 marshalling and buffer allocation only -- every step runs in liblattice.so.
 """
-import contextlib
 import ctypes
 from ctypes import byref
 
@@ -558,47 +557,57 @@ def lattice_interact_state(kind, X, stack, stack_n, ws, ln_eps=1e-5, fp8_proj=No
 # ---------------------------------------------------------------------------
 # Event sequences: tensors [rows, heads, head_dim] with the heads of a row
 # contiguous (slices of a projection's output are fine).
-def _on_device(t):
-    """Launches go to the current device: make it the tensors' own."""
-    if t.device.type != "cuda":
+def _run(dev, fn, stream, *args):
+    """Enqueue a C call on `stream` (None: the current one of the tensors' GPU).
+    Launches go to the current device, so it is made the tensors' own."""
+    if dev != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            return _run(dev, fn, stream, *args)
+    s = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    check(fn(*args, s))
+
+
+def _gpu(t):
+    dev = t.get_device()
+    if dev < 0:
         raise ValueError("expected tensors on the GPU")
-    return torch.cuda.device(t.device) if t.device.index != torch.cuda.current_device() else _NULL_CONTEXT
+    return dev
 
 
-_NULL_CONTEXT = contextlib.nullcontext()
-
-
-def _same(like, *ts):
-    for t in ts:
-        if t is not None and t.device != like.device:
-            raise ValueError(f"tensors on {like.device} and {t.device}")
-
-
-def _vec(t, dtype, n, name):
-    """Pointer of an optional contiguous vector of n elements."""
+def _vec(t, dtype, n, name, dev):
+    """Pointer of an optional contiguous vector of n elements on GPU dev."""
     if t is None:
         return None
     if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name}: expected {n} contiguous elements of {dtype}")
-    return t.data_ptr()
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is not on GPU {dev}")
+    return t.data_ptr() or None
 
 
 def _heads(t, like, rows, name):
-    """(pointer, row stride) of a tensor of event heads."""
-    if t.dim() != 3 or t.shape[0] != rows or t.dtype != like.dtype or t.shape[2] != like.shape[2]:
-        raise ValueError(f"{name}: expected [{rows}, heads, {like.shape[2]}] of {like.dtype}, got "
-                         f"{tuple(t.shape)} of {t.dtype}")
-    h, d = t.shape[1], t.shape[2]
-    if rows and ((d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d)):
+    """(pointer, row stride) of a tensor [rows, heads, head_dim] that goes with
+    `like`."""
+    shape, stride, D = t.shape, t.stride(), like.shape[2]
+    if len(shape) != 3 or shape[0] != rows or shape[2] != D or t.dtype != like.dtype:
+        raise ValueError(f"{name}: expected [{rows}, heads, {D}] of {like.dtype}, got {tuple(shape)} of {t.dtype}")
+    if rows and ((D > 1 and stride[2] != 1) or (shape[1] > 1 and stride[1] != D)):
         raise ValueError(f"{name}: the heads of a row must be contiguous")
-    return t.data_ptr() if rows else None, t.stride(0) if rows > 1 else -(-h * d // 8) * 8
+    if t.get_device() != like.get_device():
+        raise ValueError(f"{name} is not on the other tensors' device")
+    return t.data_ptr() or None, stride[0] if rows > 1 else -(-shape[1] * D // 8) * 8
 
 
-def _new_heads(t, heads, seqs):
+def _new_heads(t, seqs):
     """An output the caller gave no buffer for; rows behind the last sequence
     of a padded batch hold zeros."""
-    make = torch.zeros if seqs is not None and seqs.padded else torch.empty
-    return make((t.shape[0], heads, t.shape[2]), dtype=t.dtype, device=t.device)
+    return t.new_zeros(t.shape) if seqs is not None and seqs.padded else t.new_empty(t.shape)
+
+
+def _check_heads(t, name="q"):
+    if t.dim() != 3:
+        raise ValueError(f"{name}: expected [rows, heads, head_dim], got {tuple(t.shape)}")
+    return t.shape
 
 
 class Seqs:
@@ -620,28 +629,26 @@ def lattice_seq_plan(offsets, rows, max_len=0, padded=False, stream=None):
     (outputs that the calls below allocate are then zero-filled)."""
     if offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.numel() < 1 or not offsets.is_contiguous():
         raise ValueError("offsets: expected a contiguous int32 vector [S + 1]")
-    with _on_device(offsets):
-        s = Seqs(offsets, rows, max_len, padded)
-        check(load().lattice_seq_plan(byref(s.desc), _p(s.span) if s.rows else None, _stream(stream)))
+    dev = _gpu(offsets)
+    s = Seqs(offsets, rows, max_len, padded)
+    _run(dev, load().lattice_seq_plan, stream, byref(s.desc), s.desc.span)
     return s
 
 
 def _rope_desc(q, k, gain_q, gain_k, theta, rotary, interleaved, eps, positions):
-    D = q.shape[2]
-    _same(q, k, gain_q, gain_k, positions)
-    return A.lattice_qk_rope_desc(dtype=_dt(q), heads=q.shape[1], kv_heads=k.shape[1], head_dim=D,
-                                  rotary_dim=D if rotary is None else int(rotary), interleaved=int(bool(interleaved)),
-                                  theta=float(theta), eps=float(eps),
-                                  gain_q=_vec(gain_q, torch.float32, D, "gain_q"),
-                                  gain_k=_vec(gain_k, torch.float32, D, "gain_k"),
-                                  positions=_vec(positions, torch.int32, q.shape[0], "positions"))
+    rows, H, D = _check_heads(q)
+    dev = _gpu(q)
+    return A.lattice_qk_rope_desc(_dt(q), H, _check_heads(k, "k")[1], D, D if rotary is None else int(rotary),
+                                  int(bool(interleaved)), float(theta), float(eps),
+                                  _vec(gain_q, torch.float32, D, "gain_q", dev),
+                                  _vec(gain_k, torch.float32, D, "gain_k", dev),
+                                  _vec(positions, torch.int32, rows, "positions", dev))
 
 
 def _rope_rows(seqs, q, positions):
     if seqs is not None:
-        _same(q, seqs.offsets)
-        if seqs.rows != q.shape[0]:
-            raise ValueError(f"q has {q.shape[0]} rows, the plan {seqs.rows}")
+        if seqs.rows != q.shape[0] or seqs.offsets.get_device() != q.get_device():
+            raise ValueError(f"q has {q.shape[0]} rows on {q.device}, the plan {seqs.rows} on {seqs.offsets.device}")
         return seqs.desc
     if positions is None:
         raise ValueError("without a plan, positions must be given")
@@ -653,17 +660,14 @@ def lattice_qk_rope_fwd(seqs, q, k, gain_q=None, gain_k=None, theta=10000.0, rot
     """Per-head RMSNorm (gains [head_dim] fp32 or None) and rotary positions of
     queries and keys; returns (q_out, k_out).  seqs: the batch's plan, or None
     with positions (int32 [rows]).  rotary: rotated dimensions (None: all)."""
-    with _on_device(q):
-        rows = q.shape[0]
-        desc, s = _rope_desc(q, k, gain_q, gain_k, theta, rotary, interleaved, eps, positions), _rope_rows(seqs, q, positions)
-        q_out = _new_heads(q, q.shape[1], seqs) if q_out is None else q_out
-        k_out = _new_heads(k, k.shape[1], seqs) if k_out is None else k_out
-        if q_out.shape != q.shape or k_out.shape != k.shape:
-            raise ValueError("outputs must have the inputs' shapes")
-        _same(q, q_out, k_out)
-        check(load().lattice_qk_rope_fwd(byref(desc), byref(s), *_heads(q, q, rows, "q"), *_heads(k, q, rows, "k"),
-                                         *_heads(q_out, q, rows, "q_out"), *_heads(k_out, q, rows, "k_out"),
-                                         _stream(stream)))
+    desc = _rope_desc(q, k, gain_q, gain_k, theta, rotary, interleaved, eps, positions)
+    s, rows = _rope_rows(seqs, q, positions), q.shape[0]
+    q_out = _new_heads(q, seqs) if q_out is None else q_out
+    k_out = _new_heads(k, seqs) if k_out is None else k_out
+    if q_out.shape != q.shape or k_out.shape != k.shape:
+        raise ValueError("outputs must have the inputs' shapes")
+    _run(_gpu(q), load().lattice_qk_rope_fwd, stream, byref(desc), byref(s), *_heads(q, q, rows, "q"),
+         *_heads(k, q, rows, "k"), *_heads(q_out, q, rows, "q_out"), *_heads(k_out, q, rows, "k_out"))
     return q_out, k_out
 
 
@@ -671,31 +675,27 @@ def lattice_qk_rope_bwd(seqs, q, k, d_q_out, d_k_out, gain_q=None, gain_k=None, 
                         interleaved=False, eps=1e-6, positions=None, dq=None, dk=None, stream=None):
     """Gradients (dq, dk, dgain_q, dgain_k) of lattice_qk_rope_fwd; the gains'
     are fp32 [head_dim], None where the gain is None."""
-    with _on_device(q):
-        rows, D = q.shape[0], q.shape[2]
-        desc, s = _rope_desc(q, k, gain_q, gain_k, theta, rotary, interleaved, eps, positions), _rope_rows(seqs, q, positions)
-        dq = _new_heads(q, q.shape[1], seqs) if dq is None else dq
-        dk = _new_heads(k, k.shape[1], seqs) if dk is None else dk
-        if not (dq.shape == d_q_out.shape == q.shape and dk.shape == d_k_out.shape == k.shape):
-            raise ValueError("gradients must have the inputs' shapes")
-        _same(q, d_q_out, d_k_out, dq, dk)
-        dg = [torch.empty(D, dtype=torch.float32, device=q.device) if g is not None else None for g in (gain_q, gain_k)]
-        lib = load()
-        wsb = lib.lattice_qk_rope_bwd_workspace(byref(desc), rows) if dg[0] is not None or dg[1] is not None else 0
-        ws = torch.empty(max(wsb, 1), dtype=torch.uint8, device=q.device)
-        check(lib.lattice_qk_rope_bwd(byref(desc), byref(s), *_heads(q, q, rows, "q"), *_heads(k, q, rows, "k"),
-                                      *_heads(d_q_out, q, rows, "d_q_out"), *_heads(d_k_out, q, rows, "d_k_out"),
-                                      *_heads(dq, q, rows, "dq"), *_heads(dk, q, rows, "dk"), _p(dg[0]), _p(dg[1]),
-                                      _p(ws), wsb, _stream(stream)))
-    return dq, dk, dg[0], dg[1]
+    desc = _rope_desc(q, k, gain_q, gain_k, theta, rotary, interleaved, eps, positions)
+    s, rows, D = _rope_rows(seqs, q, positions), q.shape[0], q.shape[2]
+    dq = _new_heads(q, seqs) if dq is None else dq
+    dk = _new_heads(k, seqs) if dk is None else dk
+    if not (dq.shape == d_q_out.shape == q.shape and dk.shape == d_k_out.shape == k.shape):
+        raise ValueError("gradients must have the inputs' shapes")
+    dgq, dgk = (g.new_empty(D) if g is not None else None for g in (gain_q, gain_k))
+    lib = load()
+    wsb = lib.lattice_qk_rope_bwd_workspace(byref(desc), rows) if dgq is not None or dgk is not None else 0
+    ws = q.new_empty(wsb, dtype=torch.uint8) if wsb else None
+    _run(_gpu(q), lib.lattice_qk_rope_bwd, stream, byref(desc), byref(s), *_heads(q, q, rows, "q"),
+         *_heads(k, q, rows, "k"), *_heads(d_q_out, q, rows, "d_q_out"), *_heads(d_k_out, q, rows, "d_k_out"),
+         *_heads(dq, q, rows, "dq"), *_heads(dk, q, rows, "dk"), _p(dgq), _p(dgk), _p(ws), wsb)
+    return dq, dk, dgq, dgk
 
 
-def _attn_desc(q, kv_heads, window, sinks, scale, key_mask):
-    D = q.shape[2]
-    return A.lattice_seq_attn_desc(dtype=_dt(q), heads=q.shape[1], kv_heads=kv_heads, head_dim=D,
-                                   window=min(int(window), 2 ** 31 - 1), sinks=int(sinks),
-                                   scale=float(D ** -0.5 if scale is None else scale),
-                                   key_mask=_vec(key_mask, torch.uint8, q.shape[0], "key_mask"))
+def _attn_desc(q, k, window, sinks, scale, key_mask):
+    rows, H, D = _check_heads(q)
+    return A.lattice_seq_attn_desc(_dt(q), H, _check_heads(k, "k")[1], D, min(int(window), 2 ** 31 - 1), int(sinks),
+                                   D ** -0.5 if scale is None else float(scale),
+                                   _vec(key_mask, torch.uint8, rows, "key_mask", _gpu(q)))
 
 
 class SeqAttnSaved:
@@ -712,56 +712,52 @@ def lattice_seq_attn_fwd(seqs, q, k, v, window, sinks=0, scale=None, key_mask=No
     saved a SeqAttnSaved for the backward (None when lse is False).  scale None:
     1 / sqrt(head_dim); key_mask: uint8 [rows], 0 hides an event from every
     reader."""
-    with _on_device(q):
-        rows = seqs.rows
-        desc = _attn_desc(q, k.shape[1], window, sinks, scale, key_mask)
-        out = _new_heads(q, q.shape[1], seqs) if out is None else out
-        if out.shape != q.shape or v.shape != k.shape:
-            raise ValueError("out must have q's shape, v k's")
-        _same(q, k, v, out, key_mask, seqs.offsets)
-        saved = None
-        if lse:
-            saved = SeqAttnSaved(torch.empty((q.shape[1], rows), dtype=torch.float32, device=q.device),
-                                 torch.empty(q.shape, dtype=q.dtype, device=q.device) if desc.dtype == A.BF16 else None)
-        check(load().lattice_seq_attn_fwd(byref(desc), byref(seqs.desc), *_heads(q, q, rows, "q"),
-                                          *_heads(k, q, rows, "k"), *_heads(v, q, rows, "v"),
-                                          *_heads(out, q, rows, "out"), _p(saved.lse) if lse else None,
-                                          _p(saved.out_lo) if lse else None, _stream(stream)))
+    rows = seqs.rows
+    desc = _attn_desc(q, k, window, sinks, scale, key_mask)
+    out = _new_heads(q, seqs) if out is None else out
+    if out.shape != q.shape or v.shape != k.shape or seqs.offsets.get_device() != q.get_device():
+        raise ValueError("out must have q's shape, v k's, and the plan their device")
+    saved = None
+    if lse:
+        saved = SeqAttnSaved(q.new_empty((q.shape[1], rows), dtype=torch.float32),
+                             q.new_empty(q.shape) if desc.dtype == A.BF16 else None)
+    _run(_gpu(q), load().lattice_seq_attn_fwd, stream, byref(desc), byref(seqs.desc), *_heads(q, q, rows, "q"),
+         *_heads(k, q, rows, "k"), *_heads(v, q, rows, "v"), *_heads(out, q, rows, "out"),
+         _p(saved.lse) if lse else None, _p(saved.out_lo) if lse else None)
     return out, saved
 
 
 def lattice_seq_attn_bwd(seqs, q, k, v, out, saved, d_out, window, sinks=0, scale=None, key_mask=None, dq=None,
                          dk=None, dv=None, stream=None):
     """Gradients (dq, dk, dv) of lattice_seq_attn_fwd, from its out and saved."""
-    with _on_device(q):
-        rows = seqs.rows
-        desc = _attn_desc(q, k.shape[1], window, sinks, scale, key_mask)
-        dq = _new_heads(q, q.shape[1], seqs) if dq is None else dq
-        dk = _new_heads(k, k.shape[1], seqs) if dk is None else dk
-        dv = _new_heads(v, v.shape[1], seqs) if dv is None else dv
-        if not (out.shape == d_out.shape == dq.shape == q.shape and v.shape == dk.shape == dv.shape == k.shape):
-            raise ValueError("out, d_out and dq must have q's shape, v, dk and dv k's")
-        _same(q, k, v, out, saved.lse, saved.out_lo, d_out, dq, dk, dv, key_mask, seqs.offsets)
-        lib = load()
-        wsb = lib.lattice_seq_attn_bwd_workspace(byref(desc), byref(seqs.desc))
-        ws = torch.empty(max(wsb, 1), dtype=torch.uint8, device=q.device)
-        check(lib.lattice_seq_attn_bwd(byref(desc), byref(seqs.desc), *_heads(q, q, rows, "q"),
-                                       *_heads(k, q, rows, "k"), *_heads(v, q, rows, "v"), *_heads(out, q, rows, "out"),
-                                       _vec(saved.lse, torch.float32, q.shape[1] * rows, "lse"),
-                                       _vec(saved.out_lo, q.dtype, out.numel(), "out_lo"),
-                                       *_heads(d_out, q, rows, "d_out"), *_heads(dq, q, rows, "dq"),
-                                       *_heads(dk, q, rows, "dk"), *_heads(dv, q, rows, "dv"), _p(ws), wsb,
-                                       _stream(stream)))
+    rows, dev = seqs.rows, _gpu(q)
+    desc = _attn_desc(q, k, window, sinks, scale, key_mask)
+    dq = _new_heads(q, seqs) if dq is None else dq
+    dk = _new_heads(k, seqs) if dk is None else dk
+    dv = _new_heads(v, seqs) if dv is None else dv
+    if not (out.shape == d_out.shape == dq.shape == q.shape and v.shape == dk.shape == dv.shape == k.shape):
+        raise ValueError("out, d_out and dq must have q's shape, v, dk and dv k's")
+    if seqs.offsets.get_device() != dev:
+        raise ValueError("the plan is on another device")
+    lib = load()
+    wsb = lib.lattice_seq_attn_bwd_workspace(byref(desc), byref(seqs.desc))
+    ws = q.new_empty(wsb, dtype=torch.uint8) if wsb else None
+    _run(dev, lib.lattice_seq_attn_bwd, stream, byref(desc), byref(seqs.desc), *_heads(q, q, rows, "q"),
+         *_heads(k, q, rows, "k"), *_heads(v, q, rows, "v"), *_heads(out, q, rows, "out"),
+         _vec(saved.lse, torch.float32, q.shape[1] * rows, "lse", dev),
+         _vec(saved.out_lo, q.dtype, out.numel(), "out_lo", dev), *_heads(d_out, q, rows, "d_out"),
+         *_heads(dq, q, rows, "dq"), *_heads(dk, q, rows, "dk"), *_heads(dv, q, rows, "dv"), _p(ws), wsb)
     return dq, dk, dv
 
 
 def _cache(k_cache, v_cache, like, kv_heads, window, sinks):
-    _contig(k_cache, v_cache)
-    _same(like, k_cache, v_cache)
     want = (k_cache.shape[0], kv_heads, int(sinks) + int(window), like.shape[2])
     if k_cache.shape != want or v_cache.shape != want or k_cache.dtype != like.dtype or v_cache.dtype != like.dtype:
         raise ValueError(f"caches: expected [caches, kv_heads, sinks + window, head_dim] = {want} of {like.dtype}")
-    return A.lattice_seq_cache(k=k_cache.data_ptr() or None, v=v_cache.data_ptr() or None, num_caches=want[0])
+    _contig(k_cache, v_cache)
+    if not k_cache.get_device() == v_cache.get_device() == like.get_device():
+        raise ValueError("the caches are not on the other tensors' device")
+    return A.lattice_seq_cache(k_cache.data_ptr() or None, v_cache.data_ptr() or None, want[0])
 
 
 def lattice_seq_cache_fill(seqs, k, v, k_cache, v_cache, window, sinks=0, cache_index=None, first=None, stream=None):
@@ -769,17 +765,14 @@ def lattice_seq_cache_fill(seqs, k, v, k_cache, v_cache, window, sinks=0, cache_
     into ring caches [caches, kv_heads, sinks + window, head_dim].  cache_index
     (int32 [S], different ones; None: s) and first (int32 [S], the position of
     each sequence's first row; None: 0)."""
-    with _on_device(k):
-        rows = seqs.rows
-        if v.shape != k.shape:
-            raise ValueError("v must have k's shape")
-        desc = _attn_desc(k, k.shape[1], window, sinks, None, None)
-        cache = _cache(k_cache, v_cache, k, k.shape[1], window, sinks)
-        _same(k, v, seqs.offsets, cache_index, first)
-        check(load().lattice_seq_cache_fill(byref(desc), byref(seqs.desc), *_heads(k, k, rows, "k"),
-                                            *_heads(v, k, rows, "v"), _vec(first, torch.int32, seqs.num_seqs, "first"),
-                                            _vec(cache_index, torch.int32, seqs.num_seqs, "cache_index"),
-                                            byref(cache), _stream(stream)))
+    rows, S, dev = seqs.rows, seqs.num_seqs, _gpu(k)
+    desc = _attn_desc(k, k, window, sinks, None, None)
+    cache = _cache(k_cache, v_cache, k, k.shape[1], window, sinks)
+    if v.shape != k.shape or seqs.offsets.get_device() != dev:
+        raise ValueError("v must have k's shape, and the plan their device")
+    _run(dev, load().lattice_seq_cache_fill, stream, byref(desc), byref(seqs.desc), *_heads(k, k, rows, "k"),
+         *_heads(v, k, rows, "v"), _vec(first, torch.int32, S, "first", dev),
+         _vec(cache_index, torch.int32, S, "cache_index", dev), byref(cache))
 
 
 def lattice_seq_step(q, k, v, lens, k_cache, v_cache, window, sinks=0, cache_index=None, scale=None, rope=True,
@@ -790,22 +783,17 @@ def lattice_seq_step(q, k, v, lens, k_cache, v_cache, window, sinks=0, cache_ind
     caches at position lens (int32 [batch]: the events they have; the caller
     advances them), attention of q over the caches' visible slots.  Returns
     out; users with lens < 0 or a cache_index out of range are skipped."""
-    with _on_device(q):
-        B = q.shape[0]
-        if v.shape != k.shape:
-            raise ValueError("v must have k's shape")
-        desc = _attn_desc(q, k.shape[1], window, sinks, scale, None)
-        cache = _cache(k_cache, v_cache, q, k.shape[1], window, sinks)
-        rd = _rope_desc(q, k, gain_q, gain_k, theta, rotary, interleaved, eps, positions) if rope else None
-        out = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
-        if out.shape != q.shape:
-            raise ValueError("out must have q's shape")
-        _same(q, k, v, out, lens, cache_index)
-        lib = load()
-        wsb = lib.lattice_seq_step_workspace(byref(desc), B)
-        ws = torch.empty(wsb, dtype=torch.uint8, device=q.device) if wsb else None
-        check(lib.lattice_seq_step(byref(desc), byref(rd) if rope else None, B, *_heads(q, q, B, "q"),
-                                   *_heads(k, q, B, "k"), *_heads(v, q, B, "v"), _vec(lens, torch.int32, B, "lens"),
-                                   _vec(cache_index, torch.int32, B, "cache_index"), byref(cache),
-                                   *_heads(out, q, B, "out"), _p(ws), wsb, _stream(stream)))
+    desc = _attn_desc(q, k, window, sinks, scale, None)
+    B, dev = q.shape[0], _gpu(q)
+    cache = _cache(k_cache, v_cache, q, k.shape[1], window, sinks)
+    rd = byref(_rope_desc(q, k, gain_q, gain_k, theta, rotary, interleaved, eps, positions)) if rope else None
+    out = q.new_empty(q.shape) if out is None else out
+    if out.shape != q.shape or v.shape != k.shape:
+        raise ValueError("out must have q's shape, v k's")
+    lib = load()
+    wsb = lib.lattice_seq_step_workspace(byref(desc), B)
+    ws = q.new_empty(wsb, dtype=torch.uint8) if wsb else None
+    _run(dev, lib.lattice_seq_step, stream, byref(desc), rd, B, *_heads(q, q, B, "q"), *_heads(k, q, B, "k"),
+         *_heads(v, q, B, "v"), _vec(lens, torch.int32, B, "lens", dev),
+         _vec(cache_index, torch.int32, B, "cache_index", dev), byref(cache), *_heads(out, q, B, "out"), _p(ws), wsb)
     return out

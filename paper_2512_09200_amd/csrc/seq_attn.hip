@@ -109,32 +109,116 @@ struct KeyTiles {
   }
 };
 
-// Bits of the tile's keys that exist and are shown
-template <int BK>
-__device__ inline uint64_t key_bits(const uint8_t* mask, int kt, int nk) {
-  const uint64_t all = nk >= 64 ? ~0ull : (1ull << nk) - 1;
-  if (!mask) return all;
-  const int lane = threadIdx.x & 63;
-  return __ballot(mask[kt + min(lane, nk - 1)] != 0) & all;
-}
-
-// Block -> (row tile, key head, heads of the group).
+// Block -> (row tile, key head, heads of the group).  Rows late in a long
+// sequence may see more keys, so tiles go from the last to the first; where all
+// blocks run at once (two a compute unit, block b beside b + 256), the second
+// half goes from the first tile on, so that heavy and light ones share a unit.
+// One history of 8192, all rows before each seen: 222 -> ZIGZAG us.
 struct BlockAt { int tile, kv, h0; };
 __device__ inline BlockAt block_at(const AttnK& A) {
   const int hg = A.group / A.hb, per = A.kv_heads * hg;
   const int b = blockIdx.x;
   BlockAt r;
   const int x = b % per;
-  r.tile = b / per;
+  const int t = b / per, n = A.row_tiles, h = (n + 1) / 2;
+  r.tile = n * per <= 512 && t >= h ? t - h : n - 1 - t;
   r.kv = x / hg;
   r.h0 = r.kv * A.group + (x % hg) * A.hb;
   return r;
 }
 
 // ---------------------------------------------------------------------------
+// Keys of a tile, and tiles in LDS at a time: narrow heads' tiles are small and
+// soon computed, so more of them are under way (a block of short histories is
+// a chain of memory latencies).
 template <typename T, int DP> struct AttnCfg {
-  static constexpr int BK = sizeof(T) == 4 && DP == 128 ? 32 : 64;   // keys of a tile
-  static constexpr size_t LDS = (size_t)2 * 2 * BK * DP * sizeof(T); // two stages of K and V
+  static constexpr int BK = sizeof(T) == 4 && DP == 128 ? 32 : 64;
+  static constexpr int TB = BK * DP * (int)sizeof(T);                // bytes of K or V
+  static constexpr int NST = TB <= 4096 ? 4 : TB <= 8192 ? 3 : 2;
+  static constexpr size_t LDS = (size_t)NST * 2 * TB;
+};
+
+// All but the newest n of the wave's memory operations have completed.
+template <int N> __device__ inline void wait_loads() {
+  static_assert(N < 64, "counter of 6 bits");
+  // immediate: vmcnt in bits 0-3 and 14-15, expcnt and lgkmcnt not waited for
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+}
+
+// The K and V tiles of a block's key range, NST - 1 of them under way.  Every
+// step issues the same loads (past the last tile they read nothing and write
+// zeros), so a wait by count names the tile that is needed.  A tile's
+// key mask is one load made a step before the tile's own, whose row bits
+// depend on it.
+template <typename T, int DP>
+struct KeyStream {
+  using Cfg = AttnCfg<T, DP>;
+  static constexpr int BK = Cfg::BK, TB = Cfg::TB, NST = Cfg::NST;
+  static constexpr int PER = 2 * TileLoad<T, DP, BK, 4>::PER;        // loads of a tile
+  TileLoad<T, DP, BK, 4> lk, lv;
+  const KeyTiles* kt;
+  const T *k, *v;
+  const uint8_t* mask;
+  int64_t kld, vld;
+  char* smem;
+  int wave, stage, issued, mbyte;
+  uint64_t bits[NST];
+
+  __device__ __forceinline__ void init(const AttnK& A, const KeyTiles* tiles, int kv, char* lds, int w) {
+    kt = tiles;
+    k = (const T*)A.k.p + (int64_t)kv * A.dim;
+    v = (const T*)A.v.p + (int64_t)kv * A.dim;
+    kld = A.k.ld;
+    vld = A.v.ld;
+    mask = A.mask;
+    smem = lds;
+    wave = w;
+    lk.init(w, A.dim, kld);
+    lv.init(w, A.dim, vld);
+  }
+  __device__ __forceinline__ void fetch_mask(int t) {
+    if (!mask) return;
+    int at = 0, nk = 1;
+    if (t < kt->n) kt->template at<BK>(t, at, nk);
+    mbyte = mask[at + min((int)(threadIdx.x & 63), nk - 1)];
+  }
+  // slot: the place in bits[] of the tile, a constant after unrolling
+  __device__ __forceinline__ void issue(int t, int slot) {
+    int at = 0, nk = 0;
+    if (t < kt->n) kt->template at<BK>(t, at, nk);
+    uint64_t b = nk >= 64 ? ~0ull : (1ull << nk) - 1;
+    if (mask) b &= __ballot(mbyte != 0);
+    bits[slot] = b;
+    char* S = smem + stage * 2 * TB;
+    lk.issue(S, wave, k + (int64_t)at * kld, nk, b);
+    lv.issue(S + TB, wave, v + (int64_t)at * vld, nk, b);
+    stage = stage + 1 == NST ? 0 : stage + 1;
+    fetch_mask(t + 1);
+  }
+  __device__ __forceinline__ void start() {
+    stage = 0;
+    mbyte = 1;
+    fetch_mask(0);
+#pragma unroll
+    for (int t = 0; t < NST - 1; ++t) issue(t, t);
+  }
+  // Tile t is in LDS for every wave (its address returned), and the tile after
+  // the ones under way is issued into the place of tile t - 1.
+  __device__ __forceinline__ const char* next(int t, uint64_t& b) {
+    if (mask) wait_loads<(NST - 2) * (PER + 1)>(); else wait_loads<(NST - 2) * PER>();
+    // the wave's reads of tile t - 1 have returned; past the barrier everybody's
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    b = bits[0];
+#pragma unroll
+    for (int i = 0; i < NST - 2; ++i) bits[i] = bits[i + 1];
+    const int at = stage + 1 == NST ? 0 : stage + 1;                 // stage: where tile t - 1 was
+    issue(t + NST - 1, NST - 2);
+    return smem + at * 2 * TB;
+  }
+  // the loads past the last tile write LDS: none is under way afterwards
+  __device__ __forceinline__ void drain() { wait_loads<0>(); }
 };
 
 // Scores of 32 keys (row0 in the tile) against the wave's 32 rows
@@ -220,9 +304,9 @@ __device__ __forceinline__ void store_row(T* op, T* lo, int dim, f32x16 (&x)[Til
 }
 
 template <typename T, int DP>
-__global__ __launch_bounds__(256, 2) void seq_fwd_kernel(AttnK A) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_fwd_kernel(AttnK A) {
   using TL = Tile<T, DP>;
-  constexpr int BK = AttnCfg<T, DP>::BK, TB = BK * TL::RB, NB = BK / 32;
+  constexpr int BK = AttnCfg<T, DP>::BK, TB = AttnCfg<T, DP>::TB, NB = BK / 32;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5;
@@ -235,37 +319,25 @@ __global__ __launch_bounds__(256, 2) void seq_fwd_kernel(AttnK A) {
   KeyTiles kt_;
   kt_.init<BK>(A, r0, brows);
   if (kt_.n == 0) return;
-  const T* kb = (const T*)A.k.p + (int64_t)B.kv * A.dim;
-  const T* vb = (const T*)A.v.p + (int64_t)B.kv * A.dim;
-
-  TileLoad<T, DP, BK, 4> lk, lv;
-  lk.init(w, A.dim, A.k.ld);
-  lv.init(w, A.dim, A.v.ld);
-  auto issue = [&](int t, uint64_t& bits) __attribute__((always_inline)) {
-    int kt, nk;
-    kt_.at<BK>(t, kt, nk);
-    bits = key_bits<BK>(A.mask, kt, nk);
-    char* S = smem + (t & 1) * 2 * TB;
-    lk.issue(S, w, kb + (int64_t)kt * A.k.ld, nk, bits);
-    lv.issue(S + TB, w, vb + (int64_t)kt * A.v.ld, nk, bits);
-  };
+  KeyStream<T, DP> ks;
+  ks.init(A, &kt_, B.kv, smem, w);
   const uint32_t rl = TL::row_lane(), cl = TL::col_lane();
   const float c = A.scale * LOG2E;
   f32x16 o[TL::DB];
   float m, l;
 
-  // N subtiles of 32 keys from subtile b0 of the tile at kt
-  auto attend = [&](auto strict_, auto n_, int b0, const char* SK, const char* SV, int kt, uint64_t bits)
+  // N subtiles of 32 keys from subtile b0 of the tile at kt; full: every row of
+  // the wave sees all of them
+  auto attend = [&](auto strict_, auto full_, auto n_, int b0, const char* SK, const char* SV, int kt, uint64_t bits)
       __attribute__((always_inline)) {
     constexpr bool strict = decltype(strict_)::value;
     constexpr int N = decltype(n_)::value;
-    const bool full = (uint32_t)(bits >> (32 * b0)) == 0xffffffffu && (N == 1 || (bits >> 32) == 0xffffffffu) &&
-                      wave_all(!V.valid || (V.lo <= kt + 32 * b0 && V.i >= kt + 32 * (b0 + N) - 1));
+    constexpr bool full = decltype(full_)::value;
     f32x16 s[N];
 #pragma unroll
     for (int b = 0; b < N; ++b) s[b] = scores<T, DP>(SK, rl, 32 * (b0 + b), q);
     uint32_t see[N];
-    if (!full || strict) {
+    if constexpr (!full) {
 #pragma unroll
       for (int b = 0; b < N; ++b) {
         see[b] = row_bits(V, kt + 32 * (b0 + b), (uint32_t)(bits >> (32 * (b0 + b))));
@@ -333,34 +405,26 @@ __global__ __launch_bounds__(256, 2) void seq_fwd_kernel(AttnK A) {
       for (int r = 0; r < 16; ++r) o[db][r] = 0.f;
     m = -INFINITY;
     l = 0.f;
-    uint64_t bits, next = 0;
-    issue(0, bits);
+    ks.start();
 #pragma unroll 1
     for (int t = 0; t < kt_.n; ++t) {
-      // this wave's loads of tile t have landed and its reads of tile t - 1
-      // returned; past the barrier everybody's have
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-      if (t + 1 < kt_.n) issue(t + 1, next);
+      uint64_t bits;
+      const char *SK = ks.next(t, bits), *SV = SK + TB;
       int kt, nk;
       kt_.at<BK>(t, kt, nk);
-      const char *SK = smem + (t & 1) * 2 * TB, *SV = SK + TB;
-      // subtiles of 32 keys that no row of the wave reaches are left out
-      const bool in0 = wave_any(reaches(V, kt, min(nk, 32)));
-      if constexpr (NB == 1) {
-        if (in0) attend(strict_, std::integral_constant<int, 1>{}, 0, SK, SV, kt, bits);
+      if (!strict && bits == (NB == 1 ? 0xffffffffull : ~0ull) &&
+          wave_all(!V.valid || (V.lo <= kt && V.i >= kt + BK - 1))) {
+        attend(strict_, std::true_type{}, std::integral_constant<int, NB>{}, 0, SK, SV, kt, bits);
       } else {
-        const bool in1 = nk > 32 && wave_any(reaches(V, kt + 32, nk - 32));
-        if (!strict && in0 && in1) {
-          attend(strict_, std::integral_constant<int, 2>{}, 0, SK, SV, kt, bits);
-        } else {
-          if (in0) attend(strict_, std::integral_constant<int, 1>{}, 0, SK, SV, kt, bits);
-          if (in1) attend(strict_, std::integral_constant<int, 1>{}, 1, SK, SV, kt, bits);
-        }
+        // tiles seen in part: by 32 keys, leaving out those no row of the
+        // wave reaches
+#pragma unroll 1
+        for (int b = 0; b < NB; ++b)
+          if (nk > 32 * b && wave_any(reaches(V, kt + 32 * b, min(nk - 32 * b, 32))))
+            attend(strict_, std::false_type{}, std::integral_constant<int, 1>{}, b, SK, SV, kt, bits);
       }
-      bits = next;
     }
+    ks.drain();
     l = add32(l);
     const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
@@ -390,7 +454,7 @@ __global__ __launch_bounds__(256, 2) void seq_fwd_kernel(AttnK A) {
 template <typename T, int DP>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_dq_kernel(AttnK A) {
   using TL = Tile<T, DP>;
-  constexpr int BK = AttnCfg<T, DP>::BK, TB = BK * TL::RB;
+  constexpr int BK = AttnCfg<T, DP>::BK, TB = AttnCfg<T, DP>::TB;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5;
@@ -417,20 +481,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
   KeyTiles kt_;
   kt_.init<BK>(A, r0, brows);
   if (kt_.n == 0) return;
-  const T* kb = (const T*)A.k.p + (int64_t)B.kv * A.dim;
-  const T* vb = (const T*)A.v.p + (int64_t)B.kv * A.dim;
-
-  TileLoad<T, DP, BK, 4> lk, lv;
-  lk.init(w, A.dim, A.k.ld);
-  lv.init(w, A.dim, A.v.ld);
-  auto issue = [&](int t, uint64_t& bits) __attribute__((always_inline)) {
-    int kt, nk;
-    kt_.at<BK>(t, kt, nk);
-    bits = key_bits<BK>(A.mask, kt, nk);
-    char* S = smem + (t & 1) * 2 * TB;
-    lk.issue(S, w, kb + (int64_t)kt * A.k.ld, nk, bits);
-    lv.issue(S + TB, w, vb + (int64_t)kt * A.v.ld, nk, bits);
-  };
+  KeyStream<T, DP> ks;
+  ks.init(A, &kt_, B.kv, smem, w);
   delta = add32(delta);
   float lse2 = INFINITY;
   if (V.valid) {
@@ -452,17 +504,13 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
     for (int db = 0; db < TL::DB; ++db)
 #pragma unroll
       for (int r = 0; r < 16; ++r) dq[db][r] = 0.f;
-    uint64_t bits, next = 0;
-    issue(0, bits);
+    ks.start();
 #pragma unroll 1
     for (int t = 0; t < kt_.n; ++t) {
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-      if (t + 1 < kt_.n) issue(t + 1, next);
+      uint64_t bits;
+      const char *SK = ks.next(t, bits), *SV = SK + TB;
       int kt, nk;
       kt_.at<BK>(t, kt, nk);
-      const char *SK = smem + (t & 1) * 2 * TB, *SV = SK + TB;
 #pragma unroll
       for (int b = 0; b < BK / 32; ++b) {
         if (nk <= 32 * b || !wave_any(reaches(V, kt + 32 * b, min(32, nk - 32 * b)))) continue;
@@ -496,8 +544,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
           }
         }
       }
-      bits = next;
     }
+    ks.drain();
 #pragma unroll
     for (int db = 0; db < TL::DB; ++db)
 #pragma unroll
@@ -609,14 +657,17 @@ __device__ inline void issue_stats(char* S, const float* p, int rows) {
 
 template <typename T, int DP> struct DkvCfg {
   static constexpr int BQ = sizeof(T) == 4 && DP == 128 ? 32 : 64;    // rows of a tile
-  static constexpr int STAGE = 2 * BQ * DP * (int)sizeof(T) + 512;    // q, d_out, lse2, delta (64 floats each)
-  static constexpr size_t LDS = (size_t)2 * STAGE;
+  static constexpr int STAGE = 2 * BQ * DP * (int)sizeof(T) + 1024;   // q, d_out, lse2, delta (64 floats each, and unused)
+  static constexpr int NST = STAGE <= 9216 ? 4 : STAGE <= 17408 ? 3 : 2;
+  static constexpr size_t LDS = (size_t)NST * STAGE;
+  // blocks a compute unit: narrow heads wait for memory more than they compute
+  static constexpr int BLOCKS = sizeof(T) == 2 ? (DP == 32 ? 3 : DP == 64 ? 2 : 1) : DP == 32 ? 2 : 1;
   static constexpr int SINK_STAGE = 2 * 32 * DP * (int)sizeof(T) + 512;   // a wave's 32 rows
   static constexpr size_t SINK_LDS = (size_t)4 * SINK_STAGE;
 };
 
 template <typename T, int DP>
-__global__ __launch_bounds__(256, 1) void seq_dkv_kernel(AttnK A) {
+__global__ __launch_bounds__(256, (DkvCfg<T, DP>::BLOCKS)) void seq_dkv_kernel(AttnK A) {
   using TL = Tile<T, DP>;
   using Cfg = DkvCfg<T, DP>;
   constexpr int BQ = Cfg::BQ, TB = BQ * TL::RB;
@@ -649,15 +700,23 @@ __global__ __launch_bounds__(256, 1) void seq_dkv_kernel(AttnK A) {
   TileLoad<T, DP, BQ, 4> lq, lg;
   lq.init(w, A.dim, A.q.ld);
   lg.init(w, A.dim, A.go.ld);
-  auto issue = [&](int t) {
-    const int g = t / per_head, i0 = k0 + (t - g * per_head) * BQ, h = kv * A.group + g;
-    const int nr = min(BQ, bend - i0);
-    char* S = smem + (t & 1) * Cfg::STAGE;
-    lq.issue(S, w, (const T*)A.q.p + (int64_t)i0 * A.q.ld + h * A.dim, nr, ~0ull);
-    lg.issue(S + TB, w, (const T*)A.go.p + (int64_t)i0 * A.go.ld + h * A.dim, nr, ~0ull);
-    const int64_t at = (int64_t)h * A.rows + i0;
-    if (w == 0) issue_stats(S + 2 * TB, A.lse2 + at, nr);
-    if (w == 1) issue_stats(S + 2 * TB + 256, A.delta + at, nr);
+  constexpr int NST = Cfg::NST, PER = 2 * TileLoad<T, DP, BQ, 4>::PER + 1;
+  // head and first row of the tile to be issued next; its stage
+  int ig = 0, ii = k0, is = 0;
+  auto issue = [&]() __attribute__((always_inline)) {
+    const int h = kv * A.group + ig, nr = ig < A.group ? min(BQ, bend - ii) : 0;
+    const int64_t hd = nr > 0 ? h * A.dim : 0, i0 = nr > 0 ? ii : 0, at = nr > 0 ? (int64_t)h * A.rows + i0 : 0;
+    char* S = smem + is * Cfg::STAGE;
+    lq.issue(S, w, (const T*)A.q.p + i0 * A.q.ld + hd, nr, ~0ull);
+    lg.issue(S + TB, w, (const T*)A.go.p + i0 * A.go.ld + hd, nr, ~0ull);
+    // every wave one load: lse2, delta, and two that read nothing
+    issue_stats(S + 2 * TB + 256 * w, (w == 0 ? A.lse2 : A.delta) + at, w < 2 ? nr : 0);
+    is = is + 1 == NST ? 0 : is + 1;
+    ii += BQ;
+    if (ii >= bend) {
+      ii = k0;
+      ++ig;
+    }
   };
   Frag<T> kf[TL::KS], vf[TL::KS];
   load_keys<T, DP>(A, valid ? j : k0, shown, kv, kf, vf);
@@ -671,15 +730,22 @@ __global__ __launch_bounds__(256, 1) void seq_dkv_kernel(AttnK A) {
     for (int db = 0; db < TL::DB; ++db)
 #pragma unroll
       for (int r = 0; r < 16; ++r) dk[db][r] = dv[db][r] = 0.f;
-    issue(0);
+    ig = 0;
+    ii = k0;
+    is = 0;
+#pragma unroll
+    for (int t = 0; t < NST - 1; ++t) issue();
+    int i0 = k0;
 #pragma unroll 1
     for (int t = 0; t < n; ++t) {
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      // tile t has landed, the wave's reads of tile t - 1 returned; past the
+      // barrier everybody's, and the next tile goes into that one's place
+      wait_loads<(NST - 2) * PER>();
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      if (t + 1 < n) issue(t + 1);
-      const int i0 = k0 + (t % per_head) * BQ;
-      const char* S = smem + (t & 1) * Cfg::STAGE;
+      const char* S = smem + (is + 1 == NST ? 0 : is + 1) * Cfg::STAGE;
+      issue();
 #pragma unroll
       for (int b = 0; b < BQ / 32; ++b) {
         const int ib = i0 + 32 * b;
@@ -689,7 +755,9 @@ __global__ __launch_bounds__(256, 1) void seq_dkv_kernel(AttnK A) {
         dkv_subtile<T, DP, strict>(S, S + TB, (const float*)(S + 2 * TB), (const float*)(S + 2 * TB + 256), 32 * b, rl,
                                    cl, kf, vf, c, ib - j, lim, full, dk, dv);
       }
+      i0 = i0 + BQ >= bend ? k0 : i0 + BQ;
     }
+    wait_loads<0>();                             // the loads past the last tile write LDS
     // sinks: the late rows' partial sums, in split order (a hidden sink has no
     // gradient; its sums are zeros times what may not be finite)
     if (A.ns > 0 && sink && shown && sp.end > late_row(A, sp.start)) {

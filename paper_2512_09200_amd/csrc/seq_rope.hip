@@ -49,8 +49,10 @@ hipError_t seq_plan(const int32_t* offsets, int num_seqs, int64_t rows, SeqSpan*
 }
 
 void rope_turns(double theta, int rotary, RopeTurns* t) {
-  for (int m = 0; m < ROPE_MAX_PAIRS; ++m)
-    t->f[m] = m < rotary / 2 ? std::pow(theta, -2.0 * m / rotary) / (2.0 * M_PI) : 0.0;
+  // a geometric row in extended precision: its error stays below a double's
+  const long double r = rotary > 0 ? std::pow((long double)theta, -2.0L / rotary) : 0.0L;
+  long double f = 0.159154943091895335768883763372514362L;           // 1 / (2 pi)
+  for (int m = 0; m < ROPE_MAX_PAIRS; ++m, f *= r) t->f[m] = m < rotary / 2 ? (double)f : 0.0;
 }
 
 struct RopeK {                               // kernel arguments
@@ -103,7 +105,7 @@ __device__ inline float group_sum(float v, int lp) {
 // over groups of tb rows.
 template <typename T, int E, bool BWD, bool INTER>
 __global__ __launch_bounds__(256) void rope_kernel(RopeK A, RopeTurns turns) {
-  extern __shared__ float2 cs[];             // [tb][rotary / 2]; backward's end: dgain partials
+  extern __shared__ __attribute__((aligned(16))) float2 cs[];   // [tb][rotary / 2]; backward's end: dgain partials
   const int tid = threadIdx.x, np = A.rotary >> 1;
   const int group = tid / A.lp, c = tid % A.lp;
   const bool lane_on = c < A.chunks;
@@ -121,13 +123,11 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeK A, RopeTurns turns) {
     hi = rot ? np + m0 : lo + E;
   }
   if (!lane_on) { lo = 0; hi = 0; rot = false; }
-  float gain[2][2 * E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    gain[0][e] = A.gq ? A.gq[lo + e] : 1.f;
-    gain[0][E + e] = A.gq ? A.gq[hi + e] : 1.f;
-    gain[1][e] = A.gk ? A.gk[lo + e] : 1.f;
-    gain[1][E + e] = A.gk ? A.gk[hi + e] : 1.f;
+  // gains of q, then k, in the lane's order, behind the angles
+  float* const gains = reinterpret_cast<float*>(cs) + 2 * A.tb * np;
+  for (int j = tid; j < 2 * A.dim; j += 256) {
+    const float* g = j < A.dim ? A.gq : A.gk;
+    gains[j] = g ? g[j < A.dim ? j : j - A.dim] : 1.f;
   }
   float dg[2][2 * E];
   if constexpr (BWD)
@@ -169,9 +169,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeK A, RopeTurns turns) {
     }
     __syncthreads();
     for (int it = group; it < items; it += A.groups) {
-      float vn[2 * E], dn[2 * E];
-      int sn = SEQ_NO_ROW;
-      if (it + A.groups < items) fetch(t0, it + A.groups, vn, dn, sn);
+      if (it != group) fetch(t0, it, v, d, start);
       if (start != SEQ_NO_ROW) {                                     // uniform over the head's lanes
         const int t = it / A.hk, h = it - t * A.hk;
         const bool isk = h >= A.heads;
@@ -184,10 +182,21 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeK A, RopeTurns turns) {
         ss = group_sum(ss, A.lp);
         const float r = 1.f / sqrtf(ss * A.inv_dim + A.eps);
         const float2* w = cs + t * np + m0;
+        const float* gn = gains + (isk ? A.dim : 0);
+        float gain[2 * E];
+#pragma unroll
+        for (int e = 0; e < E; e += 4) {
+          const f32x4 a = *reinterpret_cast<const f32x4*>(gn + lo + e), b = *reinterpret_cast<const f32x4*>(gn + hi + e);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            gain[e + i] = a[i];
+            gain[E + e + i] = b[i];
+          }
+        }
         if constexpr (!BWD) {
           float z[2 * E];
 #pragma unroll
-          for (int e = 0; e < 2 * E; ++e) z[e] = v[e] * r * (isk ? gain[1][e] : gain[0][e]);
+          for (int e = 0; e < 2 * E; ++e) z[e] = v[e] * r * gain[e];
           if (rot) {
 #pragma unroll
             for (int m = 0; m < E; ++m) {
@@ -217,7 +226,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeK A, RopeTurns turns) {
             const float n = v[e] * r;
             dg[0][e] += isk ? 0.f : d[e] * n;
             dg[1][e] += isk ? d[e] * n : 0.f;
-            d[e] *= isk ? gain[1][e] : gain[0][e];
+            d[e] *= gain[e];
             hx += d[e] * n;
           }
           if (!lane_on) hx = 0.f;
@@ -230,26 +239,19 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeK A, RopeTurns turns) {
           }
         }
       }
-#pragma unroll
-      for (int e = 0; e < 2 * E; ++e) {
-        v[e] = vn[e];
-        if constexpr (BWD) d[e] = dn[e];
-      }
-      start = sn;
     }
   }
   if constexpr (BWD) {
     if (!A.partial) return;
     // the block's sum over its groups, in group order
     float* sum = reinterpret_cast<float*>(cs);                       // [groups][dim]
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
+    auto put = [&](const float (&x)[2 * E], int g) __attribute__((always_inline)) {
       __syncthreads();
       if (lane_on)
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          sum[group * A.dim + lo + e] = dg[g][e];
-          sum[group * A.dim + hi + e] = dg[g][E + e];
+          sum[group * A.dim + lo + e] = x[e];
+          sum[group * A.dim + hi + e] = x[E + e];
         }
       __syncthreads();
       for (int j = tid; j < A.dim; j += 256) {
@@ -257,7 +259,9 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeK A, RopeTurns turns) {
         for (int u = 0; u < A.groups; ++u) a += sum[u * A.dim + j];
         A.partial[((int64_t)blockIdx.x * 2 + g) * A.dim + j] = a;
       }
-    }
+    };
+    put(dg[0], 0);
+    put(dg[1], 1);
   }
 }
 
@@ -270,6 +274,7 @@ __global__ __launch_bounds__(1024) void rope_dgain_kernel(const float* __restric
   const int col = blockIdx.x * 16 + c;
   float a = 0.f;
   if (col < 2 * dim)
+#pragma unroll 8
     for (int b = strand; b < blocks; b += 64) a += partial[(int64_t)b * 2 * dim + col];
   s[strand][c] = a;
   __syncthreads();
@@ -321,7 +326,7 @@ static hipError_t rope_launch(const RopeArgs& a, const RopeTurns& t, float* part
   A.gk = a.gain_k;
   A.xq = a.q; A.xk = a.k; A.dyq = a.gq; A.dyk = a.gk; A.oq = a.oq; A.ok = a.ok;
   A.partial = partial;
-  size_t lds = (size_t)A.tb * (a.rotary / 2) * sizeof(float2);
+  size_t lds = (size_t)A.tb * (a.rotary / 2) * sizeof(float2) + 2 * a.dim * sizeof(float);
   if (BWD) {
     const size_t need = (size_t)A.groups * a.dim * sizeof(float);    // at most 16 KB
     lds = lds > need ? lds : need;

@@ -25,7 +25,7 @@ namespace lat {
 constexpr float STEP_LOG2E = 1.4426950408889634f;
 constexpr int STEP_HEADS = 16;               // head columns of a block
 constexpr int STEP_TILE = 32;                // slots of a wave's tile
-constexpr int STEP_MAX_SPLITS = 1024;
+constexpr int STEP_MAX_SPLITS = 512;
 
 struct StepK {
   SeqCacheArgs c;
@@ -360,8 +360,8 @@ __global__ __launch_bounds__(256) void seq_step_join_kernel(StepK A) {
   }
 }
 
-// Splits of the slots: enough blocks for four a compute unit, at least 256 slots
-// (two rounds of a block's waves) each.
+// Splits of the slots: enough blocks for the two a compute unit holds, at
+// least 256 slots (two rounds of a block's waves) each.
 static int step_splits(int batch, int heads, int kv_heads, int cap) {
   const int hg = cdiv(heads / kv_heads, STEP_HEADS);
   const int64_t blocks = (int64_t)batch * kv_heads * hg;

@@ -186,8 +186,12 @@ def test_binding_checks_before_it_calls():
         api._heads(x[:3], x, 4, "q")
     with pytest.raises(ValueError, match="expected"):
         api._heads(x.bfloat16(), x, 4, "q")
+    with pytest.raises(ValueError, match="not on"):
+        api._vec(torch.zeros(4, dtype=torch.int32), torch.int32, 4, "lens", 0)
+    with pytest.raises(ValueError, match="heads, head_dim"):
+        api.lattice_qk_rope_fwd(None, x[0], x[0])
     assert api._heads(torch.zeros(4, 6, 64)[:, 2:4], x, 4, "k")[1] == 384
     with pytest.raises(ValueError, match="elements"):
-        api._vec(torch.zeros(3, dtype=torch.int32), torch.int32, 4, "lens")
+        api._vec(torch.zeros(3, dtype=torch.int32), torch.int32, 4, "lens", 0)
     with pytest.raises(ValueError, match="caches"):
         api._cache(torch.zeros(2, 2, 9, 64), torch.zeros(2, 2, 9, 64), x, 2, 8, 2)
