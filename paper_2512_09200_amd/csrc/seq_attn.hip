@@ -57,18 +57,21 @@ struct AttnK {                     // kernel arguments
   float* part;                     // workspace [seqs][kv_heads][ns][2][sinks][dim]
 };
 
-// What a lane's row sees, and its wave's and block's key ranges.
+// What a lane's row sees
 struct RowView {
   int i, start, lo;                // sees lo .. i (its window) and the nsk rows from start
   unsigned nsk;
   bool valid;
 };
 
-__device__ inline RowView row_view(const AttnK& A, int i) {
+__device__ inline SeqSpan load_span(const AttnK& A, int i) {
+  const SeqSpan s = A.span[min(i, A.rows - 1)];
+  return i < A.rows ? s : SeqSpan{SEQ_NO_ROW, 0};
+}
+
+__device__ inline RowView row_view(const AttnK& A, int i, const SeqSpan& sp) {
   RowView v;
   v.i = i;
-  SeqSpan sp{SEQ_NO_ROW, 0};
-  if (i < A.rows) sp = A.span[i];
   v.valid = sp.start != SEQ_NO_ROW;
   v.start = sp.start;
   v.lo = v.valid ? max(sp.start, i - A.window + 1) : SEQ_NO_ROW;
@@ -80,23 +83,19 @@ __device__ inline RowView row_view(const AttnK& A, int i) {
 // [lo, hi], then the range's.
 struct KeyTiles {
   int s0, nsink, ts, lo, hi, n;
+  // sa, sb: the spans of rows r0 + lane and r0 + 64 + lane
   template <int BK>
-  __device__ inline void init(const AttnK& A, int r0, int nrows) {
+  __device__ inline void init(const AttnK& A, int r0, int nrows, const SeqSpan& sa, const SeqSpan& sb) {
     const int lane = threadIdx.x & 63;
-    int last = -1;
-    for (int b = 0; b < nrows; b += 64) {
-      const int i = r0 + b + lane;
-      const bool ok = b + lane < nrows && i < A.rows && A.span[i].start != SEQ_NO_ROW;
-      const uint64_t m = __ballot(ok);
-      if (m) last = r0 + b + 63 - __builtin_clzll(m);
-    }
+    const uint64_t ma = __ballot(lane < nrows && sa.start != SEQ_NO_ROW);
+    const uint64_t mb = __ballot(lane + 64 < nrows && sb.start != SEQ_NO_ROW);
+    const int last = mb ? r0 + 127 - __builtin_clzll(mb) : ma ? r0 + 63 - __builtin_clzll(ma) : -1;
     hi = last;
     n = ts = nsink = s0 = lo = 0;
     if (last < 0) return;
     // the first row that belongs to a sequence is r0 unless the offsets are malformed
-    int st = A.span[r0].start;
-    if (st == SEQ_NO_ROW) st = r0;
-    s0 = __builtin_amdgcn_readfirstlane(st);
+    s0 = __builtin_amdgcn_readfirstlane(sa.start);
+    if (s0 == SEQ_NO_ROW) s0 = r0;
     lo = max(s0, r0 - A.window + 1);
     nsink = min(A.sinks, lo - s0);
     ts = (nsink + BK - 1) / BK;
@@ -109,6 +108,18 @@ struct KeyTiles {
   }
 };
 
+// Blocks are dealt to the XCDs round-robin; this renumbers them so that an XCD
+// takes runs of 32 neighbours, whose key ranges overlap in its L2, and the runs
+// are still dealt in turn, so that work that grows along a sequence is spread.
+// 8192 histories of 20, forward / dQ / dK and dV: 75 / 87 / 85 -> 69 / 74 / 76 us.
+// (One long run an XCD: 75 / 87 / 89.)
+__device__ inline int xcd_runs(int b, int n) {
+  constexpr int RUN = 32, G = NUM_XCD * RUN;
+  if (b >= n / G * G) return b;
+  const int c = b / G, y = b - c * G;
+  return c * G + y % NUM_XCD * RUN + y / NUM_XCD;
+}
+
 // Block -> (row tile, key head, heads of the group).  Rows late in a long
 // sequence may see more keys, so tiles go from the last to the first; where all
 // blocks run at once (two a compute unit, block b beside b + 256), the second
@@ -117,7 +128,7 @@ struct KeyTiles {
 struct BlockAt { int tile, kv, h0; };
 __device__ inline BlockAt block_at(const AttnK& A) {
   const int hg = A.group / A.hb, per = A.kv_heads * hg;
-  const int b = blockIdx.x;
+  const int b = xcd_runs(blockIdx.x, gridDim.x);
   BlockAt r;
   const int x = b % per;
   const int t = b / per, n = A.row_tiles, h = (n + 1) / 2;
@@ -306,18 +317,26 @@ __device__ __forceinline__ void store_row(T* op, T* lo, int dim, f32x16 (&x)[Til
 template <typename T, int DP>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_fwd_kernel(AttnK A) {
   using TL = Tile<T, DP>;
-  constexpr int BK = AttnCfg<T, DP>::BK, TB = AttnCfg<T, DP>::TB, NB = BK / 32;
+  constexpr int BK = AttnCfg<T, DP>::BK, TB = AttnCfg<T, DP>::TB;
+  // Keys taken at a time: 32 with narrow heads, whose windows are short as a
+  // rule, leaving out those that no row of the wave reaches (window 256, heads
+  // of 64: 73 -> 63 us); a tile with wide ones, whose maximum, exchange and test
+  // are then made once.
+  constexpr bool SPLIT = DP <= 64;
+  constexpr int N = SPLIT ? 1 : BK / 32;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5;
   const BlockAt B = block_at(A);
   const int brows = 128 / A.hb, r0 = B.tile * brows;
   const int head = B.h0 + w % A.hb, row = r0 + (w / A.hb) * 32 + (lane & 31);
+  // loads that wait for nothing: spans first, the bounds depend on them
+  const SeqSpan sa = load_span(A, r0 + lane), sb = load_span(A, r0 + 64 + lane), sr = load_span(A, row);
   Frag<T> q[TL::KS];
   load_rows<T, DP>(A.q, min(row, A.rows - 1), head, A.dim, q);
-  const RowView V = row_view(A, row);
+  const RowView V = row_view(A, row, sr);
   KeyTiles kt_;
-  kt_.init<BK>(A, r0, brows);
+  kt_.init<BK>(A, r0, brows, sa, sb);
   if (kt_.n == 0) return;
   KeyStream<T, DP> ks;
   ks.init(A, &kt_, B.kv, smem, w);
@@ -326,18 +345,18 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
   f32x16 o[TL::DB];
   float m, l;
 
-  // N subtiles of 32 keys from subtile b0 of the tile at kt; full: every row of
-  // the wave sees all of them
-  auto attend = [&](auto strict_, auto full_, auto n_, int b0, const char* SK, const char* SV, int kt, uint64_t bits)
+  // N subtiles of 32 keys from subtile b0 of the tile at kt
+  auto attend = [&](auto strict_, int b0, const char* SK, const char* SV, int kt, uint64_t bits)
       __attribute__((always_inline)) {
     constexpr bool strict = decltype(strict_)::value;
-    constexpr int N = decltype(n_)::value;
-    constexpr bool full = decltype(full_)::value;
+    const uint32_t all = 0xffffffffu;
+    const bool full = (uint32_t)(bits >> (32 * b0)) == all && (N == 1 || (uint32_t)(bits >> 32) == all) &&
+                      wave_all(!V.valid || (V.lo <= kt + 32 * b0 && V.i >= kt + 32 * (b0 + N) - 1));
     f32x16 s[N];
 #pragma unroll
     for (int b = 0; b < N; ++b) s[b] = scores<T, DP>(SK, rl, 32 * (b0 + b), q);
     uint32_t see[N];
-    if constexpr (!full) {
+    if (!full || strict) {
 #pragma unroll
       for (int b = 0; b < N; ++b) {
         see[b] = row_bits(V, kt + 32 * (b0 + b), (uint32_t)(bits >> (32 * (b0 + b))));
@@ -366,13 +385,15 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
       m = mn;
     }
     const float mc = m == -INFINITY ? 0.f : m * c;
+    float ls[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int b = 0; b < N; ++b)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         s[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], c, -mc));
-        l += s[b][r];
+        ls[r & 3] += s[b][r];
       }
+    l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
     if constexpr (strict) {
 #pragma unroll
       for (int b = 0; b < N; ++b) {
@@ -412,16 +433,13 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
       const char *SK = ks.next(t, bits), *SV = SK + TB;
       int kt, nk;
       kt_.at<BK>(t, kt, nk);
-      if (!strict && bits == (NB == 1 ? 0xffffffffull : ~0ull) &&
-          wave_all(!V.valid || (V.lo <= kt && V.i >= kt + BK - 1))) {
-        attend(strict_, std::true_type{}, std::integral_constant<int, NB>{}, 0, SK, SV, kt, bits);
-      } else {
-        // tiles seen in part: by 32 keys, leaving out those no row of the
-        // wave reaches
+      if constexpr (SPLIT) {
 #pragma unroll 1
-        for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < BK / 32; ++b)
           if (nk > 32 * b && wave_any(reaches(V, kt + 32 * b, min(nk - 32 * b, 32))))
-            attend(strict_, std::false_type{}, std::integral_constant<int, 1>{}, b, SK, SV, kt, bits);
+            attend(strict_, b, SK, SV, kt, bits);
+      } else {
+        if (wave_any(reaches(V, kt, nk))) attend(strict_, 0, SK, SV, kt, bits);
       }
     }
     ks.drain();
@@ -461,6 +479,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
   const BlockAt B = block_at(A);
   const int brows = 128 / A.hb, r0 = B.tile * brows;
   const int head = B.h0 + w % A.hb, row = r0 + (w / A.hb) * 32 + (lane & 31);
+  // loads that wait for nothing: spans first, the bounds depend on them
+  const SeqSpan sa = load_span(A, r0 + lane), sb = load_span(A, r0 + 64 + lane), sr = load_span(A, row);
   Frag<T> q[TL::KS], go[TL::KS];
   float delta = 0.f;
   {
@@ -477,9 +497,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
       for (int s = 0; s < TL::KS; ++s) delta += dot_frag(go[s], ov[s]);
     }
   }
-  const RowView V = row_view(A, row);
+  const RowView V = row_view(A, row, sr);
   KeyTiles kt_;
-  kt_.init<BK>(A, r0, brows);
+  kt_.init<BK>(A, r0, brows, sa, sb);
   if (kt_.n == 0) return;
   KeyStream<T, DP> ks;
   ks.init(A, &kt_, B.kv, smem, w);
@@ -632,20 +652,6 @@ __device__ __forceinline__ void dkv_subtile(const char* SQ, const char* SG, cons
   }
 }
 
-template <typename T, int DP>
-__device__ inline void load_keys(const AttnK& A, int j, bool ok, int kv, Frag<T>* kf, Frag<T>* vf) {
-  const int half = (threadIdx.x & 63) >> 5;
-  const T* kp = (const T*)A.k.p + (int64_t)j * A.k.ld + kv * A.dim;
-  const T* vp = (const T*)A.v.p + (int64_t)j * A.v.ld + kv * A.dim;
-#pragma unroll
-  for (int s = 0; s < Tile<T, DP>::KS; ++s) {
-    const int d = 16 * s + 8 * half, dd = d < A.dim ? d : 0;
-    load_frag(kp + dd, ok && d < A.dim, kf[s]);
-    load_frag(vp + dd, ok && d < A.dim, vf[s]);
-  }
-}
-
-typedef __attribute__((address_space(3))) float seq_lds_f32;
 // `rows` values (zeros past them) straight to LDS, one per lane
 __device__ inline void issue_stats(char* S, const float* p, int rows) {
   const int lane = threadIdx.x & 63;
@@ -674,11 +680,15 @@ __global__ __launch_bounds__(256, (DkvCfg<T, DP>::BLOCKS)) void seq_dkv_kernel(A
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5;
-  const int kv = blockIdx.x % A.kv_heads, k0 = (blockIdx.x / A.kv_heads) * 128;
+  const int bid = xcd_runs(blockIdx.x, gridDim.x);
+  const int kv = bid % A.kv_heads, k0 = (bid / A.kv_heads) * 128;
   // a lane's key, and how many rows from it on see it here
   const int j = k0 + 32 * w + (lane & 31);
-  SeqSpan sp{SEQ_NO_ROW, 0};
-  if (j < A.rows) sp = A.span[j];
+  const SeqSpan sp = load_span(A, j);
+  // keys of no sequence or hidden are read too: their columns see no row
+  Frag<T> kf[TL::KS], vf[TL::KS];
+  load_rows<T, DP>(A.k, min(j, A.rows - 1), kv, A.dim, kf);
+  load_rows<T, DP>(A.v, min(j, A.rows - 1), kv, A.dim, vf);
   const bool valid = sp.start != SEQ_NO_ROW;
   const bool shown = valid && (!A.mask || A.mask[j]);
   const bool sink = valid && j - sp.start < A.sinks;
@@ -718,8 +728,6 @@ __global__ __launch_bounds__(256, (DkvCfg<T, DP>::BLOCKS)) void seq_dkv_kernel(A
       ++ig;
     }
   };
-  Frag<T> kf[TL::KS], vf[TL::KS];
-  load_keys<T, DP>(A, valid ? j : k0, shown, kv, kf, vf);
   const uint32_t rl = TL::row_lane(), cl = TL::col_lane();
   const float c = A.scale * LOG2E;
   f32x16 dk[TL::DB], dv[TL::DB];
@@ -847,7 +855,8 @@ __global__ __launch_bounds__(256, 1) void seq_sink_kernel(AttnK A, int parts, in
   lg.init(0, A.dim, A.go.ld);
   char* S = smem + w * Cfg::SINK_STAGE;
   Frag<T> kf[TL::KS], vf[TL::KS];
-  load_keys<T, DP>(A, a < A.sinks ? j : s0, shown, kv, kf, vf);
+  load_rows<T, DP>(A.k, a < A.sinks ? j : s0, kv, A.dim, kf);
+  load_rows<T, DP>(A.v, a < A.sinks ? j : s0, kv, A.dim, vf);
   const uint32_t rl = TL::row_lane(), cl = TL::col_lane();
   const float c = A.scale * LOG2E;
   f32x16 dk[TL::DB], dv[TL::DB];
@@ -917,12 +926,12 @@ static AttnK attn_args(const SeqAttnArgs& a) {
   return A;
 }
 
-// Splits of a sequence's late rows: about 256 rows each, no more than give
+// Splits of a sequence's late rows: about 128 rows each, no more than give
 // every compute unit a few blocks; 0 where no sequence has late rows.
 static int late_splits(const SeqAttnArgs& a) {
   const int64_t late = a.max_len - ((int64_t)a.sinks + a.window - 1);
   if (a.sinks == 0 || late <= 0 || a.num_seqs == 0) return 0;
-  int64_t n = cdiv(late, 256);
+  int64_t n = cdiv(late, 128);
   const int64_t most = cdiv(2048, (int64_t)a.num_seqs * a.kv_heads);
   if (n > most) n = most;
   return (int)(n > 64 ? 64 : n < 1 ? 1 : n);

@@ -221,8 +221,15 @@ struct TileLoad {
   }
 };
 
-__device__ inline float max32(float v) { return fmaxf(v, __shfl_xor(v, 32, 64)); }
-__device__ inline float add32(float v) { return v + __shfl_xor(v, 32, 64); }
+// A value of the lane and of lane +- 32 joined, in registers.
+__device__ inline float max32(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float add32(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
 __device__ inline bool wave_all(bool b) { return __ballot(!b) == 0; }
 __device__ inline bool wave_any(bool b) { return __ballot(b) != 0; }
 
