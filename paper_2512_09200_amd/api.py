@@ -567,6 +567,15 @@ def _run(dev, fn, stream, *args):
     check(fn(*args, s))
 
 
+def _used_on(stream, *ts):
+    """Memory allocated here for a call on another stream is not reused before
+    that stream has passed the call."""
+    if stream is not None:
+        for t in ts:
+            if t is not None:
+                t.record_stream(stream)
+
+
 def _gpu(t):
     dev = t.get_device()
     if dev < 0:
@@ -632,6 +641,7 @@ def lattice_seq_plan(offsets, rows, max_len=0, padded=False, stream=None):
     dev = _gpu(offsets)
     s = Seqs(offsets, rows, max_len, padded)
     _run(dev, load().lattice_seq_plan, stream, byref(s.desc), s.desc.span)
+    _used_on(stream, s.span)
     return s
 
 
@@ -668,6 +678,7 @@ def lattice_qk_rope_fwd(seqs, q, k, gain_q=None, gain_k=None, theta=10000.0, rot
         raise ValueError("outputs must have the inputs' shapes")
     _run(_gpu(q), load().lattice_qk_rope_fwd, stream, byref(desc), byref(s), *_heads(q, q, rows, "q"),
          *_heads(k, q, rows, "k"), *_heads(q_out, q, rows, "q_out"), *_heads(k_out, q, rows, "k_out"))
+    _used_on(stream, q_out, k_out)
     return q_out, k_out
 
 
@@ -688,6 +699,7 @@ def lattice_qk_rope_bwd(seqs, q, k, d_q_out, d_k_out, gain_q=None, gain_k=None, 
     _run(_gpu(q), lib.lattice_qk_rope_bwd, stream, byref(desc), byref(s), *_heads(q, q, rows, "q"),
          *_heads(k, q, rows, "k"), *_heads(d_q_out, q, rows, "d_q_out"), *_heads(d_k_out, q, rows, "d_k_out"),
          *_heads(dq, q, rows, "dq"), *_heads(dk, q, rows, "dk"), _p(dgq), _p(dgk), _p(ws), wsb)
+    _used_on(stream, dq, dk, dgq, dgk, ws)
     return dq, dk, dgq, dgk
 
 
@@ -724,6 +736,7 @@ def lattice_seq_attn_fwd(seqs, q, k, v, window, sinks=0, scale=None, key_mask=No
     _run(_gpu(q), load().lattice_seq_attn_fwd, stream, byref(desc), byref(seqs.desc), *_heads(q, q, rows, "q"),
          *_heads(k, q, rows, "k"), *_heads(v, q, rows, "v"), *_heads(out, q, rows, "out"),
          _p(saved.lse) if lse else None, _p(saved.out_lo) if lse else None)
+    _used_on(stream, out, *((saved.lse, saved.out_lo) if lse else ()))
     return out, saved
 
 
@@ -747,6 +760,7 @@ def lattice_seq_attn_bwd(seqs, q, k, v, out, saved, d_out, window, sinks=0, scal
          _vec(saved.lse, torch.float32, q.shape[1] * rows, "lse", dev),
          _vec(saved.out_lo, q.dtype, out.numel(), "out_lo", dev), *_heads(d_out, q, rows, "d_out"),
          *_heads(dq, q, rows, "dq"), *_heads(dk, q, rows, "dk"), *_heads(dv, q, rows, "dv"), _p(ws), wsb)
+    _used_on(stream, dq, dk, dv, ws)
     return dq, dk, dv
 
 
@@ -796,4 +810,5 @@ def lattice_seq_step(q, k, v, lens, k_cache, v_cache, window, sinks=0, cache_ind
     _run(dev, lib.lattice_seq_step, stream, byref(desc), rd, B, *_heads(q, q, B, "q"), *_heads(k, q, B, "k"),
          *_heads(v, q, B, "v"), _vec(lens, torch.int32, B, "lens", dev),
          _vec(cache_index, torch.int32, B, "cache_index", dev), byref(cache), *_heads(out, q, B, "out"), _p(ws), wsb)
+    _used_on(stream, out, ws)
     return out

@@ -124,7 +124,8 @@ __device__ inline int xcd_runs(int b, int n) {
 // sequence may see more keys, so tiles go from the last to the first; where all
 // blocks run at once (two a compute unit, block b beside b + 256), the second
 // half goes from the first tile on, so that heavy and light ones share a unit.
-// One history of 8192, all rows before each seen: 222 -> ZIGZAG us.
+// One history of 8192, all rows before each seen, 8 heads of 128: 252 us with
+// tiles from first to last, 233 from last to first, 215 so.
 struct BlockAt { int tile, kv, h0; };
 __device__ inline BlockAt block_at(const AttnK& A) {
   const int hg = A.group / A.hb, per = A.kv_heads * hg;
@@ -241,6 +242,19 @@ __device__ inline f32x16 scores(const char* S, uint32_t rl, int row0, const Frag
   for (int r = 0; r < 16; ++r) c[r] = 0.f;
 #pragma unroll
   for (int s = 0; s < TL::KS; ++s) mma32(TL::rowfrag(S, rl, row0, s), q[s], c);
+  return c;
+}
+
+// Scores of 32 rows (row0 of the tile at S) against 32 keys (key0 of the tile
+// at SK), both in LDS
+template <typename T, int DP>
+__device__ inline f32x16 scores_lds(const char* S, uint32_t rl, int row0, const char* SK, int key0) {
+  using TL = Tile<T, DP>;
+  f32x16 c;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) c[r] = 0.f;
+#pragma unroll
+  for (int s = 0; s < TL::KS; ++s) mma32(TL::rowfrag(S, rl, row0, s), TL::rowfrag(SK, rl, key0, s), c);
   return c;
 }
 
@@ -594,19 +608,18 @@ __device__ inline int late_row(const AttnK& A, int start) {
 // rows of a split of n late rows
 __device__ inline int late_chunk(const AttnK& A, int n) { return ((n + A.ns - 1) / A.ns + 31) & ~31; }
 
-// One 32-row subtile against the wave's 32 keys: accumulates dv and dk.
-// SQ / SG: the rows' q and d_out in LDS (row0 the subtile's first row there),
-// L / E: their lse2 and delta.  d: the subtile's first row minus the lane's
-// key; rows with d + offset < lim see it.
+// One 32-row subtile against the wave's 32 keys: accumulates dv and dk from
+// the scores p and the products ds of d_out and v.  SQ / SG: the rows' q and
+// d_out in LDS (row0 the subtile's first row there), L / E: their lse2 and
+// delta.  d: the subtile's first row minus the lane's key; rows with
+// d + offset < lim see it.
 template <typename T, int DP, bool strict>
-__device__ __forceinline__ void dkv_subtile(const char* SQ, const char* SG, const float* L, const float* E, int row0,
-                                   uint32_t rl, uint32_t cl, const Frag<T> (&kf)[Tile<T, DP>::KS],
-                                   const Frag<T> (&vf)[Tile<T, DP>::KS], float c, int d, unsigned lim, bool full,
-                                   f32x16 (&dk)[Tile<T, DP>::DB], f32x16 (&dv)[Tile<T, DP>::DB]) {
+__device__ __forceinline__ void dkv_subtile(f32x16 p, f32x16 ds, const char* SQ, const char* SG, const float* L,
+                                            const float* E, int row0, uint32_t rl, uint32_t cl, float c, int d,
+                                            unsigned lim, bool full, f32x16 (&dk)[Tile<T, DP>::DB],
+                                            f32x16 (&dv)[Tile<T, DP>::DB]) {
   using TL = Tile<T, DP>;
   const int half = (threadIdx.x & 63) >> 5;
-  f32x16 p = scores<T, DP>(SQ, rl, row0, kf);
-  f32x16 ds = scores<T, DP>(SG, rl, row0, vf);
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
     const f32x4 l4 = *reinterpret_cast<const f32x4*>(L + row0 + 8 * g + 4 * half);
@@ -665,30 +678,42 @@ template <typename T, int DP> struct DkvCfg {
   static constexpr int BQ = sizeof(T) == 4 && DP == 128 ? 32 : 64;    // rows of a tile
   static constexpr int STAGE = 2 * BQ * DP * (int)sizeof(T) + 1024;   // q, d_out, lse2, delta (64 floats each, and unused)
   static constexpr int NST = STAGE <= 9216 ? 4 : STAGE <= 17408 ? 3 : 2;
-  static constexpr size_t LDS = (size_t)NST * STAGE;
-  // blocks a compute unit: narrow heads wait for memory more than they compute
-  static constexpr int BLOCKS = sizeof(T) == 2 ? (DP == 32 ? 3 : DP == 64 ? 2 : 1) : DP == 32 ? 2 : 1;
+  // Wide bf16 heads: the accumulators of 32 keys are half of what two waves a
+  // SIMD may hold, so k and v stay in LDS and a block has eight waves, two on
+  // each 32 keys that take the two subtiles of a row tile; their sums are
+  // added at the end.  One wave a SIMD left its matrix cores idle while it
+  // made probabilities: 1460 -> 1206 us (65536 rows, 8 heads of 128,
+  // window 2048).
+  static constexpr bool WIDE = sizeof(T) == 2 && DP == 128;
+  static constexpr int NW = WIDE ? 8 : 4;
+  static constexpr int KV = WIDE ? 2 * 128 * DP * (int)sizeof(T) : 0;   // k and v of the block's keys
+  static constexpr size_t LDS = (size_t)NST * STAGE + KV;
+  // waves a SIMD: narrow heads wait for memory more than they compute
+  static constexpr int WAVES = sizeof(T) == 2 ? (DP == 32 ? 3 : 2) : DP == 32 ? 2 : 1;
   static constexpr int SINK_STAGE = 2 * 32 * DP * (int)sizeof(T) + 512;   // a wave's 32 rows
   static constexpr size_t SINK_LDS = (size_t)4 * SINK_STAGE;
 };
 
 template <typename T, int DP>
-__global__ __launch_bounds__(256, (DkvCfg<T, DP>::BLOCKS)) void seq_dkv_kernel(AttnK A) {
+__global__ __launch_bounds__((64 * DkvCfg<T, DP>::NW), (DkvCfg<T, DP>::WAVES)) void seq_dkv_kernel(AttnK A) {
   using TL = Tile<T, DP>;
   using Cfg = DkvCfg<T, DP>;
-  constexpr int BQ = Cfg::BQ, TB = BQ * TL::RB;
+  constexpr int BQ = Cfg::BQ, TB = BQ * TL::RB, NW = Cfg::NW, KB = 64 * TL::RB;
+  constexpr bool WIDE = Cfg::WIDE;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int half = lane >> 5;
+  const int half = lane >> 5, kg = w & 3, rh = w >> 2;   // 32 keys; of a row tile, subtile (wide heads)
   const int bid = xcd_runs(blockIdx.x, gridDim.x);
   const int kv = bid % A.kv_heads, k0 = (bid / A.kv_heads) * 128;
   // a lane's key, and how many rows from it on see it here
-  const int j = k0 + 32 * w + (lane & 31);
+  const int j = k0 + 32 * kg + (lane & 31);
   const SeqSpan sp = load_span(A, j);
   // keys of no sequence or hidden are read too: their columns see no row
   Frag<T> kf[TL::KS], vf[TL::KS];
-  load_rows<T, DP>(A.k, min(j, A.rows - 1), kv, A.dim, kf);
-  load_rows<T, DP>(A.v, min(j, A.rows - 1), kv, A.dim, vf);
+  if constexpr (!WIDE) {
+    load_rows<T, DP>(A.k, min(j, A.rows - 1), kv, A.dim, kf);
+    load_rows<T, DP>(A.v, min(j, A.rows - 1), kv, A.dim, vf);
+  }
   const bool valid = sp.start != SEQ_NO_ROW;
   const bool shown = valid && (!A.mask || A.mask[j]);
   const bool sink = valid && j - sp.start < A.sinks;
@@ -701,16 +726,32 @@ __global__ __launch_bounds__(256, (DkvCfg<T, DP>::BLOCKS)) void seq_dkv_kernel(A
   for (int o = 32; o > 0; o >>= 1) wend = max(wend, __shfl_xor(wend, o, 64));
   wend = __builtin_amdgcn_readfirstlane(wend);
   __shared__ int ends[4];
-  if (lane == 0) ends[w] = wend;
+  if (lane == 0 && rh == 0) ends[kg] = wend;
   __syncthreads();
   const int bend = max(max(ends[0], ends[1]), max(ends[2], ends[3]));
   if (bend <= k0) return;                      // no row of a sequence here
   const int per_head = (bend - k0 + BQ - 1) / BQ, n = per_head * A.group;
 
-  TileLoad<T, DP, BQ, 4> lq, lg;
+  TileLoad<T, DP, BQ, NW> lq, lg;
   lq.init(w, A.dim, A.q.ld);
   lg.init(w, A.dim, A.go.ld);
-  constexpr int NST = Cfg::NST, PER = 2 * TileLoad<T, DP, BQ, 4>::PER + 1;
+  char* const KV = smem + Cfg::NST * Cfg::STAGE;       // wide heads: k (two tiles of 64 rows), v
+  if constexpr (WIDE) {
+    TileLoad<T, DP, 64, NW> lk;
+    lk.init(w, A.dim, A.k.ld);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int at = min(k0 + 64 * h, A.rows - 1), nr = min(64, A.rows - (k0 + 64 * h));
+      lk.issue(KV + h * KB, w, (const T*)A.k.p + (int64_t)at * A.k.ld + kv * A.dim, nr, ~0ull);
+    }
+    lk.init(w, A.dim, A.v.ld);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int at = min(k0 + 64 * h, A.rows - 1), nr = min(64, A.rows - (k0 + 64 * h));
+      lk.issue(KV + (2 + h) * KB, w, (const T*)A.v.p + (int64_t)at * A.v.ld + kv * A.dim, nr, ~0ull);
+    }
+  }
+  constexpr int NST = Cfg::NST, PER = 2 * TileLoad<T, DP, BQ, NW>::PER + 1;
   // head and first row of the tile to be issued next; its stage
   int ig = 0, ii = k0, is = 0;
   auto issue = [&]() __attribute__((always_inline)) {
@@ -719,8 +760,8 @@ __global__ __launch_bounds__(256, (DkvCfg<T, DP>::BLOCKS)) void seq_dkv_kernel(A
     char* S = smem + is * Cfg::STAGE;
     lq.issue(S, w, (const T*)A.q.p + i0 * A.q.ld + hd, nr, ~0ull);
     lg.issue(S + TB, w, (const T*)A.go.p + i0 * A.go.ld + hd, nr, ~0ull);
-    // every wave one load: lse2, delta, and two that read nothing
-    issue_stats(S + 2 * TB + 256 * w, (w == 0 ? A.lse2 : A.delta) + at, w < 2 ? nr : 0);
+    // every wave one load: lse2, delta, and such that read nothing
+    issue_stats(S + 2 * TB + 256 * min(w, 2), (w == 0 ? A.lse2 : A.delta) + at, w < 2 ? nr : 0);
     is = is + 1 == NST ? 0 : is + 1;
     ii += BQ;
     if (ii >= bend) {
@@ -754,21 +795,50 @@ __global__ __launch_bounds__(256, (DkvCfg<T, DP>::BLOCKS)) void seq_dkv_kernel(A
       asm volatile("" ::: "memory");
       const char* S = smem + (is + 1 == NST ? 0 : is + 1) * Cfg::STAGE;
       issue();
-#pragma unroll
-      for (int b = 0; b < BQ / 32; ++b) {
+      auto subtile = [&](int b) __attribute__((always_inline)) {
         const int ib = i0 + 32 * b;
-        // rows ib .. ib+31 reach the wave's keys k0 + 32 w .. + 31
-        if (ib + 31 < k0 + 32 * w || ib >= wend) continue;
+        // rows ib .. ib+31 reach the wave's keys
+        if (ib + 31 < k0 + 32 * kg || ib >= wend) return;
         const bool full = wave_all((unsigned)(ib - j) < lim && (unsigned)(ib + 31 - j) < lim);
-        dkv_subtile<T, DP, strict>(S, S + TB, (const float*)(S + 2 * TB), (const float*)(S + 2 * TB + 256), 32 * b, rl,
-                                   cl, kf, vf, c, ib - j, lim, full, dk, dv);
+        f32x16 p, ds;
+        if constexpr (WIDE) {
+          const char* SK = KV + (kg >> 1) * KB;
+          p = scores_lds<T, DP>(S, rl, 32 * b, SK, 32 * (kg & 1));
+          ds = scores_lds<T, DP>(S + TB, rl, 32 * b, SK + 2 * KB, 32 * (kg & 1));
+        } else {
+          p = scores<T, DP>(S, rl, 32 * b, kf);
+          ds = scores<T, DP>(S + TB, rl, 32 * b, vf);
+        }
+        dkv_subtile<T, DP, strict>(p, ds, S, S + TB, (const float*)(S + 2 * TB), (const float*)(S + 2 * TB + 256),
+                                   32 * b, rl, cl, c, ib - j, lim, full, dk, dv);
+      };
+      if constexpr (WIDE) {
+        subtile(rh);
+      } else {
+#pragma unroll
+        for (int b = 0; b < BQ / 32; ++b) subtile(b);
       }
       i0 = i0 + BQ >= bend ? k0 : i0 + BQ;
     }
     wait_loads<0>();                             // the loads past the last tile write LDS
+    if constexpr (WIDE) {                        // the two waves of a key group, dk then dv, by registers
+      float* R = reinterpret_cast<float*>(smem) + kg * TL::DB * 16 * 64 + lane;
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        __syncthreads();
+        if (rh == 1)
+#pragma unroll
+          for (int x = 0; x < TL::DB * 16; ++x) R[x * 64] = (m ? dv : dk)[x >> 4][x & 15];
+        __syncthreads();
+        if (rh == 0)
+#pragma unroll
+          for (int x = 0; x < TL::DB * 16; ++x) (m ? dv : dk)[x >> 4][x & 15] += R[x * 64];
+      }
+      __syncthreads();
+    }
     // sinks: the late rows' partial sums, in split order (a hidden sink has no
     // gradient; its sums are zeros times what may not be finite)
-    if (A.ns > 0 && sink && shown && sp.end > late_row(A, sp.start)) {
+    if (A.ns > 0 && rh == 0 && sink && shown && sp.end > late_row(A, sp.start)) {
       const int late = sp.end - late_row(A, sp.start), used = (late + late_chunk(A, late) - 1) / late_chunk(A, late);
       int lo = 0, hi = A.num_seqs;               // the sequence: the last that starts at sp.start or before
       while (hi - lo > 1) {
@@ -800,19 +870,20 @@ __global__ __launch_bounds__(256, (DkvCfg<T, DP>::BLOCKS)) void seq_dkv_kernel(A
   };
   T* const kp = (T*)A.gk.p + (int64_t)j * A.gk.ld + kv * A.dim;
   T* const vp = (T*)A.gv.p + (int64_t)j * A.gv.ld + kv * A.dim;
+  const bool mine = valid && rh == 0;            // the wave that stores
   sweep(std::false_type{});
   float z = 0.f;
 #pragma unroll
   for (int db = 0; db < TL::DB; ++db)
 #pragma unroll
     for (int r = 0; r < 16; ++r) z = __builtin_fmaf(dk[db][r], 0.f, __builtin_fmaf(dv[db][r], 0.f, z));
-  if (valid) {
+  if (mine) {
     store_row<T, DP, false>(kp, nullptr, A.dim, dk);
     store_row<T, DP, false>(vp, nullptr, A.dim, dv);
   }
-  if (__syncthreads_or(valid && z != 0.f)) {
+  if (__syncthreads_or(mine && z != 0.f)) {
     sweep(std::true_type{});
-    if (valid) {
+    if (mine) {
       store_row<T, DP, true>(kp, nullptr, A.dim, dk);
       store_row<T, DP, true>(vp, nullptr, A.dim, dv);
     }
@@ -875,8 +946,9 @@ __global__ __launch_bounds__(256, 1) void seq_sink_kernel(AttnK A, int parts, in
     issue_stats(S + 2 * TB, A.lse2 + at, nr);
     issue_stats(S + 2 * TB + 256, A.delta + at, nr);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    dkv_subtile<T, DP, false>(S, S + TB, (const float*)(S + 2 * TB), (const float*)(S + 2 * TB + 256), 0, rl, cl, kf,
-                              vf, c, 0, shown ? (unsigned)nr : 0u, nr == 32 && wave_all(shown), dk, dv);
+    dkv_subtile<T, DP, false>(scores<T, DP>(S, rl, 0, kf), scores<T, DP>(S + TB, rl, 0, vf), S, S + TB,
+                              (const float*)(S + 2 * TB), (const float*)(S + 2 * TB + 256), 0, rl, cl, c, 0,
+                              shown ? (unsigned)nr : 0u, nr == 32 && wave_all(shown), dk, dv);
   }
   // waves' sums, one after the other, in LDS [2][DP][33]
   float* R = reinterpret_cast<float*>(smem);
@@ -973,7 +1045,7 @@ static hipError_t bwd_launch(const AttnK& A, hipStream_t s) {
         A, parts, pb);
     LAT_LAUNCH_CHECK();
   }
-  seq_dkv_kernel<T, DP><<<cdiv(A.rows, 128) * A.kv_heads, 256, DkvCfg<T, DP>::LDS, s>>>(A);
+  seq_dkv_kernel<T, DP><<<cdiv(A.rows, 128) * A.kv_heads, 64 * DkvCfg<T, DP>::NW, DkvCfg<T, DP>::LDS, s>>>(A);
   LAT_LAUNCH_CHECK();
   return hipSuccess;
 }

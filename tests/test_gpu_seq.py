@@ -284,6 +284,92 @@ def test_attention_twice_on_side_streams_and_in_a_graph_gives_the_same_bits():
         same(rg)
 
 
+def test_hidden_sinks_get_no_gradient_from_late_rows_that_are_not_finite():
+    from paper_2512_09200_amd import api
+    rng = np.random.default_rng(11)
+    off, rows, s = plan([200])
+    q, do = (randn(rng, rows, 2, 32).to(DEV) for _ in "qo")
+    k, v = (randn(rng, rows, 1, 32).to(DEV) for _ in "kv")
+    mask = torch.ones(rows, dtype=torch.uint8, device=DEV)
+    mask[1] = 0                                        # one of three sinks
+    q[150] = float("nan")                              # behind every sink's window
+    kw = dict(window=20, sinks=3, key_mask=mask)
+    out, saved = api.lattice_seq_attn_fwd(s, q, k, v, **kw)
+    dq, dk, dv = api.lattice_seq_attn_bwd(s, q, k, v, out, saved, do, **kw)
+    seen = np.zeros(rows, bool)
+    seen[[0, 2]] = True
+    seen[131:151] = True
+    for t in (dk, dv):
+        assert np.array_equal(np.isfinite(f64(t)).all((1, 2)), ~seen)
+    assert (dk[1] == 0).all() and (dv[1] == 0).all()
+
+
+def test_rows_beyond_4_gib():
+    """Row strides of 2^22 elements: byte offsets past 32 bits in every tensor."""
+    from paper_2512_09200_amd import api
+    rng = np.random.default_rng(2)
+    T, H, J, D, ld = 600, 2, 1, 32, 1 << 22
+    big = torch.empty(T * ld, dtype=torch.bfloat16, device=DEV).view(T, ld)
+    q = randn(rng, T, H, D).to(torch.bfloat16).to(DEV)
+    k, v = (randn(rng, T, J, D).to(torch.bfloat16).to(DEV) for _ in "kv")
+    do = randn(rng, T, H, D).to(torch.bfloat16).to(DEV)
+    wide = {}
+    for i, (n, t) in enumerate((("q", q), ("k", k), ("v", v), ("do", do))):
+        wide[n] = big[:, 256 * i:256 * i + t.shape[1] * D].view(T, t.shape[1], D)
+        wide[n].copy_(t)
+    off, rows, s = plan([T])
+    kw = dict(window=70, sinks=4)
+    out, sv = api.lattice_seq_attn_fwd(s, q, k, v, **kw)
+    ref = api.lattice_seq_attn_bwd(s, q, k, v, out, sv, do, **kw)
+    o2 = [big[:, 2048 + 256 * i:2048 + 256 * i + h * D].view(T, h, D) for i, h in enumerate((H, H, J, J, H, J))]
+    out2, sv2 = api.lattice_seq_attn_fwd(s, wide["q"], wide["k"], wide["v"], out=o2[0], **kw)
+    g2 = api.lattice_seq_attn_bwd(s, wide["q"], wide["k"], wide["v"], out2, sv2, wide["do"], dq=o2[1], dk=o2[2],
+                                  dv=o2[3], **kw)
+    assert torch.equal(out2, out) and all(torch.equal(a, b) for a, b in zip(g2, ref))
+    r = api.lattice_qk_rope_fwd(s, q, k)
+    r2 = api.lattice_qk_rope_fwd(s, wide["q"], wide["k"], q_out=o2[4], k_out=o2[5])
+    assert all(torch.equal(a, b) for a, b in zip(r, r2))
+
+
+def test_caches_beyond_4_gib():
+    from paper_2512_09200_amd import api
+    rng = np.random.default_rng(4)
+    J, D, W, N, C = 1, 128, 100_000, 4, 200              # 5 GB a cache tensor
+    kc, vc = (torch.empty(C, J, W + N, D, dtype=torch.bfloat16, device=DEV) for _ in "kv")
+    k1, v1 = (torch.zeros(1, J, W + N, D, dtype=torch.bfloat16, device=DEV) for _ in "kv")
+    hist = 3000
+    off, rows, s = plan([hist])
+    kh, vh = (randn(rng, hist, J, D).to(torch.bfloat16).to(DEV) for _ in "kv")
+    last = torch.tensor([C - 1], dtype=torch.int32, device=DEV)
+    api.lattice_seq_cache_fill(s, kh, vh, kc, vc, W, N, cache_index=last)
+    api.lattice_seq_cache_fill(s, kh, vh, k1, v1, W, N)
+    assert torch.equal(kc[-1, :, :hist], k1[0, :, :hist]) and torch.equal(vc[-1, :, :hist], v1[0, :, :hist])
+    q, k, v = (randn(rng, 1, h, D).to(torch.bfloat16).to(DEV) for h in (4, J, J))
+    lens = torch.tensor([hist], dtype=torch.int32, device=DEV)
+    a = api.lattice_seq_step(q, k, v, lens, kc, vc, W, N, cache_index=last)
+    b = api.lattice_seq_step(q, k, v, lens, k1, v1, W, N)
+    assert torch.equal(a, b) and torch.equal(kc[-1, :, hist], k1[0, :, hist])
+
+
+def test_a_stream_of_its_own_keeps_its_memory():
+    """Calls on a stream that is not the current one: their outputs and
+    workspaces are not handed out again while that stream is behind."""
+    from paper_2512_09200_amd import api
+    c = attn_case("bf16", 4, 2, 64, [700, 300], 50, 4)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = []
+    for _ in range(4):
+        p = api.lattice_seq_plan(c["s"].offsets, c["rows"], stream=s)
+        out, sv = api.lattice_seq_attn_fwd(p, c["q"], c["k"], c["v"], stream=s, **c["kw"])
+        got.append(api.lattice_seq_attn_bwd(p, c["q"], c["k"], c["v"], out, sv, c["do"], stream=s, **c["kw"]))
+        del p, out, sv
+        torch.full((1 << 20,), -1.0, device=DEV)         # the current stream writes what it is given
+    torch.cuda.synchronize()
+    for g in got:
+        assert all(torch.equal(x, c[m]) for x, m in zip(g, ("dq", "dk", "dv")))
+
+
 # ---------------------------------------------------------------------------
 @pytest.mark.parametrize("dt,J,D,W,N", [("bf16", 2, 64, 30, 3), ("f32", 1, 8, 1, 0), ("bf16", 3, 40, 7, 64),
                                         ("f32", 2, 128, 200, 1), ("bf16", 40, 128, 20, 2)])
