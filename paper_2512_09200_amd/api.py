@@ -610,7 +610,7 @@ def _heads(t, like, rows, name):
 def _new_heads(t, seqs):
     """An output the caller gave no buffer for; rows behind the last sequence
     of a padded batch hold zeros."""
-    return t.new_zeros(t.shape) if seqs is not None and seqs.padded else t.new_empty(t.shape)
+    return torch.zeros_like(t) if seqs is not None and seqs.padded else torch.empty_like(t)
 
 
 def _check_heads(t, name="q"):
@@ -732,7 +732,7 @@ def lattice_seq_attn_fwd(seqs, q, k, v, window, sinks=0, scale=None, key_mask=No
     saved = None
     if lse:
         saved = SeqAttnSaved(q.new_empty((q.shape[1], rows), dtype=torch.float32),
-                             q.new_empty(q.shape) if desc.dtype == A.BF16 else None)
+                             torch.empty(q.shape, dtype=q.dtype, device=q.device) if desc.dtype == A.BF16 else None)
     _run(_gpu(q), load().lattice_seq_attn_fwd, stream, byref(desc), byref(seqs.desc), *_heads(q, q, rows, "q"),
          *_heads(k, q, rows, "k"), *_heads(v, q, rows, "v"), *_heads(out, q, rows, "out"),
          _p(saved.lse) if lse else None, _p(saved.out_lo) if lse else None)
@@ -801,7 +801,7 @@ def lattice_seq_step(q, k, v, lens, k_cache, v_cache, window, sinks=0, cache_ind
     B, dev = q.shape[0], _gpu(q)
     cache = _cache(k_cache, v_cache, q, k.shape[1], window, sinks)
     rd = byref(_rope_desc(q, k, gain_q, gain_k, theta, rotary, interleaved, eps, positions)) if rope else None
-    out = q.new_empty(q.shape) if out is None else out
+    out = torch.empty_like(q) if out is None else out
     if out.shape != q.shape or v.shape != k.shape:
         raise ValueError("out must have q's shape, v k's")
     lib = load()

@@ -140,41 +140,36 @@ __device__ inline BlockAt block_at(const AttnK& A) {
 }
 
 // ---------------------------------------------------------------------------
-// Keys of a tile, and tiles in LDS at a time: narrow heads' tiles are small and
-// soon computed, so more of them are under way (a block of short histories is
-// a chain of memory latencies).
 template <typename T, int DP> struct AttnCfg {
-  static constexpr int BK = sizeof(T) == 4 && DP == 128 ? 32 : 64;
+  static constexpr int BK = sizeof(T) == 4 && DP == 128 ? 32 : 64;   // keys of a tile
   static constexpr int TB = BK * DP * (int)sizeof(T);                // bytes of K or V
-  static constexpr int NST = TB <= 4096 ? 4 : TB <= 8192 ? 3 : 2;
-  static constexpr size_t LDS = (size_t)NST * 2 * TB;
+  static constexpr size_t LDS = (size_t)2 * 2 * TB;                  // two stages of K and V
 };
 
-// All but the newest n of the wave's memory operations have completed.
-template <int N> __device__ inline void wait_loads() {
-  static_assert(N < 64, "counter of 6 bits");
-  // immediate: vmcnt in bits 0-3 and 14-15, expcnt and lgkmcnt not waited for
-  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+// The wave's direct loads have landed and its LDS reads returned; past the
+// barrier everybody's have.
+__device__ __forceinline__ void landed() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
 }
 
-// The K and V tiles of a block's key range, NST - 1 of them under way.  Every
-// step issues the same loads (past the last tile they read nothing and write
-// zeros), so a wait by count names the tile that is needed.  A tile's
-// key mask is one load made a step before the tile's own, whose row bits
-// depend on it.
+// The K and V tiles of a block's key range, each loaded while the one before
+// is computed.  (Three or four under way measured the same with heads of 64 and
+// 4% slower with heads of 32.)  A tile's key mask is one load made a tile
+// ahead of the tile's own, whose row bits depend on it.
 template <typename T, int DP>
 struct KeyStream {
   using Cfg = AttnCfg<T, DP>;
-  static constexpr int BK = Cfg::BK, TB = Cfg::TB, NST = Cfg::NST;
-  static constexpr int PER = 2 * TileLoad<T, DP, BK, 4>::PER;        // loads of a tile
+  static constexpr int BK = Cfg::BK, TB = Cfg::TB;
   TileLoad<T, DP, BK, 4> lk, lv;
   const KeyTiles* kt;
   const T *k, *v;
   const uint8_t* mask;
   int64_t kld, vld;
   char* smem;
-  int wave, stage, issued, mbyte;
-  uint64_t bits[NST];
+  int wave, mbyte;
+  uint64_t bits;
 
   __device__ __forceinline__ void init(const AttnK& A, const KeyTiles* tiles, int kv, char* lds, int w) {
     kt = tiles;
@@ -189,48 +184,33 @@ struct KeyStream {
     lv.init(w, A.dim, vld);
   }
   __device__ __forceinline__ void fetch_mask(int t) {
-    if (!mask) return;
-    int at = 0, nk = 1;
-    if (t < kt->n) kt->template at<BK>(t, at, nk);
+    if (!mask || t >= kt->n) return;
+    int at, nk;
+    kt->template at<BK>(t, at, nk);
     mbyte = mask[at + min((int)(threadIdx.x & 63), nk - 1)];
   }
-  // slot: the place in bits[] of the tile, a constant after unrolling
-  __device__ __forceinline__ void issue(int t, int slot) {
-    int at = 0, nk = 0;
-    if (t < kt->n) kt->template at<BK>(t, at, nk);
-    uint64_t b = nk >= 64 ? ~0ull : (1ull << nk) - 1;
-    if (mask) b &= __ballot(mbyte != 0);
-    bits[slot] = b;
-    char* S = smem + stage * 2 * TB;
-    lk.issue(S, wave, k + (int64_t)at * kld, nk, b);
-    lv.issue(S + TB, wave, v + (int64_t)at * vld, nk, b);
-    stage = stage + 1 == NST ? 0 : stage + 1;
+  __device__ __forceinline__ void issue(int t) {
+    if (t >= kt->n) return;
+    int at, nk;
+    kt->template at<BK>(t, at, nk);
+    bits = nk >= 64 ? ~0ull : (1ull << nk) - 1;          // keys that exist and are shown
+    if (mask) bits &= __ballot(mbyte != 0);
+    char* S = smem + (t & 1) * 2 * TB;
+    lk.issue(S, wave, k + (int64_t)at * kld, nk, bits);
+    lv.issue(S + TB, wave, v + (int64_t)at * vld, nk, bits);
     fetch_mask(t + 1);
   }
   __device__ __forceinline__ void start() {
-    stage = 0;
-    mbyte = 1;
     fetch_mask(0);
-#pragma unroll
-    for (int t = 0; t < NST - 1; ++t) issue(t, t);
+    issue(0);
   }
-  // Tile t is in LDS for every wave (its address returned), and the tile after
-  // the ones under way is issued into the place of tile t - 1.
+  // Tile t, in LDS for every wave; the next one goes into the place of t - 1.
   __device__ __forceinline__ const char* next(int t, uint64_t& b) {
-    if (mask) wait_loads<(NST - 2) * (PER + 1)>(); else wait_loads<(NST - 2) * PER>();
-    // the wave's reads of tile t - 1 have returned; past the barrier everybody's
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    b = bits[0];
-#pragma unroll
-    for (int i = 0; i < NST - 2; ++i) bits[i] = bits[i + 1];
-    const int at = stage + 1 == NST ? 0 : stage + 1;                 // stage: where tile t - 1 was
-    issue(t + NST - 1, NST - 2);
-    return smem + at * 2 * TB;
+    landed();
+    b = bits;
+    issue(t + 1);
+    return smem + (t & 1) * 2 * TB;
   }
-  // the loads past the last tile write LDS: none is under way afterwards
-  __device__ __forceinline__ void drain() { wait_loads<0>(); }
 };
 
 // Scores of 32 keys (row0 in the tile) against the wave's 32 rows
@@ -456,7 +436,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
         if (wave_any(reaches(V, kt, nk))) attend(strict_, 0, SK, SV, kt, bits);
       }
     }
-    ks.drain();
     l = add32(l);
     const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
@@ -579,7 +558,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
         }
       }
     }
-    ks.drain();
 #pragma unroll
     for (int db = 0; db < TL::DB; ++db)
 #pragma unroll
@@ -676,8 +654,7 @@ __device__ inline void issue_stats(char* S, const float* p, int rows) {
 
 template <typename T, int DP> struct DkvCfg {
   static constexpr int BQ = sizeof(T) == 4 && DP == 128 ? 32 : 64;    // rows of a tile
-  static constexpr int STAGE = 2 * BQ * DP * (int)sizeof(T) + 1024;   // q, d_out, lse2, delta (64 floats each, and unused)
-  static constexpr int NST = STAGE <= 9216 ? 4 : STAGE <= 17408 ? 3 : 2;
+  static constexpr int STAGE = 2 * BQ * DP * (int)sizeof(T) + 512;    // q, d_out, lse2, delta (64 floats each)
   // Wide bf16 heads: the accumulators of 32 keys are half of what two waves a
   // SIMD may hold, so k and v stay in LDS and a block has eight waves, two on
   // each 32 keys that take the two subtiles of a row tile; their sums are
@@ -687,7 +664,7 @@ template <typename T, int DP> struct DkvCfg {
   static constexpr bool WIDE = sizeof(T) == 2 && DP == 128;
   static constexpr int NW = WIDE ? 8 : 4;
   static constexpr int KV = WIDE ? 2 * 128 * DP * (int)sizeof(T) : 0;   // k and v of the block's keys
-  static constexpr size_t LDS = (size_t)NST * STAGE + KV;
+  static constexpr size_t LDS = (size_t)2 * STAGE + KV;
   // waves a SIMD: narrow heads wait for memory more than they compute
   static constexpr int WAVES = sizeof(T) == 2 ? (DP == 32 ? 3 : 2) : DP == 32 ? 2 : 1;
   static constexpr int SINK_STAGE = 2 * 32 * DP * (int)sizeof(T) + 512;   // a wave's 32 rows
@@ -735,7 +712,7 @@ __global__ __launch_bounds__((64 * DkvCfg<T, DP>::NW), (DkvCfg<T, DP>::WAVES)) v
   TileLoad<T, DP, BQ, NW> lq, lg;
   lq.init(w, A.dim, A.q.ld);
   lg.init(w, A.dim, A.go.ld);
-  char* const KV = smem + Cfg::NST * Cfg::STAGE;       // wide heads: k (two tiles of 64 rows), v
+  char* const KV = smem + 2 * Cfg::STAGE;       // wide heads: k (two tiles of 64 rows), v
   if constexpr (WIDE) {
     TileLoad<T, DP, 64, NW> lk;
     lk.init(w, A.dim, A.k.ld);
@@ -751,23 +728,15 @@ __global__ __launch_bounds__((64 * DkvCfg<T, DP>::NW), (DkvCfg<T, DP>::WAVES)) v
       lk.issue(KV + (2 + h) * KB, w, (const T*)A.v.p + (int64_t)at * A.v.ld + kv * A.dim, nr, ~0ull);
     }
   }
-  constexpr int NST = Cfg::NST, PER = 2 * TileLoad<T, DP, BQ, NW>::PER + 1;
-  // head and first row of the tile to be issued next; its stage
-  int ig = 0, ii = k0, is = 0;
-  auto issue = [&]() __attribute__((always_inline)) {
-    const int h = kv * A.group + ig, nr = ig < A.group ? min(BQ, bend - ii) : 0;
-    const int64_t hd = nr > 0 ? h * A.dim : 0, i0 = nr > 0 ? ii : 0, at = nr > 0 ? (int64_t)h * A.rows + i0 : 0;
-    char* S = smem + is * Cfg::STAGE;
-    lq.issue(S, w, (const T*)A.q.p + i0 * A.q.ld + hd, nr, ~0ull);
-    lg.issue(S + TB, w, (const T*)A.go.p + i0 * A.go.ld + hd, nr, ~0ull);
-    // every wave one load: lse2, delta, and such that read nothing
-    issue_stats(S + 2 * TB + 256 * min(w, 2), (w == 0 ? A.lse2 : A.delta) + at, w < 2 ? nr : 0);
-    is = is + 1 == NST ? 0 : is + 1;
-    ii += BQ;
-    if (ii >= bend) {
-      ii = k0;
-      ++ig;
-    }
+  auto issue = [&](int t) __attribute__((always_inline)) {
+    if (t >= n) return;
+    const int g = t / per_head, i0 = k0 + (t - g * per_head) * BQ, h = kv * A.group + g, nr = min(BQ, bend - i0);
+    char* S = smem + (t & 1) * Cfg::STAGE;
+    lq.issue(S, w, (const T*)A.q.p + (int64_t)i0 * A.q.ld + h * A.dim, nr, ~0ull);
+    lg.issue(S + TB, w, (const T*)A.go.p + (int64_t)i0 * A.go.ld + h * A.dim, nr, ~0ull);
+    const int64_t at = (int64_t)h * A.rows + i0;
+    if (w == 0) issue_stats(S + 2 * TB, A.lse2 + at, nr);
+    if (w == 1) issue_stats(S + 2 * TB + 256, A.delta + at, nr);
   };
   const uint32_t rl = TL::row_lane(), cl = TL::col_lane();
   const float c = A.scale * LOG2E;
@@ -779,22 +748,13 @@ __global__ __launch_bounds__((64 * DkvCfg<T, DP>::NW), (DkvCfg<T, DP>::WAVES)) v
     for (int db = 0; db < TL::DB; ++db)
 #pragma unroll
       for (int r = 0; r < 16; ++r) dk[db][r] = dv[db][r] = 0.f;
-    ig = 0;
-    ii = k0;
-    is = 0;
-#pragma unroll
-    for (int t = 0; t < NST - 1; ++t) issue();
+    issue(0);
     int i0 = k0;
 #pragma unroll 1
     for (int t = 0; t < n; ++t) {
-      // tile t has landed, the wave's reads of tile t - 1 returned; past the
-      // barrier everybody's, and the next tile goes into that one's place
-      wait_loads<(NST - 2) * PER>();
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-      const char* S = smem + (is + 1 == NST ? 0 : is + 1) * Cfg::STAGE;
-      issue();
+      landed();
+      issue(t + 1);
+      const char* S = smem + (t & 1) * Cfg::STAGE;
       auto subtile = [&](int b) __attribute__((always_inline)) {
         const int ib = i0 + 32 * b;
         // rows ib .. ib+31 reach the wave's keys
@@ -820,7 +780,6 @@ __global__ __launch_bounds__((64 * DkvCfg<T, DP>::NW), (DkvCfg<T, DP>::WAVES)) v
       }
       i0 = i0 + BQ >= bend ? k0 : i0 + BQ;
     }
-    wait_loads<0>();                             // the loads past the last tile write LDS
     if constexpr (WIDE) {                        // the two waves of a key group, dk then dv, by registers
       float* R = reinterpret_cast<float*>(smem) + kg * TL::DB * 16 * 64 + lane;
 #pragma unroll

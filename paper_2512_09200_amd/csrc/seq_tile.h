@@ -192,7 +192,7 @@ struct Tile {
 // Direct loads of R rows of a tensor into a Tile by NW waves: R * UPR units,
 // 64 consecutive ones a wave load.  Rows from `rows` on (or whose bit of
 // `keep` is 0), and units past dim, become zeros: their offset lies past the
-// buffer.  Issues UNITS / NW loads a wave, whatever the arguments.
+// buffer.
 template <typename T, int DP, int R, int NW>
 struct TileLoad {
   using TL = Tile<T, DP>;
