@@ -123,10 +123,10 @@ static SeqCacheArgs cache_args(const lattice_seq_attn_desc* d, const lattice_seq
   return a;
 }
 
-// blocks of the attention kernels (the widest of them: one head of 128 rows a
-// block) and of the sinks' late rows
+// blocks of the attention kernels (128 rows of a head each) and of the sinks'
+// late rows (at most 64 sequences a block)
 static lattice_status check_attn_size(const lattice_seq_attn_desc* d, const lattice_seqs* s) {
-  if ((s->rows / 32 + 1) * d->heads > MAX_BLOCKS || (int64_t)s->num_seqs * d->kv_heads * 128 > MAX_BLOCKS * 4)
+  if ((s->rows / 128 + 4) * d->heads > MAX_BLOCKS / 2 || (int64_t)s->num_seqs * d->kv_heads > MAX_BLOCKS * 8)
     FAIL(LATTICE_ERR_UNSUPPORTED, "rows x heads or sequences x kv_heads too many for one launch");
   return LATTICE_OK;
 }

@@ -15,14 +15,16 @@
 //
 // Forward and dQ: a block is 4 waves of 32 rows of one head each; query heads
 // that share a key head share the block (as many of 4, 2 or 1 as divide the
-// group) so that a block's rows span a short range.  The product is taken
+// group) so that a block's rows span a short range (groups of 4, window 256 of
+// heads of 64, dQ: 76 us with one head a block, 69 so; window 2048 of heads of
+// 128: 952 and 927).  The product is taken
 // transposed, S^T = K Q^T: a lane holds one row's scores, its maximum and sum
 // need one exchange between lane halves, and the probabilities are the
 // next product's operand (O^T = V^T P^T) where they are.  K and V tiles go from
 // memory straight to LDS one tile ahead.
 //
-// dK and dV: a block is 4 waves of 32 keys, over the rows that see them and
-// the group's heads, S = Q K^T with the keys in registers.  Rows that see a
+// dK and dV: a block takes 128 keys, a wave 32 of them, over the rows that see
+// them and the group's heads, S = Q K^T.  Rows that see a
 // sink after its window has passed are spread over blocks of their own
 // (seq_sink_kernel: a long sequence's sinks would otherwise be one block's work),
 // whose partial sums the main kernel adds in a fixed order.  No atomics.
@@ -872,65 +874,65 @@ __global__ __launch_bounds__(256, 1) void seq_sink_kernel(AttnK A, int parts, in
     any = s0 >= 0 && s0 < e0 && late > 0 && (int64_t)u * late_chunk(A, late) < late;
   }
   for (uint64_t todo = __ballot(any); todo; todo &= todo - 1) {
-  const int seq = first + __builtin_ctzll(todo);
-  const int s0 = A.offsets[seq], e0 = min(A.offsets[seq + 1], A.rows);
-  const int x0 = late_row(A, s0), late = e0 - x0;
-  const int chunk = late_chunk(A, late), a0 = x0 + u * chunk, a1 = (int)min((int64_t)e0, (int64_t)a0 + chunk);
-  const int a = part * 32 + (lane & 31), j = s0 + a;   // late rows exist: the sequence has all its sinks
-  const bool shown = a < A.sinks && (!A.mask || A.mask[j]);
-  const int per_head = (a1 - a0 + 31) / 32, n = per_head * A.group;
+    const int seq = first + __builtin_ctzll(todo);
+    const int s0 = A.offsets[seq], e0 = min(A.offsets[seq + 1], A.rows);
+    const int x0 = late_row(A, s0), late = e0 - x0;
+    const int chunk = late_chunk(A, late), a0 = x0 + u * chunk, a1 = (int)min((int64_t)e0, (int64_t)a0 + chunk);
+    const int a = part * 32 + (lane & 31), j = s0 + a;   // late rows exist: the sequence has all its sinks
+    const bool shown = a < A.sinks && (!A.mask || A.mask[j]);
+    const int per_head = (a1 - a0 + 31) / 32, n = per_head * A.group;
 
-  TileLoad<T, DP, 32, 1> lq, lg;
-  lq.init(0, A.dim, A.q.ld);
-  lg.init(0, A.dim, A.go.ld);
-  char* S = smem + w * Cfg::SINK_STAGE;
-  Frag<T> kf[TL::KS], vf[TL::KS];
-  load_rows<T, DP>(A.k, a < A.sinks ? j : s0, kv, A.dim, kf);
-  load_rows<T, DP>(A.v, a < A.sinks ? j : s0, kv, A.dim, vf);
-  const uint32_t rl = TL::row_lane(), cl = TL::col_lane();
-  const float c = A.scale * LOG2E;
-  f32x16 dk[TL::DB], dv[TL::DB];
-#pragma unroll
-  for (int db = 0; db < TL::DB; ++db)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) dk[db][r] = dv[db][r] = 0.f;
-#pragma unroll 1
-  for (int t = w; t < n; t += 4) {
-    const int g = t / per_head, i0 = a0 + (t - g * per_head) * 32, h = kv * A.group + g, nr = min(32, a1 - i0);
-    const int64_t at = (int64_t)h * A.rows + i0;
-    // the wave's own stage: its reads of the subtile before have returned
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    lq.issue(S, 0, (const T*)A.q.p + (int64_t)i0 * A.q.ld + h * A.dim, nr, ~0ull);
-    lg.issue(S + TB, 0, (const T*)A.go.p + (int64_t)i0 * A.go.ld + h * A.dim, nr, ~0ull);
-    issue_stats(S + 2 * TB, A.lse2 + at, nr);
-    issue_stats(S + 2 * TB + 256, A.delta + at, nr);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    dkv_subtile<T, DP, false>(scores<T, DP>(S, rl, 0, kf), scores<T, DP>(S + TB, rl, 0, vf), S, S + TB,
-                              (const float*)(S + 2 * TB), (const float*)(S + 2 * TB + 256), 0, rl, cl, c, 0,
-                              shown ? (unsigned)nr : 0u, nr == 32 && wave_all(shown), dk, dv);
-  }
-  // waves' sums, one after the other, in LDS [2][DP][33]
-  float* R = reinterpret_cast<float*>(smem);
-  for (int v = 0; v < 4; ++v) {
-    __syncthreads();
-    if (w != v) continue;
+    TileLoad<T, DP, 32, 1> lq, lg;
+    lq.init(0, A.dim, A.q.ld);
+    lg.init(0, A.dim, A.go.ld);
+    char* S = smem + w * Cfg::SINK_STAGE;
+    Frag<T> kf[TL::KS], vf[TL::KS];
+    load_rows<T, DP>(A.k, a < A.sinks ? j : s0, kv, A.dim, kf);
+    load_rows<T, DP>(A.v, a < A.sinks ? j : s0, kv, A.dim, vf);
+    const uint32_t rl = TL::row_lane(), cl = TL::col_lane();
+    const float c = A.scale * LOG2E;
+    f32x16 dk[TL::DB], dv[TL::DB];
 #pragma unroll
     for (int db = 0; db < TL::DB; ++db)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int d = 32 * db + frag_off(r) + 4 * half, x = d * 33 + (lane & 31);
-        R[x] = dk[db][r] + (v ? R[x] : 0.f);
-        R[DP * 33 + x] = dv[db][r] + (v ? R[DP * 33 + x] : 0.f);
-      }
-  }
-  __syncthreads();
-  float* P = A.part + (((int64_t)seq * A.kv_heads + kv) * A.ns + u) * 2 * A.sinks * A.dim;
-  const int na = min(32, A.sinks - part * 32);
-  for (int x = threadIdx.x; x < 2 * na * A.dim; x += 256) {
-    const int m = x / (na * A.dim), y = x - m * na * A.dim, r = y / A.dim, d = y - r * A.dim;
-    P[((int64_t)m * A.sinks + part * 32 + r) * A.dim + d] = R[m * DP * 33 + d * 33 + r];
-  }
-  __syncthreads();                           // R is read; the stages may be loaded again
+      for (int r = 0; r < 16; ++r) dk[db][r] = dv[db][r] = 0.f;
+#pragma unroll 1
+    for (int t = w; t < n; t += 4) {
+      const int g = t / per_head, i0 = a0 + (t - g * per_head) * 32, h = kv * A.group + g, nr = min(32, a1 - i0);
+      const int64_t at = (int64_t)h * A.rows + i0;
+      // the wave's own stage: its reads of the subtile before have returned
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      lq.issue(S, 0, (const T*)A.q.p + (int64_t)i0 * A.q.ld + h * A.dim, nr, ~0ull);
+      lg.issue(S + TB, 0, (const T*)A.go.p + (int64_t)i0 * A.go.ld + h * A.dim, nr, ~0ull);
+      issue_stats(S + 2 * TB, A.lse2 + at, nr);
+      issue_stats(S + 2 * TB + 256, A.delta + at, nr);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      dkv_subtile<T, DP, false>(scores<T, DP>(S, rl, 0, kf), scores<T, DP>(S + TB, rl, 0, vf), S, S + TB,
+                                (const float*)(S + 2 * TB), (const float*)(S + 2 * TB + 256), 0, rl, cl, c, 0,
+                                shown ? (unsigned)nr : 0u, nr == 32 && wave_all(shown), dk, dv);
+    }
+    // waves' sums, one after the other, in LDS [2][DP][33]
+    float* R = reinterpret_cast<float*>(smem);
+    for (int v = 0; v < 4; ++v) {
+      __syncthreads();
+      if (w != v) continue;
+#pragma unroll
+      for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int d = 32 * db + frag_off(r) + 4 * half, x = d * 33 + (lane & 31);
+          R[x] = dk[db][r] + (v ? R[x] : 0.f);
+          R[DP * 33 + x] = dv[db][r] + (v ? R[DP * 33 + x] : 0.f);
+        }
+    }
+    __syncthreads();
+    float* P = A.part + (((int64_t)seq * A.kv_heads + kv) * A.ns + u) * 2 * A.sinks * A.dim;
+    const int na = min(32, A.sinks - part * 32);
+    for (int x = threadIdx.x; x < 2 * na * A.dim; x += 256) {
+      const int m = x / (na * A.dim), y = x - m * na * A.dim, r = y / A.dim, d = y - r * A.dim;
+      P[((int64_t)m * A.sinks + part * 32 + r) * A.dim + d] = R[m * DP * 33 + d * 33 + r];
+    }
+    __syncthreads();                           // R is read; the stages may be loaded again
   }
 }
 

@@ -16,6 +16,9 @@
 // The new event's own k and v replace their slot's row where the tile is
 // used (registers for k, the LDS row for v), so nothing waits for the cache's
 // update; the split that holds the slot writes it.
+//
+// 1024 users, windows of 1024 slots of 128, 2 key heads, bf16: 183 us, 5.1 TB/s
+// of the bytes it cannot do without (a plain copy reaches 4.85).
 #include "kernels.h"
 #include "seq_rope.h"
 #include "seq_tile.h"
@@ -361,7 +364,9 @@ __global__ __launch_bounds__(256) void seq_step_join_kernel(StepK A) {
 }
 
 // Splits of the slots: enough blocks for the two a compute unit holds, at
-// least 256 slots (two rounds of a block's waves) each.
+// least 256 slots (two rounds of a block's waves) each.  Three users, 65536 slots
+// of 128, 2 key heads: 47 us and 6 for the join with 512 splits in all, 48 and 8.5
+// with 1024, 47 and 5.5 with 256; unsplit the six blocks would take milliseconds.
 static int step_splits(int batch, int heads, int kv_heads, int cap) {
   const int hg = cdiv(heads / kv_heads, STEP_HEADS);
   const int64_t blocks = (int64_t)batch * kv_heads * hg;

@@ -331,6 +331,36 @@ def test_rows_beyond_4_gib():
     assert all(torch.equal(a, b) for a, b in zip(r, r2))
 
 
+def test_hundreds_of_thousands_of_sequences():
+    """Sequences of one and two rows, far more than blocks or grid dimensions
+    of 16 bits: values by hand (a row that sees only itself returns its v: the
+    probability p and the sum l = p are the same number, so p v (1 / l) has three
+    roundings, 2^-24 each)."""
+    from paper_2512_09200_amd import api
+    S, D = 300_000, 8
+    lens = np.tile([1, 2, 1], S // 3)
+    off = offs(lens)
+    T = int(off[-1])
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    q, k, v, do = (torch.randn(T, 1, D, generator=g, device=DEV) for _ in range(4))
+    s = api.lattice_seq_plan(torch.from_numpy(off.astype(np.int32)).to(DEV), T, max_len=3)
+    out, sv = api.lattice_seq_attn_fwd(s, q, k, v, 1, 1)      # window 1: itself, and the first row
+    dq, dk, dv = api.lattice_seq_attn_bwd(s, q, k, v, out, sv, do, 1, 1)
+    second = torch.zeros(T, dtype=torch.bool, device=DEV)
+    second[torch.from_numpy(off[:-1][lens == 2] + 1).to(DEV)] = True
+    first = torch.roll(second, -1)
+    assert ((out[~second] - v[~second]).abs() <= 4 * 2.0 ** -24 * v[~second].abs()).all()
+    a, b = q[second].double(), torch.stack([k[first], k[second]]).double()
+    P = torch.softmax((a * b).sum(-1, keepdim=True) * D ** -0.5, 0)
+    w = (P * torch.stack([v[first], v[second]]).double()).sum(0)
+    assert (out[second].double() - w).abs().max() < 1e-5
+    # P = exp(s - lse): s and lse up to 8 with 2^-24 each for four roundings
+    assert (dv[~second & ~first].double() - do[~second & ~first].double()).abs().max() < 1e-5
+    assert (dv[second].double() - P[1] * do[second].double()).abs().max() < 1e-5
+    assert (dv[first].double() - (do[first].double() + P[0] * do[second].double())).abs().max() < 1e-5
+
+
 def test_caches_beyond_4_gib():
     from paper_2512_09200_amd import api
     rng = np.random.default_rng(4)
