@@ -594,16 +594,17 @@ def _vec(t, dtype, n, name, dev):
     return t.data_ptr() or None
 
 
-def _heads(t, like, rows, name):
-    """(pointer, row stride) of a tensor [rows, heads, head_dim] that goes with
-    `like`."""
-    shape, stride, D = t.shape, t.stride(), like.shape[2]
-    if len(shape) != 3 or shape[0] != rows or shape[2] != D or t.dtype != like.dtype:
-        raise ValueError(f"{name}: expected [{rows}, heads, {D}] of {like.dtype}, got {tuple(shape)} of {t.dtype}")
+def _heads(t, like, name):
+    """(pointer, row stride) of a tensor [rows, heads, head_dim]; like: the
+    (rows, head_dim, dtype, GPU) that a call's tensors share."""
+    rows, D, dtype, dev = like
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != rows or shape[2] != D or t.dtype != dtype:
+        raise ValueError(f"{name}: expected [{rows}, heads, {D}] of {dtype}, got {tuple(shape)} of {t.dtype}")
     if rows and ((D > 1 and stride[2] != 1) or (shape[1] > 1 and stride[1] != D)):
         raise ValueError(f"{name}: the heads of a row must be contiguous")
-    if t.get_device() != like.get_device():
-        raise ValueError(f"{name} is not on the other tensors' device")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is not on GPU {dev}")
     return t.data_ptr() or None, stride[0] if rows > 1 else -(-shape[1] * D // 8) * 8
 
 
@@ -625,7 +626,7 @@ class Seqs:
 
     def __init__(self, offsets, rows, max_len, padded):
         self.rows, self.num_seqs, self.offsets, self.padded = int(rows), offsets.numel() - 1, offsets, padded
-        self.span = torch.empty((self.rows, 2), dtype=torch.int32, device=offsets.device)
+        self.span = offsets.new_empty((self.rows, 2))
         self.desc = A.lattice_seqs(rows=self.rows, num_seqs=self.num_seqs, offsets=offsets.data_ptr(),
                                    span=self.span.data_ptr() if self.rows else None, max_len=int(max_len))
 
@@ -671,13 +672,14 @@ def lattice_qk_rope_fwd(seqs, q, k, gain_q=None, gain_k=None, theta=10000.0, rot
     queries and keys; returns (q_out, k_out).  seqs: the batch's plan, or None
     with positions (int32 [rows]).  rotary: rotated dimensions (None: all)."""
     desc = _rope_desc(q, k, gain_q, gain_k, theta, rotary, interleaved, eps, positions)
-    s, rows = _rope_rows(seqs, q, positions), q.shape[0]
+    s, dev = _rope_rows(seqs, q, positions), _gpu(q)
+    like = q.shape[0], q.shape[2], q.dtype, dev
     q_out = _new_heads(q, seqs) if q_out is None else q_out
     k_out = _new_heads(k, seqs) if k_out is None else k_out
     if q_out.shape != q.shape or k_out.shape != k.shape:
         raise ValueError("outputs must have the inputs' shapes")
-    _run(_gpu(q), load().lattice_qk_rope_fwd, stream, byref(desc), byref(s), *_heads(q, q, rows, "q"),
-         *_heads(k, q, rows, "k"), *_heads(q_out, q, rows, "q_out"), *_heads(k_out, q, rows, "k_out"))
+    _run(dev, load().lattice_qk_rope_fwd, stream, byref(desc), byref(s), *_heads(q, like, "q"),
+         *_heads(k, like, "k"), *_heads(q_out, like, "q_out"), *_heads(k_out, like, "k_out"))
     _used_on(stream, q_out, k_out)
     return q_out, k_out
 
@@ -687,7 +689,8 @@ def lattice_qk_rope_bwd(seqs, q, k, d_q_out, d_k_out, gain_q=None, gain_k=None, 
     """Gradients (dq, dk, dgain_q, dgain_k) of lattice_qk_rope_fwd; the gains'
     are fp32 [head_dim], None where the gain is None."""
     desc = _rope_desc(q, k, gain_q, gain_k, theta, rotary, interleaved, eps, positions)
-    s, rows, D = _rope_rows(seqs, q, positions), q.shape[0], q.shape[2]
+    s, rows, D, dev = _rope_rows(seqs, q, positions), q.shape[0], q.shape[2], _gpu(q)
+    like = rows, D, q.dtype, dev
     dq = _new_heads(q, seqs) if dq is None else dq
     dk = _new_heads(k, seqs) if dk is None else dk
     if not (dq.shape == d_q_out.shape == q.shape and dk.shape == d_k_out.shape == k.shape):
@@ -696,9 +699,9 @@ def lattice_qk_rope_bwd(seqs, q, k, d_q_out, d_k_out, gain_q=None, gain_k=None, 
     lib = load()
     wsb = lib.lattice_qk_rope_bwd_workspace(byref(desc), rows) if dgq is not None or dgk is not None else 0
     ws = q.new_empty(wsb, dtype=torch.uint8) if wsb else None
-    _run(_gpu(q), lib.lattice_qk_rope_bwd, stream, byref(desc), byref(s), *_heads(q, q, rows, "q"),
-         *_heads(k, q, rows, "k"), *_heads(d_q_out, q, rows, "d_q_out"), *_heads(d_k_out, q, rows, "d_k_out"),
-         *_heads(dq, q, rows, "dq"), *_heads(dk, q, rows, "dk"), _p(dgq), _p(dgk), _p(ws), wsb)
+    _run(dev, lib.lattice_qk_rope_bwd, stream, byref(desc), byref(s), *_heads(q, like, "q"),
+         *_heads(k, like, "k"), *_heads(d_q_out, like, "d_q_out"), *_heads(d_k_out, like, "d_k_out"),
+         *_heads(dq, like, "dq"), *_heads(dk, like, "dk"), _p(dgq), _p(dgk), _p(ws), wsb)
     _used_on(stream, dq, dk, dgq, dgk, ws)
     return dq, dk, dgq, dgk
 
@@ -706,7 +709,7 @@ def lattice_qk_rope_bwd(seqs, q, k, d_q_out, d_k_out, gain_q=None, gain_k=None, 
 def _attn_desc(q, k, window, sinks, scale, key_mask):
     rows, H, D = _check_heads(q)
     return A.lattice_seq_attn_desc(_dt(q), H, _check_heads(k, "k")[1], D, min(int(window), 2 ** 31 - 1), int(sinks),
-                                   D ** -0.5 if scale is None else float(scale),
+                                   max(D, 1) ** -0.5 if scale is None else float(scale),
                                    _vec(key_mask, torch.uint8, rows, "key_mask", _gpu(q)))
 
 
@@ -724,17 +727,18 @@ def lattice_seq_attn_fwd(seqs, q, k, v, window, sinks=0, scale=None, key_mask=No
     saved a SeqAttnSaved for the backward (None when lse is False).  scale None:
     1 / sqrt(head_dim); key_mask: uint8 [rows], 0 hides an event from every
     reader."""
-    rows = seqs.rows
     desc = _attn_desc(q, k, window, sinks, scale, key_mask)
+    rows, dev = seqs.rows, _gpu(q)
+    like = rows, q.shape[2], q.dtype, dev
     out = _new_heads(q, seqs) if out is None else out
-    if out.shape != q.shape or v.shape != k.shape or seqs.offsets.get_device() != q.get_device():
+    if out.shape != q.shape or v.shape != k.shape or seqs.offsets.get_device() != dev:
         raise ValueError("out must have q's shape, v k's, and the plan their device")
     saved = None
     if lse:
         saved = SeqAttnSaved(q.new_empty((q.shape[1], rows), dtype=torch.float32),
                              torch.empty(q.shape, dtype=q.dtype, device=q.device) if desc.dtype == A.BF16 else None)
-    _run(_gpu(q), load().lattice_seq_attn_fwd, stream, byref(desc), byref(seqs.desc), *_heads(q, q, rows, "q"),
-         *_heads(k, q, rows, "k"), *_heads(v, q, rows, "v"), *_heads(out, q, rows, "out"),
+    _run(dev, load().lattice_seq_attn_fwd, stream, byref(desc), byref(seqs.desc), *_heads(q, like, "q"),
+         *_heads(k, like, "k"), *_heads(v, like, "v"), *_heads(out, like, "out"),
          _p(saved.lse) if lse else None, _p(saved.out_lo) if lse else None)
     _used_on(stream, out, *((saved.lse, saved.out_lo) if lse else ()))
     return out, saved
@@ -743,8 +747,9 @@ def lattice_seq_attn_fwd(seqs, q, k, v, window, sinks=0, scale=None, key_mask=No
 def lattice_seq_attn_bwd(seqs, q, k, v, out, saved, d_out, window, sinks=0, scale=None, key_mask=None, dq=None,
                          dk=None, dv=None, stream=None):
     """Gradients (dq, dk, dv) of lattice_seq_attn_fwd, from its out and saved."""
-    rows, dev = seqs.rows, _gpu(q)
     desc = _attn_desc(q, k, window, sinks, scale, key_mask)
+    rows, dev = seqs.rows, _gpu(q)
+    like = rows, q.shape[2], q.dtype, dev
     dq = _new_heads(q, seqs) if dq is None else dq
     dk = _new_heads(k, seqs) if dk is None else dk
     dv = _new_heads(v, seqs) if dv is None else dv
@@ -755,11 +760,11 @@ def lattice_seq_attn_bwd(seqs, q, k, v, out, saved, d_out, window, sinks=0, scal
     lib = load()
     wsb = lib.lattice_seq_attn_bwd_workspace(byref(desc), byref(seqs.desc))
     ws = q.new_empty(wsb, dtype=torch.uint8) if wsb else None
-    _run(dev, lib.lattice_seq_attn_bwd, stream, byref(desc), byref(seqs.desc), *_heads(q, q, rows, "q"),
-         *_heads(k, q, rows, "k"), *_heads(v, q, rows, "v"), *_heads(out, q, rows, "out"),
+    _run(dev, lib.lattice_seq_attn_bwd, stream, byref(desc), byref(seqs.desc), *_heads(q, like, "q"),
+         *_heads(k, like, "k"), *_heads(v, like, "v"), *_heads(out, like, "out"),
          _vec(saved.lse, torch.float32, q.shape[1] * rows, "lse", dev),
-         _vec(saved.out_lo, q.dtype, out.numel(), "out_lo", dev), *_heads(d_out, q, rows, "d_out"),
-         *_heads(dq, q, rows, "dq"), *_heads(dk, q, rows, "dk"), *_heads(dv, q, rows, "dv"), _p(ws), wsb)
+         _vec(saved.out_lo, q.dtype, out.numel(), "out_lo", dev), *_heads(d_out, like, "d_out"),
+         *_heads(dq, like, "dq"), *_heads(dk, like, "dk"), *_heads(dv, like, "dv"), _p(ws), wsb)
     _used_on(stream, dq, dk, dv, ws)
     return dq, dk, dv
 
@@ -779,13 +784,14 @@ def lattice_seq_cache_fill(seqs, k, v, k_cache, v_cache, window, sinks=0, cache_
     into ring caches [caches, kv_heads, sinks + window, head_dim].  cache_index
     (int32 [S], different ones; None: s) and first (int32 [S], the position of
     each sequence's first row; None: 0)."""
-    rows, S, dev = seqs.rows, seqs.num_seqs, _gpu(k)
-    desc = _attn_desc(k, k, window, sinks, None, None)
+    desc = _attn_desc(k, k, window, sinks, 1.0, None)
+    S, dev = seqs.num_seqs, _gpu(k)
+    like = seqs.rows, k.shape[2], k.dtype, dev
     cache = _cache(k_cache, v_cache, k, k.shape[1], window, sinks)
     if v.shape != k.shape or seqs.offsets.get_device() != dev:
         raise ValueError("v must have k's shape, and the plan their device")
-    _run(dev, load().lattice_seq_cache_fill, stream, byref(desc), byref(seqs.desc), *_heads(k, k, rows, "k"),
-         *_heads(v, k, rows, "v"), _vec(first, torch.int32, S, "first", dev),
+    _run(dev, load().lattice_seq_cache_fill, stream, byref(desc), byref(seqs.desc), *_heads(k, like, "k"),
+         *_heads(v, like, "v"), _vec(first, torch.int32, S, "first", dev),
          _vec(cache_index, torch.int32, S, "cache_index", dev), byref(cache))
 
 
@@ -799,6 +805,7 @@ def lattice_seq_step(q, k, v, lens, k_cache, v_cache, window, sinks=0, cache_ind
     out; users with lens < 0 or a cache_index out of range are skipped."""
     desc = _attn_desc(q, k, window, sinks, scale, None)
     B, dev = q.shape[0], _gpu(q)
+    like = B, q.shape[2], q.dtype, dev
     cache = _cache(k_cache, v_cache, q, k.shape[1], window, sinks)
     rd = byref(_rope_desc(q, k, gain_q, gain_k, theta, rotary, interleaved, eps, positions)) if rope else None
     out = torch.empty_like(q) if out is None else out
@@ -807,8 +814,8 @@ def lattice_seq_step(q, k, v, lens, k_cache, v_cache, window, sinks=0, cache_ind
     lib = load()
     wsb = lib.lattice_seq_step_workspace(byref(desc), B)
     ws = q.new_empty(wsb, dtype=torch.uint8) if wsb else None
-    _run(dev, lib.lattice_seq_step, stream, byref(desc), rd, B, *_heads(q, q, B, "q"), *_heads(k, q, B, "k"),
-         *_heads(v, q, B, "v"), _vec(lens, torch.int32, B, "lens", dev),
-         _vec(cache_index, torch.int32, B, "cache_index", dev), byref(cache), *_heads(out, q, B, "out"), _p(ws), wsb)
+    _run(dev, lib.lattice_seq_step, stream, byref(desc), rd, B, *_heads(q, like, "q"), *_heads(k, like, "k"),
+         *_heads(v, like, "v"), _vec(lens, torch.int32, B, "lens", dev),
+         _vec(cache_index, torch.int32, B, "cache_index", dev), byref(cache), *_heads(out, like, "out"), _p(ws), wsb)
     _used_on(stream, out, ws)
     return out

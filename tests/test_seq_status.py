@@ -176,21 +176,24 @@ def test_cache_and_step(lib):
 
 def test_binding_checks_before_it_calls():
     x = torch.zeros(4, 2, 64)
+    like = 4, 64, torch.float32, -1
     with pytest.raises(ValueError, match="GPU"):
         api.lattice_qk_rope_fwd(None, x, x, positions=torch.zeros(4, dtype=torch.int32))
     with pytest.raises(ValueError, match="int32"):
         api.lattice_seq_plan(torch.zeros(3), 4)
     with pytest.raises(ValueError, match="contiguous"):
-        api._heads(torch.zeros(4, 64, 2).transpose(1, 2), x, 4, "q")
+        api._heads(torch.zeros(4, 64, 2).transpose(1, 2), like, "q")
     with pytest.raises(ValueError, match="expected"):
-        api._heads(x[:3], x, 4, "q")
+        api._heads(x[:3], like, "q")
     with pytest.raises(ValueError, match="expected"):
-        api._heads(x.bfloat16(), x, 4, "q")
+        api._heads(x.bfloat16(), like, "q")
     with pytest.raises(ValueError, match="not on"):
         api._vec(torch.zeros(4, dtype=torch.int32), torch.int32, 4, "lens", 0)
     with pytest.raises(ValueError, match="heads, head_dim"):
         api.lattice_qk_rope_fwd(None, x[0], x[0])
-    assert api._heads(torch.zeros(4, 6, 64)[:, 2:4], x, 4, "k")[1] == 384
+    assert api._heads(torch.zeros(4, 6, 64)[:, 2:4], like, "k")[1] == 384
+    with pytest.raises(ValueError, match="not on GPU"):
+        api._heads(x, like[:3] + (0,), "q")
     with pytest.raises(ValueError, match="elements"):
         api._vec(torch.zeros(3, dtype=torch.int32), torch.int32, 4, "lens", 0)
     with pytest.raises(ValueError, match="caches"):
