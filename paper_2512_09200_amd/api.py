@@ -557,23 +557,41 @@ def lattice_interact_state(kind, X, stack, stack_n, ws, ln_eps=1e-5, fp8_proj=No
 # ---------------------------------------------------------------------------
 # Event sequences: tensors [rows, heads, head_dim] with the heads of a row
 # contiguous (slices of a projection's output are fine).
-def _run(dev, fn, stream, *args):
-    """Enqueue a C call on `stream` (None: the current one of the tensors' GPU).
-    Launches go to the current device, so it is made the tensors' own."""
+def _run(dev, fn, *args):
+    """Enqueue a C call on the current stream of the tensors' GPU.  Launches go
+    to the current device, so it is made the tensors' own."""
     if dev != torch.cuda.current_device():
         with torch.cuda.device(dev):
-            return _run(dev, fn, stream, *args)
-    s = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
-    check(fn(*args, s))
+            return _run(dev, fn, *args)
+    check(fn(*args, torch._C._cuda_getCurrentRawStream(dev)))
 
 
-def _used_on(stream, *ts):
-    """Memory allocated here for a call on another stream is not reused before
-    that stream has passed the call."""
-    if stream is not None:
-        for t in ts:
-            if t is not None:
-                t.record_stream(stream)
+def _memory(xs):
+    """The tensors of a call's arguments or results."""
+    for x in xs:
+        if isinstance(x, Seqs):
+            yield from (x.offsets, x.span)
+        elif isinstance(x, SeqAttnSaved):
+            yield from _memory((x.lse, x.out_lo))
+        elif isinstance(x, torch.Tensor):
+            yield x
+
+
+def _on(stream, t, fn, *args):
+    """fn(*args) with `stream` current: what it allocates and zero-fills then
+    belongs to that stream (memory of the caller's stream could still be in use
+    by work queued there).  The arguments' memory is not reused before `stream`
+    has passed the call, nor the results' before the caller's stream has."""
+    if stream.device != t.device:
+        raise ValueError(f"the stream is on {stream.device}, the tensors on {t.device}")
+    back = torch.cuda.current_stream(t.device)
+    with torch.cuda.stream(stream):
+        out = fn(*args)
+    for x in _memory(args):
+        x.record_stream(stream)
+    for x in _memory(out if isinstance(out, tuple) else (out,)):
+        x.record_stream(back)
+    return out
 
 
 def _gpu(t):
@@ -637,12 +655,13 @@ def lattice_seq_plan(offsets, rows, max_len=0, padded=False, stream=None):
     serves every layer and direction of the batch.  max_len: a bound of the
     sequences' lengths (0: unknown); padded: offsets[S] may be less than rows
     (outputs that the calls below allocate are then zero-filled)."""
+    if stream is not None:
+        return _on(stream, offsets, lattice_seq_plan, offsets, rows, max_len, padded)
     if offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.numel() < 1 or not offsets.is_contiguous():
         raise ValueError("offsets: expected a contiguous int32 vector [S + 1]")
     dev = _gpu(offsets)
     s = Seqs(offsets, rows, max_len, padded)
-    _run(dev, load().lattice_seq_plan, stream, byref(s.desc), s.desc.span)
-    _used_on(stream, s.span)
+    _run(dev, load().lattice_seq_plan, byref(s.desc), s.desc.span)
     return s
 
 
@@ -671,6 +690,9 @@ def lattice_qk_rope_fwd(seqs, q, k, gain_q=None, gain_k=None, theta=10000.0, rot
     """Per-head RMSNorm (gains [head_dim] fp32 or None) and rotary positions of
     queries and keys; returns (q_out, k_out).  seqs: the batch's plan, or None
     with positions (int32 [rows]).  rotary: rotated dimensions (None: all)."""
+    if stream is not None:
+        return _on(stream, q, lattice_qk_rope_fwd, seqs, q, k, gain_q, gain_k, theta, rotary,
+                   interleaved, eps, positions, q_out, k_out)
     desc = _rope_desc(q, k, gain_q, gain_k, theta, rotary, interleaved, eps, positions)
     s, dev = _rope_rows(seqs, q, positions), _gpu(q)
     like = q.shape[0], q.shape[2], q.dtype, dev
@@ -678,9 +700,8 @@ def lattice_qk_rope_fwd(seqs, q, k, gain_q=None, gain_k=None, theta=10000.0, rot
     k_out = _new_heads(k, seqs) if k_out is None else k_out
     if q_out.shape != q.shape or k_out.shape != k.shape:
         raise ValueError("outputs must have the inputs' shapes")
-    _run(dev, load().lattice_qk_rope_fwd, stream, byref(desc), byref(s), *_heads(q, like, "q"),
+    _run(dev, load().lattice_qk_rope_fwd, byref(desc), byref(s), *_heads(q, like, "q"),
          *_heads(k, like, "k"), *_heads(q_out, like, "q_out"), *_heads(k_out, like, "k_out"))
-    _used_on(stream, q_out, k_out)
     return q_out, k_out
 
 
@@ -688,6 +709,9 @@ def lattice_qk_rope_bwd(seqs, q, k, d_q_out, d_k_out, gain_q=None, gain_k=None, 
                         interleaved=False, eps=1e-6, positions=None, dq=None, dk=None, stream=None):
     """Gradients (dq, dk, dgain_q, dgain_k) of lattice_qk_rope_fwd; the gains'
     are fp32 [head_dim], None where the gain is None."""
+    if stream is not None:
+        return _on(stream, q, lattice_qk_rope_bwd, seqs, q, k, d_q_out, d_k_out, gain_q, gain_k,
+                   theta, rotary, interleaved, eps, positions, dq, dk)
     desc = _rope_desc(q, k, gain_q, gain_k, theta, rotary, interleaved, eps, positions)
     s, rows, D, dev = _rope_rows(seqs, q, positions), q.shape[0], q.shape[2], _gpu(q)
     like = rows, D, q.dtype, dev
@@ -699,10 +723,9 @@ def lattice_qk_rope_bwd(seqs, q, k, d_q_out, d_k_out, gain_q=None, gain_k=None, 
     lib = load()
     wsb = lib.lattice_qk_rope_bwd_workspace(byref(desc), rows) if dgq is not None or dgk is not None else 0
     ws = q.new_empty(wsb, dtype=torch.uint8) if wsb else None
-    _run(dev, lib.lattice_qk_rope_bwd, stream, byref(desc), byref(s), *_heads(q, like, "q"),
+    _run(dev, lib.lattice_qk_rope_bwd, byref(desc), byref(s), *_heads(q, like, "q"),
          *_heads(k, like, "k"), *_heads(d_q_out, like, "d_q_out"), *_heads(d_k_out, like, "d_k_out"),
          *_heads(dq, like, "dq"), *_heads(dk, like, "dk"), _p(dgq), _p(dgk), _p(ws), wsb)
-    _used_on(stream, dq, dk, dgq, dgk, ws)
     return dq, dk, dgq, dgk
 
 
@@ -727,6 +750,9 @@ def lattice_seq_attn_fwd(seqs, q, k, v, window, sinks=0, scale=None, key_mask=No
     saved a SeqAttnSaved for the backward (None when lse is False).  scale None:
     1 / sqrt(head_dim); key_mask: uint8 [rows], 0 hides an event from every
     reader."""
+    if stream is not None:
+        return _on(stream, q, lattice_seq_attn_fwd, seqs, q, k, v, window, sinks, scale, key_mask, lse,
+                   out)
     desc = _attn_desc(q, k, window, sinks, scale, key_mask)
     rows, dev = seqs.rows, _gpu(q)
     like = rows, q.shape[2], q.dtype, dev
@@ -737,16 +763,18 @@ def lattice_seq_attn_fwd(seqs, q, k, v, window, sinks=0, scale=None, key_mask=No
     if lse:
         saved = SeqAttnSaved(q.new_empty((q.shape[1], rows), dtype=torch.float32),
                              torch.empty(q.shape, dtype=q.dtype, device=q.device) if desc.dtype == A.BF16 else None)
-    _run(dev, load().lattice_seq_attn_fwd, stream, byref(desc), byref(seqs.desc), *_heads(q, like, "q"),
+    _run(dev, load().lattice_seq_attn_fwd, byref(desc), byref(seqs.desc), *_heads(q, like, "q"),
          *_heads(k, like, "k"), *_heads(v, like, "v"), *_heads(out, like, "out"),
          _p(saved.lse) if lse else None, _p(saved.out_lo) if lse else None)
-    _used_on(stream, out, *((saved.lse, saved.out_lo) if lse else ()))
     return out, saved
 
 
 def lattice_seq_attn_bwd(seqs, q, k, v, out, saved, d_out, window, sinks=0, scale=None, key_mask=None, dq=None,
                          dk=None, dv=None, stream=None):
     """Gradients (dq, dk, dv) of lattice_seq_attn_fwd, from its out and saved."""
+    if stream is not None:
+        return _on(stream, q, lattice_seq_attn_bwd, seqs, q, k, v, out, saved, d_out, window, sinks,
+                   scale, key_mask, dq, dk, dv)
     desc = _attn_desc(q, k, window, sinks, scale, key_mask)
     rows, dev = seqs.rows, _gpu(q)
     like = rows, q.shape[2], q.dtype, dev
@@ -760,12 +788,11 @@ def lattice_seq_attn_bwd(seqs, q, k, v, out, saved, d_out, window, sinks=0, scal
     lib = load()
     wsb = lib.lattice_seq_attn_bwd_workspace(byref(desc), byref(seqs.desc))
     ws = q.new_empty(wsb, dtype=torch.uint8) if wsb else None
-    _run(dev, lib.lattice_seq_attn_bwd, stream, byref(desc), byref(seqs.desc), *_heads(q, like, "q"),
+    _run(dev, lib.lattice_seq_attn_bwd, byref(desc), byref(seqs.desc), *_heads(q, like, "q"),
          *_heads(k, like, "k"), *_heads(v, like, "v"), *_heads(out, like, "out"),
          _vec(saved.lse, torch.float32, q.shape[1] * rows, "lse", dev),
          _vec(saved.out_lo, q.dtype, out.numel(), "out_lo", dev), *_heads(d_out, like, "d_out"),
          *_heads(dq, like, "dq"), *_heads(dk, like, "dk"), *_heads(dv, like, "dv"), _p(ws), wsb)
-    _used_on(stream, dq, dk, dv, ws)
     return dq, dk, dv
 
 
@@ -784,13 +811,16 @@ def lattice_seq_cache_fill(seqs, k, v, k_cache, v_cache, window, sinks=0, cache_
     into ring caches [caches, kv_heads, sinks + window, head_dim].  cache_index
     (int32 [S], different ones; None: s) and first (int32 [S], the position of
     each sequence's first row; None: 0)."""
+    if stream is not None:
+        return _on(stream, k, lattice_seq_cache_fill, seqs, k, v, k_cache, v_cache, window, sinks,
+                   cache_index, first)
     desc = _attn_desc(k, k, window, sinks, 1.0, None)
     S, dev = seqs.num_seqs, _gpu(k)
     like = seqs.rows, k.shape[2], k.dtype, dev
     cache = _cache(k_cache, v_cache, k, k.shape[1], window, sinks)
     if v.shape != k.shape or seqs.offsets.get_device() != dev:
         raise ValueError("v must have k's shape, and the plan their device")
-    _run(dev, load().lattice_seq_cache_fill, stream, byref(desc), byref(seqs.desc), *_heads(k, like, "k"),
+    _run(dev, load().lattice_seq_cache_fill, byref(desc), byref(seqs.desc), *_heads(k, like, "k"),
          *_heads(v, like, "v"), _vec(first, torch.int32, S, "first", dev),
          _vec(cache_index, torch.int32, S, "cache_index", dev), byref(cache))
 
@@ -803,6 +833,9 @@ def lattice_seq_step(q, k, v, lens, k_cache, v_cache, window, sinks=0, cache_ind
     caches at position lens (int32 [batch]: the events they have; the caller
     advances them), attention of q over the caches' visible slots.  Returns
     out; users with lens < 0 or a cache_index out of range are skipped."""
+    if stream is not None:
+        return _on(stream, q, lattice_seq_step, q, k, v, lens, k_cache, v_cache, window, sinks, cache_index,
+                   scale, rope, gain_q, gain_k, theta, rotary, interleaved, eps, positions, out)
     desc = _attn_desc(q, k, window, sinks, scale, None)
     B, dev = q.shape[0], _gpu(q)
     like = B, q.shape[2], q.dtype, dev
@@ -814,8 +847,7 @@ def lattice_seq_step(q, k, v, lens, k_cache, v_cache, window, sinks=0, cache_ind
     lib = load()
     wsb = lib.lattice_seq_step_workspace(byref(desc), B)
     ws = q.new_empty(wsb, dtype=torch.uint8) if wsb else None
-    _run(dev, lib.lattice_seq_step, stream, byref(desc), rd, B, *_heads(q, like, "q"), *_heads(k, like, "k"),
+    _run(dev, lib.lattice_seq_step, byref(desc), rd, B, *_heads(q, like, "q"), *_heads(k, like, "k"),
          *_heads(v, like, "v"), _vec(lens, torch.int32, B, "lens", dev),
          _vec(cache_index, torch.int32, B, "cache_index", dev), byref(cache), *_heads(out, like, "out"), _p(ws), wsb)
-    _used_on(stream, out, ws)
     return out

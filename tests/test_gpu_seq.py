@@ -400,6 +400,68 @@ def test_a_stream_of_its_own_keeps_its_memory():
         assert all(torch.equal(x, c[m]) for x, m in zip(g, ("dq", "dk", "dv")))
 
 
+def test_a_padded_batch_on_a_stream_of_its_own_while_the_current_one_is_behind():
+    """Outputs of a padded plan are zero-filled on the call's own stream: a fill
+    still queued on the current one would wipe them afterwards."""
+    from paper_2512_09200_amd import api
+    c = attn_case("bf16", 4, 2, 64, [700, 300], 50, 4, pad=40)
+    s = torch.cuda.Stream()
+    q0, k0 = api.lattice_qk_rope_fwd(c["s"], c["q"], c["k"])
+    g0 = api.lattice_qk_rope_bwd(c["s"], c["q"], c["k"], c["do"], c["k"])[:2]
+    want = [c["out"], c["dq"], c["dk"], c["dv"], q0, k0, *g0]
+    busy = torch.zeros(8192, 8192, device=DEV)
+    torch.mm(busy, busy)
+    torch.cuda.synchronize()
+    for _ in range(16):                                     # about a tenth of a second
+        busy = torch.mm(busy, busy)
+    out, sv = api.lattice_seq_attn_fwd(c["s"], c["q"], c["k"], c["v"], stream=s, **c["kw"])
+    got = [out, *api.lattice_seq_attn_bwd(c["s"], c["q"], c["k"], c["v"], out, sv, c["do"], stream=s, **c["kw"])]
+    got += api.lattice_qk_rope_fwd(c["s"], c["q"], c["k"], stream=s)
+    got += api.lattice_qk_rope_bwd(c["s"], c["q"], c["k"], c["do"], c["k"], stream=s)[:2]
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert torch.equal(g, w)
+
+
+def test_memory_of_a_call_on_its_own_stream_is_not_still_in_use_by_the_current_one():
+    """Memory that was just freed while the current stream has yet to write it
+    is not handed to a call on another stream."""
+    from paper_2512_09200_amd import api
+    c = attn_case("bf16", 4, 2, 64, [700, 300], 50, 4)
+    s = torch.cuda.Stream()
+    busy = torch.zeros(8192, 8192, device=DEV)
+    torch.mm(busy, busy)
+    torch.cuda.synchronize()
+    for _ in range(16):
+        busy = torch.mm(busy, busy)
+    late = [torch.empty_like(c["q"]).fill_(-1.0) for _ in range(8)]
+    del late
+    out, sv = api.lattice_seq_attn_fwd(c["s"], c["q"], c["k"], c["v"], stream=s, **c["kw"])
+    torch.cuda.synchronize()
+    assert torch.equal(out, c["out"])
+
+
+def test_a_step_and_a_fill_on_a_stream_of_its_own():
+    from paper_2512_09200_amd import api
+    rng = np.random.default_rng(11)
+    s = torch.cuda.Stream()
+    x = [randn(rng, 3, h, 64).to(DEV) for h in (4, 2, 2)]
+    plan = api.lattice_seq_plan(torch.tensor([0, 3], dtype=torch.int32, device=DEV), 3)
+    lens = torch.tensor([3, -1, 0], dtype=torch.int32, device=DEV)
+    got = []
+    for st in (None, s):
+        kc, vc = (torch.zeros(3, 2, 12, 64, device=DEV) for _ in range(2))
+        out = torch.full_like(x[0], 7.0)
+        torch.cuda.synchronize()
+        api.lattice_seq_cache_fill(plan, x[1], x[2], kc, vc, 8, 4, stream=st)
+        assert api.lattice_seq_step(*x, lens, kc, vc, 8, 4, out=out, stream=st) is out
+        torch.cuda.synchronize()
+        got.append((out, kc, vc))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    assert torch.all(got[0][0][1] == 7.0)
+
+
 # ---------------------------------------------------------------------------
 @pytest.mark.parametrize("dt,J,D,W,N", [("bf16", 2, 64, 30, 3), ("f32", 1, 8, 1, 0), ("bf16", 3, 40, 7, 64),
                                         ("f32", 2, 128, 200, 1), ("bf16", 40, 128, 20, 2)])

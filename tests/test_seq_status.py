@@ -3,6 +3,7 @@ machine without a GPU (raised before anything is enqueued; the pointers are
 placeholders), the workspace queries, and the binding's own checks."""
 import ctypes
 from ctypes import byref
+from types import SimpleNamespace
 
 import pytest
 import torch
@@ -198,3 +199,14 @@ def test_binding_checks_before_it_calls():
         api._vec(torch.zeros(3, dtype=torch.int32), torch.int32, 4, "lens", 0)
     with pytest.raises(ValueError, match="caches"):
         api._cache(torch.zeros(2, 2, 9, 64), torch.zeros(2, 2, 9, 64), x, 2, 8, 2)
+
+
+def test_a_stream_of_another_device_is_refused():
+    other = SimpleNamespace(device=torch.device("cuda:1"))
+    q = torch.zeros(2, 1, 8)
+    with pytest.raises(ValueError, match="the stream is on cuda:1"):
+        api.lattice_seq_plan(torch.zeros(2, dtype=torch.int32), 0, stream=other)
+    with pytest.raises(ValueError, match="the stream is on cuda:1"):
+        api.lattice_qk_rope_fwd(None, q, q, positions=torch.zeros(2, dtype=torch.int32), stream=other)
+    with pytest.raises(ValueError, match="the stream is on cuda:1"):
+        api.lattice_seq_step(q, q, q, torch.zeros(2, dtype=torch.int32), q, q, 1, stream=other)
