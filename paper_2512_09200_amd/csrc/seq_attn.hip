@@ -349,6 +349,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
   const float c = A.scale * LOG2E;
   f32x16 o[TL::DB];
   float m, l;
+  uint32_t seen;                     // not 0: the row sees a key (of the half's)
 
   // N subtiles of 32 keys from subtile b0 of the tile at kt
   auto attend = [&](auto strict_, int b0, const char* SK, const char* SV, int kt, uint64_t bits)
@@ -367,7 +368,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
         see[b] = row_bits(V, kt + 32 * (b0 + b), (uint32_t)(bits >> (32 * (b0 + b))));
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[b][r] = keep_or(s[b][r], bit_mask(see[b], r), 0xff800000u);
+        seen |= see[b];
       }
+    } else {
+      seen = 1;
     }
     float tm = s[0][0];
 #pragma unroll
@@ -431,6 +435,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
       for (int r = 0; r < 16; ++r) o[db][r] = 0.f;
     m = -INFINITY;
     l = 0.f;
+    seen = 0;
     ks.start();
 #pragma unroll 1
     for (int t = 0; t < kt_.n; ++t) {
@@ -448,6 +453,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
       }
     }
     l = add32(l);
+    // nothing seen: zeros; keys seen, but with scores of -inf alone: 0 / 0
+    const float any = max32(seen ? 1.f : 0.f);
+    if (l == 0.f && any > 0.f) l = NAN;
     const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
     for (int db = 0; db < TL::DB; ++db)

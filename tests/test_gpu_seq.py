@@ -246,6 +246,41 @@ def test_nonfinite_values_reach_only_rows_that_see_them(dt, D, bad):
             assert np.allclose(g[~touched], w[~touched], rtol=2e-2, atol=1e-2 if dt == "bf16" else 1e-5), (which, at, m)
 
 
+@pytest.mark.parametrize("dt,D,W,N", [("bf16", 64, 24, 2), ("f32", 32, 24, 2), ("bf16", 128, 24, 0), ("bf16", 32, 200, 0),
+                                      ("f32", 128, 1, 0)])
+def test_rows_whose_scores_are_all_minus_infinity(dt, D, W, N):
+    """Such a row is not one that sees nothing: its softmax is 0 / 0, in the
+    batch and in the step alike; rows that see nothing keep their zeros."""
+    from paper_2512_09200_amd import api
+    c = attn_case(dt, 4, 2, D, [90, 1, 140], W, N, hidden=0.2)
+    see = np.zeros((231, 231), bool)
+    for a, e in zip(c["off"][:-1], c["off"][1:]):
+        see[a:e, a:e] = o.visible(e - a, W, N, c["shown"][a:e])
+    q, k = c["q"].clone(), c["k"].clone()
+    k[:, :, 3] = k[:, :, 3].abs() + 1
+    at = [0, 33, 90, 91, 130, 230] + list(np.flatnonzero(~see.any(1))[:3])
+    q[at, :, 3] = -float("inf")
+    out, sv = api.lattice_seq_attn_fwd(c["s"], q, k, c["v"], **c["kw"])
+    dq, dk, dv = api.lattice_seq_attn_bwd(c["s"], q, k, c["v"], out, sv, c["do"], **c["kw"])
+    bad = np.zeros(231, bool)
+    bad[at] = True
+    none = ~see.any(1)
+    want = bad & ~none
+    assert want.sum() >= 4 and (W > 1 or none.any())
+    for x in (out, dq):
+        x = f64(x)
+        assert np.isnan(x[want]).all() and np.isfinite(x[~want]).all() and (x[none] == 0).all()
+    L = f64(sv.lse)
+    assert np.isnan(L[:, want]).all() and np.isneginf(L[:, none]).all() and np.isfinite(L[:, ~want & ~none]).all()
+    keys = see[want].any(0)
+    for x in (dk, dv):
+        assert np.isnan(f64(x)[keys]).all() and np.isfinite(f64(x)[~keys]).all()
+    kc, vc = (torch.zeros(1, 2, N + W, D, dtype=TT[dt], device=DEV) for _ in range(2))
+    step = api.lattice_seq_step(q[:1], k[:1], c["v"][:1], torch.zeros(1, dtype=torch.int32, device=DEV), kc, vc, W, N,
+                                rope=False)
+    assert torch.isnan(step).all()
+
+
 def test_attention_twice_on_side_streams_and_in_a_graph_gives_the_same_bits():
     from paper_2512_09200_amd import api
     c = attn_case("bf16", 8, 2, 64, LENS["mixed"], 60, 4, hidden=0.1)
