@@ -502,7 +502,8 @@ lattice_status lattice_qk_rope_bwd(const lattice_qk_rope_desc* desc, const latti
  * every reader; their k and v are never used).
  *   out_i = sum_j P_ij v_j,  P_ij = exp(scale <q_i, k_j> - lse_i).
  * A row that sees nothing gets out = 0 and lse = -inf, and passes no
- * gradient; one that sees keys but whose scores are all -inf gets NaN.  A non-finite value reaches only rows that see it. */
+ * gradient; one that sees keys but whose scores are all -inf gets NaN.  A
+ * non-finite value reaches only rows that see it. */
 #define LATTICE_SEQ_MAX_SINKS 64
 typedef struct {
   lattice_dtype dtype;
