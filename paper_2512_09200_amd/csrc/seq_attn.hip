@@ -55,6 +55,7 @@ struct AttnK {                     // kernel arguments
   int rows, dim, heads, kv_heads, group, window, sinks;
   int hb, row_tiles;               // heads of a block (forward, dQ), its row tiles
   int ns;                          // splits of a sequence's late rows (sinks' gradients)
+  int by_start;                    // which of `part` is a sequence's: late_slot()
   int num_seqs;
   float scale;
   const int32_t* offsets;
@@ -65,7 +66,7 @@ struct AttnK {                     // kernel arguments
   void* out_lo;                    // [rows, heads, dim] or null: what rounding took from o (bf16)
   float* lse2;                     // workspace [heads, rows]: lse log2 e, +inf where nothing is seen
   float* delta;                    // workspace [heads, rows]
-  float* part;                     // workspace [seqs][kv_heads][ns][2][sinks][dim]
+  float* part;                     // workspace [late_slots][kv_heads][ns][2][sinks][dim]
 };
 
 // What a lane's row sees
@@ -602,6 +603,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
 __device__ inline int late_row(const AttnK& A, int start) {
   return (int)min((int64_t)start + A.sinks + A.window - 1, (int64_t)SEQ_NO_ROW);
 }
+// Where the partial sums of a sequence with late rows lie.  It has at least
+// sinks + window rows, so start / (sinks + window) differs between such
+// sequences; its own number is taken where there are fewer sequences than that.
+__device__ inline int late_slot(const AttnK& A, int seq, int start) {
+  return A.by_start ? start / (A.sinks + A.window) : seq;
+}
 // rows of a split of n late rows
 __device__ inline int late_chunk(const AttnK& A, int n) { return ((n + A.ns - 1) / A.ns + 31) & ~31; }
 
@@ -819,10 +826,11 @@ __global__ __launch_bounds__((64 * DkvCfg<T, DP>::NW), (DkvCfg<T, DP>::WAVES)) v
     if (A.ns > 0 && rh == 0 && sink && shown && sp.end > late_row(A, sp.start)) {
       const int late = sp.end - late_row(A, sp.start), used = (late + late_chunk(A, late) - 1) / late_chunk(A, late);
       int lo = 0, hi = A.num_seqs;               // the sequence: the last that starts at sp.start or before
-      while (hi - lo > 1) {
+      while (!A.by_start && hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (A.offsets[mid] <= sp.start) lo = mid; else hi = mid;
       }
+      lo = late_slot(A, lo, sp.start);
       for (int u = 0; u < used; ++u) {
         const float* P = A.part + ((((int64_t)lo * A.kv_heads + kv) * A.ns + u) * 2 * A.sinks + (j - sp.start)) * A.dim;
 #pragma unroll
@@ -943,7 +951,7 @@ __global__ __launch_bounds__(256, 1) void seq_sink_kernel(AttnK A, int parts, in
         }
     }
     __syncthreads();
-    float* P = A.part + (((int64_t)seq * A.kv_heads + kv) * A.ns + u) * 2 * A.sinks * A.dim;
+    float* P = A.part + (((int64_t)late_slot(A, seq, s0) * A.kv_heads + kv) * A.ns + u) * 2 * A.sinks * A.dim;
     const int na = min(32, A.sinks - part * 32);
     for (int x = threadIdx.x; x < 2 * na * A.dim; x += 256) {
       const int m = x / (na * A.dim), y = x - m * na * A.dim, r = y / A.dim, d = y - r * A.dim;
@@ -987,12 +995,18 @@ static int late_splits(const SeqAttnArgs& a) {
   return (int)(n > 64 ? 64 : n < 1 ? 1 : n);
 }
 
+// Sequences that can have late rows: those of sinks + window rows at least.
+static int64_t late_slots(const SeqAttnArgs& a) {
+  const int64_t most = a.rows / ((int64_t)a.sinks + a.window);
+  return a.num_seqs < most ? a.num_seqs : most;
+}
+
 static size_t stats_bytes(const SeqAttnArgs& a) {
   return ((size_t)a.heads * a.rows * sizeof(float) + 255) & ~(size_t)255;
 }
 
 size_t seq_attn_bwd_workspace(const SeqAttnArgs& a) {
-  return 2 * stats_bytes(a) + (size_t)a.num_seqs * a.kv_heads * late_splits(a) * 2 * a.sinks * a.dim * sizeof(float);
+  return 2 * stats_bytes(a) + (size_t)late_slots(a) * a.kv_heads * late_splits(a) * 2 * a.sinks * a.dim * sizeof(float);
 }
 
 template <typename T, int DP>
@@ -1046,6 +1060,7 @@ hipError_t seq_attn_bwd(const SeqAttnArgs& a, void* ws, hipStream_t s) {
   A.delta = (float*)((char*)ws + stats);
   A.part = (float*)((char*)ws + 2 * stats);
   A.ns = late_splits(a);
+  A.by_start = late_slots(a) < a.num_seqs;
   if (a.dt == DT_BF16)
     return a.dim <= 32 ? bwd_launch<bf16_t, 32>(A, s) : a.dim <= 64 ? bwd_launch<bf16_t, 64>(A, s)
                                                                   : bwd_launch<bf16_t, 128>(A, s);

@@ -190,6 +190,17 @@ def test_sinks_of_very_long_sequences_in_many_splits():
     check_attn(attn_case("bf16", 2, 1, 32, [3, 2600, 10], 8, 35), "bf16", 8, 35)
 
 
+@pytest.mark.parametrize("dt,H,J,D", [("bf16", 4, 2, 32), ("f32", 2, 1, 40), ("bf16", 2, 2, 128)])
+@pytest.mark.parametrize("W,N", [(30, 5), (1, 1), (6, 64), (200, 3)])
+@pytest.mark.parametrize("known", [False, True])
+def test_a_long_history_among_many_short_ones(dt, H, J, D, W, N, known):
+    """Far more sequences than rows / (sinks + window), some of which just have
+    rows behind every sink's window or just do not."""
+    edge = [W + N - 1, W + N, W + N + 1]
+    lens = [3, 20, 1, 0, 9] * 20 + edge + [900] + edge[::-1] + [7, 2, 2] * 30
+    check_attn(attn_case(dt, H, J, D, lens, W, N, pad=3, max_len=900 if known else 0), dt, W, N)
+
+
 @pytest.mark.parametrize("dt,D", [("bf16", 64), ("f32", 128)])
 def test_rows_behind_the_last_sequence_stay(dt, D):
     from paper_2512_09200_amd import api

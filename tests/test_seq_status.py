@@ -148,6 +148,24 @@ def test_attn_tensors(lib):
     assert small < lib.lattice_seq_attn_bwd_workspace(byref(attn(window=80, sinks=2)), byref(seqs(max_len=91)))
 
 
+@pytest.mark.parametrize("rows,S,kw", [
+    (1_000_000, 500_000, dict(heads=2, kv_heads=2, head_dim=64, sinks=64, window=2048)),
+    (10_000_000, 500_000, dict(heads=8, kv_heads=8, head_dim=128, sinks=4, window=256)),
+    (1 << 20, 1, dict(heads=4, kv_heads=4, head_dim=128, sinks=64, window=1))])
+@pytest.mark.parametrize("max_len", [0, 5000])
+def test_backward_workspace_goes_by_rows_not_by_sequences(lib, rows, S, kw, max_len):
+    """A sequence whose sinks need room of their own has sinks + window rows or
+    more, so there are at most rows / (sinks + window) of them: their partial
+    sums are at most 2 * 4 * rows * kv_heads * head_dim bytes for one split
+    each, and another 4096 splits (of at most 64 sinks) for the whole call."""
+    d, s = attn(dtype=A.BF16, **kw), seqs(rows=rows, num_seqs=S, max_len=max_len)
+    need = lib.lattice_seq_attn_bwd_workspace(byref(d), byref(s))
+    L, D, J = kw["sinks"] + kw["window"], kw["head_dim"], kw["kv_heads"]
+    stats = 2 * (4 * rows * kw["heads"] + 256)
+    part = 8 * kw["sinks"] * D
+    assert 2 * 4 * rows * kw["heads"] < need <= stats + part * (J * (rows // L) + 4096 + 64 * J)
+
+
 def test_cache_and_step(lib):
     d, c, r = attn(), cache(), rope()
 
