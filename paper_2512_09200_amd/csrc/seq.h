@@ -46,7 +46,6 @@ struct SeqAttnArgs {
   int64_t rows = 0;
   int num_seqs = 0;
   int64_t max_len = 0;                 // 1 .. rows
-  const int32_t* offsets = nullptr;
   const SeqSpan* span = nullptr;
   const uint8_t* key_mask = nullptr;
   int heads = 0, kv_heads = 0, dim = 0, window = 0, sinks = 0;

@@ -97,7 +97,6 @@ static SeqAttnArgs attn_args(const lattice_seq_attn_desc* d, const lattice_seqs*
   a.rows = s->rows;
   a.num_seqs = s->num_seqs;
   a.max_len = s->max_len > 0 && s->max_len < s->rows ? s->max_len : s->rows;
-  a.offsets = s->offsets;
   a.span = reinterpret_cast<const SeqSpan*>(s->span);
   a.key_mask = d->key_mask;
   a.heads = d->heads;
@@ -123,11 +122,10 @@ static SeqCacheArgs cache_args(const lattice_seq_attn_desc* d, const lattice_seq
   return a;
 }
 
-// blocks of the attention kernels (128 rows of a head each) and of the sinks'
-// late rows (at most 64 sequences a block)
+// blocks of the attention kernels: 128 rows of a head each
 static lattice_status check_attn_size(const lattice_seq_attn_desc* d, const lattice_seqs* s) {
-  if ((s->rows / 128 + 4) * d->heads > MAX_BLOCKS / 2 || (int64_t)s->num_seqs * d->kv_heads > MAX_BLOCKS * 8)
-    FAIL(LATTICE_ERR_UNSUPPORTED, "rows x heads or sequences x kv_heads too many for one launch");
+  if ((s->rows / 128 + 4) * d->heads > MAX_BLOCKS / 2)
+    FAIL(LATTICE_ERR_UNSUPPORTED, "rows x heads too many for one launch");
   return LATTICE_OK;
 }
 

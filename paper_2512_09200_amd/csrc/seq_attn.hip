@@ -42,6 +42,7 @@
 // 32768 rows, heads of 64, window 256, hidden keys: 58, 67 and 71 us, half of the
 // cycles issuing vector instructions.  8192 histories of 20, 4 heads of 32: 64,
 // 73 and 73 us for 210, 294 and 252 MB (43, 60 and 52 us of copy time).
+#include <algorithm>
 #include <type_traits>
 
 #include "kernels.h"
@@ -54,11 +55,8 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 struct AttnK {                     // kernel arguments
   int rows, dim, heads, kv_heads, group, window, sinks;
   int hb, row_tiles;               // heads of a block (forward, dQ), its row tiles
-  int ns;                          // splits of a sequence's late rows (sinks' gradients)
-  int by_start;                    // which of `part` is a sequence's: late_slot()
-  int num_seqs;
+  int chunk;                       // rows of a tile of seq_sink_kernel (0: no sequence has late rows)
   float scale;
-  const int32_t* offsets;
   const SeqSpan* span;
   const uint8_t* mask;
   SeqTensor q, k, v, o, go, gq, gk, gv;
@@ -66,7 +64,7 @@ struct AttnK {                     // kernel arguments
   void* out_lo;                    // [rows, heads, dim] or null: what rounding took from o (bf16)
   float* lse2;                     // workspace [heads, rows]: lse log2 e, +inf where nothing is seen
   float* delta;                    // workspace [heads, rows]
-  float* part;                     // workspace [late_slots][kv_heads][ns][2][sinks][dim]
+  float* part;                     // workspace [late_slots][kv_heads][2][sinks][dim]
 };
 
 // What a lane's row sees
@@ -603,14 +601,17 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
 __device__ inline int late_row(const AttnK& A, int start) {
   return (int)min((int64_t)start + A.sinks + A.window - 1, (int64_t)SEQ_NO_ROW);
 }
-// Where the partial sums of a sequence with late rows lie.  It has at least
-// sinks + window rows, so start / (sinks + window) differs between such
-// sequences; its own number is taken where there are fewer sequences than that.
-__device__ inline int late_slot(const AttnK& A, int seq, int start) {
-  return A.by_start ? start / (A.sinks + A.window) : seq;
+// Their partial sums are taken over pieces of this many of a sequence's n late
+// rows: whole subtiles, at most 64 pieces, which one block adds up, none shorter
+// than a tile.
+__device__ inline int late_piece(const AttnK& A, int n) { return max(A.chunk, ((n + 2047) >> 11) << 5); }
+// Where those of the piece that begins at a row lie.  A sequence with late rows
+// has at least sinks + window rows, so start / (sinks + window) grows from one
+// such sequence to the next, and the row's tile does not fall; within a sequence
+// the tile grows.  So no two pieces share a slot.
+__device__ inline int late_slot(const AttnK& A, int start, int row) {
+  return start / (A.sinks + A.window) + row / A.chunk;
 }
-// rows of a split of n late rows
-__device__ inline int late_chunk(const AttnK& A, int n) { return ((n + A.ns - 1) / A.ns + 31) & ~31; }
 
 // One 32-row subtile against the wave's 32 keys: accumulates dv and dk from
 // the scores p and the products ds of d_out and v.  SQ / SG: the rows' q and
@@ -821,18 +822,14 @@ __global__ __launch_bounds__((64 * DkvCfg<T, DP>::NW), (DkvCfg<T, DP>::WAVES)) v
       }
       __syncthreads();
     }
-    // sinks: the late rows' partial sums, in split order (a hidden sink has no
+    // sinks: the late rows' partial sums, in the pieces' order (a hidden sink has no
     // gradient; its sums are zeros times what may not be finite)
-    if (A.ns > 0 && rh == 0 && sink && shown && sp.end > late_row(A, sp.start)) {
-      const int late = sp.end - late_row(A, sp.start), used = (late + late_chunk(A, late) - 1) / late_chunk(A, late);
-      int lo = 0, hi = A.num_seqs;               // the sequence: the last that starts at sp.start or before
-      while (!A.by_start && hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (A.offsets[mid] <= sp.start) lo = mid; else hi = mid;
-      }
-      lo = late_slot(A, lo, sp.start);
-      for (int u = 0; u < used; ++u) {
-        const float* P = A.part + ((((int64_t)lo * A.kv_heads + kv) * A.ns + u) * 2 * A.sinks + (j - sp.start)) * A.dim;
+    if (A.chunk > 0 && rh == 0 && sink && lim > 0 && sp.end > late_row(A, sp.start)) {
+      const int l0 = late_row(A, sp.start), piece = late_piece(A, sp.end - l0);
+#pragma unroll 1
+      for (int i = l0; i < sp.end; i += piece) {
+        const float* P = A.part + ((int64_t)late_slot(A, sp.start, i) * A.kv_heads * 2 * A.sinks +
+                                   (kv * 2 * A.sinks + j - sp.start)) * A.dim;
 #pragma unroll
         for (int db = 0; db < TL::DB; ++db)
 #pragma unroll
@@ -876,88 +873,115 @@ __global__ __launch_bounds__((64 * DkvCfg<T, DP>::NW), (DkvCfg<T, DP>::WAVES)) v
   }
 }
 
-// Partial dk and dv of a sequence's sinks over a split of its late rows, every
-// one of which sees every sink.  A block: 32 sinks of one key head; its waves
-// take every fourth subtile of rows, their sums are added in wave order.
+// Partial dk and dv of a sequence's sinks over a piece of its late rows, every
+// one of which sees every sink.  A block: 32 sinks of one key head, and the
+// pieces that begin in a tile of rows; its waves take every fourth subtile of
+// rows, their sums are added in wave order.  Tiles lie on the packed rows and a
+// sequence has pieces by its own length, so the work is even whatever else is
+// in the batch: one history of 32000 events among 3000 of 20, 8 heads of 64 over 2,
+// window 256: 37 us here and 180 in the dK/dV kernel, which adds up 64 pieces in
+// one block (1520 and 128 with one piece).
 template <typename T, int DP>
-__global__ __launch_bounds__(256, 1) void seq_sink_kernel(AttnK A, int parts, int per_block) {
+__global__ __launch_bounds__(256, 1) void seq_sink_kernel(AttnK A, int parts) {
   using TL = Tile<T, DP>;
   using Cfg = DkvCfg<T, DP>;
-  constexpr int TB = 32 * TL::RB;
+  constexpr int TB = 32 * TL::RB, SCAN = 4;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5;
   int b = blockIdx.x;
   const int part = b % parts; b /= parts;
-  const int u = b % A.ns; b /= A.ns;
-  const int kv = b % A.kv_heads, first = b / A.kv_heads * per_block;
-  // which of the block's sequences have late rows in this split
-  bool any = false;
-  if (lane < per_block && first + lane < A.num_seqs) {
-    const int s0 = A.offsets[first + lane], e0 = min(A.offsets[first + lane + 1], A.rows);
-    const int late = e0 - late_row(A, max(s0, 0));
-    any = s0 >= 0 && s0 < e0 && late > 0 && (int64_t)u * late_chunk(A, late) < late;
-  }
-  for (uint64_t todo = __ballot(any); todo; todo &= todo - 1) {
-    const int seq = first + __builtin_ctzll(todo);
-    const int s0 = A.offsets[seq], e0 = min(A.offsets[seq + 1], A.rows);
-    const int x0 = late_row(A, s0), late = e0 - x0;
-    const int chunk = late_chunk(A, late), a0 = x0 + u * chunk, a1 = (int)min((int64_t)e0, (int64_t)a0 + chunk);
-    const int a = part * 32 + (lane & 31), j = s0 + a;   // late rows exist: the sequence has all its sinks
-    const bool shown = a < A.sinks && (!A.mask || A.mask[j]);
-    const int per_head = (a1 - a0 + 31) / 32, n = per_head * A.group;
-
-    TileLoad<T, DP, 32, 1> lq, lg;
-    lq.init(0, A.dim, A.q.ld);
-    lg.init(0, A.dim, A.go.ld);
-    char* S = smem + w * Cfg::SINK_STAGE;
-    Frag<T> kf[TL::KS], vf[TL::KS];
-    load_rows<T, DP>(A.k, a < A.sinks ? j : s0, kv, A.dim, kf);
-    load_rows<T, DP>(A.v, a < A.sinks ? j : s0, kv, A.dim, vf);
-    const uint32_t rl = TL::row_lane(), cl = TL::col_lane();
-    const float c = A.scale * LOG2E;
-    f32x16 dk[TL::DB], dv[TL::DB];
+  const int kv = b % A.kv_heads;
+  const int x0 = b / A.kv_heads * A.chunk, x1 = min(x0 + A.chunk, A.rows);
+  // of the rows xb + lane + 64 e: those that begin a piece
+  auto pieces = [&](int xb) __attribute__((always_inline)) {
+    unsigned heads = 0;
 #pragma unroll
-    for (int db = 0; db < TL::DB; ++db)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) dk[db][r] = dv[db][r] = 0.f;
-#pragma unroll 1
-    for (int t = w; t < n; t += 4) {
-      const int g = t / per_head, i0 = a0 + (t - g * per_head) * 32, h = kv * A.group + g, nr = min(32, a1 - i0);
-      const int64_t at = (int64_t)h * A.rows + i0;
-      // the wave's own stage: its reads of the subtile before have returned
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      lq.issue(S, 0, (const T*)A.q.p + (int64_t)i0 * A.q.ld + h * A.dim, nr, ~0ull);
-      lg.issue(S + TB, 0, (const T*)A.go.p + (int64_t)i0 * A.go.ld + h * A.dim, nr, ~0ull);
-      issue_stats(S + 2 * TB, A.lse2 + at, nr);
-      issue_stats(S + 2 * TB + 256, A.delta + at, nr);
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      dkv_subtile<T, DP, false>(scores<T, DP>(S, rl, 0, kf), scores<T, DP>(S + TB, rl, 0, vf), S, S + TB,
-                                (const float*)(S + 2 * TB), (const float*)(S + 2 * TB + 256), 0, rl, cl, c, 0,
-                                shown ? (unsigned)nr : 0u, nr == 32 && wave_all(shown), dk, dv);
+    for (int e = 0; e < SCAN; ++e) {
+      const int i = xb + lane + 64 * e;
+      const SeqSpan sp = A.span[min(i, x1 - 1)];
+      const int l0 = late_row(A, sp.start), n = sp.end - l0;
+      bool head = i == l0;
+      const bool more = i > l0 && n > A.chunk;                  // may begin a later piece
+      if (wave_any(more)) head |= more && (i - l0) % late_piece(A, n) == 0;
+      if (head && i < x1 && n > 0) heads |= 1u << e;
     }
-    // waves' sums, one after the other, in LDS [2][DP][33]
-    float* R = reinterpret_cast<float*>(smem);
-    for (int v = 0; v < 4; ++v) {
-      __syncthreads();
-      if (w != v) continue;
+    return heads;
+  };
+  // most tiles of short sequences have none: they end before anything else is set up
+  int xb = x0;
+  unsigned heads = pieces(xb);
+  while (!wave_any(heads != 0)) {
+    if ((xb += 64 * SCAN) >= x1) return;
+    heads = pieces(xb);
+  }
+#pragma unroll 1
+  for (;;) {
+    for (uint64_t found; (found = __ballot(heads != 0)) != 0;) {
+      const int from = __builtin_ctzll(found), bits = __builtin_amdgcn_readlane((int)heads, from);
+      if (lane == from) heads &= heads - 1;
+      const int a0 = xb + from + 64 * __builtin_ctz(bits);
+      const SeqSpan sp = A.span[a0];
+      const int s0 = __builtin_amdgcn_readfirstlane(sp.start), end = __builtin_amdgcn_readfirstlane(sp.end);
+      const int a1 = min(end, a0 + late_piece(A, end - late_row(A, s0)));   // the piece: rows a0 .. a1 - 1
+      const int a = part * 32 + (lane & 31), j = s0 + a;   // late rows exist: the sequence has all its sinks
+      const bool shown = a < A.sinks && (!A.mask || A.mask[j]);
+      const int per_head = (a1 - a0 + 31) / 32, n = per_head * A.group;
+
+      TileLoad<T, DP, 32, 1> lq, lg;
+      lq.init(0, A.dim, A.q.ld);
+      lg.init(0, A.dim, A.go.ld);
+      char* S = smem + w * Cfg::SINK_STAGE;
+      Frag<T> kf[TL::KS], vf[TL::KS];
+      load_rows<T, DP>(A.k, a < A.sinks ? j : s0, kv, A.dim, kf);
+      load_rows<T, DP>(A.v, a < A.sinks ? j : s0, kv, A.dim, vf);
+      const uint32_t rl = TL::row_lane(), cl = TL::col_lane();
+      const float c = A.scale * LOG2E;
+      f32x16 dk[TL::DB], dv[TL::DB];
 #pragma unroll
       for (int db = 0; db < TL::DB; ++db)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int d = 32 * db + frag_off(r) + 4 * half, x = d * 33 + (lane & 31);
-          R[x] = dk[db][r] + (v ? R[x] : 0.f);
-          R[DP * 33 + x] = dv[db][r] + (v ? R[DP * 33 + x] : 0.f);
-        }
+        for (int r = 0; r < 16; ++r) dk[db][r] = dv[db][r] = 0.f;
+#pragma unroll 1
+      for (int t = w; t < n; t += 4) {
+        const int g = t / per_head, i0 = a0 + (t - g * per_head) * 32, h = kv * A.group + g, nr = min(32, a1 - i0);
+        const int64_t at = (int64_t)h * A.rows + i0;
+        // the wave's own stage: its reads of the subtile before have returned
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        lq.issue(S, 0, (const T*)A.q.p + (int64_t)i0 * A.q.ld + h * A.dim, nr, ~0ull);
+        lg.issue(S + TB, 0, (const T*)A.go.p + (int64_t)i0 * A.go.ld + h * A.dim, nr, ~0ull);
+        issue_stats(S + 2 * TB, A.lse2 + at, nr);
+        issue_stats(S + 2 * TB + 256, A.delta + at, nr);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        dkv_subtile<T, DP, false>(scores<T, DP>(S, rl, 0, kf), scores<T, DP>(S + TB, rl, 0, vf), S, S + TB,
+                                  (const float*)(S + 2 * TB), (const float*)(S + 2 * TB + 256), 0, rl, cl, c, 0,
+                                  shown ? (unsigned)nr : 0u, nr == 32 && wave_all(shown), dk, dv);
+      }
+      // waves' sums, one after the other, in LDS [2][DP][33]
+      float* R = reinterpret_cast<float*>(smem);
+      for (int v = 0; v < 4; ++v) {
+        __syncthreads();
+        if (w != v) continue;
+#pragma unroll
+        for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int d = 32 * db + frag_off(r) + 4 * half, x = d * 33 + (lane & 31);
+            R[x] = dk[db][r] + (v ? R[x] : 0.f);
+            R[DP * 33 + x] = dv[db][r] + (v ? R[DP * 33 + x] : 0.f);
+          }
+      }
+      __syncthreads();
+      float* P = A.part + ((int64_t)late_slot(A, s0, a0) * A.kv_heads + kv) * 2 * A.sinks * A.dim;
+      const int na = min(32, A.sinks - part * 32);
+      for (int x = threadIdx.x; x < 2 * na * A.dim; x += 256) {
+        const int m = x / (na * A.dim), y = x - m * na * A.dim, r = y / A.dim, d = y - r * A.dim;
+        P[((int64_t)m * A.sinks + part * 32 + r) * A.dim + d] = R[m * DP * 33 + d * 33 + r];
+      }
+      __syncthreads();                           // R is read; the stages may be loaded again
     }
-    __syncthreads();
-    float* P = A.part + (((int64_t)late_slot(A, seq, s0) * A.kv_heads + kv) * A.ns + u) * 2 * A.sinks * A.dim;
-    const int na = min(32, A.sinks - part * 32);
-    for (int x = threadIdx.x; x < 2 * na * A.dim; x += 256) {
-      const int m = x / (na * A.dim), y = x - m * na * A.dim, r = y / A.dim, d = y - r * A.dim;
-      P[((int64_t)m * A.sinks + part * 32 + r) * A.dim + d] = R[m * DP * 33 + d * 33 + r];
-    }
-    __syncthreads();                           // R is read; the stages may be loaded again
+    if ((xb += 64 * SCAN) >= x1) break;
+    heads = pieces(xb);
   }
 }
 
@@ -973,9 +997,7 @@ static AttnK attn_args(const SeqAttnArgs& a) {
   A.sinks = a.sinks;
   A.hb = A.group % 4 == 0 ? 4 : A.group % 2 == 0 ? 2 : 1;
   A.row_tiles = cdiv(a.rows, 128 / A.hb);
-  A.num_seqs = a.num_seqs;
   A.scale = a.scale;
-  A.offsets = a.offsets;
   A.span = a.span;
   A.mask = a.key_mask;
   A.q = a.q; A.k = a.k; A.v = a.v; A.o = a.o; A.go = a.go; A.gq = a.gq; A.gk = a.gk; A.gv = a.gv;
@@ -984,21 +1006,18 @@ static AttnK attn_args(const SeqAttnArgs& a) {
   return A;
 }
 
-// Splits of a sequence's late rows: about 128 rows each, no more than give
-// every compute unit a few blocks; 0 where no sequence has late rows.
-static int late_splits(const SeqAttnArgs& a) {
-  const int64_t late = a.max_len - ((int64_t)a.sinks + a.window - 1);
-  if (a.sinks == 0 || late <= 0 || a.num_seqs == 0) return 0;
-  int64_t n = cdiv(late, 128);
-  const int64_t most = cdiv(2048, (int64_t)a.num_seqs * a.kv_heads);
-  if (n > most) n = most;
-  return (int)(n > 64 ? 64 : n < 1 ? 1 : n);
+// Rows of a tile of seq_sink_kernel: 128, more where that would be more than 4096
+// blocks, which fill the chip several times and bound the workspace.  0 where no
+// sequence has late rows.
+static int late_chunk(const SeqAttnArgs& a) {
+  if (a.sinks == 0 || a.num_seqs == 0 || a.max_len < (int64_t)a.sinks + a.window) return 0;
+  const int64_t n = std::max<int64_t>(128, (a.rows * a.kv_heads + 4095) / 4096);
+  return (int)((n + 31) / 32 * 32);
 }
 
-// Sequences that can have late rows: those of sinks + window rows at least.
-static int64_t late_slots(const SeqAttnArgs& a) {
-  const int64_t most = a.rows / ((int64_t)a.sinks + a.window);
-  return a.num_seqs < most ? a.num_seqs : most;
+// Slots that late_slot() counts.
+static int64_t late_slots(const SeqAttnArgs& a, int chunk) {
+  return chunk == 0 ? 0 : a.rows / ((int64_t)a.sinks + a.window) + cdiv(a.rows, chunk);
 }
 
 static size_t stats_bytes(const SeqAttnArgs& a) {
@@ -1006,7 +1025,7 @@ static size_t stats_bytes(const SeqAttnArgs& a) {
 }
 
 size_t seq_attn_bwd_workspace(const SeqAttnArgs& a) {
-  return 2 * stats_bytes(a) + (size_t)late_slots(a) * a.kv_heads * late_splits(a) * 2 * a.sinks * a.dim * sizeof(float);
+  return 2 * stats_bytes(a) + (size_t)late_slots(a, late_chunk(a)) * a.kv_heads * 2 * a.sinks * a.dim * sizeof(float);
 }
 
 template <typename T, int DP>
@@ -1027,14 +1046,9 @@ static hipError_t bwd_launch(const AttnK& A, hipStream_t s) {
   // dQ also writes the rows' statistics that the other two read
   seq_dq_kernel<T, DP><<<A.row_tiles * (A.heads / A.hb), 256, AttnCfg<T, DP>::LDS, s>>>(A);
   LAT_LAUNCH_CHECK();
-  if (A.ns > 0) {
+  if (A.chunk > 0) {
     const int parts = (A.sinks + 31) / 32;
-    // a block looks at several sequences where there are many: most of many
-    // are short and have no late rows
-    const int64_t all = (int64_t)A.num_seqs * A.kv_heads * A.ns * parts;
-    const int pb = (int)(all < 2048 ? 1 : all / 2048 > 64 ? 64 : all / 2048);
-    seq_sink_kernel<T, DP><<<cdiv(A.num_seqs, pb) * A.kv_heads * A.ns * parts, 256, DkvCfg<T, DP>::SINK_LDS, s>>>(
-        A, parts, pb);
+    seq_sink_kernel<T, DP><<<cdiv(A.rows, A.chunk) * A.kv_heads * parts, 256, DkvCfg<T, DP>::SINK_LDS, s>>>(A, parts);
     LAT_LAUNCH_CHECK();
   }
   seq_dkv_kernel<T, DP><<<cdiv(A.rows, 128) * A.kv_heads, 64 * DkvCfg<T, DP>::NW, DkvCfg<T, DP>::LDS, s>>>(A);
@@ -1059,8 +1073,7 @@ hipError_t seq_attn_bwd(const SeqAttnArgs& a, void* ws, hipStream_t s) {
   A.lse2 = (float*)ws;
   A.delta = (float*)((char*)ws + stats);
   A.part = (float*)((char*)ws + 2 * stats);
-  A.ns = late_splits(a);
-  A.by_start = late_slots(a) < a.num_seqs;
+  A.chunk = late_chunk(a);
   if (a.dt == DT_BF16)
     return a.dim <= 32 ? bwd_launch<bf16_t, 32>(A, s) : a.dim <= 64 ? bwd_launch<bf16_t, 64>(A, s)
                                                                   : bwd_launch<bf16_t, 128>(A, s);

@@ -166,6 +166,15 @@ def test_backward_workspace_goes_by_rows_not_by_sequences(lib, rows, S, kw, max_
     assert 2 * 4 * rows * kw["heads"] < need <= stats + part * (J * (rows // L) + 4096 + 64 * J)
 
 
+def test_late_rows_of_one_long_history_are_spread_whatever_else_is_in_the_batch(lib):
+    """Room for its partial sums: as many as it has when it is alone."""
+    d = attn(dtype=A.BF16, heads=8, kv_heads=2, head_dim=64, sinks=16, window=2048)
+    alone, batch = seqs(rows=32000, num_seqs=1, max_len=32000), seqs(rows=92000, num_seqs=3001, max_len=32000)
+    a, b = (lib.lattice_seq_attn_bwd_workspace(byref(d), byref(s)) - 2 * ((4 * s.rows * 8 + 255) // 256 * 256)
+            for s in (alone, batch))
+    assert b >= a >= 32 * 2 * 2 * 16 * 64 * 4                # 32 tiles of 1000 rows, 2 key heads
+
+
 def test_cache_and_step(lib):
     d, c, r = attn(), cache(), rope()
 
