@@ -503,7 +503,8 @@ lattice_status lattice_qk_rope_bwd(const lattice_qk_rope_desc* desc, const latti
  *   out_i = sum_j P_ij v_j,  P_ij = exp(scale <q_i, k_j> - lse_i).
  * A row that sees nothing gets out = 0 and lse = -inf, and passes no
  * gradient; one that sees keys but whose scores are all -inf gets NaN.  A
- * non-finite value reaches only rows that see it. */
+ * non-finite value reaches only rows that see it, and of a sum of rows (out of
+ * v, dq of k, dk of q, dv of d_out) only its own dimension. */
 #define LATTICE_SEQ_MAX_SINKS 64
 typedef struct {
   lattice_dtype dtype;

@@ -29,10 +29,10 @@
 // (seq_sink_kernel: a long sequence's sinks would otherwise be one block's work),
 // whose partial sums the main kernel adds in a fixed order.  No atomics.
 //
-// A masked pair has P = 0, but 0 * (a non-finite value) is not 0: where a
-// wave's result is not finite, the block repeats its sweep with the non-finite
-// values of the second operand replaced by zeros, and those pairs that see
-// them poisoned, and takes the elements that this finds finite.
+// A masked pair has P = 0, but 0 * (a non-finite value) is not 0: where an
+// element of a wave's result is not finite, the block sweeps again for such
+// elements alone (RepairPass, below), so that they are what the rows they see make
+// of them.
 //
 // Bound.  65536 rows in 4 histories, 8 heads of 128 over 2, window 2048, bf16:
 // forward 690 us (0.8 PFLOP/s), dQ 890, dK/dV 1220 (0.88 and 0.85 of their three
@@ -273,6 +273,62 @@ __device__ inline bool reaches(const RowView& v, int kt, int nk) {
   return v.valid && ((kt <= v.i && v.lo < kt + nk) || (v.start < kt + nk && v.start + (int)v.nsk > kt));
 }
 
+// Elements that came out non-finite are made again from the pairs that do see
+// each other: the sum over the finite values of the second operand, and what its
+// non-finite ones bring.  A term of coefficient x and value +-inf is an infinity
+// of their signs' product, any other (x = 0, NaN) is NaN; which they make is
+// known from whether there are terms other than +inf, and other than -inf.  Both
+// are sums of ones, products of the mask and of the operand's non-finite values:
+// for x not negative those that are not the infinity in question, for x not
+// positive those that are not the other.  Sweeps 0 to 3 count, sweep 4 adds values.
+struct RepairPass {
+  static constexpr int N = 5;
+  uint32_t drop;                   // sweeps 0 to 3: the infinity that is not counted
+  bool neg;                        // they take coefficients that are not positive
+  __device__ inline explicit RepairPass(int i)
+      : drop(i == 4 ? 0u : i == 0 || i == 3 ? 0x7f800000u : 0xff800000u), neg(i & 1) {}
+  // element r's coefficient, x, in this sweep
+  __device__ inline float coef(float x, uint32_t see, int r) const {
+    return drop == 0 ? x : bit_mask(see, r) && (neg ? !(x > 0.f) : !(x < 0.f)) ? 1.f : 0.f;
+  }
+};
+// What sweeps 0 and 1 (2 and 3) found: bit 16 db + r for accumulator [db][r]
+template <int DB> struct RepairBits {
+  uint64_t not_pos = 0, not_neg = 0;
+  __device__ inline void note(int pass, const f32x16 (&x)[DB]) {
+    uint64_t b = 0;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) b |= x[db][r] > 0.f ? 1ull << (16 * db + r) : 0ull;
+    if (pass < 2) not_pos |= b; else if (pass < 4) not_neg |= b;
+  }
+  __device__ inline void add_to(f32x16 (&x)[DB]) const {
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const bool p = (not_pos >> (16 * db + r)) & 1, n = (not_neg >> (16 * db + r)) & 1;
+        x[db][r] += p && n ? NAN : n ? INFINITY : p ? -INFINITY : 0.f;
+      }
+  }
+};
+// A sweep's step of 32 pairs a lane, coefficients x, second operand in LDS
+template <typename T, int DP>
+__device__ __forceinline__ void repair_step(const RepairPass& P, const char* S, uint32_t cl, int row0, uint32_t see,
+                                            f32x16 x, f32x16 (&c)[Tile<T, DP>::DB]) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) x[r] = P.coef(x[r], see, r);
+#pragma unroll
+  for (int hf = 0; hf < 2; ++hf) {
+    Frag<T> f;
+    pack_frag(x, hf, f);
+#pragma unroll
+    for (int db = 0; db < Tile<T, DP>::DB; ++db)
+      mma32(finite_or_count(Tile<T, DP>::colfrag(S, cl, row0 + 16 * hf, db), P.drop), f, c[db]);
+  }
+}
+
 // The row of a lane and its fragments of q (or d_out, ...): loads that depend
 // on nothing but the row's number, made before the tile's bounds are known.
 template <typename T, int DP>
@@ -287,8 +343,8 @@ __device__ __forceinline__ void load_rows(const SeqTensor& t, int i, int head, i
 }
 
 // Elements of O^T-shaped accumulators (lane: one row, element r of block db is
-// column 32 db + frag_off(r) + 4 (lane / 32)) to a row of memory.  PATCH:
-// non-finite elements keep what memory holds.  lo: what the rounding to bf16
+// column 32 db + frag_off(r) + 4 (lane / 32)) to a row of memory.  PATCH: only
+// elements that are not finite in memory.  lo: what the rounding to bf16
 // took, rounded to bf16.
 template <typename T, int DP, bool PATCH>
 __device__ __forceinline__ void store_row(T* op, T* lo, int dim, f32x16 (&x)[Tile<T, DP>::DB]) {
@@ -298,14 +354,18 @@ __device__ __forceinline__ void store_row(T* op, T* lo, int dim, f32x16 (&x)[Til
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const int d = 32 * db + 8 * g + 4 * half;
-      if (d >= dim) continue;
+      if (32 * db + 8 * g >= dim) continue;
       float y[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         y[e] = x[db][4 * g + e];
-        if (PATCH && nonfinite(y[e])) y[e] = ld(op + d + e);
+        if (PATCH && nonfinite(ld(op + d + e))) {
+          st(op + d + e, y[e]);
+          if (sizeof(T) == 2 && lo) st(lo + d + e, y[e] - bf2f(f2bf(y[e])));
+        }
       }
-      if constexpr (sizeof(T) == 2) {
+      if constexpr (PATCH) {
+      } else if constexpr (sizeof(T) == 2) {
         *reinterpret_cast<u32x2*>(op + d) = u32x2{pack_bf2(y[0], y[1]), pack_bf2(y[2], y[3])};
         if (lo) {
 #pragma unroll
@@ -351,9 +411,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
   uint32_t seen;                     // not 0: the row sees a key (of the half's)
 
   // N subtiles of 32 keys from subtile b0 of the tile at kt
-  auto attend = [&](auto strict_, int b0, const char* SK, const char* SV, int kt, uint64_t bits)
-      __attribute__((always_inline)) {
-    constexpr bool strict = decltype(strict_)::value;
+  auto attend = [&](int b0, const char* SK, const char* SV, int kt, uint64_t bits) __attribute__((always_inline)) {
     const uint32_t all = 0xffffffffu;
     const bool full = (uint32_t)(bits >> (32 * b0)) == all && (N == 1 || (uint32_t)(bits >> 32) == all) &&
                       wave_all(!V.valid || (V.lo <= kt + 32 * b0 && V.i >= kt + 32 * (b0 + N) - 1));
@@ -361,7 +419,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
 #pragma unroll
     for (int b = 0; b < N; ++b) s[b] = scores<T, DP>(SK, rl, 32 * (b0 + b), q);
     uint32_t see[N];
-    if (!full || strict) {
+    if (!full) {
 #pragma unroll
       for (int b = 0; b < N; ++b) {
         see[b] = row_bits(V, kt + 32 * (b0 + b), (uint32_t)(bits >> (32 * (b0 + b))));
@@ -402,15 +460,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
         ls[r & 3] += s[b][r];
       }
     l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
-    if constexpr (strict) {
-#pragma unroll
-      for (int b = 0; b < N; ++b) {
-        const f32x16 bad = TL::count_nonfinite(SV, rl, 32 * (b0 + b));
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (bad[r] > 0.f && bit_mask(see[b], r)) s[b][r] = NAN;
-      }
-    }
 #pragma unroll
     for (int b = 0; b < N; ++b)
 #pragma unroll
@@ -418,53 +467,50 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
         Frag<T> p;
         pack_frag(s[b], hf, p);
 #pragma unroll
-        for (int db = 0; db < TL::DB; ++db) {
-          Frag<T> f = TL::colfrag(SV, cl, 32 * (b0 + b) + 16 * hf, db);
-          if (strict) f = finite_part(f);
-          mma32(f, p, o[db]);
-        }
+        for (int db = 0; db < TL::DB; ++db) mma32(TL::colfrag(SV, cl, 32 * (b0 + b) + 16 * hf, db), p, o[db]);
       }
   };
-  // One pass over the block's keys.  strict: see the head of this file.
-  auto sweep = [&](auto strict_) __attribute__((always_inline)) {
-    constexpr bool strict = decltype(strict_)::value;
+  auto zero = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int db = 0; db < TL::DB; ++db)
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[db][r] = 0.f;
-    m = -INFINITY;
-    l = 0.f;
-    seen = 0;
-    ks.start();
-#pragma unroll 1
-    for (int t = 0; t < kt_.n; ++t) {
-      uint64_t bits;
-      const char *SK = ks.next(t, bits), *SV = SK + TB;
-      int kt, nk;
-      kt_.at<BK>(t, kt, nk);
-      if constexpr (SPLIT) {
-#pragma unroll 1
-        for (int b = 0; b < BK / 32; ++b)
-          if (nk > 32 * b && wave_any(reaches(V, kt + 32 * b, min(nk - 32 * b, 32))))
-            attend(strict_, b, SK, SV, kt, bits);
-      } else {
-        if (wave_any(reaches(V, kt, nk))) attend(strict_, 0, SK, SV, kt, bits);
-      }
-    }
-    l = add32(l);
-    // nothing seen: zeros; keys seen, but with scores of -inf alone: 0 / 0
-    const float any = max32(seen ? 1.f : 0.f);
-    if (l == 0.f && any > 0.f) l = NAN;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+  };
+  auto scale = [&](float f) __attribute__((always_inline)) {
 #pragma unroll
     for (int db = 0; db < TL::DB; ++db)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[db][r] *= inv;
+      for (int r = 0; r < 16; ++r) o[db][r] *= f;
   };
+  // one pass over the block's keys
+  zero();
+  m = -INFINITY;
+  l = 0.f;
+  seen = 0;
+  ks.start();
+#pragma unroll 1
+  for (int t = 0; t < kt_.n; ++t) {
+    uint64_t bits;
+    const char *SK = ks.next(t, bits), *SV = SK + TB;
+    int kt, nk;
+    kt_.at<BK>(t, kt, nk);
+    if constexpr (SPLIT) {
+#pragma unroll 1
+      for (int b = 0; b < BK / 32; ++b)
+        if (nk > 32 * b && wave_any(reaches(V, kt + 32 * b, min(nk - 32 * b, 32)))) attend(b, SK, SV, kt, bits);
+    } else {
+      if (wave_any(reaches(V, kt, nk))) attend(0, SK, SV, kt, bits);
+    }
+  }
+  l = add32(l);
+  // nothing seen: zeros; keys seen, but with scores of -inf alone: 0 / 0
+  const float any = max32(seen ? 1.f : 0.f);
+  if (l == 0.f && any > 0.f) l = NAN;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  scale(inv);
 
   T* const op = (T*)A.o.p + (int64_t)V.i * A.o.ld + head * A.dim;
   T* const lo = A.out_lo ? (T*)A.out_lo + ((int64_t)V.i * A.heads + head) * A.dim : nullptr;
-  sweep(std::false_type{});
   if (A.lse && V.valid && half == 0)
     A.lse[(int64_t)head * A.rows + V.i] = l == 0.f ? -INFINITY : (m * c + __builtin_amdgcn_logf(l)) * LN2;
   float z = 0.f;
@@ -474,7 +520,34 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
     for (int r = 0; r < 16; ++r) z = __builtin_fmaf(o[db][r], 0.f, z);
   if (V.valid) store_row<T, DP, false>(op, lo, A.dim, o);
   if (__syncthreads_or(V.valid && z != 0.f)) {
-    sweep(std::true_type{});
+    const float mc = m == -INFINITY ? 0.f : m * c;
+    RepairBits<TL::DB> R;
+#pragma unroll 1
+    for (int pass = 0; pass < RepairPass::N; ++pass) {
+      const RepairPass P(pass);
+      zero();
+      ks.start();
+#pragma unroll 1
+      for (int t = 0; t < kt_.n; ++t) {
+        uint64_t bits;
+        const char *SK = ks.next(t, bits), *SV = SK + TB;
+        int kt, nk;
+        kt_.at<BK>(t, kt, nk);
+#pragma unroll 1
+        for (int b = 0; b < BK / 32; ++b) {
+          f32x16 p = scores<T, DP>(SK, rl, 32 * b, q);
+          const uint32_t see = row_bits(V, kt + 32 * b, (uint32_t)(bits >> (32 * b)));
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            p[r] = keep_or(__builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c, -mc)), bit_mask(see, r), 0u);
+          repair_step<T, DP>(P, SV, cl, 32 * b, see, p, o);
+        }
+      }
+      __syncthreads();                           // the last tile is read; the next pass loads the first
+      R.note(pass, o);
+    }
+    scale(inv);
+    R.add_to(o);
     if (V.valid) store_row<T, DP, true>(op, lo, A.dim, o);
   }
 }
@@ -529,61 +602,58 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
   const float c = A.scale * LOG2E;
   f32x16 dq[TL::DB];
 
-  auto sweep = [&](auto strict_) __attribute__((always_inline)) {
-    constexpr bool strict = decltype(strict_)::value;
+  auto zero = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int db = 0; db < TL::DB; ++db)
 #pragma unroll
       for (int r = 0; r < 16; ++r) dq[db][r] = 0.f;
-    ks.start();
-#pragma unroll 1
-    for (int t = 0; t < kt_.n; ++t) {
-      uint64_t bits;
-      const char *SK = ks.next(t, bits), *SV = SK + TB;
-      int kt, nk;
-      kt_.at<BK>(t, kt, nk);
-#pragma unroll
-      for (int b = 0; b < BK / 32; ++b) {
-        if (nk <= 32 * b || !wave_any(reaches(V, kt + 32 * b, min(32, nk - 32 * b)))) continue;
-        const bool full = (uint32_t)(bits >> (32 * b)) == 0xffffffffu &&
-                          wave_all(!V.valid || (V.lo <= kt + 32 * b && V.i >= kt + 32 * b + 31));
-        f32x16 p = scores<T, DP>(SK, rl, 32 * b, q);
-        const f32x16 dp = scores<T, DP>(SV, rl, 32 * b, go);
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c, -lse2)) * (dp[r] - delta);
-        if (!full || strict) {
-          const uint32_t see = row_bits(V, kt + 32 * b, (uint32_t)(bits >> (32 * b)));
-#pragma unroll
-          for (int r = 0; r < 16; ++r) p[r] = keep_or(p[r], bit_mask(see, r), 0u);
-          if constexpr (strict) {
-            const f32x16 bad = TL::count_nonfinite(SK, rl, 32 * b);
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              if (bad[r] > 0.f && bit_mask(see, r)) p[r] = NAN;
-          }
-        }
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          Frag<T> f;
-          pack_frag(p, hf, f);
-#pragma unroll
-          for (int db = 0; db < TL::DB; ++db) {
-            Frag<T> kf = TL::colfrag(SK, cl, 32 * b + 16 * hf, db);
-            if (strict) kf = finite_part(kf);
-            mma32(kf, f, dq[db]);
-          }
-        }
-      }
-    }
+  };
+  auto scale = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int db = 0; db < TL::DB; ++db)
 #pragma unroll
       for (int r = 0; r < 16; ++r) dq[db][r] *= A.scale;
   };
+  // dS of the wave's rows and 32 keys of the tile
+  auto dscores = [&](const char* SK, const char* SV, int b) __attribute__((always_inline)) {
+    f32x16 p = scores<T, DP>(SK, rl, 32 * b, q);
+    const f32x16 dp = scores<T, DP>(SV, rl, 32 * b, go);
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c, -lse2)) * (dp[r] - delta);
+    return p;
+  };
+  auto masked = [&](f32x16& p, uint32_t see) __attribute__((always_inline)) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) p[r] = keep_or(p[r], bit_mask(see, r), 0u);
+  };
+  zero();
+  ks.start();
+#pragma unroll 1
+  for (int t = 0; t < kt_.n; ++t) {
+    uint64_t bits;
+    const char *SK = ks.next(t, bits), *SV = SK + TB;
+    int kt, nk;
+    kt_.at<BK>(t, kt, nk);
+#pragma unroll
+    for (int b = 0; b < BK / 32; ++b) {
+      if (nk <= 32 * b || !wave_any(reaches(V, kt + 32 * b, min(32, nk - 32 * b)))) continue;
+      const bool full = (uint32_t)(bits >> (32 * b)) == 0xffffffffu &&
+                        wave_all(!V.valid || (V.lo <= kt + 32 * b && V.i >= kt + 32 * b + 31));
+      f32x16 p = dscores(SK, SV, b);
+      if (!full) masked(p, row_bits(V, kt + 32 * b, (uint32_t)(bits >> (32 * b))));
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        Frag<T> f;
+        pack_frag(p, hf, f);
+#pragma unroll
+        for (int db = 0; db < TL::DB; ++db) mma32(TL::colfrag(SK, cl, 32 * b + 16 * hf, db), f, dq[db]);
+      }
+    }
+  }
+  scale();
 
   T* const op = (T*)A.gq.p + (int64_t)V.i * A.gq.ld + head * A.dim;
-  sweep(std::false_type{});
   float z = 0.f;
 #pragma unroll
   for (int db = 0; db < TL::DB; ++db)
@@ -591,7 +661,31 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void seq_
     for (int r = 0; r < 16; ++r) z = __builtin_fmaf(dq[db][r], 0.f, z);
   if (V.valid) store_row<T, DP, false>(op, nullptr, A.dim, dq);
   if (__syncthreads_or(V.valid && z != 0.f)) {
-    sweep(std::true_type{});
+    RepairBits<TL::DB> R;
+#pragma unroll 1
+    for (int pass = 0; pass < RepairPass::N; ++pass) {
+      const RepairPass P(pass);
+      zero();
+      ks.start();
+#pragma unroll 1
+      for (int t = 0; t < kt_.n; ++t) {
+        uint64_t bits;
+        const char *SK = ks.next(t, bits), *SV = SK + TB;
+        int kt, nk;
+        kt_.at<BK>(t, kt, nk);
+#pragma unroll 1
+        for (int b = 0; b < BK / 32; ++b) {
+          f32x16 p = dscores(SK, SV, b);
+          const uint32_t see = row_bits(V, kt + 32 * b, (uint32_t)(bits >> (32 * b)));
+          masked(p, see);
+          repair_step<T, DP>(P, SK, cl, 32 * b, see, p, dq);
+        }
+      }
+      __syncthreads();
+      R.note(pass, dq);
+    }
+    scale();
+    R.add_to(dq);
     if (V.valid) store_row<T, DP, true>(op, nullptr, A.dim, dq);
   }
 }
@@ -618,9 +712,9 @@ __device__ inline int late_slot(const AttnK& A, int start, int row) {
 // d_out in LDS (row0 the subtile's first row there), L / E: their lse2 and
 // delta.  d: the subtile's first row minus the lane's key; rows with
 // d + offset < lim see it.
-template <typename T, int DP, bool strict>
+template <typename T, int DP>
 __device__ __forceinline__ void dkv_subtile(f32x16 p, f32x16 ds, const char* SQ, const char* SG, const float* L,
-                                            const float* E, int row0, uint32_t rl, uint32_t cl, float c, int d,
+                                            const float* E, int row0, uint32_t cl, float c, int d,
                                             unsigned lim, bool full, f32x16 (&dk)[Tile<T, DP>::DB],
                                             f32x16 (&dv)[Tile<T, DP>::DB]) {
   using TL = Tile<T, DP>;
@@ -636,20 +730,12 @@ __device__ __forceinline__ void dkv_subtile(f32x16 p, f32x16 ds, const char* SQ,
       ds[r] = p[r] * (ds[r] - e4[e]);
     }
   }
-  if (!full || strict) {
+  if (!full) {
     const uint32_t see = bit_range(-d, (int)lim - 1 - d) >> (4 * half);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       p[r] = keep_or(p[r], bit_mask(see, r), 0u);
       ds[r] = keep_or(ds[r], bit_mask(see, r), 0u);
-    }
-    if constexpr (strict) {
-      const f32x16 bq = TL::count_nonfinite(SQ, rl, row0), bg = TL::count_nonfinite(SG, rl, row0);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        if (bg[r] > 0.f && bit_mask(see, r)) p[r] = NAN;
-        if (bq[r] > 0.f && bit_mask(see, r)) ds[r] = NAN;
-      }
     }
   }
 #pragma unroll
@@ -659,11 +745,7 @@ __device__ __forceinline__ void dkv_subtile(f32x16 p, f32x16 ds, const char* SQ,
     pack_frag(ds, hf, df);
 #pragma unroll
     for (int db = 0; db < TL::DB; ++db) {
-      Frag<T> g = TL::colfrag(SG, cl, row0 + 16 * hf, db), q = TL::colfrag(SQ, cl, row0 + 16 * hf, db);
-      if (strict) {
-        g = finite_part(g);
-        q = finite_part(q);
-      }
+      const Frag<T> g = TL::colfrag(SG, cl, row0 + 16 * hf, db), q = TL::colfrag(SQ, cl, row0 + 16 * hf, db);
       mma32(g, pf, dv[db]);
       mma32(q, df, dk[db]);
     }
@@ -704,6 +786,7 @@ __global__ __launch_bounds__((64 * DkvCfg<T, DP>::NW), (DkvCfg<T, DP>::WAVES)) v
   using Cfg = DkvCfg<T, DP>;
   constexpr int BQ = Cfg::BQ, TB = BQ * TL::RB, NW = Cfg::NW, KB = 64 * TL::RB;
   constexpr bool WIDE = Cfg::WIDE;
+  constexpr int WAVES = NW / 4;                // of a key group
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5, kg = w & 3, rh = w >> 2;   // 32 keys; of a row tile, subtile (wide heads)
@@ -768,13 +851,14 @@ __global__ __launch_bounds__((64 * DkvCfg<T, DP>::NW), (DkvCfg<T, DP>::WAVES)) v
   const uint32_t rl = TL::row_lane(), cl = TL::col_lane();
   const float c = A.scale * LOG2E;
   f32x16 dk[TL::DB], dv[TL::DB];
-
-  auto sweep = [&](auto strict_) __attribute__((always_inline)) {
-    constexpr bool strict = decltype(strict_)::value;
+  auto zero = [&](f32x16 (&x)[TL::DB]) __attribute__((always_inline)) {
 #pragma unroll
     for (int db = 0; db < TL::DB; ++db)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) dk[db][r] = dv[db][r] = 0.f;
+      for (int r = 0; r < 16; ++r) x[db][r] = 0.f;
+  };
+  // f(stage, subtile of it, the subtile's first row) for those that reach the wave's keys
+  auto rows = [&](auto f) __attribute__((always_inline)) {
     issue(0);
     int i0 = k0;
 #pragma unroll 1
@@ -782,79 +866,94 @@ __global__ __launch_bounds__((64 * DkvCfg<T, DP>::NW), (DkvCfg<T, DP>::WAVES)) v
       landed();
       issue(t + 1);
       const char* S = smem + (t & 1) * Cfg::STAGE;
-      auto subtile = [&](int b) __attribute__((always_inline)) {
+      auto reached = [&](int b) __attribute__((always_inline)) {
         const int ib = i0 + 32 * b;
-        // rows ib .. ib+31 reach the wave's keys
-        if (ib + 31 < k0 + 32 * kg || ib >= wend) return;
-        const bool full = wave_all((unsigned)(ib - j) < lim && (unsigned)(ib + 31 - j) < lim);
-        f32x16 p, ds;
-        if constexpr (WIDE) {
-          const char* SK = KV + (kg >> 1) * KB;
-          p = scores_lds<T, DP>(S, rl, 32 * b, SK, 32 * (kg & 1));
-          ds = scores_lds<T, DP>(S + TB, rl, 32 * b, SK + 2 * KB, 32 * (kg & 1));
-        } else {
-          p = scores<T, DP>(S, rl, 32 * b, kf);
-          ds = scores<T, DP>(S + TB, rl, 32 * b, vf);
-        }
-        dkv_subtile<T, DP, strict>(p, ds, S, S + TB, (const float*)(S + 2 * TB), (const float*)(S + 2 * TB + 256),
-                                   32 * b, rl, cl, c, ib - j, lim, full, dk, dv);
+        if (ib + 31 >= k0 + 32 * kg && ib < wend) f(S, b, ib);
       };
       if constexpr (WIDE) {
-        subtile(rh);
+        reached(rh);
       } else {
 #pragma unroll
-        for (int b = 0; b < BQ / 32; ++b) subtile(b);
+        for (int b = 0; b < BQ / 32; ++b) reached(b);
       }
       i0 = i0 + BQ >= bend ? k0 : i0 + BQ;
     }
-    if constexpr (WIDE) {                        // the two waves of a key group, dk then dv, by registers
+  };
+  // scores of the wave's keys (what 0) or their products with d_out (1)
+  auto products = [&](const char* S, int b, int what) __attribute__((always_inline)) {
+    if constexpr (WIDE)
+      return scores_lds<T, DP>(S + what * TB, rl, 32 * b, KV + (kg >> 1) * KB + what * 2 * KB, 32 * (kg & 1));
+    else
+      return scores<T, DP>(S + what * TB, rl, 32 * b, what ? vf : kf);
+  };
+  // the sum of the two waves of a key group, by registers
+  auto both_waves = [&](f32x16 (&x)[TL::DB]) __attribute__((always_inline)) {
+    if constexpr (WIDE) {
       float* R = reinterpret_cast<float*>(smem) + kg * TL::DB * 16 * 64 + lane;
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        __syncthreads();
-        if (rh == 1)
-#pragma unroll
-          for (int x = 0; x < TL::DB * 16; ++x) R[x * 64] = (m ? dv : dk)[x >> 4][x & 15];
-        __syncthreads();
-        if (rh == 0)
-#pragma unroll
-          for (int x = 0; x < TL::DB * 16; ++x) (m ? dv : dk)[x >> 4][x & 15] += R[x * 64];
-      }
       __syncthreads();
+      if (rh == 1)
+#pragma unroll
+        for (int i = 0; i < TL::DB * 16; ++i) R[i * 64] = x[i >> 4][i & 15];
+      __syncthreads();
+      if (rh == 0)
+#pragma unroll
+        for (int i = 0; i < TL::DB * 16; ++i) x[i >> 4][i & 15] += R[i * 64];
     }
-    // sinks: the late rows' partial sums, in the pieces' order (a hidden sink has no
-    // gradient; its sums are zeros times what may not be finite)
-    if (A.chunk > 0 && rh == 0 && sink && lim > 0 && sp.end > late_row(A, sp.start)) {
+  };
+  // f(partial sums of the lane's key) for the pieces of its late rows, in their order,
+  // the two waves of a key group in turn (a hidden sink has no gradient; its sums are zeros times what may not be finite)
+  auto late_sums = [&](auto f) __attribute__((always_inline)) {
+    if (A.chunk > 0 && sink && lim > 0 && sp.end > late_row(A, sp.start)) {
       const int l0 = late_row(A, sp.start), piece = late_piece(A, sp.end - l0);
 #pragma unroll 1
-      for (int i = l0; i < sp.end; i += piece) {
-        const float* P = A.part + ((int64_t)late_slot(A, sp.start, i) * A.kv_heads * 2 * A.sinks +
-                                   (kv * 2 * A.sinks + j - sp.start)) * A.dim;
-#pragma unroll
-        for (int db = 0; db < TL::DB; ++db)
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const int dd = 32 * db + 8 * g + 4 * half;
-            if (dd >= A.dim) continue;
-            const f32x4 a = *reinterpret_cast<const f32x4*>(P + dd);
-            const f32x4 b = *reinterpret_cast<const f32x4*>(P + (int64_t)A.sinks * A.dim + dd);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              dk[db][4 * g + e] += a[e];
-              dv[db][4 * g + e] += b[e];
-            }
-          }
-      }
+      for (int i = l0 + rh * piece; i < sp.end; i += WAVES * piece)
+        f(A.part + ((int64_t)late_slot(A, sp.start, i) * A.kv_heads * 2 * A.sinks +
+                    (kv * 2 * A.sinks + j - sp.start)) * A.dim);
     }
+  };
+  // f(accumulator block, first of four elements, columns there) for the columns of dim
+  auto columns = [&](auto f) __attribute__((always_inline)) {
 #pragma unroll
     for (int db = 0; db < TL::DB; ++db)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) dk[db][r] *= A.scale;
+      for (int g = 0; g < 4; ++g) {
+        // those past dim, which are not stored, take others' sums: no branch between
+        // the loads, so that they go out together; wide heads have no registers for that
+        const int dd = 32 * db + 8 * g + 4 * half;
+        if (DP < 128 || 32 * db + 8 * g < A.dim) f(db, 4 * g, dd < A.dim ? dd : 0);
+      }
   };
+  auto add4 = [&](f32x16& x, int r, const float* P) __attribute__((always_inline)) {
+    const f32x4 a = *reinterpret_cast<const f32x4*>(P);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[r + e] += a[e];
+  };
+  auto scale = [&](f32x16 (&x)[TL::DB]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int db = 0; db < TL::DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[db][r] *= A.scale;
+  };
+
+  zero(dk);
+  zero(dv);
+  rows([&](const char* S, int b, int ib) __attribute__((always_inline)) {
+    const bool full = wave_all((unsigned)(ib - j) < lim && (unsigned)(ib + 31 - j) < lim);
+    dkv_subtile<T, DP>(products(S, b, 0), products(S, b, 1), S, S + TB, (const float*)(S + 2 * TB),
+                       (const float*)(S + 2 * TB + 256), 32 * b, cl, c, ib - j, lim, full, dk, dv);
+  });
+  late_sums([&](const float* P) __attribute__((always_inline)) {
+    columns([&](int db, int r, int d) __attribute__((always_inline)) {
+      add4(dk[db], r, P + d);
+      add4(dv[db], r, P + (int64_t)A.sinks * A.dim + d);
+    });
+  });
+  both_waves(dk);
+  both_waves(dv);
+  scale(dk);
   T* const kp = (T*)A.gk.p + (int64_t)j * A.gk.ld + kv * A.dim;
   T* const vp = (T*)A.gv.p + (int64_t)j * A.gv.ld + kv * A.dim;
   const bool mine = valid && rh == 0;            // the wave that stores
-  sweep(std::false_type{});
   float z = 0.f;
 #pragma unroll
   for (int db = 0; db < TL::DB; ++db)
@@ -864,12 +963,42 @@ __global__ __launch_bounds__((64 * DkvCfg<T, DP>::NW), (DkvCfg<T, DP>::WAVES)) v
     store_row<T, DP, false>(kp, nullptr, A.dim, dk);
     store_row<T, DP, false>(vp, nullptr, A.dim, dv);
   }
-  if (__syncthreads_or(mine && z != 0.f)) {
-    sweep(std::true_type{});
-    if (mine) {
-      store_row<T, DP, true>(kp, nullptr, A.dim, dk);
-      store_row<T, DP, true>(vp, nullptr, A.dim, dv);
+  if (!__syncthreads_or(mine && z != 0.f)) return;
+  // dv, then dk, in dk's registers
+#pragma unroll 1
+  for (int what = 0; what < 2; ++what) {
+    RepairBits<TL::DB> R;
+#pragma unroll 1
+    for (int pass = 0; pass < RepairPass::N; ++pass) {
+      zero(dk);
+      rows([&](const char* S, int b, int ib) __attribute__((always_inline)) {
+        f32x16 p = products(S, b, 0);
+        const float *L = (const float*)(S + 2 * TB) + 32 * b + 4 * half, *E = L + 64;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c, -L[frag_off(r)]));
+        if (what) {
+          const f32x16 d = products(S, b, 1);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) p[r] *= d[r] - E[frag_off(r)];
+        }
+        const uint32_t see = bit_range(j - ib, (int)lim - 1 + j - ib) >> (4 * half);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p[r] = keep_or(p[r], bit_mask(see, r), 0u);
+        repair_step<T, DP>(RepairPass(pass), what ? S : S + TB, cl, 32 * b, see, p, dk);
+      });
+      if (pass == RepairPass::N - 1)
+        late_sums([&](const float* P) __attribute__((always_inline)) {
+          columns([&](int db, int r, int d) __attribute__((always_inline)) {
+            add4(dk[db], r, P + (what ? 0 : (int64_t)A.sinks * A.dim) + d);
+          });
+        });
+      both_waves(dk);
+      __syncthreads();                           // the next sweep loads over what this one read
+      R.note(pass, dk);
     }
+    if (what) scale(dk);
+    R.add_to(dk);
+    if (mine) store_row<T, DP, true>(what ? kp : vp, nullptr, A.dim, dk);
   }
 }
 
@@ -953,8 +1082,8 @@ __global__ __launch_bounds__(256, 1) void seq_sink_kernel(AttnK A, int parts) {
         issue_stats(S + 2 * TB, A.lse2 + at, nr);
         issue_stats(S + 2 * TB + 256, A.delta + at, nr);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        dkv_subtile<T, DP, false>(scores<T, DP>(S, rl, 0, kf), scores<T, DP>(S + TB, rl, 0, vf), S, S + TB,
-                                  (const float*)(S + 2 * TB), (const float*)(S + 2 * TB + 256), 0, rl, cl, c, 0,
+        dkv_subtile<T, DP>(scores<T, DP>(S, rl, 0, kf), scores<T, DP>(S + TB, rl, 0, vf), S, S + TB,
+                                  (const float*)(S + 2 * TB), (const float*)(S + 2 * TB + 256), 0, cl, c, 0,
                                   shown ? (unsigned)nr : 0u, nr == 32 && wave_all(shown), dk, dv);
       }
       // waves' sums, one after the other, in LDS [2][DP][33]

@@ -69,39 +69,28 @@ __device__ inline float dot_frag(const Frag<float>& a, const Frag<float>& b) {
   return s;
 }
 
-// Non-finite values as zeros, and their indicator (1 where non-finite).
 __device__ inline bool nonfinite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
-__device__ inline Frag<float> finite_part(const Frag<float>& f) {
+// A fragment's finite values, zeros elsewhere (drop 0); or ones where it is
+// neither finite nor the infinity whose 32 bits are `drop`.
+__device__ inline Frag<float> finite_or_count(const Frag<float>& f, uint32_t drop) {
   Frag<float> o;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) o.v[e] = nonfinite(f.v[e]) ? 0.f : f.v[e];
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t x = __float_as_uint(f.v[e]);
+    const bool nf = nonfinite(f.v[e]);
+    o.v[e] = __uint_as_float(drop ? (nf && x != drop ? 0x3f800000u : 0u) : nf ? 0u : x);
+  }
   return o;
 }
-__device__ inline Frag<float> nonfinite_part(const Frag<float>& f) {
-  Frag<float> o;
+__device__ inline Frag<bf16_t> finite_or_count(const Frag<bf16_t>& f, uint32_t drop) {
+  u32x4 w = __builtin_bit_cast(u32x4, f.v);
+  auto half = [&](uint32_t x) __attribute__((always_inline)) {     // a bf16 in the upper half of x
+    const bool nf = (x & 0x7f800000u) == 0x7f800000u;
+    return drop ? (nf && x != drop ? 0x3f800000u : 0u) : nf ? 0u : x;
+  };
 #pragma unroll
-  for (int e = 0; e < 8; ++e) o.v[e] = nonfinite(f.v[e]) ? 1.f : 0.f;
-  return o;
-}
-__device__ inline Frag<bf16_t> finite_part(const Frag<bf16_t>& f) {
-  float u[8];
-  Vec16<bf16_t>::unpack(__builtin_bit_cast(u32x4, f.v), u);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) u[e] = nonfinite(u[e]) ? 0.f : u[e];
-  return {__builtin_bit_cast(bf16x8, Vec16<bf16_t>::pack(u))};
-}
-__device__ inline Frag<bf16_t> nonfinite_part(const Frag<bf16_t>& f) {
-  float u[8];
-  Vec16<bf16_t>::unpack(__builtin_bit_cast(u32x4, f.v), u);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) u[e] = nonfinite(u[e]) ? 1.f : 0.f;
-  return {__builtin_bit_cast(bf16x8, Vec16<bf16_t>::pack(u))};
-}
-template <typename T> __device__ inline Frag<T> ones_frag() {
-  Frag<T> f;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) f.v[e] = 1.f;
-  return f;
+  for (int i = 0; i < 4; ++i) w[i] = half(w[i] & 0xffff0000u) | (half(w[i] << 16) >> 16);
+  return {__builtin_bit_cast(bf16x8, w)};
 }
 
 typedef __attribute__((address_space(3))) void seq_lds_void;
@@ -175,17 +164,6 @@ struct Tile {
         f.v[e] = *reinterpret_cast<const float*>(S + at(cl, row0 + 8 * (e >> 2) + (e & 3), 8 * db));
     }
     return f;
-  }
-  // How many of each row's elements are non-finite, in the layout of a product
-  // whose A rows are these (row0 a multiple of 32).
-  __device__ static inline f32x16 count_nonfinite(const char* S, uint32_t rl, int row0) {
-    f32x16 c;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) c[r] = 0.f;
-    const Frag<T> one = ones_frag<T>();
-#pragma unroll
-    for (int s = 0; s < KS; ++s) mma32(nonfinite_part(rowfrag(S, rl, row0, s)), one, c);
-    return c;
   }
 };
 

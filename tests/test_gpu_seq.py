@@ -257,6 +257,84 @@ def test_nonfinite_values_reach_only_rows_that_see_them(dt, D, bad):
             assert np.allclose(g[~touched], w[~touched], rtol=2e-2, atol=1e-2 if dt == "bf16" else 1e-5), (which, at, m)
 
 
+@pytest.mark.parametrize("dt,D,W,N", [("bf16", 64, 64, 2), ("f32", 32, 64, 0), ("bf16", 128, 64, 2), ("f32", 128, 12, 3),
+                                      ("bf16", 32, 12, 3), ("bf16", 128, 12, 3)])
+def test_nonfinite_values_stay_in_their_sequence_and_dimension(dt, D, W, N):
+    """Bad values in different dimensions of two sequences that share tiles: an
+    element is what the rows it is made of give, +-inf or NaN included."""
+    from paper_2512_09200_amd import api
+    inf, nan = float("inf"), float("nan")
+    c = attn_case(dt, 2, 1, D, [40, 50], W, N)
+    kw, n = c["kw"], 90
+    see = np.zeros((n, n), bool)
+    for a, e in ((0, 40), (40, 90)):
+        see[a:e, a:e] = o.visible(e - a, W, N, np.ones(e - a, bool))
+
+    def terms(bad, pairs):
+        """What the bad elements (row, dimension, value) make of the elements
+        [rows, dimensions] that have a positive weight for the row by pairs."""
+        w = np.zeros((n, D))
+        with np.errstate(invalid="ignore"):
+            for at, d, x in bad:
+                w[:, d] += np.where(pairs[:, at], x, 0.0)
+        return w
+
+    def check(got, want, bound, add, what):
+        g = f64(got)
+        add = np.broadcast_to(add[:, None, :], g.shape)
+        ok = np.isfinite(add)
+        assert np.array_equal(g[~ok], add[~ok], equal_nan=True), what
+        over = np.where(ok, np.abs(g - want) - bound, -1.0)
+        assert (over <= 1e-30).all(), (what, np.argwhere(~(over <= 1e-30))[:3])
+
+    A3 = [f64(c[m]) for m in ("q", "k", "v")]
+    all_shown, sc = np.ones(n, bool), D ** -0.5
+    # v: +inf, -inf and both in one dimension, -inf and NaN of the other sequence in two others
+    bad = [(5, 3, inf), (9, 3, -inf), (60, 5, nan), (45, 4, -inf)]
+    v = c["v"].clone()
+    for at, d, x in bad:
+        v[at, :, d] = x
+    out, sv = api.lattice_seq_attn_fwd(c["s"], c["q"], c["k"], v, **kw)
+    f = o.attn(*A3, c["off"], W, N, sc, all_shown, dt)
+    add = terms(bad, see)
+    check(out, f["o"], f["o_bound"], add, "out")
+    if sv.out_lo is not None:
+        fine = torch.from_numpy(np.isfinite(add)).to(DEV)[:, None, :].expand_as(out)
+        assert (sv.out_lo[fine].float().abs() <= 2.0 ** -8 * out[fine].float().abs()).all()
+    # d_out: dv is its sum with positive weights
+    bad = [(30, 3, inf), (33, 3, inf), (35, 2, -inf), (70, 5, nan), (66, 4, inf)]
+    do = c["do"].clone()
+    for at, d, x in bad:
+        do[at, :, d] = x
+    dq, dk, dv = api.lattice_seq_attn_bwd(c["s"], c["q"], c["k"], c["v"], c["out"], c["lse"], do, **kw)
+    g, b = o.attn_bwd(*A3, c["off"], W, N, sc, all_shown, f64(c["do"]), dt)
+    check(dv, g["dv"], b["dv"], terms(bad, see.T), "dv")
+    touched = see[[at for at, _, _ in bad]].any(0)
+    assert np.isfinite(f64(dk)[~touched]).all()
+    # k: a key whose score is -inf has no weight, but 0 * inf in one dimension of
+    # dq, and the other sequence's NaN is in another
+    q, k = c["q"].clone(), c["k"].clone()
+    q[:40, :, 3] = -q[:40, :, 3].abs() - 0.5
+    k[7, :, 3], k[60, :, 5] = inf, nan
+    out, sv = api.lattice_seq_attn_fwd(c["s"], q, k, c["v"], **kw)
+    dq, dk, dv = api.lattice_seq_attn_bwd(c["s"], q, k, c["v"], out, sv, c["do"], **kw)
+    k0 = c["k"].clone()
+    shown = all_shown.copy()
+    shown[7] = False
+    B3 = f64(q), f64(k0), f64(c["v"])
+    f = o.attn(*B3, c["off"], W, N, sc, shown, dt)
+    g, b = o.attn_bwd(*B3, c["off"], W, N, sc, shown, f64(c["do"]), dt)
+    rows = see[:, 60]                                            # all of their scores are NaN
+    keys = see[rows].any(0)
+    mine = see[:, 7].copy()
+    for got, want, bound, hit, dims in ((out, f["o"], f["o_bound"], rows, []), (dk, g["dk"], b["dk"], keys, []),
+                                        (dv, g["dv"], b["dv"], keys, []), (dq, g["dq"], b["dq"], rows, [3])):
+        add = np.zeros((n, D))
+        add[np.ix_(mine, dims)] = nan
+        add[hit] = nan
+        check(got, want, bound, add, "k")
+
+
 @pytest.mark.parametrize("dt,D,W,N", [("bf16", 64, 24, 2), ("f32", 32, 24, 2), ("bf16", 128, 24, 0), ("bf16", 32, 200, 0),
                                       ("f32", 128, 1, 0)])
 def test_rows_whose_scores_are_all_minus_infinity(dt, D, W, N):
