@@ -558,7 +558,10 @@ typedef struct {
  * Other slots stay as they were.  cache_index: device [S] or NULL (s); a
  * sequence whose index is outside 0 .. num_caches - 1 is skipped; indexes
  * must differ.  first: device [S] (>= 0) or NULL (0).  desc: dtype, kv_heads,
- * head_dim, window and sinks are read.  Errors: INVALID_ARG, UNSUPPORTED, HIP. */
+ * head_dim, window and sinks are read; key_mask must be NULL: a ring shows every
+ * slot, so events that training hides would be seen once served, and a history
+ * without them has other positions, window and sinks than the trained one.
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP. */
 lattice_status lattice_seq_cache_fill(const lattice_seq_attn_desc* desc, const lattice_seqs* seqs,
                                       const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                                       const int32_t* first, const int32_t* cache_index,
@@ -572,8 +575,8 @@ lattice_status lattice_seq_cache_fill(const lattice_seq_attn_desc* desc, const l
  * the user already has (int32 positions in the sequence; the caller advances
  * them); rope->positions, if given, is [batch].  cache_index as above
  * ([batch]); a user with an index out of range or lens < 0 is skipped: nothing
- * of it is read or written.  key_mask must be NULL (hidden events are not
- * appended); dtype, heads, kv_heads and head_dim of rope and desc agree.
+ * of it is read or written.  key_mask must be NULL, as for the fill; dtype,
+ * heads, kv_heads and head_dim of rope and desc agree.
  * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, HIP. */
 size_t lattice_seq_step_workspace(const lattice_seq_attn_desc* desc, int32_t batch);
 lattice_status lattice_seq_step(const lattice_seq_attn_desc* desc, const lattice_qk_rope_desc* rope,

@@ -275,6 +275,7 @@ lattice_status lattice_seq_cache_fill(const lattice_seq_attn_desc* d, const latt
                                       int64_t k_stride, const void* v, int64_t v_stride, const int32_t* first,
                                       const int32_t* cache_index, const lattice_seq_cache* cache, void* stream) {
   TRY(check_attn(d));
+  REQUIRE(!d->key_mask, "a cache takes no key_mask");
   TRY(check_seqs(seqs));
   TRY(check_cache(d, cache));
   if (seqs->rows == 0 || seqs->num_seqs == 0 || cache->num_caches == 0) return LATTICE_OK;

@@ -202,6 +202,15 @@ def test_cache_and_step(lib):
     assert fill(s=seqs(rows=0)) == OK and fill(c=cache(num_caches=0)) == OK
 
 
+def test_a_cache_takes_no_hidden_events(lib):
+    """Neither the fill nor the step: every slot of a ring is seen."""
+    d, s, c = attn(key_mask=P), seqs(), cache()
+    assert lib.lattice_seq_cache_fill(byref(d), byref(s), P, KS, P, KS, None, None, byref(c), None) == INVALID_ARG
+    assert b"key_mask" in lib.lattice_last_error()
+    assert lib.lattice_seq_step(byref(d), None, 2, P, QS, P, KS, P, KS, P, None, byref(c), P, QS, P, 1 << 40,
+                                None) == INVALID_ARG
+
+
 def test_binding_checks_before_it_calls():
     x = torch.zeros(4, 2, 64)
     like = 4, 64, torch.float32, -1
