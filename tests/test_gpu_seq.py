@@ -201,6 +201,128 @@ def test_a_long_history_among_many_short_ones(dt, H, J, D, W, N, known):
     check_attn(attn_case(dt, H, J, D, lens, W, N, pad=3, max_len=900 if known else 0), dt, W, N)
 
 
+def banded(q, k, v, do, start, W, N, dt, longest):
+    """One head over rows of sequences that begin at `start`, in float64 by each
+    row's W + N keys: values and bounds of out, dq, dk, dv as oracle.seqattn has
+    them."""
+    T, D = q.shape
+    u, U, scale = o.HALF_STEP[dt], o.U32, D ** -0.5
+    r = u if dt == "bf16" else 0.0
+    row = torch.arange(T, device=DEV)[:, None]
+    win, sink = row - torch.arange(W, device=DEV), start[:, None] + torch.arange(N, device=DEV)
+    ok = torch.cat([win >= start[:, None], sink <= row - W], 1)
+    at = torch.cat([win, sink], 1).clamp(0, T - 1)
+    K, V, Q, G = k[at], v[at], q[:, None], do[:, None]
+    score = (Q * K).sum(-1) * scale
+    P = torch.softmax(torch.where(ok, score, -torch.inf), 1)
+    size = torch.where(ok, (Q.abs() * K.abs()).sum(-1) * scale, 0.0).amax(1, keepdim=True)
+    es = (D + 8) * U * size + 4 * U * (1 + size) + (W + N + 8) * U
+    out, mag = (P[..., None] * V).sum(1), (P[..., None] * V.abs()).sum(1)
+    wide = (r + 2 * es + (W + N + 4) * U) * mag
+    e_out, wide = wide * (1 + u) + u * out.abs(), wide + min(u, 2.0 ** -16) * out.abs() * (1 + u)
+    dP, absdP = (G * V).sum(-1), (G.abs() * V.abs()).sum(-1)
+    delta = (do * out).sum(1, keepdim=True)
+    e_delta = (do.abs() * wide).sum(1, keepdim=True) + (D + 2) * U * (do.abs() * out.abs()).sum(1, keepdim=True)
+    dS = P * (dP - delta)
+    e_dS = P * ((D + 2) * U * absdP + e_delta) + (2 * es + r) * dS.abs() + 4 * U * P * (dP.abs() + delta.abs())
+    n = longest + 8
+
+    def per_key(w, x):                                       # sum over the rows of w x
+        y = torch.zeros_like(x)
+        return y.index_add_(0, at[ok], (w[..., None] * x[:, None])[ok])
+    dq = scale * (dS[..., None] * K).sum(1)
+    b = scale * ((e_dS + (W + N + 4) * U * dS.abs())[..., None] * K.abs()).sum(1)
+    dk, bk = scale * per_key(dS, q), scale * per_key(e_dS + n * U * dS.abs(), q.abs())
+    dv, bv = per_key(P, do), per_key((r + 2 * es + n * U) * P, do.abs())
+    return [(out, e_out)] + [(x, y * (1 + u) + u * x.abs()) for x, y in ((dq, b), (dk, bk), (dv, bv))]
+
+
+@pytest.mark.parametrize("dt,D,lens,W,N", [
+    # more than 8192 late rows: pieces longer than a tile, up to 64 of them
+    ("bf16", 32, [7, 12000, 300], 8, 5), ("f32", 40, [9000], 3, 40), ("bf16", 128, [20, 8300, 40, 9500], 40, 16),
+    # more than 524288 rows: tiles above 128 rows
+    ("bf16", 8, [3, 1, 11, 2] * 30000 + [20000] + [9, 4] * 4000, 4, 3)])
+@pytest.mark.parametrize("known", [False, True])
+def test_late_rows_in_long_pieces(dt, D, lens, W, N, known):
+    off, T, s = plan(lens, max_len=max(lens) if known else 0)
+    from paper_2512_09200_amd import api
+    g = torch.Generator(device=DEV)
+    g.manual_seed(D)
+    q, k, v, do = (torch.randn(T, 1, D, generator=g, device=DEV).to(TT[dt]) for _ in range(4))
+    out, saved = api.lattice_seq_attn_fwd(s, q, k, v, W, N)
+    got = (out,) + tuple(api.lattice_seq_attn_bwd(s, q, k, v, out, saved, do, W, N))
+    start = torch.from_numpy(np.repeat(off[:-1], np.diff(off))).to(DEV)
+    want = banded(*(x[:, 0].double() for x in (q, k, v, do)), start, W, N, dt, max(lens))
+    for x, (w, b), name in zip(got, want, ("out", "dq", "dk", "dv")):
+        over = (x[:, 0].double() - w).abs() - b
+        assert over.max() <= 1e-30, (name, int(over.amax(1).argmax()), float(over.max()))
+
+
+@pytest.mark.parametrize("n,D", [(20, 64), (20, 32), (37, 128), (20, 8)])
+def test_what_rounding_took_from_out_reaches_the_gradients(n, D):
+    """Scores of 0 (q or k all zeros), so that probabilities are 1 / row count
+    without rounding, and values between 1 and 1 + 3 / 128, whose differences are
+    no larger than the rounding of out: a backward whose delta is from out
+    alone is 5 to 80 times over these bounds."""
+    from paper_2512_09200_amd import api
+    rng = np.random.default_rng(n + D)
+    U, u, sc = o.U32, o.HALF_STEP["bf16"], D ** -0.5
+    off, rows, s = plan([n])
+    bf = lambda x: torch.from_numpy(x.astype(np.float32)).to(torch.bfloat16)[:, None].to(DEV)  # noqa: E731
+    V, DO = 1 + rng.integers(0, 4, (n, D)) * 2.0 ** -7, rng.choice([-1.0, 1.0], (n, D))
+    x, zero = bf(1 + 0.5 * rng.random((n, D))), bf(np.zeros((n, D)))
+    v, do, X = bf(V), bf(DO), f64(x)[:, 0]
+    count = np.arange(1, n + 1)[:, None]
+    P = np.tril(np.ones((n, n))) / count
+    out = P @ V
+    dP, delta = DO @ V.T, (DO * out).sum(1, keepdims=True)
+    dS = P * (dP - delta)
+    # out and out_lo: 2^-8 of 2^-8 of out, and the sum of `count` values
+    e_out = (2.0 ** -16 + (count + 4) * U) * out
+    e_dS = P * (D * U * np.abs(DO) @ V.T + (e_out + D * U * out).sum(1, keepdims=True)) + (u + 24 * U) * np.abs(dS)
+    for q, k, which in ((zero, x, 1), (x, zero, 2)):
+        y, saved = api.lattice_seq_attn_fwd(s, q, k, v, n)
+        within(y.float() + saved.out_lo.float(), out[:, None], e_out[:, None], "out + out_lo")
+        g = api.lattice_seq_attn_bwd(s, q, k, v, y, saved, do, n)[which - 1]
+        w, e = (dS, e_dS) if which == 1 else (dS.T, e_dS.T)
+        want = sc * w @ X
+        bound = sc * (e @ X + (n + 4) * U * np.abs(w) @ X)
+        within(g, want[:, None], (bound * (1 + u) + u * np.abs(want))[:, None], ("dq", "dk")[which - 1])
+
+
+@pytest.mark.parametrize("dt,H,J,D", [("bf16", 4, 2, 64), ("f32", 2, 1, 40), ("bf16", 2, 1, 128)])
+def test_attention_without_statistics_and_without_out_lo(dt, H, J, D):
+    """lse=False gives the same out; without out_lo the rounding of out (u of it)
+    enters delta."""
+    from paper_2512_09200_amd import api
+    W, N, n = 30, 3, 170
+    c = attn_case(dt, H, J, D, [90, 80], W, N, hidden=0.1)
+    out, none = api.lattice_seq_attn_fwd(c["s"], c["q"], c["k"], c["v"], lse=False, **c["kw"])
+    assert none is None and torch.equal(out, c["out"])
+    saved = api.SeqAttnSaved(c["lse"].lse, None)
+    got = api.lattice_seq_attn_bwd(c["s"], c["q"], c["k"], c["v"], out, saved, c["do"], **c["kw"])
+    if dt == "f32":
+        assert all(torch.equal(a, c[m]) for a, m in zip(got, ("dq", "dk", "dv")))
+        return
+    q, k, v, do = (f64(c[m]) for m in ("q", "k", "v", "do"))
+    sc, u = D ** -0.5, o.HALF_STEP[dt]
+    f = o.attn(q, k, v, c["off"], W, N, sc, c["shown"], dt)
+    g, b = o.attn_bwd(q, k, v, c["off"], W, N, sc, c["shown"], do, dt)
+    assert torch.equal(got[2], c["dv"])
+    e = u * (np.abs(do) * np.abs(f["o"])).sum(-1)                    # [rows, heads]
+    for a, z in ((0, 90), (90, 170)):
+        see = o.visible(z - a, W, N, c["shown"][a:z])
+        for h in range(H):
+            j = h // (H // J)
+            P, _, _ = o._probabilities(q[a:z, h], np.where(c["shown"][a:z, None], k[a:z, j], 0), see, sc)
+            w = P * e[a:z, h][:, None] * sc * (1 + u)
+            b["dq"][a:z, h] += w @ np.where(c["shown"][a:z, None], np.abs(k[a:z, j]), 0)
+            b["dk"][a:z, j] += w.T @ np.abs(q[a:z, h])
+    assert n == c["rows"]
+    within(got[0], g["dq"], b["dq"], "dq")
+    within(got[1], g["dk"], b["dk"], "dk")
+
+
 @pytest.mark.parametrize("dt,D", [("bf16", 64), ("f32", 128)])
 def test_rows_behind_the_last_sequence_stay(dt, D):
     from paper_2512_09200_amd import api
@@ -671,6 +793,36 @@ def test_step_against_the_definition(dt, H, J, D, W, N, rope):
             bound = (r + 2 * np.expm1(es)) * (P @ np.abs(vv)) + u * np.abs(P @ vv) * (1 + r)
             within(out[b, h], P @ vv, bound, f"out {b} {h}")
     _ = eq
+
+
+@pytest.mark.parametrize("H,J,D,W,N", [(8, 2, 64, 30, 3), (4, 4, 32, 5, 0), (20, 1, 40, 64, 36), (6, 3, 128, 20, 4)])
+@pytest.mark.parametrize("rope", [True, False])
+def test_step_rounds_the_query_and_the_probabilities_in_two_parts(H, J, D, W, N, rope):
+    """Few slots, where one bf16 part of either would be 1.8 to 8 times over the
+    bound: 2^-8 of 2^-8 for each, fp32 sums, one rounding of out."""
+    from paper_2512_09200_amd import api
+    rng = np.random.default_rng(D + W)
+    B, cap, U, u = 6, W + N, o.U32, o.HALF_STEP["bf16"]
+    q, k, v = (randn(rng, B, h, D).to(torch.bfloat16).to(DEV) for h in (H, J, J))
+    kc, vc = (randn(rng, B, J, cap, D).to(torch.bfloat16).to(DEV) for _ in "kv")
+    lens = torch.tensor([cap, cap + 1, 3 * cap, cap - 1, cap // 2, 5 * cap], dtype=torch.int32, device=DEV)
+    gq, gk = (1 + 0.1 * randn(rng, D)).to(DEV), (1 + 0.1 * randn(rng, D)).to(DEV)
+    kw = dict(gain_q=gq, gain_k=gk) if rope else dict(rope=False)
+    out = api.lattice_seq_step(q, k, v, lens, kc, vc, W, N, **kw)
+    Q, KC, VC = f64(q), f64(kc), f64(vc)
+    if rope:
+        Q, _ = o.qk_rope(Q, f64(gq), lens.cpu().numpy(), D, 1e4, 1e-6, False)
+    for b in range(B):
+        n = min(int(lens[b]) + 1, cap)
+        for h in range(H):
+            kk, vv = KC[b, h // (H // J), :n], VC[b, h // (H // J), :n]
+            s = kk @ Q[b, h] / np.sqrt(D)
+            P = np.exp(s - s.max())
+            P /= P.sum()
+            size = (np.abs(kk) @ np.abs(Q[b, h])).max() / np.sqrt(D)
+            es = (2.0 ** -16 if rope else 0) * size + (2 * D + 48) * U * size * 1.5 + (n + 16) * U
+            bound = (2.0 ** -16 + 2 * np.expm1(es)) * (P @ np.abs(vv)) + u * np.abs(P @ vv) * (1 + 2.0 ** -16)
+            within(out[b, h], P @ vv, bound, f"out {b} {h}")
 
 
 @pytest.mark.parametrize("dt,H,J,D,W,N", [("bf16", 4, 2, 64, 16, 2), ("f32", 4, 1, 32, 40, 0)])
