@@ -1025,11 +1025,12 @@ __global__ __launch_bounds__(256, 1) void seq_sink_kernel(AttnK A, int parts) {
   // of the rows xb + lane + 64 e: those that begin a piece
   auto pieces = [&](int xb) __attribute__((always_inline)) {
     unsigned heads = 0;
+    SeqSpan sp[SCAN];                          // all loads before the first branch
+#pragma unroll
+    for (int e = 0; e < SCAN; ++e) sp[e] = A.span[min(xb + lane + 64 * e, x1 - 1)];
 #pragma unroll
     for (int e = 0; e < SCAN; ++e) {
-      const int i = xb + lane + 64 * e;
-      const SeqSpan sp = A.span[min(i, x1 - 1)];
-      const int l0 = late_row(A, sp.start), n = sp.end - l0;
+      const int i = xb + lane + 64 * e, l0 = late_row(A, sp[e].start), n = sp[e].end - l0;
       bool head = i == l0;
       const bool more = i > l0 && n > A.chunk;                  // may begin a later piece
       if (wave_any(more)) head |= more && (i - l0) % late_piece(A, n) == 0;
