@@ -810,7 +810,8 @@ def lattice_seq_cache_fill(seqs, k, v, k_cache, v_cache, window, sinks=0, cache_
     """Lays the sequences' keys (as lattice_qk_rope_fwd gives them) and values
     into ring caches [caches, kv_heads, sinks + window, head_dim].  cache_index
     (int32 [S], different ones; None: s) and first (int32 [S], the position of
-    each sequence's first row; None: 0)."""
+    each sequence's first row; None: 0).  Every slot of a ring is seen: events
+    that a key_mask hides in training have no place in it."""
     if stream is not None:
         return _on(stream, k, lattice_seq_cache_fill, seqs, k, v, k_cache, v_cache, window, sinks,
                    cache_index, first)
@@ -832,7 +833,8 @@ def lattice_seq_step(q, k, v, lens, k_cache, v_cache, window, sinks=0, cache_ind
     and k (rope False: taken as they are), append of k and v to the users' ring
     caches at position lens (int32 [batch]: the events they have; the caller
     advances them), attention of q over the caches' visible slots.  Returns
-    out; users with lens < 0 or a cache_index out of range are skipped."""
+    out; users with lens < 0 or a cache_index out of range are skipped (their
+    rows of out are not written)."""
     if stream is not None:
         return _on(stream, q, lattice_seq_step, q, k, v, lens, k_cache, v_cache, window, sinks, cache_index,
                    scale, rope, gain_q, gain_k, theta, rotary, interleaved, eps, positions, out)

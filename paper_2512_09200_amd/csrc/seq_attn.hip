@@ -21,7 +21,11 @@
 // transposed, S^T = K Q^T: a lane holds one row's scores, its maximum and sum
 // need one exchange between lane halves, and the probabilities are the
 // next product's operand (O^T = V^T P^T) where they are.  K and V tiles go from
-// memory straight to LDS one tile ahead.
+// memory straight to LDS; the next tile's loads go out when a tile's first
+// product begins and have until its second one: the compiler cannot tell the
+// places that transposed LDS reads take from those that direct loads write, and
+// waits for all loads before the first such read (bf16; fp32 reads columns
+// with ordinary loads and has the whole tile).
 //
 // dK and dV: a block takes 128 keys, a wave 32 of them, over the rows that see
 // them and the group's heads, S = Q K^T.  Rows that see a
@@ -34,14 +38,23 @@
 // elements alone (RepairPass, below), so that they are what the rows they see make
 // of them.
 //
-// Bound.  65536 rows in 4 histories, 8 heads of 128 over 2, window 2048, bf16:
-// forward 690 us (0.8 PFLOP/s), dQ 890, dK/dV 1220 (0.88 and 0.85 of their three
+// Roundings (bf16).  P and dS are operands of one bf16 part: every term of a sum
+// is off by up to 2^-8 of itself, each on its own.  In the measured cases out is off
+// by 2.0e-3 of its norm and dq, dk by 2.4e-3, where one rounding of the exact
+// result gives 1.5e-3 to 1.7e-3.  A second part, as the single-event step takes, would double the
+// second products, which the matrix cores do not have free here.  Scores, maxima,
+// sums, lse, delta and accumulators are fp32.
+//
+// Bound.  65536 rows in 4 histories, 8 heads of 128 over 2, window 2048, bf16 (shortest
+// of six dispatches here and below; the means are 2 to 15% longer):
+// forward 687 us (0.75 PFLOP/s), dQ 881, dK/dV 1191 (0.88 and 0.87 of their three
 // and four products); the matrix cores are busy 42-47% of the cycles, beside
 // the scores' vector work (an exponential of 16 cycles, the subtraction, sum,
-// maximum and rounding for every 32 x 32 x 16 product's share), LDS 21-40%.
-// 32768 rows, heads of 64, window 256, hidden keys: 58, 67 and 71 us, half of the
-// cycles issuing vector instructions.  8192 histories of 20, 4 heads of 32: 64,
-// 73 and 73 us for 210, 294 and 252 MB (43, 60 and 52 us of copy time).
+// maximum and rounding for every 32 x 32 x 16 product's share) and the wait for the
+// next tile before the second product, LDS 21-40%.
+// 32768 rows, heads of 64, window 256, hidden keys: 58, 66 and 68 us, half of the
+// cycles issuing vector instructions.  8192 histories of 20, 4 heads of 32: 63,
+// 72 and 71 us for 210, 294 and 252 MB (43, 60 and 52 us of copy time).
 #include <algorithm>
 #include <type_traits>
 
@@ -135,7 +148,8 @@ __device__ inline int xcd_runs(int b, int n) {
 // blocks run at once (two a compute unit, block b beside b + 256), the second
 // half goes from the first tile on, so that heavy and light ones share a unit.
 // One history of 8192, all rows before each seen, 8 heads of 128: 252 us with
-// tiles from first to last, 233 from last to first, 215 so.
+// tiles from first to last, 233 from last to first, 215 so.  (Measured there
+// alone: narrower heads hold more than two, fp32 heads of 128 one.)
 struct BlockAt { int tile, kv, h0; };
 __device__ inline BlockAt block_at(const AttnK& A) {
   const int hg = A.group / A.hb, per = A.kv_heads * hg;
@@ -164,10 +178,9 @@ __device__ __forceinline__ void landed() {
   asm volatile("" ::: "memory");
 }
 
-// The K and V tiles of a block's key range, each loaded while the one before
-// is computed.  (Three or four under way measured the same with heads of 64 and
-// 4% slower with heads of 32.)  A tile's key mask is one load made a tile
-// ahead of the tile's own, whose row bits depend on it.
+// The K and V tiles of a block's key range, each loaded beside the first product
+// of the one before (see the head of this file).  A tile's key mask is one load
+// made a tile ahead of the tile's own, whose row bits depend on it.
 template <typename T, int DP>
 struct KeyStream {
   using Cfg = AttnCfg<T, DP>;
@@ -345,7 +358,7 @@ __device__ __forceinline__ void load_rows(const SeqTensor& t, int i, int head, i
 // Elements of O^T-shaped accumulators (lane: one row, element r of block db is
 // column 32 db + frag_off(r) + 4 (lane / 32)) to a row of memory.  PATCH: only
 // elements that are not finite in memory.  lo: what the rounding to bf16
-// took, rounded to bf16.
+// took, rounded to bf16: the pair is off by 2^-16 of out.
 template <typename T, int DP, bool PATCH>
 __device__ __forceinline__ void store_row(T* op, T* lo, int dim, f32x16 (&x)[Tile<T, DP>::DB]) {
   const int half = (threadIdx.x & 63) >> 5;

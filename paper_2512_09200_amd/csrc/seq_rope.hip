@@ -269,7 +269,8 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeK A, RopeTurns turns) {
   }
 }
 
-// dgain[j] = sum over blocks, 16 columns and 64 strands of blocks a workgroup
+// dgain[j] = sum over blocks (fp32, as a lane's sum over its head vectors and the
+// block's over its lane groups before it: three short sums, not one long one), 16 columns and 64 strands of blocks a workgroup
 // of 1024; the strands' sums are added in a fixed tree.
 __global__ __launch_bounds__(1024) void rope_dgain_kernel(const float* __restrict__ partial, int blocks, int dim,
                                                           float* __restrict__ dgq, float* __restrict__ dgk) {
@@ -293,7 +294,9 @@ __global__ __launch_bounds__(1024) void rope_dgain_kernel(const float* __restric
 }
 
 // Rows a block takes at a time.  Many share the lanes better between angles
-// and heads, few give a small batch more blocks and shorter chains.  131072
+// and heads, few give a small batch more blocks and shorter chains.  Measured at
+// these two sizes; that rows x heads fill whole rounds of a block's lane groups is
+// not looked at.  131072
 // rows, 10 heads of 128, bf16: 131 us with 16 rows, 148 with 4, 318 with 1; 5021
 // rows, 9 heads of 96, fp32, forward: 14.6, 13.1, 14.7, backward: 21.4, 24.9, 32.8.
 static int rope_tb(int64_t rows, bool bwd) {

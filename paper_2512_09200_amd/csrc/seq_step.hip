@@ -11,7 +11,9 @@
 // matrix cores are far from the bound.  A lane then holds one head's
 // probabilities of 8 slots, which are the next product's operand
 // (O^T = V^T P^T); only V passes through LDS, to be read transposed.  The next
-// tile's loads are in flight while a tile is computed.
+// tile's loads go out before a tile's scores; before the tile's first transposed
+// read of V the compiler waits for all of them (bf16), as it cannot tell that
+// they write elsewhere.
 //
 // The new event's own k and v replace their slot's row where the tile is
 // used (registers for k, the LDS row for v), so nothing waits for the cache's
