@@ -443,8 +443,9 @@ typedef struct {
   const int32_t* offsets;  /* device [S+1], offsets[0] = 0, non-decreasing, offsets[S] <= rows */
   const int32_t* span;     /* device [rows, 2], 8-byte aligned: written by lattice_seq_plan, read by
                               every other call */
-  int64_t max_len;         /* no sequence is longer; 0: unknown (rows is used).  With a bound that a
-                              sequence exceeds, lattice_seq_attn_bwd drops gradients of its sinks. */
+  int64_t max_len;         /* no sequence is longer; 0: unknown (rows is used).  With a bound below
+                              sinks + window that a sequence exceeds, lattice_seq_attn_bwd drops
+                              gradients of its sinks. */
 } lattice_seqs;
 
 /* Span of every row: the first row of its sequence and the row behind its
