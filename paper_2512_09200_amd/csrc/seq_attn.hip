@@ -1021,8 +1021,8 @@ __global__ __launch_bounds__((64 * DkvCfg<T, DP>::NW), (DkvCfg<T, DP>::WAVES)) v
 // rows, their sums are added in wave order.  Tiles lie on the packed rows and a
 // sequence has pieces by its own length, so the work is even whatever else is
 // in the batch: one history of 32000 events among 3000 of 20, 8 heads of 64 over 2,
-// window 256: 37 us here and 180 in the dK/dV kernel, which adds up 64 pieces in
-// one block (1520 and 128 with one piece).
+// window 256: 40 us here and 134 in the dK/dV kernel, which adds up 64 pieces in
+// one block (1510 and 126 with one piece).
 template <typename T, int DP>
 __global__ __launch_bounds__(256, 1) void seq_sink_kernel(AttnK A, int parts) {
   using TL = Tile<T, DP>;
