@@ -47,7 +47,7 @@
 extern "C" {
 #endif
 
-#define LATTICE_ABI_VERSION 11
+#define LATTICE_ABI_VERSION 12
 #define LATTICE_MAX_LAYERS 8
 
 typedef enum {
@@ -585,6 +585,117 @@ lattice_status lattice_seq_step(const lattice_seq_attn_desc* desc, const lattice
                                 int64_t k_stride, const void* v, int64_t v_stride, const int32_t* lens,
                                 const int32_t* cache_index, const lattice_seq_cache* cache, void* out,
                                 int64_t out_stride, void* ws, size_t ws_bytes, void* stream);
+
+/* The same ring in 8 bits: e4m3 codes (as lattice_fp8_quantize's) with one fp32
+ * scale for the keys and one for the values of every
+ * LATTICE_SEQ_CACHE8_BLOCK neighbouring slots (0 .. 15, 16 .. 31, ...) of a cache
+ * and key head.  A scale is the smallest power of two s >= 2^-117 with |x| <= 448 s
+ * for every finite x of its block's reached slots (1 where all are 0): an event
+ * that changes it has the block's codes rounded anew, exactly but for codes
+ * that become subnormal.  A value that is not finite is kept as NaN (0x7f).  Half the memory and
+ * the memory time of bf16; codes are off by 2^-4 of themselves at most.
+ * Slots that no position has reached have no value: their codes and, where a
+ * block has none that is reached, its scales are never used. */
+#define LATTICE_SEQ_CACHE8_BLOCK 16
+typedef struct {
+  uint8_t* k;               /* device [num_caches, kv_heads, sinks + window, ld] codes, ld = head_dim rounded
+                               up to a multiple of 16 (bytes past head_dim: zeros, never used) */
+  uint8_t* v;
+  float* k_scale;           /* device [num_caches, kv_heads, ceil((sinks + window) / 16)] */
+  float* v_scale;
+  int32_t num_caches;
+} lattice_seq_cache8;
+
+/* lattice_seq_cache_fill for 8-bit caches: k and v in desc's dtype.  Blocks
+ * that take rows are scaled anew, what positions before first[s] left in them
+ * included.  Other arguments and errors as there. */
+lattice_status lattice_seq_cache8_fill(const lattice_seq_attn_desc* desc, const lattice_seqs* seqs,
+                                       const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                                       const int32_t* first, const int32_t* cache_index,
+                                       const lattice_seq_cache8* cache, void* stream);
+
+/* lattice_seq_step over 8-bit caches: the event's k is rounded to desc's dtype
+ * (as lattice_qk_rope_fwd gives it), then k and v to codes, and out_b is the
+ * attention over the codes, the event's own included.  A non-finite k or v
+ * reaches what sees it as NaN.  Two users of a call must not share a cache.
+ * Other arguments and errors as for lattice_seq_step. */
+size_t lattice_seq_step8_workspace(const lattice_seq_attn_desc* desc, int32_t batch);
+lattice_status lattice_seq_step8(const lattice_seq_attn_desc* desc, const lattice_qk_rope_desc* rope,
+                                 int32_t batch, const void* q, int64_t q_stride, const void* k,
+                                 int64_t k_stride, const void* v, int64_t v_stride, const int32_t* lens,
+                                 const int32_t* cache_index, const lattice_seq_cache8* cache, void* out,
+                                 int64_t out_stride, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Between the products of an event block (Sections 3.3.4, 3.5.2)           */
+/* ------------------------------------------------------------------------ */
+
+/* Dropout from a counter-based generator: which elements stay is a function
+ * of seed, step, site, row and column, so that no mask is stored and the
+ * backward is the same call on the gradient.  Eight neighbouring columns (8 g
+ * .. 8 g + 7) of a row take the eight 16-bit numbers of one Philox4x32-10 block
+ * (counter: g, row, site, low word of the step; key: seed; word e / 2, low half
+ * first).  With t = p 65536 rounded to the nearest integer (halves up), element
+ * x becomes x * 65536 / (65536 - t) (the product in fp32, rounded to the
+ * storage type) where its number is >= t, and 0 elsewhere, whatever it held. */
+typedef struct {
+  double p;                 /* 0 .. 65535.5 / 65536 (excluded) */
+  const uint64_t* rng;      /* device [2], 8-byte aligned: seed, step; read when the kernel runs, so a
+                               captured graph draws anew once the caller advances the step */
+  uint32_t site;            /* which dropout of the model (layer and place): those of one step differ */
+} lattice_dropout_desc;
+
+/* out = dropout(x) over [rows, cols] with row strides in elements, any
+ * alignment; out may be x (same stride).  rows < 2^30, cols < 2^30.  rng may be
+ * NULL when t = 0.  Errors: INVALID_ARG, UNSUPPORTED (sizes), HIP. */
+lattice_status lattice_dropout(const lattice_dropout_desc* desc, lattice_dtype dtype, int64_t rows,
+                               int32_t cols, const void* x, int64_t x_stride, void* out,
+                               int64_t out_stride, void* stream);
+
+/* Residual sum and root-mean-square norm in one pass:
+ *   h = round(dropout(x) + residual),  y = gain * h / sqrt(mean(h^2) + eps)
+ * over rows of cols elements, h rounded to the storage type (what the next
+ * layer adds to and what the backward needs), arithmetic in fp32.  The norm
+ * leaves as y in the storage type, as e4m3 codes with a scale for each row (the
+ * format of lattice_fp8_quantize, row-wise, from the fp32 norm: the operand of
+ * lattice_linear_fp8_fwd), or both.  A row whose sum of squares or whose norm is not finite
+ * gets NaN as its scale and in its codes. */
+#define LATTICE_NORM_MAX_COLS 16384
+typedef struct {
+  lattice_dtype dtype;
+  int32_t cols;             /* 1 .. LATTICE_NORM_MAX_COLS */
+  float eps;                /* >= 0 */
+  const float* gain;        /* device [cols] fp32, or NULL: ones */
+  const lattice_dropout_desc* dropout;  /* host, of x, or NULL: none */
+} lattice_add_rmsnorm_desc;
+
+/* residual may be NULL (h = round(dropout(x))), h may be NULL (not stored), and one of
+ * y and q but not both (q needs scales [rows]; q is [rows, ldq] bytes, ldq a
+ * multiple of 16 and >= cols, 16-byte aligned, bytes cols .. ldq - 1 are
+ * written as 0).  Row strides are in elements, >= cols; any alignment of the
+ * elements' own size.  h and y may be x or residual (same stride), not each
+ * other.  Errors: INVALID_ARG, UNSUPPORTED (cols, rows >= 2^30), HIP. */
+lattice_status lattice_add_rmsnorm_fwd(const lattice_add_rmsnorm_desc* desc, int64_t rows,
+                                       const void* x, int64_t x_stride, const void* residual,
+                                       int64_t residual_stride, void* h, int64_t h_stride, void* y,
+                                       int64_t y_stride, uint8_t* q, int64_t ldq, float* scales,
+                                       void* stream);
+
+/* Gradients of lattice_add_rmsnorm_fwd from h (x where nothing was added or
+ * dropped), dy = the gradient of the norm (quantisation is taken as the
+ * identity) and dh = what reaches h by the residual stream (or NULL): writes
+ * d_residual and dx (storage dtype, each may be NULL; without dropout they are
+ * equal) and, where not NULL, dgain [cols] (fp32, overwritten, summed over rows
+ * in a fixed order; needs a workspace).  rng must hold what it held in the
+ * forward.  d_residual and dx may be dy or dh (same stride), not each other.
+ * Errors: as the forward, WORKSPACE. */
+size_t lattice_add_rmsnorm_bwd_workspace(const lattice_add_rmsnorm_desc* desc, int64_t rows);
+lattice_status lattice_add_rmsnorm_bwd(const lattice_add_rmsnorm_desc* desc, int64_t rows,
+                                       const void* h, int64_t h_stride, const void* dy,
+                                       int64_t dy_stride, const void* dh, int64_t dh_stride,
+                                       void* d_residual, int64_t d_residual_stride, void* dx,
+                                       int64_t dx_stride, float* dgain, void* ws, size_t ws_bytes,
+                                       void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Whole training step                                                      */

@@ -6,7 +6,7 @@ loading fails loudly otherwise.
 """
 import ctypes
 import os
-from ctypes import POINTER, Structure, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import POINTER, Structure, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_uint32, c_void_p
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "liblattice.so")
@@ -136,6 +136,23 @@ class lattice_seq_cache(Structure):
     _fields_ = [("k", c_void_p), ("v", c_void_p), ("num_caches", c_int32)]
 
 
+SEQ_CACHE8_BLOCK = 16
+
+
+class lattice_seq_cache8(Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("k_scale", c_void_p), ("v_scale", c_void_p),
+                ("num_caches", c_int32)]
+
+
+class lattice_dropout_desc(Structure):
+    _fields_ = [("p", c_double), ("rng", c_void_p), ("site", c_uint32)]
+
+
+class lattice_add_rmsnorm_desc(Structure):
+    _fields_ = [("dtype", c_int), ("cols", c_int32), ("eps", c_float), ("gain", c_void_p),
+                ("dropout", POINTER(lattice_dropout_desc))]
+
+
 _ROWS = [c_void_p, c_int64]          # a tensor of event rows and its row stride
 
 # (name, restype, argtypes)
@@ -191,6 +208,17 @@ _SIGS = [
     ("lattice_seq_step_workspace", c_size_t, [POINTER(lattice_seq_attn_desc), c_int32]),
     ("lattice_seq_step", c_int, [POINTER(lattice_seq_attn_desc), POINTER(lattice_qk_rope_desc), c_int32]
      + 3 * _ROWS + [c_void_p, c_void_p, POINTER(lattice_seq_cache)] + _ROWS + [c_void_p, c_size_t, c_void_p]),
+    ("lattice_seq_cache8_fill", c_int, [POINTER(lattice_seq_attn_desc), POINTER(lattice_seqs)] + 2 * _ROWS
+     + [c_void_p, c_void_p, POINTER(lattice_seq_cache8), c_void_p]),
+    ("lattice_seq_step8_workspace", c_size_t, [POINTER(lattice_seq_attn_desc), c_int32]),
+    ("lattice_seq_step8", c_int, [POINTER(lattice_seq_attn_desc), POINTER(lattice_qk_rope_desc), c_int32]
+     + 3 * _ROWS + [c_void_p, c_void_p, POINTER(lattice_seq_cache8)] + _ROWS + [c_void_p, c_size_t, c_void_p]),
+    ("lattice_dropout", c_int, [POINTER(lattice_dropout_desc), c_int, c_int64, c_int32] + 2 * _ROWS + [c_void_p]),
+    ("lattice_add_rmsnorm_fwd", c_int, [POINTER(lattice_add_rmsnorm_desc), c_int64] + 5 * _ROWS
+     + [c_void_p, c_void_p]),
+    ("lattice_add_rmsnorm_bwd_workspace", c_size_t, [POINTER(lattice_add_rmsnorm_desc), c_int64]),
+    ("lattice_add_rmsnorm_bwd", c_int, [POINTER(lattice_add_rmsnorm_desc), c_int64] + 5 * _ROWS
+     + [c_void_p, c_void_p, c_size_t, c_void_p]),
     ("lattice_status_string", c_char_p, [c_int]),
     ("lattice_last_error", c_char_p, []),
     ("lattice_abi_version", c_int, []),

@@ -573,6 +573,8 @@ def _memory(xs):
             yield from (x.offsets, x.span)
         elif isinstance(x, SeqAttnSaved):
             yield from _memory((x.lse, x.out_lo))
+        elif isinstance(x, tuple):
+            yield from _memory(x)
         elif isinstance(x, torch.Tensor):
             yield x
 
@@ -853,3 +855,173 @@ def lattice_seq_step(q, k, v, lens, k_cache, v_cache, window, sinks=0, cache_ind
          *_heads(v, like, "v"), _vec(lens, torch.int32, B, "lens", dev),
          _vec(cache_index, torch.int32, B, "cache_index", dev), byref(cache), *_heads(out, like, "out"), _p(ws), wsb)
     return out
+
+
+def _cache8(caches, like, kv_heads, window, sinks):
+    k, v, ks, vs = caches
+    cap = int(sinks) + int(window)
+    want = (k.shape[0], kv_heads, cap, fp8_ld(like.shape[2]))
+    if k.shape != want or v.shape != want or k.dtype != torch.uint8 or v.dtype != torch.uint8:
+        raise ValueError(f"caches: expected [caches, kv_heads, sinks + window, fp8_ld(head_dim)] = {want} of uint8")
+    want = (k.shape[0], kv_heads, -(-cap // A.SEQ_CACHE8_BLOCK))
+    if ks.shape != want or vs.shape != want or ks.dtype != torch.float32 or vs.dtype != torch.float32:
+        raise ValueError(f"scales: expected [caches, kv_heads, blocks of {A.SEQ_CACHE8_BLOCK} slots] = {want} of float32")
+    _contig(*caches)
+    if any(t.get_device() != like.get_device() for t in caches):
+        raise ValueError("the caches are not on the other tensors' device")
+    return A.lattice_seq_cache8(*(t.data_ptr() or None for t in caches), k.shape[0])
+
+
+def lattice_seq_cache8_fill(seqs, k, v, k_cache, v_cache, k_scale, v_scale, window, sinks=0, cache_index=None,
+                            first=None, stream=None):
+    """lattice_seq_cache_fill for ring caches of e4m3 codes: k_cache and v_cache
+    uint8 [caches, kv_heads, sinks + window, fp8_ld(head_dim)], k_scale and
+    v_scale fp32 [caches, kv_heads, ceil((sinks + window) / 16)]."""
+    if stream is not None:
+        return _on(stream, k, lattice_seq_cache8_fill, seqs, k, v, k_cache, v_cache, k_scale, v_scale, window, sinks,
+                   cache_index, first)
+    desc = _attn_desc(k, k, window, sinks, 1.0, None)
+    S, dev = seqs.num_seqs, _gpu(k)
+    like = seqs.rows, k.shape[2], k.dtype, dev
+    cache = _cache8((k_cache, v_cache, k_scale, v_scale), k, k.shape[1], window, sinks)
+    if v.shape != k.shape or seqs.offsets.get_device() != dev:
+        raise ValueError("v must have k's shape, and the plan their device")
+    _run(dev, load().lattice_seq_cache8_fill, byref(desc), byref(seqs.desc), *_heads(k, like, "k"),
+         *_heads(v, like, "v"), _vec(first, torch.int32, S, "first", dev),
+         _vec(cache_index, torch.int32, S, "cache_index", dev), byref(cache))
+
+
+def lattice_seq_step8(q, k, v, lens, k_cache, v_cache, k_scale, v_scale, window, sinks=0, cache_index=None, scale=None,
+                      rope=True, gain_q=None, gain_k=None, theta=10000.0, rotary=None, interleaved=False, eps=1e-6,
+                      positions=None, out=None, stream=None):
+    """lattice_seq_step over ring caches of e4m3 codes (as
+    lattice_seq_cache8_fill has them), whose scales go with the events; no two
+    users of a call may share a cache."""
+    if stream is not None:
+        return _on(stream, q, lattice_seq_step8, q, k, v, lens, k_cache, v_cache, k_scale, v_scale, window, sinks,
+                   cache_index, scale, rope, gain_q, gain_k, theta, rotary, interleaved, eps, positions, out)
+    desc = _attn_desc(q, k, window, sinks, scale, None)
+    B, dev = q.shape[0], _gpu(q)
+    like = B, q.shape[2], q.dtype, dev
+    cache = _cache8((k_cache, v_cache, k_scale, v_scale), q, k.shape[1], window, sinks)
+    rd = byref(_rope_desc(q, k, gain_q, gain_k, theta, rotary, interleaved, eps, positions)) if rope else None
+    out = torch.empty_like(q) if out is None else out
+    if out.shape != q.shape or v.shape != k.shape:
+        raise ValueError("out must have q's shape, v k's")
+    lib = load()
+    wsb = lib.lattice_seq_step8_workspace(byref(desc), B)
+    ws = q.new_empty(wsb, dtype=torch.uint8) if wsb else None
+    _run(dev, lib.lattice_seq_step8, byref(desc), rd, B, *_heads(q, like, "q"), *_heads(k, like, "k"),
+         *_heads(v, like, "v"), _vec(lens, torch.int32, B, "lens", dev),
+         _vec(cache_index, torch.int32, B, "cache_index", dev), byref(cache), *_heads(out, like, "out"), _p(ws), wsb)
+    return out
+
+
+# ---------------------------------------------------------------------------
+def _drop_desc(dropout, dev):
+    """Descriptor of (p, rng, site); rng: int64 or uint64 [2] on the GPU, seed and step."""
+    if dropout is None:
+        return None
+    p, rng, site = dropout
+    if rng is not None and rng.dtype not in (torch.int64, torch.uint64):
+        raise ValueError("rng: expected two elements of int64 or uint64")
+    return A.lattice_dropout_desc(float(p), _vec(rng, rng.dtype, 2, "rng", dev) if rng is not None else None,
+                                  int(site) & 0xffffffff)
+
+
+def _row_ptr(t, like, name):
+    """(pointer, row stride) of a tensor [rows, cols]; like: one whose shape,
+    dtype and GPU it must have."""
+    if t is None:
+        return None, 0
+    if t.shape != like.shape or t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{name}: expected {tuple(like.shape)} of {like.dtype} on {like.device}, "
+                         f"got {tuple(t.shape)} of {t.dtype} on {t.device}")
+    rows, cols = t.shape
+    if rows and cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: expected unit column stride")
+    return t.data_ptr() or None, t.stride(0) if rows > 1 else cols
+
+
+def _rows2(t, name):
+    if t.dim() != 2:
+        raise ValueError(f"{name}: expected [rows, cols], got {tuple(t.shape)}")
+    return t.shape
+
+
+def lattice_dropout(x, p, rng, site=0, out=None, stream=None):
+    """Dropout of x [rows, cols] with probability p (a multiple of 2^-16 is
+    taken); rng: int64 [2] on the GPU, the seed and the step's number, read when
+    the kernel runs; site: which dropout of the model.  The gradient of x is the
+    same call on the gradient of the result.  out may be x."""
+    if stream is not None:
+        return _on(stream, x, lattice_dropout, x, p, rng, site, out)
+    rows, cols = _rows2(x, "x")
+    dev = _gpu(x)
+    desc = _drop_desc((p, rng, site), dev)
+    out = torch.empty((rows, cols), dtype=x.dtype, device=x.device) if out is None else out
+    _run(dev, load().lattice_dropout, byref(desc), _dt(x), rows, cols, *_row_ptr(x, x, "x"), *_row_ptr(out, x, "out"))
+    return out
+
+
+def _norm_desc(x, gain, eps, dropout, dev):
+    cols = x.shape[1]
+    drop = _drop_desc(dropout, dev)
+    return A.lattice_add_rmsnorm_desc(_dt(x), cols, float(eps), _vec(gain, torch.float32, cols, "gain", dev),
+                                      ctypes.pointer(drop) if drop is not None else None)
+
+
+def lattice_add_rmsnorm_fwd(x, residual=None, gain=None, eps=1e-6, dropout=None, out="y", h=None, y=None, stream=None):
+    """h = dropout(x) + residual and its root-mean-square norm with gain (fp32
+    [cols] or None), over [rows, cols].  dropout: None or (p, rng, site) as for
+    lattice_dropout.  out: "y" (storage type), "fp8" (e4m3 codes [rows,
+    fp8_ld(cols)] and scales [rows], the operands of lattice_linear_fp8_fwd) or
+    "both".  Returns (h, y, codes, scales), None for what was not asked; without
+    residual and dropout h is x itself."""
+    if stream is not None:
+        return _on(stream, x, lattice_add_rmsnorm_fwd, x, residual, gain, eps, dropout, out, h, y)
+    if out not in ("y", "fp8", "both"):
+        raise ValueError(f"out: expected 'y', 'fp8' or 'both', got {out!r}")
+    rows, cols = _rows2(x, "x")
+    dev = _gpu(x)
+    desc = _norm_desc(x, gain, eps, dropout, dev)
+    h_out = h
+    if residual is not None or dropout is not None:
+        h_out = h = torch.empty((rows, cols), dtype=x.dtype, device=x.device) if h is None else h
+    elif h is None:
+        h = x
+    if out == "fp8":
+        y = None
+    elif y is None:
+        y = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    codes = scales = None
+    if out != "y":
+        codes = torch.empty((rows, fp8_ld(cols)), dtype=torch.uint8, device=x.device)
+        scales = torch.empty(rows, dtype=torch.float32, device=x.device)
+    _run(dev, load().lattice_add_rmsnorm_fwd, byref(desc), rows, *_row_ptr(x, x, "x"),
+         *_row_ptr(residual, x, "residual"), *_row_ptr(h_out, x, "h"), *_row_ptr(y, x, "y"),
+         _p(codes), codes.stride(0) if codes is not None else 0, _p(scales))
+    return h, y, codes, scales
+
+
+def lattice_add_rmsnorm_bwd(h, dy, dh=None, gain=None, eps=1e-6, dropout=None, d_residual=None, dx=None, stream=None):
+    """Gradients (d_residual, dx, dgain) of lattice_add_rmsnorm_fwd from its h,
+    the gradient dy of the norm and dh of h itself (or None).  Without dropout dx
+    is d_residual; dgain (fp32 [cols]) is None where gain is.  dropout: the
+    forward's, its rng unchanged."""
+    if stream is not None:
+        return _on(stream, h, lattice_add_rmsnorm_bwd, h, dy, dh, gain, eps, dropout, d_residual, dx)
+    rows, cols = _rows2(h, "h")
+    dev = _gpu(h)
+    desc = _norm_desc(h, gain, eps, dropout, dev)
+    d_residual = torch.empty((rows, cols), dtype=h.dtype, device=h.device) if d_residual is None else d_residual
+    if dropout is not None and dx is None:
+        dx = torch.empty((rows, cols), dtype=h.dtype, device=h.device)
+    dgain = gain.new_empty(cols) if gain is not None else None
+    lib = load()
+    wsb = lib.lattice_add_rmsnorm_bwd_workspace(byref(desc), rows) if dgain is not None else 0
+    ws = h.new_empty(wsb, dtype=torch.uint8) if wsb else None
+    _run(dev, lib.lattice_add_rmsnorm_bwd, byref(desc), rows, *_row_ptr(h, h, "h"), *_row_ptr(dy, h, "dy"),
+         *_row_ptr(dh, h, "dh"), *_row_ptr(d_residual, h, "d_residual"), *_row_ptr(dx, h, "dx"),
+         _p(dgain), _p(ws), wsb)
+    return d_residual, d_residual if dx is None else dx, dgain

@@ -33,20 +33,12 @@
 // alignment is relative to its own 128 products only.
 
 #include "common.h"
+#include "e4m3.h"
 #include "kernels.h"
 
 namespace lat {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-
-// Four fp32 values (already scaled) -> four e4m3 codes in one word, byte e
-// = value e: round to nearest even, saturating at +-448.
-__device__ inline uint32_t e4m3x4(float a, float b, float c, float d) {
-  auto cl = [](float v) { return __builtin_amdgcn_fmed3f(v, -448.f, 448.f); };
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(cl(a), cl(b), 0, false);
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(cl(c), cl(d), w, true);
-  return (uint32_t)w;
-}
 
 __device__ inline float wave_max(float v) {
 #pragma unroll

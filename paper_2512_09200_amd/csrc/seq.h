@@ -84,6 +84,22 @@ struct SeqStepArgs {
 size_t seq_step_workspace(int batch, int heads, int kv_heads, int dim, int cap);
 hipError_t seq_step(const SeqStepArgs& a, const RopeTurns& t, void* ws, hipStream_t s);
 
+// The same ring in 8 bits: e4m3 codes, a scale for every 16 slots.
+struct SeqCache8Args {
+  DType dt = DT_BF16;                  // of the events' rows
+  int kv_heads = 0, dim = 0, window = 0, sinks = 0;
+  uint8_t *kc = nullptr, *vc = nullptr;
+  float *ks = nullptr, *vs = nullptr;
+  int num_caches = 0;
+  const int32_t* index = nullptr;
+};
+inline int cache8_ld(int dim) { return (dim + 15) / 16 * 16; }   // bytes of a slot's codes
+hipError_t seq_cache8_fill(const SeqCache8Args& c, int64_t rows, const int32_t* offsets, int num_seqs,
+                           const int32_t* first, SeqTensor k, SeqTensor v, hipStream_t s);
+size_t seq_step8_workspace(int batch, int heads, int kv_heads, int dim, int cap);
+// a.c is not read
+hipError_t seq_step8(const SeqStepArgs& a, const SeqCache8Args& c, const RopeTurns& t, void* ws, hipStream_t s);
+
 // Slot of position p in a ring of sinks + window slots.
 __host__ __device__ inline int seq_slot(int p, int sinks, int window) {
   return p < sinks ? p : sinks + (p - sinks) % window;

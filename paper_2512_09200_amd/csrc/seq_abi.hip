@@ -72,6 +72,18 @@ static lattice_status check_cache(const lattice_seq_attn_desc* d, const lattice_
   return LATTICE_OK;
 }
 
+static lattice_status check_cache8(const lattice_seq_attn_desc* d, const lattice_seq_cache8* c) {
+  REQUIRE(c, "null cache");
+  REQUIRE(c->num_caches >= 0, "negative num_caches");
+  if ((int64_t)d->window + d->sinks > MAX_ROWS) FAIL(LATTICE_ERR_UNSUPPORTED, "sinks + window above 2^30 slots");
+  if (c->num_caches > 0) {
+    REQUIRE(c->k && c->v && c->k_scale && c->v_scale, "null cache memory");
+    REQUIRE((uintptr_t)c->k % 16 == 0 && (uintptr_t)c->v % 16 == 0, "cache memory is not 16-byte aligned");
+    REQUIRE((uintptr_t)c->k_scale % 4 == 0 && (uintptr_t)c->v_scale % 4 == 0, "scales are not 4-byte aligned");
+  }
+  return LATTICE_OK;
+}
+
 static SeqTensor tensor(const void* p, int64_t ld) { return {const_cast<void*>(p), ld}; }
 
 static RopeArgs rope_args(const lattice_qk_rope_desc* d, const lattice_seqs* s) {
@@ -120,6 +132,66 @@ static SeqCacheArgs cache_args(const lattice_seq_attn_desc* d, const lattice_seq
   a.num_caches = c->num_caches;
   a.index = index;
   return a;
+}
+
+static SeqCache8Args cache8_args(const lattice_seq_attn_desc* d, const lattice_seq_cache8* c, const int32_t* index) {
+  SeqCache8Args a;
+  a.dt = dt_of(d->dtype);
+  a.kv_heads = d->kv_heads;
+  a.dim = d->head_dim;
+  a.window = d->window;
+  a.sinks = d->sinks;
+  a.kc = c->k;
+  a.vc = c->v;
+  a.ks = c->k_scale;
+  a.vs = c->v_scale;
+  a.num_caches = c->num_caches;
+  a.index = index;
+  return a;
+}
+
+static lattice_status check_step(const lattice_seq_attn_desc* d, const lattice_qk_rope_desc* rope, int32_t batch) {
+  TRY(check_attn(d));
+  REQUIRE(!d->key_mask, "a cache takes no key_mask");
+  if (rope) {
+    TRY(check_rope(rope));
+    REQUIRE(rope->dtype == d->dtype && rope->heads == d->heads && rope->kv_heads == d->kv_heads &&
+                rope->head_dim == d->head_dim, "rope and attention descriptors differ");
+  }
+  REQUIRE(batch >= 0, "negative batch");
+  return LATTICE_OK;
+}
+
+// Everything of a step but its cache
+static lattice_status step_args(const lattice_seq_attn_desc* d, const lattice_qk_rope_desc* rope, int32_t batch,
+                                const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                                int64_t v_stride, const int32_t* lens, void* out, int64_t out_stride, SeqStepArgs* a,
+                                RopeTurns* t) {
+  REQUIRE(lens, "null lens");
+  TRY(check_tensor("q", q, q_stride, d->heads, d->head_dim));
+  TRY(check_tensor("k", k, k_stride, d->kv_heads, d->head_dim));
+  TRY(check_tensor("v", v, v_stride, d->kv_heads, d->head_dim));
+  TRY(check_tensor("out", out, out_stride, d->heads, d->head_dim));
+  if ((int64_t)batch * d->heads > MAX_BLOCKS / 2) FAIL(LATTICE_ERR_UNSUPPORTED, "batch x heads too large for one launch");
+  a->batch = batch;
+  a->heads = d->heads;
+  a->scale = d->scale;
+  a->q = tensor(q, q_stride);
+  a->k = tensor(k, k_stride);
+  a->v = tensor(v, v_stride);
+  a->out = tensor(out, out_stride);
+  a->lens = lens;
+  if (rope) {
+    a->rope = 1;
+    a->rotary = rope->rotary_dim;
+    a->interleaved = rope->interleaved != 0;
+    a->eps = rope->eps;
+    a->gain_q = rope->gain_q;
+    a->gain_k = rope->gain_k;
+    a->positions = rope->positions;
+    rope_turns(rope->theta, rope->rotary_dim, t);
+  }
+  return LATTICE_OK;
 }
 
 // blocks of the attention kernels: 128 rows of a head each
@@ -297,46 +369,55 @@ lattice_status lattice_seq_step(const lattice_seq_attn_desc* d, const lattice_qk
                                 int64_t v_stride, const int32_t* lens, const int32_t* cache_index,
                                 const lattice_seq_cache* cache, void* out, int64_t out_stride, void* ws,
                                 size_t ws_bytes, void* stream) {
-  TRY(check_attn(d));
-  REQUIRE(!d->key_mask, "a cache takes no key_mask");
-  if (rope) {
-    TRY(check_rope(rope));
-    REQUIRE(rope->dtype == d->dtype && rope->heads == d->heads && rope->kv_heads == d->kv_heads &&
-                rope->head_dim == d->head_dim, "rope and attention descriptors differ");
-  }
-  REQUIRE(batch >= 0, "negative batch");
+  TRY(check_step(d, rope, batch));
   TRY(check_cache(d, cache));
   if (batch == 0 || cache->num_caches == 0) return LATTICE_OK;
-  REQUIRE(lens, "null lens");
-  TRY(check_tensor("q", q, q_stride, d->heads, d->head_dim));
-  TRY(check_tensor("k", k, k_stride, d->kv_heads, d->head_dim));
-  TRY(check_tensor("v", v, v_stride, d->kv_heads, d->head_dim));
-  TRY(check_tensor("out", out, out_stride, d->heads, d->head_dim));
-  if ((int64_t)batch * d->heads > MAX_BLOCKS / 2) FAIL(LATTICE_ERR_UNSUPPORTED, "batch x heads too large for one launch");
+  SeqStepArgs a;
+  RopeTurns t{};
+  TRY(step_args(d, rope, batch, q, q_stride, k, k_stride, v, v_stride, lens, out, out_stride, &a, &t));
   const size_t need = seq_step_workspace(batch, d->heads, d->kv_heads, d->head_dim, d->sinks + d->window);
   if (need > 0 && (!ws || ws_bytes < need)) FAIL(LATTICE_ERR_WORKSPACE, "workspace %zu < %zu", ws_bytes, need);
-  SeqStepArgs a;
   a.c = cache_args(d, cache, cache_index);
-  a.batch = batch;
-  a.heads = d->heads;
-  a.scale = d->scale;
-  a.q = tensor(q, q_stride);
-  a.k = tensor(k, k_stride);
-  a.v = tensor(v, v_stride);
-  a.out = tensor(out, out_stride);
-  a.lens = lens;
-  RopeTurns t{};
-  if (rope) {
-    a.rope = 1;
-    a.rotary = rope->rotary_dim;
-    a.interleaved = rope->interleaved != 0;
-    a.eps = rope->eps;
-    a.gain_q = rope->gain_q;
-    a.gain_k = rope->gain_k;
-    a.positions = rope->positions;
-    rope_turns(rope->theta, rope->rotary_dim, &t);
-  }
   HIPRET(seq_step(a, t, ws, strm(stream)));
+  return LATTICE_OK;
+}
+
+lattice_status lattice_seq_cache8_fill(const lattice_seq_attn_desc* d, const lattice_seqs* seqs, const void* k,
+                                       int64_t k_stride, const void* v, int64_t v_stride, const int32_t* first,
+                                       const int32_t* cache_index, const lattice_seq_cache8* cache, void* stream) {
+  TRY(check_attn(d));
+  REQUIRE(!d->key_mask, "a cache takes no key_mask");
+  TRY(check_seqs(seqs));
+  TRY(check_cache8(d, cache));
+  if (seqs->rows == 0 || seqs->num_seqs == 0 || cache->num_caches == 0) return LATTICE_OK;
+  REQUIRE(seqs->offsets, "null offsets");
+  TRY(check_tensor("k", k, k_stride, d->kv_heads, d->head_dim));
+  TRY(check_tensor("v", v, v_stride, d->kv_heads, d->head_dim));
+  HIPRET(seq_cache8_fill(cache8_args(d, cache, cache_index), seqs->rows, seqs->offsets, seqs->num_seqs, first,
+                         tensor(k, k_stride), tensor(v, v_stride), strm(stream)));
+  return LATTICE_OK;
+}
+
+size_t lattice_seq_step8_workspace(const lattice_seq_attn_desc* d, int32_t batch) {
+  if (check_attn(d) != LATTICE_OK || batch <= 0 || (int64_t)d->window + d->sinks > MAX_ROWS) return 0;
+  return seq_step8_workspace(batch, d->heads, d->kv_heads, d->head_dim, d->sinks + d->window);
+}
+
+lattice_status lattice_seq_step8(const lattice_seq_attn_desc* d, const lattice_qk_rope_desc* rope, int32_t batch,
+                                 const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                                 int64_t v_stride, const int32_t* lens, const int32_t* cache_index,
+                                 const lattice_seq_cache8* cache, void* out, int64_t out_stride, void* ws,
+                                 size_t ws_bytes, void* stream) {
+  TRY(check_step(d, rope, batch));
+  TRY(check_cache8(d, cache));
+  if (batch == 0 || cache->num_caches == 0) return LATTICE_OK;
+  SeqStepArgs a;
+  RopeTurns t{};
+  TRY(step_args(d, rope, batch, q, q_stride, k, k_stride, v, v_stride, lens, out, out_stride, &a, &t));
+  const size_t need = seq_step8_workspace(batch, d->heads, d->kv_heads, d->head_dim, d->sinks + d->window);
+  if (need > 0 && (!ws || ws_bytes < need)) FAIL(LATTICE_ERR_WORKSPACE, "workspace %zu < %zu", ws_bytes, need);
+  if (need > 0) REQUIRE((uintptr_t)ws % 4 == 0, "workspace is not 4-byte aligned");
+  HIPRET(seq_step8(a, cache8_args(d, cache, cache_index), t, ws, strm(stream)));
   return LATTICE_OK;
 }
 
