@@ -19,6 +19,7 @@
 // so that the backward differentiates what the forward computed.
 #include "e4m3.h"
 #include "kernels.h"
+#include "lanes.h"
 #include "norm.h"
 #include "row8.h"
 
@@ -51,9 +52,7 @@ struct NormK {
 template <typename C, typename V, int N, typename F>
 __device__ inline void row_join(V (&v)[N], F f, V* red, int& turn) {
 #pragma unroll
-  for (int o = C::LPR / 2; o > 0; o >>= 1)
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = f(v[i], __shfl_xor(v[i], o, 64));
+  for (int i = 0; i < N; ++i) v[i] = lanes_join<C::LPR>(v[i], f);
   if constexpr (C::WPR > 1) {
     V* p = red + turn * N * C::WPR;
     turn ^= 1;
@@ -82,15 +81,15 @@ template <typename C> struct RowAt {
   }
 };
 
-template <typename C>
+template <typename C, bool TAIL>
 __device__ inline void load_gain(const NormK& A, int lane, float (&g)[C::CH][8]) {
+  Row8<float> r[C::CH];
 #pragma unroll
-  for (int i = 0; i < C::CH; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int c = 8 * (lane + i * C::STEP) + e;
-      g[i][e] = A.gain ? A.gain[c < A.cols ? c : A.cols - 1] : 1.f;
-    }
+  for (int i = 0; i < C::CH; ++i) {
+    if (A.gain) r[i] = load8<float, TAIL>(A.gain, lane + i * C::STEP, A.cols);
+    else r[i].w[0] = r[i].w[1] = u32x4{0x3f800000u, 0x3f800000u, 0x3f800000u, 0x3f800000u};
+    r[i].get(g[i]);
+  }
 }
 
 template <typename T>
@@ -105,7 +104,7 @@ __global__ __launch_bounds__(C::THREADS) void add_rmsnorm_fwd_kernel(NormK A) {
   const RowAt<C> at;
   const DropKey key = drop_key(A.drop);
   float gain[C::CH][8];
-  load_gain<C>(A, at.lane, gain);
+  load_gain<C, TAIL>(A, at.lane, gain);
   const int64_t step = (int64_t)gridDim.x * C::RPB;
   Row8<T> xr[C::CH], rr[C::CH];
   auto fetch = [&](int64_t base) {
@@ -142,7 +141,7 @@ __global__ __launch_bounds__(C::THREADS) void add_rmsnorm_fwd_kernel(NormK A) {
     for (int i = 0; i < C::CH; ++i)
 #pragma unroll
       for (int e = 0; e < 8; ++e) s[0] += h[i][e] * h[i][e];
-    row_join<C>(s, [](float a, float b) { return a + b; }, red, turn);
+    row_join<C>(s, Add(), red, turn);
     const float rho = 1.f / sqrtf(s[0] * A.inv_cols + A.eps);
     uint32_t top[1] = {0u};                        // of |y|, in its bits: NaN is above all
 #pragma unroll
@@ -159,7 +158,7 @@ __global__ __launch_bounds__(C::THREADS) void add_rmsnorm_fwd_kernel(NormK A) {
       }
     }
     if (!A.q) continue;
-    row_join<C>(top, [](uint32_t a, uint32_t b) { return max(a, b); }, red_top, turn_top);
+    row_join<C>(top, Max(), red_top, turn_top);
     // a row that is not finite says so: NaN scale and codes
     const float amax = __uint_as_float(top[0]);
     const bool bad = !(s[0] < INFINITY) || !(amax < INFINITY);
@@ -191,7 +190,7 @@ __global__ __launch_bounds__(C::THREADS) void add_rmsnorm_bwd_kernel(NormK A) {
   const RowAt<C> at;
   const DropKey key = drop_key(A.drop);
   float gain[C::CH][8], dg[C::CH][8];
-  load_gain<C>(A, at.lane, gain);
+  load_gain<C, TAIL>(A, at.lane, gain);
 #pragma unroll
   for (int i = 0; i < C::CH; ++i)
 #pragma unroll
@@ -228,7 +227,7 @@ __global__ __launch_bounds__(C::THREADS) void add_rmsnorm_bwd_kernel(NormK A) {
       }
     }
     if (base + step < A.rows) fetch(base + step);
-    row_join<C>(s, [](float a, float b) { return a + b; }, red, turn);
+    row_join<C>(s, Add(), red, turn);
     const float rho = 1.f / sqrtf(s[0] * A.inv_cols + A.eps);
     const float c = rho * rho * s[1] * A.inv_cols;             // mean(dn n) rho
 #pragma unroll
@@ -294,6 +293,7 @@ __global__ __launch_bounds__(1024) void norm_dgain_kernel(const float* __restric
   const int x = threadIdx.x & 15, y = threadIdx.x >> 4, c = blockIdx.x * 16 + x;
   float v = 0.f;
   if (c < cols)
+#pragma unroll 8
     for (int i = y; i < n; i += 64) v += part[(int64_t)i * cols + c];
   sum[y][x] = v;
   __syncthreads();
@@ -313,9 +313,9 @@ static auto with_cfg(int cols, F f) {
   if (g <= 32) return f(RowCfg<32, 1, 1>());
   if (g <= 64) return f(RowCfg<64, 1, 1>());
   if (g <= 128) return f(RowCfg<64, 2, 1>());
-  if (g <= 256) return f(RowCfg<64, 4, 1>());
+  if (g <= 256) return f(RowCfg<64, 2, 2>());
   if (g <= 512) return f(RowCfg<64, 2, 4>());
-  if (g <= 1024) return f(RowCfg<64, 4, 4>());
+  if (g <= 1024) return f(RowCfg<64, 2, 8>());
   return f(RowCfg<64, 4, 8>());
 }
 
@@ -325,7 +325,7 @@ static int norm_blocks(int64_t rows, int most) {
   const int64_t n = cdiv(rows, C::RPB), cap = most / (C::THREADS / 64);
   return (int)(n < cap ? n : cap);
 }
-constexpr int NORM_FWD_WAVES = 8192, NORM_BWD_WAVES = 4096;
+constexpr int NORM_FWD_WAVES = 4096, NORM_BWD_WAVES = 2048;
 
 static NormK norm_k(const NormArgs& a) {
   NormK A{};

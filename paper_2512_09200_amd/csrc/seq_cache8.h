@@ -9,6 +9,7 @@
 // large neighbour sets the scale.
 #pragma once
 #include "e4m3.h"
+#include "lanes.h"
 #include "seq_tile.h"
 
 namespace lat {
@@ -49,68 +50,76 @@ __device__ inline uint32_t cache8_codes(const float* x, float s) {
 }
 
 // A wave's view of a block: lane l holds slot l / 4, elements (l % 4) E .. + E - 1
-// of a row padded to DP.
-template <int DP> struct Block8 {
-  static constexpr int E = DP / 4, W = E / 4;        // elements, code words
-  float x[E];
+// of a row padded to DP, as the memory words of a fresh row (of T) or of old codes.
+// Values are decoded where they are used, eight at a time: once for the scale,
+// once for the codes.
+template <typename T, int DP> struct Block8 {
+  static constexpr int E = DP / 4, C = E / 8;        // elements, chunks of eight
+  Frag<T> row[C];
+  u32x2 code[C];
+  bool fresh, old;
+  float s0;
+
   __device__ static inline int slot() { return (threadIdx.x & 63) >> 2; }
   __device__ static inline int first() { return (threadIdx.x & 3) * E; }
 
-  // rows of the storage type; p: the row's first element (valid memory whether `on` or not)
-  template <typename T>
-  __device__ inline void from_row(const T* p, int dim, bool on) {
+  // p: the row's first element, valid memory in any case
+  __device__ inline void load_row(const T* p, int dim, bool on) {
+    fresh = on;
 #pragma unroll
-    for (int i = 0; i < E; i += 8) {
-      const int d = first() + i;
-      const bool ok = on && d < dim;
-      Frag<T> f;
-      load_frag(p + (d < dim ? d : 0), ok, f);
-      float y[8];
-      if constexpr (sizeof(T) == 2) {
-        Vec16<bf16_t>::unpack(__builtin_bit_cast(u32x4, f.v), y);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = f.v[e];
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[i + e] = y[e];
+    for (int i = 0; i < C; ++i) {
+      const int d = first() + 8 * i;
+      load_frag(p + (d < dim ? d : 0), on && d < dim, row[i]);
     }
   }
-  // codes of a row (ld bytes); adds to x where `on`, which the caller cleared
-  __device__ inline void from_codes(const uint8_t* p, float s, int dim, int ld, bool on) {
+  // p: a row of ld bytes, valid memory in any case
+  __device__ inline void load_codes(const uint8_t* p, int ld) {
 #pragma unroll
-    for (int i = 0; i < E; i += 8) {
-      const int d = first() + i;
-      const u32x2 w = *reinterpret_cast<const u32x2*>(p + (d < ld ? d : 0));
-      const bool ok = on && d < dim;
+    for (int i = 0; i < C; ++i) {
+      const int d = first() + 8 * i;
+      code[i] = *reinterpret_cast<const u32x2*>(p + (d < ld ? d : 0));
+    }
+  }
+  __device__ inline void chunk(int i, int dim, float (&x)[8]) const {
+    if constexpr (sizeof(T) == 2) {
+      Vec16<bf16_t>::unpack(__builtin_bit_cast(u32x4, row[i].v), x);
+    } else {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const f32x2_t a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[j], false);
-        const f32x2_t b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[j], true);
-        const float y[4] = {a[0] * s, a[1] * s, b[0] * s, b[1] * s};
+      for (int e = 0; e < 8; ++e) x[e] = row[i].v[e];
+    }
+    const bool on = old && first() + 8 * i < dim;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[i + 4 * j + e] = ok ? y[e] : x[i + 4 * j + e];
-      }
+    for (int j = 0; j < 4; ++j) {
+      const f32x2_t a = j & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)code[i][j >> 1], true)
+                              : __builtin_amdgcn_cvt_pk_f32_fp8((int)code[i][j >> 1], false);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) x[2 * j + e] = fresh ? x[2 * j + e] : on ? a[e] * s0 : 0.f;
     }
   }
   // the wave's scale
-  __device__ inline float scale() const {
+  __device__ inline float scale(int dim) const {
     float top = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) top = fmaxf(top, nonfinite(x[e]) ? 0.f : fabsf(x[e]));
+    for (int i = 0; i < C; ++i) {
+      float x[8];
+      chunk(i, dim, x);
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-    return cache8_scale(top);
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, nonfinite(x[e]) ? 0.f : fabsf(x[e]));
+    }
+    return cache8_scale(lanes_join<64>(top, Max()));
   }
-  __device__ inline void codes(float s, uint32_t (&w)[W]) const {
+  // Codes under scale s to p (a row of ld bytes) where `write`, and to q (DP bytes)
+  // where it is not null.
+  __device__ inline void encode(float s, int dim, uint8_t* p, int ld, bool write, uint8_t* q) const {
 #pragma unroll
-    for (int i = 0; i < W; ++i) w[i] = cache8_codes(x + 4 * i, s);
-  }
-  // a row's codes to memory, `ld` bytes of it
-  __device__ static inline void store(uint8_t* p, int ld, const uint32_t (&w)[W]) {
-#pragma unroll
-    for (int i = 0; i < W; i += 2)
-      if (first() + 4 * i < ld) *reinterpret_cast<u32x2*>(p + first() + 4 * i) = u32x2{w[i], w[i + 1]};
+    for (int i = 0; i < C; ++i) {
+      float x[8];
+      chunk(i, dim, x);
+      const u32x2 w{cache8_codes(x, s), cache8_codes(x + 4, s)};
+      const int d = first() + 8 * i;
+      if (write && d < ld) *reinterpret_cast<u32x2*>(p + d) = w;
+      if (q) *reinterpret_cast<u32x2*>(q + d) = w;
+    }
   }
 };
 

@@ -4,7 +4,7 @@
 //
 // Memory bound: every visible slot's two rows of codes are read once, half the
 // bytes of bf16.  Work is split as in the bf16 step: a block is a user, a key head
-// and a split of the slots, its four waves take tiles of 64 slots in turn with
+// and a split of the slots, its four waves take tiles of 32 slots in turn with
 // their own running maximum, sum and output.  Codes become bf16 in registers
 // (exactly: three bits of fraction) and go to 16x16x32 matrix instructions; a
 // block's scale multiplies the 16 scores of its slots and their probabilities.
@@ -14,26 +14,30 @@
 // Keys are fragments straight from memory.  Values are loaded to registers, go
 // through the wave's own LDS rows and come back transposed, eight codes of one
 // dimension a lane: a direct load to LDS would have the compiler wait for the
-// next tile's loads before the first transposed read.
+// next tile's loads before the first transposed read.  The query's parts lie in LDS
+// as fragments, one read of each a tile, so that sixteen waves fit a compute unit.
 //
 // The new event may change its block's scale, and with it the codes of the block's
 // other slots.  The split that holds the slot makes the block anew before its
-// tiles (one wave for k, one for v), writes it, and puts a copy into LDS that
+// tiles (wave 0 its keys, wave 1 its values), writes it, and puts a copy into LDS that
 // replaces what the tiles load of it; no other block of the launch reads these
-// slots.  More than 16 query heads on a key head are taken in turn by the same
-// block for the same reason.
+// slots.  Query heads above 16 on a key head are taken by a second launch, which
+// finds the block as it is now, for the same reason.
 #include "kernels.h"
+#include "lanes.h"
 #include "seq_cache8.h"
 #include "seq_rope.h"
 #include "seq_step.h"
 
 namespace lat {
 
-constexpr int STEP8_TILE = 64;               // slots of a wave's tile
+constexpr int STEP8_TILE = 32;               // slots of a wave's tile
 
 struct Step8K {
   SeqCache8Args c;
   int heads, group, cap, ld, nb;             // bytes of a slot, blocks of a cache and head
+  int work;                                  // bytes of LDS for tiles and join
+  int hg0, hgs, append;                      // this launch's groups of 16 query heads; whether it brings the events
   float eps, inv_dim;
   int rope, rotary, inter;
   SeqTensor q, k, v;
@@ -83,30 +87,36 @@ template <int DP> struct Tile8 {
   __device__ static inline int at(int row, int unit) { return row * DP + ((unit ^ swz(row)) << 4); }
 };
 
+// LDS: the waves' value tiles, over them the join of the waves (`heads` of 16 head
+// columns); the query's fragments; the new k and v; the block's codes, k then v,
+// and its scales.
 template <typename T, int DP> struct Step8Cfg {
   static constexpr int PARTS = sizeof(T) == 2 ? 2 : 3;
-  static constexpr int JOIN = 4 * STEP_HEADS * (DP + 4) * 4, VT = 4 * Tile8<DP>::BYTES;
-  static constexpr int WORK = JOIN > VT ? JOIN : VT;                  // tiles, then the join of the waves
-  static constexpr int QN = WORK, KN = QN + STEP_HEADS * DP * 4;      // q rows; new k, v; all fp32
-  static constexpr int COPY = KN + 2 * DP * 4;                        // the block's codes, k then v
-  static constexpr int SC = COPY + 2 * CACHE8_BLOCK * DP;             // its scales
-  static constexpr size_t LDS = SC + 16;
+  static constexpr int JROW = DP + 4, VT = 4 * Tile8<DP>::BYTES;
+  static constexpr int QF = DP / 32 * PARTS * 1024;
+  static constexpr int KN = QF, COPY = KN + 2 * DP * 4, SC = COPY + 2 * CACHE8_BLOCK * DP, REST = SC + 16;
+  __host__ __device__ static constexpr int work(int heads) {
+    return 16 * heads * JROW > VT ? 16 * heads * JROW : VT;
+  }
 };
 
 template <typename T, int DP>
-__global__ __launch_bounds__(256, 2) void seq_step8_kernel(Step8K A, RopeTurns turns) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 2 : 3) void seq_step8_kernel(Step8K A, RopeTurns turns) {
   using Cfg = Step8Cfg<T, DP>;
   using TL = Tile8<DP>;
-  using B8 = Block8<DP>;
+  using B8 = Block8<float, DP>;
   constexpr int NP = Cfg::PARTS, KS = DP / 32, OB = DP / 16, KV = DP == 128 ? 2 : 1, UPR = TL::UPR;
+  constexpr int R = STEP8_TILE / CACHE8_BLOCK, VL = R * UPR / 4;     // scale blocks of a tile, value loads of a lane
   typedef typename std::conditional<DP == 32, u32x2, u32x4>::type KVec;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g16 = lane >> 4, l16 = lane & 15, D = A.c.dim, ns = A.j.ns;
   int blk = blockIdx.x;
   const int u = blk % ns; blk /= ns;
+  const int hg = A.hg0 + blk % A.hgs; blk /= A.hgs;
   const int kv = blk % A.c.kv_heads, b = blk / A.c.kv_heads;
-  const int p = A.j.lens[b], ci = A.c.index ? A.c.index[b] : b;
+  const int p = __builtin_amdgcn_readfirstlane(A.j.lens[b]);
+  const int ci = __builtin_amdgcn_readfirstlane(A.c.index ? A.c.index[b] : b);
   if (p < 0 || ci < 0 || ci >= A.c.num_caches) return;
   const int n = min(p, A.cap - 1) + 1, slot = seq_slot(p, A.c.sinks, A.c.window);
   // the split's slots, whole rounds of the four waves
@@ -118,259 +128,288 @@ __global__ __launch_bounds__(256, 2) void seq_step8_kernel(Step8K A, RopeTurns t
   uint8_t* const vc = A.c.vc + head * A.cap * A.ld;
   float* const ks = A.c.ks + head * A.nb;
   float* const vs = A.c.vs + head * A.nb;
-  float* const qn = reinterpret_cast<float*>(smem + Cfg::QN);         // [16][DP]
-  float* const kn = reinterpret_cast<float*>(smem + Cfg::KN);         // k, v
-  char* const copy = smem + Cfg::COPY;
-  float* const sc = reinterpret_cast<float*>(smem + Cfg::SC);
+  char* const rest = smem + A.work;
+  float* const kn = reinterpret_cast<float*>(rest + Cfg::KN);         // k, v
+  char* const copy = rest + Cfg::COPY;
+  float* const sc = reinterpret_cast<float*>(rest + Cfg::SC);
   char* const VS = smem + w * TL::BYTES;
 
+  // The event's block: made anew by waves 0 (keys) and 1 (values) of the split that
+  // holds the slot (in a launch for further query heads it has been)
+  const bool owner = A.append && slot >= a0 && slot < a1;
+  const int sb = slot & ~(CACHE8_BLOCK - 1);
+  const bool remake = owner && w < 2;
+  B8 x8;
+  if (remake) {
+    x8.load_codes((w == 0 ? kc : vc) + (int64_t)min(sb + B8::slot(), n - 1) * A.ld, A.ld);
+    x8.s0 = (w == 0 ? ks : vs)[sb / CACHE8_BLOCK];
+  }
+  // the event's own vectors, a row a wave: pairs (x0, y0) of dimensions
+  const int np = A.rotary >> 1, nh = min(STEP_HEADS, A.group - hg * STEP_HEADS), h0 = kv * A.group + hg * STEP_HEADS;
+  const bool rot = lane < np;
+  int x0, y0;
+  if (A.inter || !rot) { x0 = 2 * lane; y0 = x0 + 1; } else { x0 = lane; y0 = np + lane; }
+  const bool on = x0 < D;
+  const int xl = on ? x0 : 0, yl = on ? y0 : 0;      // (loads are made by every lane, in no branch)
+  auto row_of = [&](const SeqTensor& t, int h, float& x, float& y) {
+    const T* src = (const T*)t.p + (int64_t)b * t.ld + h * D;
+    x = ld(src + xl);
+    y = ld(src + yl);
+  };
+  const int first_q = (w + 2) & 3;                   // query rows: waves 2 and 3 first
+  float qx, qy, ex = 0.f, ey = 0.f, gqx = 1.f, gqy = 1.f, gkx = 1.f, gky = 1.f;
+  row_of(A.q, h0 + min(first_q, nh - 1), qx, qy);
+  if (remake) row_of(w == 0 ? A.k : A.v, kv, ex, ey);
+  if (A.gq) { gqx = A.gq[xl]; gqy = A.gq[yl]; }
+  if (A.gk) { gkx = A.gk[xl]; gky = A.gk[yl]; }
+  const int pos = A.pos ? A.pos[b] : p;
+
   // a lane's share of a tile: keys (slot 16 r + l16), values, the blocks' scales
-  struct Load { KVec k[4 * KV]; u32x4 v[UPR]; float ks, vs; };
-  Load L;
+  // (lanes 0 .. R - 1 of every 2 R the keys', the others the values')
+  KVec lk[R * KV];
+  u32x4 lv[VL];
+  float ls;
   const int tiles = a1 > a0 ? (a1 - a0 + STEP8_TILE - 1) / STEP8_TILE : 0;
-  auto issue = [&](int t) {
+  auto issue_v = [&](int t) {
     const int j0 = a0 + t * STEP8_TILE, nk = min(STEP8_TILE, a1 - j0);
-    const uint8_t* kp = kc + (int64_t)j0 * A.ld;
     const uint8_t* vp = vc + (int64_t)j0 * A.ld;
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int i = 0; i < VL; ++i) {
+      const int x = i * 64 + lane, row = min(x / UPR, nk - 1), c = 16 * (x % UPR);
+      lv[i] = *reinterpret_cast<const u32x4*>(vp + (__umul24(row, A.ld) + (c < A.ld ? c : 0)));
+    }
+  };
+  auto issue_k = [&](int t) {
+    const int j0 = a0 + t * STEP8_TILE, nk = min(STEP8_TILE, a1 - j0);
+    const uint8_t* kp = kc + (int64_t)j0 * A.ld;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int i = 0; i < KV; ++i) {
         const int row = min(16 * r + l16, nk - 1), d = DP == 32 ? 8 * g16 : 64 * i + 16 * g16;
-        L.k[r * KV + i] = *reinterpret_cast<const KVec*>(kp + row * A.ld + (d < A.ld ? d : 0));
+        lk[r * KV + i] = *reinterpret_cast<const KVec*>(kp + (__umul24(row, A.ld) + (d < A.ld ? d : 0)));
       }
-#pragma unroll
-    for (int i = 0; i < UPR; ++i) {
-      const int x = i * 64 + lane, row = min(x / UPR, nk - 1), c = 16 * (x % UPR);
-      L.v[i] = *reinterpret_cast<const u32x4*>(vp + row * A.ld + (c < A.ld ? c : 0));
-    }
-    const int at = min(j0 / CACHE8_BLOCK + (lane & 3), (n - 1) / CACHE8_BLOCK);
-    L.ks = ks[at];
-    L.vs = vs[at];
+    ls = (lane & R ? vs : ks)[min(j0 / CACHE8_BLOCK + (lane & (R - 1)), (n - 1) / CACHE8_BLOCK)];
   };
 
-  const bool owner = slot >= a0 && slot < a1;
-  const int sb = slot & ~(CACHE8_BLOCK - 1);         // the first slot of the event's block
-  const int hgs = (A.group + STEP_HEADS - 1) / STEP_HEADS;
-#pragma unroll 1
-  for (int hg = 0; hg < hgs; ++hg) {
-    const int nh = min(STEP_HEADS, A.group - hg * STEP_HEADS), h0 = kv * A.group + hg * STEP_HEADS;
-    if (hg > 0) __syncthreads();                     // the join's reads of LDS
-    if (w < tiles) issue(w);
+  if (w < tiles) {
+    issue_v(w);
+    issue_k(w);
+  }
 
-    // the event's own vectors: rows of qn (zeros past the heads), kn, vn
-    {
-      const int np = A.rotary >> 1;
-      const bool rot = lane < np;
-      int x, y;
-      if (A.inter || !rot) { x = 2 * lane; y = x + 1; } else { x = lane; y = np + lane; }
-      const bool on = x < D;
-      const int pos = A.pos ? A.pos[b] : p;
-      float2 cs{1.f, 0.f};
-      if (A.rope && rot) cs = rope_cs(pos, turns.f[lane]);
-      for (int r = w; r < (hg == 0 ? STEP_HEADS + 2 : STEP_HEADS); r += 4) {
-        const bool isq = r < STEP_HEADS, live = !isq || r < nh;
-        const T* src = isq ? (const T*)A.q.p + (int64_t)b * A.q.ld + (h0 + min(r, nh - 1)) * D
-                     : r == STEP_HEADS ? (const T*)A.k.p + (int64_t)b * A.k.ld + kv * D
-                                       : (const T*)A.v.p + (int64_t)b * A.v.ld + kv * D;
-        float zx = on ? ld(src + x) : 0.f, zy = on ? ld(src + y) : 0.f;
-        if (sizeof(T) == 4 && A.rope && r == STEP_HEADS) {
-          // An fp32 key is rounded to eight bits next; its norm and rotation are
-          // taken in 64, so that which code it gets does not hang on the order of
-          // a sum (one row a user: no time is seen).
-          const double dx = zx, dy = zy;
-          const double rr = 1.0 / sqrt(wave_sum(dx * dx + dy * dy) / D + (double)A.eps);
-          const double ux = dx * rr * (A.gk && on ? A.gk[x] : 1.f), uy = dy * rr * (A.gk && on ? A.gk[y] : 1.f);
-          double c = 1.0, s = 0.0;
-          if (rot) {
-            const double t = (double)pos * turns.f[lane];
-            sincospi(2.0 * (t - rint(t)), &s, &c);
-          }
-          zx = (float)(ux * c - uy * s);
-          zy = (float)(ux * s + uy * c);
-        } else if (A.rope && r <= STEP_HEADS) {
-          const float rr = 1.f / sqrtf(wave_sum(zx * zx + zy * zy) * A.inv_dim + A.eps);
-          const float* g = isq ? A.gq : A.gk;
-          zx *= rr * (g && on ? g[x] : 1.f);
-          zy *= rr * (g && on ? g[y] : 1.f);
-          const float tx = zx * cs.x - zy * cs.y, ty = zx * cs.y + zy * cs.x;
-          zx = tx;
-          zy = ty;
+  float2 cs{1.f, 0.f};
+  if (A.rope && rot) cs = rope_cs(pos, turns.f[lane]);
+  auto norm_rope = [&](float& zx, float& zy, float gx, float gy) {
+    const float rr = 1.f / sqrtf(lanes_join<64>(zx * zx + zy * zy, Add()) * A.inv_dim + A.eps);
+    zx *= rr * gx;
+    zy *= rr * gy;
+    const float tx = zx * cs.x - zy * cs.y, ty = zx * cs.y + zy * cs.x;
+    zx = tx;
+    zy = ty;
+  };
+  if (remake) {
+    if (!on) ex = ey = 0.f;
+    if (A.rope && w == 0) {
+      if constexpr (sizeof(T) == 4) {
+        // An fp32 key is rounded to eight bits next; its norm and rotation are
+        // taken in 64, so that which code it gets does not hang on the order of
+        // a sum (one row a user).
+        const double dx = ex, dy = ey, rr = 1.0 / sqrt(wave_sum(dx * dx + dy * dy) / D + (double)A.eps);
+        const double ux = dx * rr * gkx, uy = dy * rr * gky;
+        double c = 1.0, s = 0.0;
+        if (rot) {
+          const double t = (double)pos * turns.f[lane];
+          sincospi(2.0 * (t - rint(t)), &s, &c);
         }
-        zx = live && on ? zx : 0.f;
-        zy = live && on ? zy : 0.f;
-        if (x < DP) {
-          float* dst = isq ? qn + r * DP : kn + (r - STEP_HEADS) * DP;
-          dst[x] = isq ? zx : ld_round<T>(zx);
-          dst[y] = isq ? zy : ld_round<T>(zy);
-        }
+        ex = (float)(ux * c - uy * s);
+        ey = (float)(ux * s + uy * c);
+      } else {
+        norm_rope(ex, ey, gkx, gky);
       }
     }
-    __syncthreads();
-    if (hg == 0 && owner && w < 2) {
-      // the event's block anew: wave 0 its keys, wave 1 its values
-      uint8_t* const c = w == 0 ? kc : vc;
-      float* const s = (w == 0 ? ks : vs) + sb / CACHE8_BLOCK;
-      const int row = sb + B8::slot();
-      const bool mine = row == slot, old = !mine && row < n;
-      const float s0 = *s;
-      B8 x;
-      x.from_row(kn + w * DP, DP, mine);
-      x.from_codes(c + (int64_t)min(row, n - 1) * A.ld, s0, D, A.ld, old);
-      const float s1 = x.scale();
-      uint32_t code[B8::W];
-      x.codes(s1, code);
-      if (mine || (old && s1 != s0)) B8::store(c + (int64_t)row * A.ld, A.ld, code);
-      if (lane == 0) {
-        *s = s1;
-        sc[w] = s1;
-      }
-      B8::store(reinterpret_cast<uint8_t*>(copy) + (w * CACHE8_BLOCK + B8::slot()) * DP, DP, code);
+    if (x0 < DP) {
+      kn[w * DP + x0] = on ? ld_round<T>(ex) : 0.f;
+      kn[w * DP + y0] = on ? ld_round<T>(ey) : 0.f;
     }
-    __syncthreads();
-    Bf16Parts<NP> qf[KS];
-#pragma unroll
-    for (int i = 0; i < KS; ++i) {
-      Frag<float> f;
-      load_frag(qn + l16 * DP + (DP == 32 ? 8 * g16 : 64 * (i >> 1) + 16 * g16 + 8 * (i & 1)), true, f);
-      split(f.v, qf[i]);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the wave reads what its other lanes have just written
+    const int row = sb + B8::slot();
+    x8.load_row(kn + w * DP, DP, row == slot);
+    x8.old = row != slot && row < n;
+    const float s1 = x8.scale(D);
+    x8.encode(s1, D, (w == 0 ? kc : vc) + (int64_t)row * A.ld, A.ld, x8.fresh || (x8.old && s1 != x8.s0),
+              reinterpret_cast<uint8_t*>(copy) + (w * CACHE8_BLOCK + B8::slot()) * DP);
+    if (lane == 0) {
+      (w == 0 ? ks : vs)[sb / CACHE8_BLOCK] = s1;
+      sc[w] = s1;
     }
-
-    const float c = A.j.scale * STEP_LOG2E;
-    f32x4 o[OB];
+  }
+  // The query's parts: those of element d of row r are element e of lane 16 g + r in
+  // the fragment of step i, (i, g, e) as the keys' loads have them.
+  for (int r = first_q; r < STEP_HEADS; r += 4) {
+    float zx = qx, zy = qy;
+    if (r + 4 < nh) row_of(A.q, h0 + r + 4, qx, qy);
+    if (!on || r >= nh) zx = zy = 0.f;
+    if (A.rope && r < nh) norm_rope(zx, zy, gqx, gqy);
+    auto put = [&](int d, float z) {
+      const int i = DP == 32 ? 0 : 2 * (d >> 6) + ((d >> 3) & 1), g = DP == 32 ? d >> 3 : (d >> 4) & 3, e = d & 7;
 #pragma unroll
-    for (int i = 0; i < OB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;
-    auto tile = [&](int t) {
-      const int j0 = a0 + t * STEP8_TILE, nk = min(STEP8_TILE, a1 - j0);
-      const int nr = owner && sb >= j0 && sb < j0 + STEP8_TILE ? (sb - j0) / CACHE8_BLOCK : -1;   // the event's block here
-      // values to the wave's LDS rows; slots that are not there are zeros
-#pragma unroll
-      for (int i = 0; i < UPR; ++i) {
-        const int x = i * 64 + lane, row = x / UPR;
-        u32x4 v = L.v[i];
-        if (row >= nk) v = u32x4{0u, 0u, 0u, 0u};
-        *reinterpret_cast<u32x4*>(VS + TL::at(row, x % UPR)) = v;
-      }
-      if (nr >= 0)
-        for (int x = lane; x < CACHE8_BLOCK * UPR; x += 64)
-          *reinterpret_cast<u32x4*>(VS + TL::at(CACHE8_BLOCK * nr + x / UPR, x % UPR)) =
-              *reinterpret_cast<const u32x4*>(copy + CACHE8_BLOCK * DP + 16 * x);
-      float x[16], pv[4], tm = -INFINITY;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        f32x4 s{0.f, 0.f, 0.f, 0.f};
-        float kscale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(L.ks), r));
-        // (behind the last slot: weights 0 under a scale that may be anything)
-        pv[r] = 16 * r < nk ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(L.vs), r)) : 0.f;
-        if (r == nr) {
-          kscale = sc[0];
-          pv[r] = sc[1];
-        }
-#pragma unroll
-        for (int i = 0; i < KV; ++i) {
-          KVec kw = L.k[r * KV + i];
-          const int d = DP == 32 ? 8 * g16 : 64 * i + 16 * g16;
-          if (r == nr) kw = *reinterpret_cast<const KVec*>(copy + l16 * DP + d);
-#pragma unroll
-          for (int h = 0; h < (DP == 32 ? 1 : 2); ++h) {
-            u32x2 w8{kw[2 * h], kw[2 * h + 1]};
-            if (d + 8 * h >= D) w8 = u32x2{0u, 0u};
-            const Frag<bf16_t> f = decode(w8);
-            const Bf16Parts<NP>& q = qf[DP == 32 ? 0 : 2 * i + h];
-#pragma unroll
-            for (int y = NP - 1; y >= 0; --y) mma16(f, q.p[y], s);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x[4 * r + i] = 16 * r + 4 * g16 + i < nk ? s[i] * kscale : -INFINITY;
-          tm = fmaxf(tm, x[4 * r + i]);
-        }
-      }
-      if (t + 4 < tiles) issue(t + 4);                     // into the registers that are free now
-      tm = fmaxf(tm, __shfl_xor(tm, 16, 64));
-      tm = fmaxf(tm, __shfl_xor(tm, 32, 64));
-      const bool up = (tm - m) * c > 8.f;                  // as in the batch's forward
-      if (wave_any(up)) {
-        const float mn = up ? tm : m, f = up ? __builtin_amdgcn_exp2f((m - mn) * c) : 1.f;
-        l *= f;
-#pragma unroll
-        for (int i = 0; i < OB; ++i)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) o[i][r] *= f;
-        m = mn;
-      }
-      const float mc = m == -INFINITY ? 0.f : m * c;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], c, -mc));
-        l += x[e];
-        x[e] *= pv[e >> 2];
-      }
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        Bf16Parts<NP> pf;
-        split(x + 8 * h, pf);
-        // lane's piece of the transposed read: row 32 h + 16 (e / 4) + 4 g16 + e % 4, e = l16 / 2
-        const int e = l16 >> 1, row = 32 * h + 16 * (e >> 2) + 4 * g16 + (e & 3);
-#pragma unroll
-        for (int i = 0; i < OB; ++i) {
-          typedef int i32x2 __attribute__((ext_vector_type(2)));
-          typedef __attribute__((address_space(3))) i32x2 lds_v2;
-          const i32x2 w8 = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2*)(VS + TL::at(row, i) + 8 * (l16 & 1)));
-          const Frag<bf16_t> f = decode(u32x2{(uint32_t)w8[0], (uint32_t)w8[1]});
-#pragma unroll
-          for (int y = NP - 1; y >= 0; --y) mma16(f, pf.p[y], o[i]);
-        }
+      for (int y = 0; y < NP; ++y) {
+        const bf16_t h = f2bf(z);
+        *reinterpret_cast<bf16_t*>(rest + ((i * NP + y) * 64 + 16 * g + r) * 16 + 2 * e) = h;
+        z -= bf2f(h);
       }
     };
+    if (x0 < DP) {
+      put(x0, zx);
+      put(y0, zy);
+    }
+  }
+  __syncthreads();
+
+  const float c = A.j.scale * STEP_LOG2E;
+  f32x4 o[OB];
+#pragma unroll
+  for (int i = 0; i < OB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
 #pragma unroll 1
-    for (int t = w; t < tiles; t += 4) tile(t);
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
-    // join of the waves: O[w][head][DP], then m and l
-    float* const J = reinterpret_cast<float*>(smem);
-    __syncthreads();
-    float* const Jw = J + (w * STEP_HEADS + l16) * (DP + 4);
+  for (int t = w; t < tiles; t += 4) {
+    const int j0 = a0 + t * STEP8_TILE, nk = min(STEP8_TILE, a1 - j0);
+    const int nr = owner && sb >= j0 && sb < j0 + STEP8_TILE ? (sb - j0) / CACHE8_BLOCK : -1;   // the event's block here
+    // values to the wave's LDS rows; slots that are not there are zeros
+#pragma unroll
+    for (int i = 0; i < VL; ++i) {
+      const int x = i * 64 + lane, row = x / UPR;
+      u32x4 v = lv[i];
+      if (row >= nk) v = u32x4{0u, 0u, 0u, 0u};
+      *reinterpret_cast<u32x4*>(VS + TL::at(row, x % UPR)) = v;
+    }
+    if (nr >= 0) {
+      for (int x = lane; x < CACHE8_BLOCK * UPR; x += 64)
+        *reinterpret_cast<u32x4*>(VS + TL::at(CACHE8_BLOCK * nr + x / UPR, x % UPR)) =
+            *reinterpret_cast<const u32x4*>(copy + CACHE8_BLOCK * DP + 16 * x);
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        if (r == nr)
+#pragma unroll
+          for (int i = 0; i < KV; ++i)
+            lk[r * KV + i] = *reinterpret_cast<const KVec*>(copy + l16 * DP + (DP == 32 ? 8 * g16 : 64 * i + 16 * g16));
+    }
+    if (t + 4 < tiles) issue_v(t + 4);                   // into the registers that are free now
+    f32x4 s[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) s[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      Frag<bf16_t> q[NP];
+#pragma unroll
+      for (int y = 0; y < NP; ++y) q[y].v = *reinterpret_cast<const bf16x8*>(rest + ((i * NP + y) * 64 + lane) * 16);
+      const int d = DP == 32 ? 8 * g16 : 64 * (i >> 1) + 16 * g16 + 8 * (i & 1);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const KVec& kw = lk[r * KV + (i >> 1)];
+        u32x2 w8{kw[2 * (i & 1)], kw[2 * (i & 1) + 1]};
+        if (d >= D) w8 = u32x2{0u, 0u};
+        const Frag<bf16_t> f = decode(w8);
+#pragma unroll
+        for (int y = NP - 1; y >= 0; --y) mma16(f, q[y], s[r]);
+      }
+    }
+    float x[4 * R], pv[R], tm = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float kscale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ls), r));
+      // (behind the last slot: weights 0 under a scale that may be anything)
+      pv[r] = 16 * r < nk ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ls), R + r)) : 0.f;
+      if (r == nr) {
+        kscale = sc[0];
+        pv[r] = sc[1];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[4 * r + i] = 16 * r + 4 * g16 + i < nk ? s[r][i] * kscale : -INFINITY;
+        tm = fmaxf(tm, x[4 * r + i]);
+      }
+    }
+    if (t + 4 < tiles) issue_k(t + 4);
+    tm = fmaxf(tm, __shfl_xor(tm, 16, 64));
+    tm = max32(tm);
+    const bool up = (tm - m) * c > 8.f;                  // as in the batch's forward
+    if (wave_any(up)) {
+      const float mn = up ? tm : m, f = up ? __builtin_amdgcn_exp2f((m - mn) * c) : 1.f;
+      l *= f;
+#pragma unroll
+      for (int i = 0; i < OB; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[i][r] *= f;
+      m = mn;
+    }
+    const float mc = m == -INFINITY ? 0.f : m * c;
+#pragma unroll
+    for (int e = 0; e < 4 * R; ++e) {
+      x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], c, -mc));
+      l += x[e];
+      x[e] *= pv[e >> 2];
+    }
+    static_assert(R == 2, "one product over the tile's 32 slots");
+    Bf16Parts<NP> pf;
+    split(x, pf);
+    // lane's piece of the transposed read: row 16 (e / 4) + 4 g16 + e % 4, e = l16 / 2
+    const int e = l16 >> 1, row = 16 * (e >> 2) + 4 * g16 + (e & 3);
+#pragma unroll
+    for (int i = 0; i < OB; ++i) {
+      typedef int i32x2 __attribute__((ext_vector_type(2)));
+      typedef __attribute__((address_space(3))) i32x2 lds_v2;
+      const i32x2 w8 = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2*)(VS + TL::at(row, i) + 8 * (l16 & 1)));
+      const Frag<bf16_t> f = decode(u32x2{(uint32_t)w8[0], (uint32_t)w8[1]});
+#pragma unroll
+      for (int y = NP - 1; y >= 0; --y) mma16(f, pf.p[y], o[i]);
+    }
+  }
+  l += __shfl_xor(l, 16, 64);
+  l = add32(l);
+  // join of the waves: O[w][head][DP], then m and l
+  float* const J = reinterpret_cast<float*>(smem);
+  __syncthreads();
+  if (l16 < nh) {
+    float* const Jw = J + (w * nh + l16) * Cfg::JROW;
 #pragma unroll
     for (int i = 0; i < OB; ++i) *reinterpret_cast<f32x4*>(Jw + 16 * i + 4 * g16) = o[i];
     if (g16 == 0) {
       Jw[DP] = m;
       Jw[DP + 1] = l;
     }
-    __syncthreads();
-    for (int x = threadIdx.x; x < nh * D; x += 256) {
-      const int h = x / D, d = x - h * D;
-      float mm[4], M = -INFINITY;
+  }
+  __syncthreads();
+  for (int x = threadIdx.x; x < nh * D; x += 256) {
+    const int h = x / D, d = x - h * D;
+    float mm[4], M = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        mm[i] = J[(i * STEP_HEADS + h) * (DP + 4) + DP];
-        M = fmaxf(M, mm[i]);
-      }
-      float S = 0.f, O = 0.f;
+    for (int i = 0; i < 4; ++i) {
+      mm[i] = J[(i * nh + h) * Cfg::JROW + DP];
+      M = fmaxf(M, mm[i]);
+    }
+    float S = 0.f, O = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float* P = J + (i * STEP_HEADS + h) * (DP + 4);
-        const float f = mm[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mm[i] - M) * c);
-        S += P[DP + 1] * f;
-        O += P[d] * f;
-      }
-      if (ns == 1) {
-        st((T*)A.j.out.p + (int64_t)b * A.j.out.ld + (h0 + h) * D + d, O / S);
-      } else {
-        float* P = A.part + (((int64_t)b * A.heads + h0 + h) * ns + u) * (D + 2);
-        P[d] = O;
-        if (d == 0) {
-          P[D] = M;
-          P[D + 1] = S;
-        }
+    for (int i = 0; i < 4; ++i) {
+      const float* P = J + (i * nh + h) * Cfg::JROW;
+      const float f = mm[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mm[i] - M) * c);
+      S += P[DP + 1] * f;
+      O += P[d] * f;
+    }
+    if (ns == 1) {
+      st((T*)A.j.out.p + (int64_t)b * A.j.out.ld + (h0 + h) * D + d, O / S);
+    } else {
+      float* P = A.part + (((int64_t)b * A.heads + h0 + h) * ns + u) * (D + 2);
+      P[d] = O;
+      if (d == 0) {
+        P[D] = M;
+        P[D + 1] = S;
       }
     }
   }
 }
 
-// Blocks of one launch do not go by 16 query heads here: those share a block.
+// (the launch that brings the events has one group of query heads)
 static int step8_splits(int batch, int kv_heads, int cap) { return step_splits(batch, kv_heads, kv_heads, cap); }
 
 size_t seq_step8_workspace(int batch, int heads, int kv_heads, int dim, int cap) {
@@ -380,12 +419,22 @@ size_t seq_step8_workspace(int batch, int heads, int kv_heads, int dim, int cap)
 }
 
 template <typename T, int DP>
-static hipError_t step8_launch(const Step8K& A, const RopeTurns& t, int batch, hipStream_t s) {
-  constexpr size_t lds = Step8Cfg<T, DP>::LDS;
-  static LdsLimit lim;
-  LAT_HIP_CHECK(lds_limit(seq_step8_kernel<T, DP>, lds, lim));
+static hipError_t step8_launch(Step8K A, const RopeTurns& t, int batch, hipStream_t s) {
+  using Cfg = Step8Cfg<T, DP>;
+  A.work = Cfg::work(A.group < STEP_HEADS ? A.group : STEP_HEADS);
+  const size_t lds = (size_t)A.work + Cfg::REST;      // at most 64 KB: no limit to raise
+  static_assert(Cfg::work(STEP_HEADS) + Cfg::REST <= 65536, "LDS");
+  A.hg0 = 0;
+  A.hgs = A.append = 1;
   seq_step8_kernel<T, DP><<<batch * A.c.kv_heads * A.j.ns, 256, lds, s>>>(A, t);
   LAT_LAUNCH_CHECK();
+  if (A.group > STEP_HEADS) {
+    A.hg0 = 1;
+    A.hgs = cdiv(A.group, STEP_HEADS) - 1;
+    A.append = 0;
+    seq_step8_kernel<T, DP><<<batch * A.c.kv_heads * A.hgs * A.j.ns, 256, lds, s>>>(A, t);
+    LAT_LAUNCH_CHECK();
+  }
   if (A.j.ns > 1) {
     seq_step_join_kernel<T, DP><<<batch * A.heads, 256, 0, s>>>(A.j);
     LAT_LAUNCH_CHECK();
@@ -465,7 +514,7 @@ template <typename T, int DP>
 __global__ __launch_bounds__(256) void seq_fill8_kernel(SeqCache8Args C, int rows, const int32_t* __restrict__ off, int S,
                                                         const int32_t* __restrict__ first, SeqTensor k, SeqTensor v,
                                                         int ld, int nb) {
-  using B8 = Block8<DP>;
+  using B8 = Block8<T, DP>;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), cap = C.sinks + C.window;
   for (int s = blockIdx.y; s < S; s += gridDim.y) {
     const int ci = C.index ? C.index[s] : s;
@@ -486,16 +535,14 @@ __global__ __launch_bounds__(256) void seq_fill8_kernel(SeqCache8Args C, int row
       const bool reached = slot < cap && (uint32_t)slot < total;
       uint32_t p = (uint32_t)slot;
       if (reached && slot >= C.sinks) p = total - 1 - (total - 1 - (uint32_t)slot) % (uint32_t)C.window;
-      const bool fresh = reached && p >= (uint32_t)f, old = reached && !fresh;
-      const float s0 = *sp;
+      const bool fresh = reached && p >= (uint32_t)f;
       B8 x;
-      x.from_row((const T*)t.p + (a + (int64_t)(fresh ? p - (uint32_t)f : 0u)) * t.ld + h * C.dim, C.dim, fresh);
-      const bool any_old = wave_any(old);
-      if (any_old) x.from_codes(codes + (int64_t)(old ? slot : blk * CACHE8_BLOCK) * ld, s0, C.dim, ld, old);
-      const float s1 = x.scale();
-      uint32_t code[B8::W];
-      x.codes(s1, code);
-      if (fresh || (old && s1 != s0)) B8::store(codes + (int64_t)slot * ld, ld, code);
+      x.s0 = *sp;
+      x.old = reached && !fresh;
+      x.load_row((const T*)t.p + (a + (int64_t)(fresh ? p - (uint32_t)f : 0u)) * t.ld + h * C.dim, C.dim, fresh);
+      if (wave_any(x.old)) x.load_codes(codes + (int64_t)(x.old ? slot : blk * CACHE8_BLOCK) * ld, ld);
+      const float s1 = x.scale(C.dim);
+      x.encode(s1, C.dim, codes + (int64_t)slot * ld, ld, fresh || (x.old && s1 != x.s0), nullptr);
       if ((threadIdx.x & 63) == 0) *sp = s1;
     }
   }
