@@ -48,7 +48,8 @@ __device__ inline void shift8(Row8<float>& r, int n) {
 // row are zeros.  TAIL: cols is no multiple of 8; the last group is then read as
 // the row's last eight elements and shifted, so that no load leaves the row and
 // none is in a branch (a load in a branch is waited for there).
-template <typename T, bool TAIL>
+// NT: past the caches (data that is larger than they are).
+template <typename T, bool TAIL, bool NT = false>
 __device__ inline Row8<T> load8(const T* row, int g, int cols) {
   Row8<T> r;
   if (TAIL && cols < 8) {
@@ -72,13 +73,16 @@ __device__ inline Row8<T> load8(const T* row, int g, int cols) {
   const int c = 8 * g < cols - 8 ? 8 * g : cols - 8;
   const char* p = reinterpret_cast<const char*>(row + c);
 #pragma unroll
-  for (int i = 0; i < Row8<T>::W; ++i) r.w[i] = *reinterpret_cast<const u32x4_any*>(p + 16 * i);
+  for (int i = 0; i < Row8<T>::W; ++i) {
+    const u32x4_any* q = reinterpret_cast<const u32x4_any*>(p + 16 * i);
+    r.w[i] = NT ? __builtin_nontemporal_load(q) : *q;
+  }
   if (TAIL && 8 * g > cols - 8) shift8(r, 8 - (cols & 7));
   if (8 * g >= cols) r.clear();
   return r;
 }
 
-template <typename T, bool TAIL>
+template <typename T, bool TAIL, bool NT = false>
 __device__ inline void store8(T* row, int g, int cols, const Row8<T>& r) {
   if (8 * g >= cols) return;
   if (TAIL && 8 * g > cols - 8) {
@@ -92,7 +96,10 @@ __device__ inline void store8(T* row, int g, int cols, const Row8<T>& r) {
   }
   char* p = reinterpret_cast<char*>(row + 8 * g);
 #pragma unroll
-  for (int i = 0; i < Row8<T>::W; ++i) *reinterpret_cast<u32x4_any*>(p + 16 * i) = r.w[i];
+  for (int i = 0; i < Row8<T>::W; ++i) {
+    u32x4_any* q = reinterpret_cast<u32x4_any*>(p + 16 * i);
+    if (NT) __builtin_nontemporal_store((u32x4_any)r.w[i], q); else *q = r.w[i];
+  }
 }
 
 }  // namespace lat

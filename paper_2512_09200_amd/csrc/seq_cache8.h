@@ -49,26 +49,31 @@ __device__ inline uint32_t cache8_codes(const float* x, float s) {
   return u;
 }
 
-// A wave's view of a block: lane l holds slot l / 4, elements (l % 4) E .. + E - 1
-// of a row padded to DP, as the memory words of a fresh row (of T) or of old codes.
+// A wave's view of a block: lane l holds slot l / 4, of its row (padded to DP) the
+// elements 16 (l % 4) .. + 15 of every 64 (8 (l % 4) .. + 7 where DP is 32) in chunks
+// of eight, as the memory words of a fresh row (of T) or of old codes.  Four lanes'
+// codes are 64 neighbouring bytes.
 // Values are decoded where they are used, eight at a time: once for the scale,
 // once for the codes.
 template <typename T, int DP> struct Block8 {
-  static constexpr int E = DP / 4, C = E / 8;        // elements, chunks of eight
+  static constexpr int C = DP / 32;                  // chunks of a lane
   Frag<T> row[C];
   u32x2 code[C];
   bool fresh, old;
   float s0;
 
   __device__ static inline int slot() { return (threadIdx.x & 63) >> 2; }
-  __device__ static inline int first() { return (threadIdx.x & 3) * E; }
+  __device__ static inline int at(int i) {           // the chunk's first element
+    const int l = threadIdx.x & 3;
+    return DP == 32 ? 8 * l : 16 * (l + 4 * (i >> 1)) + 8 * (i & 1);
+  }
 
   // p: the row's first element, valid memory in any case
   __device__ inline void load_row(const T* p, int dim, bool on) {
     fresh = on;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      const int d = first() + 8 * i;
+      const int d = at(i);
       load_frag(p + (d < dim ? d : 0), on && d < dim, row[i]);
     }
   }
@@ -76,7 +81,7 @@ template <typename T, int DP> struct Block8 {
   __device__ inline void load_codes(const uint8_t* p, int ld) {
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      const int d = first() + 8 * i;
+      const int d = at(i);
       code[i] = *reinterpret_cast<const u32x2*>(p + (d < ld ? d : 0));
     }
   }
@@ -87,13 +92,65 @@ template <typename T, int DP> struct Block8 {
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = row[i].v[e];
     }
-    const bool on = old && first() + 8 * i < dim;
+    const bool on = old && at(i) < dim;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const f32x2_t a = j & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)code[i][j >> 1], true)
                               : __builtin_amdgcn_cvt_pk_f32_fp8((int)code[i][j >> 1], false);
 #pragma unroll
       for (int e = 0; e < 2; ++e) x[2 * j + e] = fresh ? x[2 * j + e] : on ? a[e] * s0 : 0.f;
+    }
+  }
+  // The scale of a block of fresh rows alone, all finite (else false: the general
+  // way).  The largest magnitude is that of the bits, two bf16 an operation; the general
+  // way's 25 operations an element would be above the fill's memory time.
+  __device__ inline bool fresh_scale(float* s) const {
+    uint32_t top = 0;
+    if constexpr (sizeof(T) == 2) {
+      typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+      u16x2 m{0, 0};
+#pragma unroll
+      for (int i = 0; i < C; ++i) {
+        const u32x4 w = __builtin_bit_cast(u32x4, row[i].v);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[j] & 0x7fff7fffu));
+      }
+      top = (uint32_t)max(m[0], m[1]) << 16;
+    } else {
+#pragma unroll
+      for (int i = 0; i < C; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(row[i].v[e]) & 0x7fffffffu);
+    }
+    top = __builtin_amdgcn_readfirstlane(lanes_join<64>(top, Max()));
+    *s = cache8_scale(__uint_as_float(top));
+    return top < 0x7f800000u && *s < 0x1p120f;
+  }
+  // Their codes: |x| <= 448 s, nothing to clamp
+  __device__ inline void encode_fresh(float s, uint8_t* p, int ld) const {
+    constexpr int N = DP == 32 ? 1 : 2;
+    typedef typename std::conditional<N == 1, u32x2, u32x4>::type V;
+    const float inv = pow2_inv(s);
+#pragma unroll
+    for (int i = 0; i < C; i += N) {
+      V w;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        float x[8];
+        if constexpr (sizeof(T) == 2) {
+          Vec16<bf16_t>::unpack(__builtin_bit_cast(u32x4, row[i + j].v), x);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = row[i + j].v[e];
+        }
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          int c = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * y] * inv, x[4 * y + 1] * inv, 0, false);
+          c = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * y + 2] * inv, x[4 * y + 3] * inv, c, true);
+          w[2 * j + y] = (uint32_t)c;
+        }
+      }
+      if (fresh && at(i) < ld) *reinterpret_cast<V*>(p + at(i)) = w;
     }
   }
   // the wave's scale
@@ -111,14 +168,21 @@ template <typename T, int DP> struct Block8 {
   // Codes under scale s to p (a row of ld bytes) where `write`, and to q (DP bytes)
   // where it is not null.
   __device__ inline void encode(float s, int dim, uint8_t* p, int ld, bool write, uint8_t* q) const {
+    constexpr int N = DP == 32 ? 1 : 2;               // chunks of a store
+    typedef typename std::conditional<N == 1, u32x2, u32x4>::type V;
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
-      float x[8];
-      chunk(i, dim, x);
-      const u32x2 w{cache8_codes(x, s), cache8_codes(x + 4, s)};
-      const int d = first() + 8 * i;
-      if (write && d < ld) *reinterpret_cast<u32x2*>(p + d) = w;
-      if (q) *reinterpret_cast<u32x2*>(q + d) = w;
+    for (int i = 0; i < C; i += N) {
+      V w;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        float x[8];
+        chunk(i + j, dim, x);
+        w[2 * j] = cache8_codes(x, s);
+        w[2 * j + 1] = cache8_codes(x + 4, s);
+      }
+      const int d = at(i);                            // (ld is a multiple of 16)
+      if (write && d < ld) *reinterpret_cast<V*>(p + d) = w;
+      if (q) *reinterpret_cast<V*>(q + d) = w;
     }
   }
 };

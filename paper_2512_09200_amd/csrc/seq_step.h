@@ -74,10 +74,10 @@ __global__ __launch_bounds__(256) void seq_step_join_kernel(StepJoin A) {
 // least 256 slots (two rounds of a block's waves) each.  Three users, 65536 slots
 // of 128, 2 key heads: 47 us and 6 for the join with 512 splits in all, 48 and 8.5
 // with 1024, 47 and 5.5 with 256; unsplit the six blocks would take milliseconds.
-inline int step_splits(int batch, int heads, int kv_heads, int cap) {
+inline int step_splits(int batch, int heads, int kv_heads, int cap, int all = STEP_MAX_SPLITS) {
   const int hg = cdiv(heads / kv_heads, STEP_HEADS);
   const int64_t blocks = (int64_t)batch * kv_heads * hg;
-  int64_t n = cdiv(STEP_MAX_SPLITS, blocks);
+  int64_t n = cdiv(all, blocks);
   if (n > cdiv(cap, 256)) n = cdiv(cap, 256);
   return (int)n;
 }

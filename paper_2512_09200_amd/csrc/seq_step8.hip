@@ -176,7 +176,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 2 : 3) void seq_
 #pragma unroll
     for (int i = 0; i < VL; ++i) {
       const int x = i * 64 + lane, row = min(x / UPR, nk - 1), c = 16 * (x % UPR);
-      lv[i] = *reinterpret_cast<const u32x4*>(vp + (__umul24(row, A.ld) + (c < A.ld ? c : 0)));
+      lv[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(vp + (__umul24(row, A.ld) + (c < A.ld ? c : 0))));
     }
   };
   auto issue_k = [&](int t) {
@@ -187,7 +187,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 2 : 3) void seq_
 #pragma unroll
       for (int i = 0; i < KV; ++i) {
         const int row = min(16 * r + l16, nk - 1), d = DP == 32 ? 8 * g16 : 64 * i + 16 * g16;
-        lk[r * KV + i] = *reinterpret_cast<const KVec*>(kp + (__umul24(row, A.ld) + (d < A.ld ? d : 0)));
+        lk[r * KV + i] = __builtin_nontemporal_load(
+            reinterpret_cast<const KVec*>(kp + (__umul24(row, A.ld) + (d < A.ld ? d : 0))));
       }
     ls = (lane & R ? vs : ks)[min(j0 / CACHE8_BLOCK + (lane & (R - 1)), (n - 1) / CACHE8_BLOCK)];
   };
@@ -410,7 +411,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 2 : 3) void seq_
 }
 
 // (the launch that brings the events has one group of query heads)
-static int step8_splits(int batch, int kv_heads, int cap) { return step_splits(batch, kv_heads, kv_heads, cap); }
+static int step8_splits(int batch, int kv_heads, int cap) { return step_splits(batch, kv_heads, kv_heads, cap, 768); }
 
 size_t seq_step8_workspace(int batch, int heads, int kv_heads, int dim, int cap) {
   if (batch == 0) return 0;
@@ -517,9 +518,10 @@ __global__ __launch_bounds__(256) void seq_fill8_kernel(SeqCache8Args C, int row
   using B8 = Block8<T, DP>;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), cap = C.sinks + C.window;
   for (int s = blockIdx.y; s < S; s += gridDim.y) {
-    const int ci = C.index ? C.index[s] : s;
+    const int ci = __builtin_amdgcn_readfirstlane(C.index ? C.index[s] : s);
     if (ci < 0 || ci >= C.num_caches) continue;
-    const int a = max(off[s], 0), e = min(off[s + 1], rows), f = first ? first[s] : 0;
+    const int a = max(__builtin_amdgcn_readfirstlane(off[s]), 0), e = min(__builtin_amdgcn_readfirstlane(off[s + 1]), rows);
+    const int f = first ? __builtin_amdgcn_readfirstlane(first[s]) : 0;
     if (e <= a || f < 0) continue;
     const uint32_t total = (uint32_t)f + (uint32_t)(e - a);
     const SlotRanges R((uint32_t)f, total, C.sinks, C.window);
@@ -537,12 +539,17 @@ __global__ __launch_bounds__(256) void seq_fill8_kernel(SeqCache8Args C, int row
       if (reached && slot >= C.sinks) p = total - 1 - (total - 1 - (uint32_t)slot) % (uint32_t)C.window;
       const bool fresh = reached && p >= (uint32_t)f;
       B8 x;
-      x.s0 = *sp;
-      x.old = reached && !fresh;
       x.load_row((const T*)t.p + (a + (int64_t)(fresh ? p - (uint32_t)f : 0u)) * t.ld + h * C.dim, C.dim, fresh);
-      if (wave_any(x.old)) x.load_codes(codes + (int64_t)(x.old ? slot : blk * CACHE8_BLOCK) * ld, ld);
-      const float s1 = x.scale(C.dim);
-      x.encode(s1, C.dim, codes + (int64_t)slot * ld, ld, fresh || (x.old && s1 != x.s0), nullptr);
+      x.old = reached && !fresh;
+      float s1;
+      if (!wave_any(x.old) && x.fresh_scale(&s1)) {
+        x.encode_fresh(s1, codes + (int64_t)slot * ld, ld);
+      } else {
+        x.s0 = *sp;
+        x.load_codes(codes + (int64_t)(x.old ? slot : blk * CACHE8_BLOCK) * ld, ld);
+        s1 = x.scale(C.dim);
+        x.encode(s1, C.dim, codes + (int64_t)slot * ld, ld, fresh || (x.old && s1 != x.s0), nullptr);
+      }
       if ((threadIdx.x & 63) == 0) *sp = s1;
     }
   }
