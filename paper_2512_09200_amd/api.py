@@ -859,17 +859,19 @@ def lattice_seq_step(q, k, v, lens, k_cache, v_cache, window, sinks=0, cache_ind
 
 def _cache8(caches, like, kv_heads, window, sinks):
     k, v, ks, vs = caches
-    cap = int(sinks) + int(window)
-    want = (k.shape[0], kv_heads, cap, fp8_ld(like.shape[2]))
-    if k.shape != want or v.shape != want or k.dtype != torch.uint8 or v.dtype != torch.uint8:
-        raise ValueError(f"caches: expected [caches, kv_heads, sinks + window, fp8_ld(head_dim)] = {want} of uint8")
-    want = (k.shape[0], kv_heads, -(-cap // A.SEQ_CACHE8_BLOCK))
-    if ks.shape != want or vs.shape != want or ks.dtype != torch.float32 or vs.dtype != torch.float32:
-        raise ValueError(f"scales: expected [caches, kv_heads, blocks of {A.SEQ_CACHE8_BLOCK} slots] = {want} of float32")
-    _contig(*caches)
-    if any(t.get_device() != like.get_device() for t in caches):
-        raise ValueError("the caches are not on the other tensors' device")
-    return A.lattice_seq_cache8(*(t.data_ptr() or None for t in caches), k.shape[0])
+    cap, n, dev = int(sinks) + int(window), k.shape[0], like.get_device()
+    want, scales = (n, kv_heads, cap, fp8_ld(like.shape[2])), (n, kv_heads, -(-cap // A.SEQ_CACHE8_BLOCK))
+    for t, shape, dtype in ((k, want, torch.uint8), (v, want, torch.uint8), (ks, scales, torch.float32),
+                            (vs, scales, torch.float32)):
+        if t.shape != shape or t.dtype != dtype:
+            raise ValueError(f"caches: expected codes [caches, kv_heads, sinks + window, fp8_ld(head_dim)] = {want} of "
+                             f"uint8 and scales [caches, kv_heads, blocks of {A.SEQ_CACHE8_BLOCK} slots] = {scales} of "
+                             f"float32, got {tuple(t.shape)} of {t.dtype}")
+        if not t.is_contiguous():
+            raise ValueError("tensor must be contiguous")
+        if t.get_device() != dev:
+            raise ValueError("the caches are not on the other tensors' device")
+    return A.lattice_seq_cache8(k.data_ptr() or None, v.data_ptr() or None, ks.data_ptr() or None, vs.data_ptr() or None, n)
 
 
 def lattice_seq_cache8_fill(seqs, k, v, k_cache, v_cache, k_scale, v_scale, window, sinks=0, cache_index=None,
@@ -930,17 +932,24 @@ def _drop_desc(dropout, dev):
 
 
 def _row_ptr(t, like, name):
-    """(pointer, row stride) of a tensor [rows, cols]; like: one whose shape,
-    dtype and GPU it must have."""
+    """(pointer, row stride) of a tensor [rows, cols]; like: the (shape, dtype,
+    GPU) that a call's tensors share."""
     if t is None:
         return None, 0
-    if t.shape != like.shape or t.dtype != like.dtype or t.device != like.device:
-        raise ValueError(f"{name}: expected {tuple(like.shape)} of {like.dtype} on {like.device}, "
+    shape, dtype, dev = like
+    if t.shape != shape or t.dtype != dtype or t.get_device() != dev:
+        raise ValueError(f"{name}: expected {tuple(shape)} of {dtype} on GPU {dev}, "
                          f"got {tuple(t.shape)} of {t.dtype} on {t.device}")
-    rows, cols = t.shape
-    if rows and cols > 1 and t.stride(1) != 1:
+    stride, cols = t.stride(), shape[1]
+    if stride[1] != 1 and cols > 1 and shape[0]:
         raise ValueError(f"{name}: expected unit column stride")
-    return t.data_ptr() or None, t.stride(0) if rows > 1 else cols
+    return t.data_ptr() or None, stride[0] if shape[0] > 1 else cols
+
+
+def _new_rows(t, shape):
+    """(tensor, pointer, row stride) of a new contiguous tensor of t's type."""
+    o = t.new_empty(shape)
+    return o, (o.data_ptr() or None, shape[1])
 
 
 def _rows2(t, name):
@@ -956,19 +965,21 @@ def lattice_dropout(x, p, rng, site=0, out=None, stream=None):
     same call on the gradient of the result.  out may be x."""
     if stream is not None:
         return _on(stream, x, lattice_dropout, x, p, rng, site, out)
-    rows, cols = _rows2(x, "x")
-    dev = _gpu(x)
-    desc = _drop_desc((p, rng, site), dev)
-    out = torch.empty((rows, cols), dtype=x.dtype, device=x.device) if out is None else out
-    _run(dev, load().lattice_dropout, byref(desc), _dt(x), rows, cols, *_row_ptr(x, x, "x"), *_row_ptr(out, x, "out"))
+    shape, dev = _rows2(x, "x"), _gpu(x)
+    desc, like = _drop_desc((p, rng, site), dev), (shape, x.dtype, dev)
+    if out is None:
+        out, o = _new_rows(x, shape)
+    else:
+        o = _row_ptr(out, like, "out")
+    _run(dev, load().lattice_dropout, byref(desc), _dt(x), *shape, *_row_ptr(x, like, "x"), *o)
     return out
 
 
-def _norm_desc(x, gain, eps, dropout, dev):
-    cols = x.shape[1]
-    drop = _drop_desc(dropout, dev)
-    return A.lattice_add_rmsnorm_desc(_dt(x), cols, float(eps), _vec(gain, torch.float32, cols, "gain", dev),
-                                      ctypes.pointer(drop) if drop is not None else None)
+def _norm_desc(x, cols, gain, eps, dropout, dev):
+    d = A.lattice_add_rmsnorm_desc(_dt(x), cols, eps, _vec(gain, torch.float32, cols, "gain", dev))
+    if dropout is not None:
+        d.dropout = ctypes.pointer(_drop_desc(dropout, dev))
+    return d
 
 
 def lattice_add_rmsnorm_fwd(x, residual=None, gain=None, eps=1e-6, dropout=None, out="y", h=None, y=None, stream=None):
@@ -982,25 +993,29 @@ def lattice_add_rmsnorm_fwd(x, residual=None, gain=None, eps=1e-6, dropout=None,
         return _on(stream, x, lattice_add_rmsnorm_fwd, x, residual, gain, eps, dropout, out, h, y)
     if out not in ("y", "fp8", "both"):
         raise ValueError(f"out: expected 'y', 'fp8' or 'both', got {out!r}")
-    rows, cols = _rows2(x, "x")
-    dev = _gpu(x)
-    desc = _norm_desc(x, gain, eps, dropout, dev)
-    h_out = h
-    if residual is not None or dropout is not None:
-        h_out = h = torch.empty((rows, cols), dtype=x.dtype, device=x.device) if h is None else h
-    elif h is None:
-        h = x
+    shape, dev = _rows2(x, "x"), _gpu(x)
+    rows, cols = shape
+    desc, like = _norm_desc(x, cols, gain, eps, dropout, dev), (shape, x.dtype, dev)
+    xp, rp = _row_ptr(x, like, "x"), _row_ptr(residual, like, "residual")
+    if h is not None:
+        hp = _row_ptr(h, like, "h")
+    elif residual is not None or dropout is not None:
+        h, hp = _new_rows(x, shape)
+    else:
+        h, hp = x, (None, 0)
     if out == "fp8":
-        y = None
+        y, yp = None, (None, 0)
     elif y is None:
-        y = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-    codes = scales = None
+        y, yp = _new_rows(x, shape)
+    else:
+        yp = _row_ptr(y, like, "y")
+    codes = scales = cp = sp = None
+    ldq = 0
     if out != "y":
-        codes = torch.empty((rows, fp8_ld(cols)), dtype=torch.uint8, device=x.device)
-        scales = torch.empty(rows, dtype=torch.float32, device=x.device)
-    _run(dev, load().lattice_add_rmsnorm_fwd, byref(desc), rows, *_row_ptr(x, x, "x"),
-         *_row_ptr(residual, x, "residual"), *_row_ptr(h_out, x, "h"), *_row_ptr(y, x, "y"),
-         _p(codes), codes.stride(0) if codes is not None else 0, _p(scales))
+        ldq = fp8_ld(cols)
+        codes, scales = x.new_empty((rows, ldq), dtype=torch.uint8), x.new_empty(rows, dtype=torch.float32)
+        cp, sp = codes.data_ptr() or None, scales.data_ptr() or None
+    _run(dev, load().lattice_add_rmsnorm_fwd, byref(desc), rows, *xp, *rp, *hp, *yp, cp, ldq, sp)
     return h, y, codes, scales
 
 
@@ -1011,17 +1026,29 @@ def lattice_add_rmsnorm_bwd(h, dy, dh=None, gain=None, eps=1e-6, dropout=None, d
     forward's, its rng unchanged."""
     if stream is not None:
         return _on(stream, h, lattice_add_rmsnorm_bwd, h, dy, dh, gain, eps, dropout, d_residual, dx)
-    rows, cols = _rows2(h, "h")
-    dev = _gpu(h)
-    desc = _norm_desc(h, gain, eps, dropout, dev)
-    d_residual = torch.empty((rows, cols), dtype=h.dtype, device=h.device) if d_residual is None else d_residual
-    if dropout is not None and dx is None:
-        dx = torch.empty((rows, cols), dtype=h.dtype, device=h.device)
-    dgain = gain.new_empty(cols) if gain is not None else None
+    shape, dev = _rows2(h, "h"), _gpu(h)
+    rows, cols = shape
+    desc, like = _norm_desc(h, cols, gain, eps, dropout, dev), (shape, h.dtype, dev)
+    if d_residual is None:
+        d_residual, drp = _new_rows(h, shape)
+    else:
+        drp = _row_ptr(d_residual, like, "d_residual")
+    if dx is not None:
+        dxp = _row_ptr(dx, like, "dx")
+    elif dropout is not None:
+        dx, dxp = _new_rows(h, shape)
+    else:
+        dx, dxp = d_residual, (None, 0)
     lib = load()
-    wsb = lib.lattice_add_rmsnorm_bwd_workspace(byref(desc), rows) if dgain is not None else 0
-    ws = h.new_empty(wsb, dtype=torch.uint8) if wsb else None
-    _run(dev, lib.lattice_add_rmsnorm_bwd, byref(desc), rows, *_row_ptr(h, h, "h"), *_row_ptr(dy, h, "dy"),
-         *_row_ptr(dh, h, "dh"), *_row_ptr(d_residual, h, "d_residual"), *_row_ptr(dx, h, "dx"),
-         _p(dgain), _p(ws), wsb)
-    return d_residual, d_residual if dx is None else dx, dgain
+    dgain = ws = gp = wp = None
+    wsb = 0
+    if gain is not None:
+        dgain = gain.new_empty(cols)
+        gp = dgain.data_ptr()
+        wsb = lib.lattice_add_rmsnorm_bwd_workspace(byref(desc), rows)
+        if wsb:
+            ws = h.new_empty(wsb, dtype=torch.uint8)
+            wp = ws.data_ptr()
+    _run(dev, lib.lattice_add_rmsnorm_bwd, byref(desc), rows, *_row_ptr(h, like, "h"), *_row_ptr(dy, like, "dy"),
+         *_row_ptr(dh, like, "dh"), *drp, *dxp, gp, wp, wsb)
+    return d_residual, dx, dgain
