@@ -687,7 +687,7 @@ lattice_status lattice_add_rmsnorm_fwd(const lattice_add_rmsnorm_desc* desc, int
  * d_residual and dx (storage dtype, each may be NULL; without dropout they are
  * equal) and, where not NULL, dgain [cols] (fp32, overwritten, summed over rows
  * in a fixed order; needs a workspace).  rng must hold what it held in the
- * forward.  d_residual and dx may be dy or dh (same stride), not each other.
+ * forward.  d_residual and dx may be h, dy or dh (same stride), not each other.
  * Errors: as the forward, WORKSPACE. */
 size_t lattice_add_rmsnorm_bwd_workspace(const lattice_add_rmsnorm_desc* desc, int64_t rows);
 lattice_status lattice_add_rmsnorm_bwd(const lattice_add_rmsnorm_desc* desc, int64_t rows,

@@ -560,7 +560,7 @@ def lattice_interact_state(kind, X, stack, stack_n, ws, ln_eps=1e-5, fp8_proj=No
 def _run(dev, fn, *args):
     """Enqueue a C call on the current stream of the tensors' GPU.  Launches go
     to the current device, so it is made the tensors' own."""
-    if dev != torch.cuda.current_device():
+    if dev != torch._C._cuda_getDevice():
         with torch.cuda.device(dev):
             return _run(dev, fn, *args)
     check(fn(*args, torch._C._cuda_getCurrentRawStream(dev)))

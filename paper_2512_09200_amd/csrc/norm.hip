@@ -33,6 +33,7 @@ template <int LPR_, int CH_, int WPR_> struct RowCfg {
   static constexpr int RPB = WPR > 1 ? 1 : 4 * RPW;          // rows of a block
   static constexpr int STEP = LPR * WPR;                     // groups between a lane's own
   static constexpr int COLS = 8 * CH * STEP;
+  static constexpr bool AHEAD = CH <= 2;                     // the next row's loads before a row's sums (registers)
 };
 
 struct NormK {
@@ -116,8 +117,9 @@ __global__ __launch_bounds__(C::THREADS) void add_rmsnorm_fwd_kernel(NormK A) {
 #pragma unroll
       for (int i = 0; i < C::CH; ++i) rr[i] = load8<T, TAIL>(row_of<T>(A.r, row), at.lane + i * C::STEP, A.cols);
   };
-  if (at.first < A.rows) fetch(at.first);
+  if (C::AHEAD && at.first < A.rows) fetch(at.first);
   for (int64_t base = at.first; base < A.rows; base += step) {
+    if (!C::AHEAD) fetch(base);
     const int64_t row = base + at.sub;
     const bool live = row < A.rows;
     float h[C::CH][8], s[1] = {0.f};
@@ -136,7 +138,7 @@ __global__ __launch_bounds__(C::THREADS) void add_rmsnorm_fwd_kernel(NormK A) {
       if (A.h.p && live) store8<T, TAIL>((T*)A.h.p + row * A.h.ld, at.lane + i * C::STEP, A.cols, o);
       o.get(h[i]);
     }
-    if (base + step < A.rows) fetch(base + step);
+    if (C::AHEAD && base + step < A.rows) fetch(base + step);
 #pragma unroll
     for (int i = 0; i < C::CH; ++i)
 #pragma unroll
@@ -174,7 +176,11 @@ __global__ __launch_bounds__(C::THREADS) void add_rmsnorm_fwd_kernel(NormK A) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = c + e < A.cols ? h[i][e] * inv : 0.f;
       u32x2 w{e4m3x4(v[0], v[1], v[2], v[3]), e4m3x4(v[4], v[5], v[6], v[7])};
-      if (bad) w = u32x2{0x7f7f7f7fu, 0x7f7f7f7fu};
+      if (bad) {
+        const int k = A.cols - c;                        // columns of the group (bytes behind them stay 0)
+        const uint64_t n = k >= 8 ? ~0ull : k > 0 ? (1ull << (8 * k)) - 1 : 0ull;
+        w = __builtin_bit_cast(u32x2, n & 0x7f7f7f7f7f7f7f7full);
+      }
       *reinterpret_cast<u32x2*>(q + c) = w;
     }
     for (int64_t c = C::COLS + 8 * at.lane; c < A.ldq; c += 8 * C::STEP) *reinterpret_cast<u32x2*>(q + c) = u32x2{0u, 0u};
@@ -209,8 +215,9 @@ __global__ __launch_bounds__(C::THREADS) void add_rmsnorm_bwd_kernel(NormK A) {
 #pragma unroll
       for (int i = 0; i < C::CH; ++i) rr[i] = load8<T, TAIL, NT>(row_of<T>(A.dh, row), at.lane + i * C::STEP, A.cols);
   };
-  if (at.first < A.rows) fetch(at.first);
+  if (C::AHEAD && at.first < A.rows) fetch(at.first);
   for (int64_t base = at.first; base < A.rows; base += step) {
+    if (!C::AHEAD) fetch(base);
     const int64_t row = base + at.sub;
     const bool live = row < A.rows;
     float h[C::CH][8], dn[C::CH][8], s[2] = {0.f, 0.f};
@@ -226,7 +233,7 @@ __global__ __launch_bounds__(C::THREADS) void add_rmsnorm_bwd_kernel(NormK A) {
         s[1] += dn[i][e] * gain[i][e] * h[i][e];
       }
     }
-    if (base + step < A.rows) fetch(base + step);
+    if (C::AHEAD && base + step < A.rows) fetch(base + step);
     row_join<C>(s, Add(), red, turn);
     const float rho = 1.f / sqrtf(s[0] * A.inv_cols + A.eps);
     const float c = rho * rho * s[1] * A.inv_cols;             // mean(dn n) rho

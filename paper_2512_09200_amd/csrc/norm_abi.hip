@@ -36,6 +36,12 @@ static lattice_status check_rows(const char* name, const void* p, int64_t stride
   return LATTICE_OK;
 }
 
+// Where a result takes the place of an input, row by row.
+static lattice_status check_same(const char* name, const void* out, int64_t out_stride, const void* in, int64_t in_stride) {
+  REQUIRE(!out || out != in || out_stride == in_stride, "%s is an input's memory with another row stride", name);
+  return LATTICE_OK;
+}
+
 static lattice_status check_norm(const lattice_add_rmsnorm_desc* d, int64_t rows, DropArgs* drop) {
   REQUIRE(d, "null norm descriptor");
   REQUIRE(d->dtype == LATTICE_F32 || d->dtype == LATTICE_BF16, "bad dtype");
@@ -74,6 +80,7 @@ lattice_status lattice_dropout(const lattice_dropout_desc* d, lattice_dtype dtyp
   if (rows >= MAX_ROWS || cols >= MAX_ROWS) FAIL(LATTICE_ERR_UNSUPPORTED, "rows and cols must be < 2^30");
   TRY(check_rows("x", x, x_stride, cols, dtype));
   TRY(check_rows("out", out, out_stride, cols, dtype));
+  TRY(check_same("out", out, out_stride, x, x_stride));
   if (rows * (((int64_t)cols + 7) / 8) > MAX_BLOCKS * 1024)
     FAIL(LATTICE_ERR_UNSUPPORTED, "rows x cols too many for one launch");
   HIPRET(dropout(dt_of(dtype), rows, cols, drop, tensor(x, x_stride), tensor(out, out_stride), strm(stream)));
@@ -93,6 +100,10 @@ lattice_status lattice_add_rmsnorm_fwd(const lattice_add_rmsnorm_desc* d, int64_
   if (y) TRY(check_rows("y", y, y_stride, d->cols, d->dtype));
   REQUIRE(y || q, "neither y nor q");
   REQUIRE(!h || h != y, "h and y are the same memory");
+  TRY(check_same("h", h, h_stride, x, x_stride));
+  TRY(check_same("h", h, h_stride, residual, residual_stride));
+  TRY(check_same("y", y, y_stride, x, x_stride));
+  TRY(check_same("y", y, y_stride, residual, residual_stride));
   if (q) {
     REQUIRE(scales, "q without scales");
     REQUIRE(ldq >= d->cols && ldq % 16 == 0, "ldq %lld is no multiple of 16 that holds a row", (long long)ldq);
@@ -129,6 +140,11 @@ lattice_status lattice_add_rmsnorm_bwd(const lattice_add_rmsnorm_desc* d, int64_
     if (d_residual) TRY(check_rows("d_residual", d_residual, d_residual_stride, d->cols, d->dtype));
     if (dx) TRY(check_rows("dx", dx, dx_stride, d->cols, d->dtype));
     REQUIRE(!dx || dx != d_residual, "d_residual and dx are the same memory");
+    const struct { const void* p; int64_t stride; } in[] = {{h, h_stride}, {dy, dy_stride}, {dh, dh_stride}};
+    for (const auto& t : in) {
+      TRY(check_same("d_residual", d_residual, d_residual_stride, t.p, t.stride));
+      TRY(check_same("dx", dx, dx_stride, t.p, t.stride));
+    }
     if (dgain) {
       const size_t need = add_rmsnorm_bwd_workspace(rows, d->cols);
       if (!ws || ws_bytes < need) FAIL(LATTICE_ERR_WORKSPACE, "workspace %zu < %zu", ws_bytes, need);

@@ -101,7 +101,7 @@ template <typename T, int DP> struct Step8Cfg {
 };
 
 template <typename T, int DP>
-__global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 2 : 3) void seq_step8_kernel(Step8K A, RopeTurns turns) {
+__global__ __launch_bounds__(256, 3) void seq_step8_kernel(Step8K A, RopeTurns turns) {
   using Cfg = Step8Cfg<T, DP>;
   using TL = Tile8<DP>;
   using B8 = Block8<float, DP>;

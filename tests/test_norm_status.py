@@ -49,6 +49,7 @@ def test_dropout(lib):
     assert f(x=None) == INVALID_ARG and f(out=None) == INVALID_ARG
     assert f(x=P + 1) == INVALID_ARG and f(dt=F32, x=P + 2) == INVALID_ARG
     assert f(xs=7) == INVALID_ARG and f(os=7) == INVALID_ARG
+    assert f(xs=16, os=24) == INVALID_ARG                                  # in place, other rows
     # nothing to do: no pointer is looked at
     assert f(rows=0, x=None, out=None) == OK and f(cols=0, x=None, out=None) == OK
 
@@ -69,6 +70,9 @@ def test_norm_forward(lib):
     assert f(norm(dtype=F32), y=P + 2) == INVALID_ARG
     assert f(norm(), y=None) == INVALID_ARG
     assert f(norm(), h=P, hs=64, y=P) == INVALID_ARG
+    assert f(norm(), h=P, hs=72) == INVALID_ARG and f(norm(), y=P, ys=72) == INVALID_ARG       # in place, other rows
+    assert f(norm(), r=P + 8192, rs=64, h=P + 8192, hs=72) == INVALID_ARG
+    assert f(norm(), r=P + 8192, rs=64, y=P + 8192, ys=72) == INVALID_ARG
     q = dict(y=None, q=P, ldq=64, sc=P)
     assert f(norm(), **{**q, "sc": None}) == INVALID_ARG
     assert f(norm(), **{**q, "ldq": 48}) == INVALID_ARG and f(norm(), **{**q, "ldq": 72}) == INVALID_ARG
@@ -85,6 +89,8 @@ def test_norm_backward(lib):
     assert f(norm(), hs=63) == INVALID_ARG and f(norm(), dys=63) == INVALID_ARG and f(norm(), dh=P, dhs=63) == INVALID_ARG
     assert f(norm(), drs=63) == INVALID_ARG and f(norm(), dx=P + 4096, dxs=63) == INVALID_ARG
     assert f(norm(), dx=P, dxs=64) == INVALID_ARG                          # the same memory as d_residual
+    for at in (dict(h=P + 64), dict(dy=P + 64), dict(dh=P + 64, dhs=64)):  # in place, other rows
+        assert f(norm(), **at, dr=P + 64, drs=72) == INVALID_ARG and f(norm(), **at, dx=P + 64, dxs=72) == INVALID_ARG
     assert f(norm(cols=16385), hs=16385, dys=16385, drs=16385) == UNSUPPORTED
     w = lib.lattice_add_rmsnorm_bwd_workspace
     need = w(byref(norm()), 5)
