@@ -8,7 +8,7 @@ namespace lat {
 
 constexpr float STEP_LOG2E = 1.4426950408889634f;
 constexpr int STEP_HEADS = 16;               // head columns of a block
-constexpr int STEP_MAX_SPLITS = 512;
+constexpr int STEP_MAX_SPLITS = 512;         // of a user's slots: places of the join's LDS
 
 __device__ inline void mma16(const Frag<bf16_t>& a, const Frag<bf16_t>& b, f32x4& c) {
   c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
@@ -74,10 +74,10 @@ __global__ __launch_bounds__(256) void seq_step_join_kernel(StepJoin A) {
 // least 256 slots (two rounds of a block's waves) each.  Three users, 65536 slots
 // of 128, 2 key heads: 47 us and 6 for the join with 512 splits in all, 48 and 8.5
 // with 1024, 47 and 5.5 with 256; unsplit the six blocks would take milliseconds.
-inline int step_splits(int batch, int heads, int kv_heads, int cap, int all = STEP_MAX_SPLITS) {
+inline int step_splits(int batch, int heads, int kv_heads, int cap) {
   const int hg = cdiv(heads / kv_heads, STEP_HEADS);
   const int64_t blocks = (int64_t)batch * kv_heads * hg;
-  int64_t n = cdiv(all, blocks);
+  int64_t n = cdiv(STEP_MAX_SPLITS, blocks);
   if (n > cdiv(cap, 256)) n = cdiv(cap, 256);
   return (int)n;
 }

@@ -410,8 +410,19 @@ __global__ __launch_bounds__(256, 3) void seq_step8_kernel(Step8K A, RopeTurns t
   }
 }
 
-// (the launch that brings the events has one group of query heads)
-static int step8_splits(int batch, int kv_heads, int cap) { return step_splits(batch, kv_heads, kv_heads, cap, 768); }
+// Splits of the slots: as many as leave all blocks of the launch on the chip at once
+// (three a compute unit), of 128 slots (a round of a block's waves) or more, and
+// no more than the join holds.  Three users, 131049 slots of 128, 2 key heads: 32 us with
+// 768 blocks in all, 38 with 512, 36 with 1024 (whose join takes 8 us instead of 5).
+// One user, 1020 / 4000 / 16000 slots: 12.4 / 13.4 / 15.2 us a step, with splits of 256
+// or more 13.1 / 14.4 / 16.2, of 1024 16.0 / 22.3 / 21.3.
+constexpr int STEP8_BLOCKS = 768, STEP8_SPLIT = 4 * STEP8_TILE;
+static int step8_splits(int batch, int kv_heads, int cap) {
+  int64_t n = STEP8_BLOCKS / ((int64_t)batch * kv_heads);
+  if (n > cap / STEP8_SPLIT) n = cap / STEP8_SPLIT;
+  if (n > STEP_MAX_SPLITS) n = STEP_MAX_SPLITS;
+  return n > 1 ? (int)n : 1;
+}
 
 size_t seq_step8_workspace(int batch, int heads, int kv_heads, int dim, int cap) {
   if (batch == 0) return 0;

@@ -243,7 +243,9 @@ def test_step_against_the_definition(dt, H, J, D, W, N, rope):
             within(out[b, h], want, (r + 2 * np.expm1(es)) * mass + u * np.abs(want) * (1 + r), f"out {b} {h}")
 
 
-@pytest.mark.parametrize("dt,H,J,D,W,N,S", [("bf16", 16, 2, 128, 70000, 36, 2), ("f32", 2, 1, 64, 20000, 0, 1)])
+# (the last: more rounds of slots than a join has places for splits)
+@pytest.mark.parametrize("dt,H,J,D,W,N,S", [("bf16", 16, 2, 128, 70000, 36, 2), ("f32", 2, 1, 64, 20000, 0, 1),
+                                            ("bf16", 3, 1, 32, 150001, 7, 1)])
 def test_step_of_long_windows_in_splits(dt, H, J, D, W, N, S):
     from paper_2512_09200_amd import api
     rng = np.random.default_rng(9)
