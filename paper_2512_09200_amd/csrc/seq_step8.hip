@@ -32,6 +32,7 @@
 namespace lat {
 
 constexpr int STEP8_TILE = 32;               // slots of a wave's tile
+constexpr int STEP8_ROUND = 4 * STEP8_TILE;  // of a block's four waves
 
 struct Step8K {
   SeqCache8Args c;
@@ -120,8 +121,7 @@ __global__ __launch_bounds__(256, 3) void seq_step8_kernel(Step8K A, RopeTurns t
   if (p < 0 || ci < 0 || ci >= A.c.num_caches) return;
   const int n = min(p, A.cap - 1) + 1, slot = seq_slot(p, A.c.sinks, A.c.window);
   // the split's slots, whole rounds of the four waves
-  constexpr int ROUND = 4 * STEP8_TILE;
-  const int chunk = ((n + ns - 1) / ns + ROUND - 1) & ~(ROUND - 1);
+  const int chunk = ((n + ns - 1) / ns + STEP8_ROUND - 1) & ~(STEP8_ROUND - 1);
   const int a0 = (int)min((int64_t)u * chunk, (int64_t)n), a1 = (int)min((int64_t)a0 + chunk, (int64_t)n);
   const int64_t head = (int64_t)ci * A.c.kv_heads + kv;
   uint8_t* const kc = A.c.kc + head * A.cap * A.ld;
@@ -414,12 +414,14 @@ __global__ __launch_bounds__(256, 3) void seq_step8_kernel(Step8K A, RopeTurns t
 // (three a compute unit), of 128 slots (a round of a block's waves) or more, and
 // no more than the join holds.  Three users, 131049 slots of 128, 2 key heads: 32 us with
 // 768 blocks in all, 38 with 512, 36 with 1024 (whose join takes 8 us instead of 5).
-// One user, 1020 / 4000 / 16000 slots: 12.4 / 13.4 / 15.2 us a step, with splits of 256
-// or more 13.1 / 14.4 / 16.2, of 1024 16.0 / 22.3 / 21.3.
-constexpr int STEP8_BLOCKS = 768, STEP8_SPLIT = 4 * STEP8_TILE;
+// One user, 1020 / 4000 / 16000 slots: 12.4 / 13.5 / 15.3 us a step, with splits of 256
+// or more 13.1 / 14.4 / 16.2, of 1024 16.0 / 22.3 / 21.3.  Up to four rounds of slots
+// a block alone is faster than its parts and their join: 500 slots 11.1 and 11.8 us.
+constexpr int STEP8_BLOCKS = 768;
 static int step8_splits(int batch, int kv_heads, int cap) {
   int64_t n = STEP8_BLOCKS / ((int64_t)batch * kv_heads);
-  if (n > cap / STEP8_SPLIT) n = cap / STEP8_SPLIT;
+  if (cap <= 4 * STEP8_ROUND) n = 1;
+  if (n > cap / STEP8_ROUND) n = cap / STEP8_ROUND;
   if (n > STEP_MAX_SPLITS) n = STEP_MAX_SPLITS;
   return n > 1 ? (int)n : 1;
 }
