@@ -6,8 +6,8 @@
 
 namespace lat {
 
-// f over the lane's LANES (16, 32 or 64) neighbours: quads, halves of 16 lanes, 16,
-// 32, 64.  Every level joins two equal shares, so all lanes get the same bits.
+// f over the lane's LANES (2, 4, .. 64) neighbours.  Every level joins two equal
+// shares, so all lanes get the same bits.
 template <int LANES, typename V, typename F>
 __device__ inline V lanes_join(V x, F f) {
   auto dpp = [&](auto ctrl) __attribute__((always_inline)) {
@@ -15,9 +15,9 @@ __device__ inline V lanes_join(V x, F f) {
     x = f(x, __builtin_bit_cast(V, o));
   };
   dpp(std::integral_constant<int, 0xB1>());        // lane ^ 1
-  dpp(std::integral_constant<int, 0x4E>());        // lane ^ 2
-  dpp(std::integral_constant<int, 0x141>());       // mirrored in 8
-  dpp(std::integral_constant<int, 0x140>());       // mirrored in 16
+  if constexpr (LANES >= 4) dpp(std::integral_constant<int, 0x4E>());      // lane ^ 2
+  if constexpr (LANES >= 8) dpp(std::integral_constant<int, 0x141>());     // mirrored in 8
+  if constexpr (LANES >= 16) dpp(std::integral_constant<int, 0x140>());    // mirrored in 16
   if constexpr (LANES >= 32) {
     const uint32_t u = __builtin_bit_cast(uint32_t, x);
     const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);

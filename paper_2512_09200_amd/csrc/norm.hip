@@ -8,8 +8,8 @@
 // the backward needs no statistic of the forward.
 //
 // Bound by memory: every tensor is read or written once.  A row's elements stay
-// in registers between the sums and the results.  Narrow rows share a wave (16
-// or 32 lanes each), a row of up to 2048 columns has a wave, longer ones a
+// in registers between the sums and the results.  Narrow rows share a wave (2
+// to 32 lanes each), a row of up to 2048 columns has a wave, longer ones a
 // block.  Lanes hold groups of eight neighbouring columns (the generator's and
 // the codes' unit); waves walk the rows in steps of the grid with the gains
 // (and the gains' gradient) in registers, and the next row's loads go out before
@@ -87,8 +87,10 @@ __device__ inline void load_gain(const NormK& A, int lane, float (&g)[C::CH][8])
   Row8<float> r[C::CH];
 #pragma unroll
   for (int i = 0; i < C::CH; ++i) {
-    if (A.gain) r[i] = load8<float, TAIL>(A.gain, lane + i * C::STEP, A.cols);
-    else r[i].w[0] = r[i].w[1] = u32x4{0x3f800000u, 0x3f800000u, 0x3f800000u, 0x3f800000u};
+    if (A.gain) {
+      r[i] = load8<float, TAIL>(A.gain, lane + i * C::STEP, A.cols);
+      fix8<float, TAIL>(r[i], lane + i * C::STEP, A.cols);
+    } else r[i].w[0] = r[i].w[1] = u32x4{0x3f800000u, 0x3f800000u, 0x3f800000u, 0x3f800000u};
     r[i].get(g[i]);
   }
 }
@@ -125,10 +127,12 @@ __global__ __launch_bounds__(C::THREADS) void add_rmsnorm_fwd_kernel(NormK A) {
     float h[C::CH][8], s[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < C::CH; ++i) {
+      fix8<T, TAIL>(xr[i], at.lane + i * C::STEP, A.cols);
       xr[i].get(h[i]);
       if (A.drop.t) drop8(A.drop, key, at.lane + i * C::STEP, (uint32_t)row, h[i]);
       if (A.r.p) {
         float r[8];
+        fix8<T, TAIL>(rr[i], at.lane + i * C::STEP, A.cols);
         rr[i].get(r);
 #pragma unroll
         for (int e = 0; e < 8; ++e) h[i][e] += r[e];
@@ -224,6 +228,8 @@ __global__ __launch_bounds__(C::THREADS) void add_rmsnorm_bwd_kernel(NormK A) {
     Row8<T> add[C::CH];
 #pragma unroll
     for (int i = 0; i < C::CH; ++i) {
+      fix8<T, TAIL>(hr[i], at.lane + i * C::STEP, A.cols);
+      fix8<T, TAIL>(yr[i], at.lane + i * C::STEP, A.cols);
       hr[i].get(h[i]);
       yr[i].get(dn[i]);
       add[i] = rr[i];
@@ -240,6 +246,7 @@ __global__ __launch_bounds__(C::THREADS) void add_rmsnorm_bwd_kernel(NormK A) {
 #pragma unroll
     for (int i = 0; i < C::CH; ++i) {
       float r[8];
+      fix8<T, TAIL>(add[i], at.lane + i * C::STEP, A.cols);
       add[i].get(r);
       float g[8];
 #pragma unroll
@@ -316,6 +323,9 @@ __global__ __launch_bounds__(1024) void norm_dgain_kernel(const float* __restric
 template <typename F>
 static auto with_cfg(int cols, F f) {
   const int g = cdiv(cols, 8);
+  if (g <= 2) return f(RowCfg<2, 1, 1>());
+  if (g <= 4) return f(RowCfg<4, 1, 1>());
+  if (g <= 8) return f(RowCfg<8, 1, 1>());
   if (g <= 16) return f(RowCfg<16, 1, 1>());
   if (g <= 32) return f(RowCfg<32, 1, 1>());
   if (g <= 64) return f(RowCfg<64, 1, 1>());
@@ -435,6 +445,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(int64_t total, int cols, u
 #pragma unroll
   for (int i = 0; i < DROP_PER; ++i) {
     float f[8];
+    fix8<T, TAIL>(v[i], (int)g[i], cols);
     v[i].get(f);
     if (d.t) drop8(d, key, g[i], (uint32_t)row[i], f);
     v[i].put(f);

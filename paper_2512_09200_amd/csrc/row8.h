@@ -44,11 +44,11 @@ __device__ inline void shift8(Row8<float>& r, int n) {
   r.w[1] = b;
 }
 
-// Group g (columns 8 g .. 8 g + 7) of a row of `cols` elements; columns past the
-// row are zeros.  TAIL: cols is no multiple of 8; the last group is then read as
-// the row's last eight elements and shifted, so that no load leaves the row and
-// none is in a branch (a load in a branch is waited for there).
-// NT: past the caches (data that is larger than they are).
+// Group g (columns 8 g .. 8 g + 7) of a row of `cols` elements, as memory words that
+// fix8 makes the group's values of, where they are used: a load whose value is
+// selected or branched on at once is waited for there.  TAIL: cols is no multiple of
+// 8; the last group is read as the row's last eight elements, so that no load
+// leaves the row.  NT: past the caches (data that is larger than they are).
 template <typename T, bool TAIL, bool NT = false>
 __device__ inline Row8<T> load8(const T* row, int g, int cols) {
   Row8<T> r;
@@ -57,9 +57,7 @@ __device__ inline Row8<T> load8(const T* row, int g, int cols) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const T v = row[e < cols ? e : 0];
-      uint32_t u;
-      if constexpr (sizeof(T) == 2) u = v; else u = __float_as_uint(v);
-      x[e] = e < cols && g == 0 ? u : 0u;
+      if constexpr (sizeof(T) == 2) x[e] = v; else x[e] = __float_as_uint(v);
     }
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
@@ -77,24 +75,57 @@ __device__ inline Row8<T> load8(const T* row, int g, int cols) {
     const u32x4_any* q = reinterpret_cast<const u32x4_any*>(p + 16 * i);
     r.w[i] = NT ? __builtin_nontemporal_load(q) : *q;
   }
-  if (TAIL && 8 * g > cols - 8) shift8(r, 8 - (cols & 7));
-  if (8 * g >= cols) r.clear();
   return r;
+}
+
+// The group's values; columns past the row are zeros.
+template <typename T, bool TAIL>
+__device__ inline void fix8(Row8<T>& r, int g, int cols) {
+  if (TAIL && 8 * g > cols - 8) {
+    if (cols < 8) {                                   // (read in their own places)
+      Row8<T> m = r;
+      r.clear();
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < cols) {
+          if constexpr (sizeof(T) == 2) r.w[0][e >> 1] |= m.w[0][e >> 1] & (e & 1 ? 0xffff0000u : 0xffffu);
+          else r.w[e >> 2][e & 3] = m.w[e >> 2][e & 3];
+        }
+    } else {
+      shift8(r, 8 - (cols & 7));
+    }
+  }
+  if (8 * g >= cols) r.clear();
 }
 
 template <typename T, bool TAIL, bool NT = false>
 __device__ inline void store8(T* row, int g, int cols, const Row8<T>& r) {
   if (8 * g >= cols) return;
+  char* p = reinterpret_cast<char*>(row + 8 * g);
   if (TAIL && 8 * g > cols - 8) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (8 * g + e < cols) {
-        if constexpr (sizeof(T) == 2) row[8 * g + e] = (bf16_t)(r.w[0][e >> 1] >> (16 * (e & 1)));
-        else row[8 * g + e] = __uint_as_float(r.w[e >> 2][e & 3]);
-      }
+    // four, two and one elements, as cols has them
+    Row8<T> s = r;
+    typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+    typedef uint32_t u32_any __attribute__((aligned(2)));
+    constexpr int B = sizeof(T);
+    if (cols & 4) {
+      if constexpr (B == 2) *reinterpret_cast<u32x2_any*>(p) = u32x2_any{s.w[0][0], s.w[0][1]};
+      else *reinterpret_cast<u32x4_any*>(p) = s.w[0];
+      p += 4 * B;
+      shift8(s, 4);
+    }
+    if (cols & 2) {
+      if constexpr (B == 2) *reinterpret_cast<u32_any*>(p) = s.w[0][0];
+      else *reinterpret_cast<u32x2_any*>(p) = u32x2_any{s.w[0][0], s.w[0][1]};
+      p += 2 * B;
+      shift8(s, 2);
+    }
+    if (cols & 1) {
+      if constexpr (B == 2) *reinterpret_cast<bf16_t*>(p) = (bf16_t)s.w[0][0];
+      else *reinterpret_cast<float*>(p) = __uint_as_float(s.w[0][0]);
+    }
     return;
   }
-  char* p = reinterpret_cast<char*>(row + 8 * g);
 #pragma unroll
   for (int i = 0; i < Row8<T>::W; ++i) {
     u32x4_any* q = reinterpret_cast<u32x4_any*>(p + 16 * i);
