@@ -7,13 +7,15 @@
 // mean(dn n) = rho sum(dn h) / cols, so one sweep takes both sums of a row, and
 // the backward needs no statistic of the forward.
 //
-// Bound by memory: every tensor is read or written once.  A row's elements stay
-// in registers between the sums and the results.  Narrow rows share a wave (2
-// to 32 lanes each), a row of up to 2048 columns has a wave, longer ones a
-// block.  Lanes hold groups of eight neighbouring columns (the generator's and
-// the codes' unit); waves walk the rows in steps of the grid with the gains
-// (and the gains' gradient) in registers, and the next row's loads go out before
-// a row's sums.
+// Bound by memory: every tensor is read or written once.  131072 rows of 1024, bf16,
+// residual and dropout: forward 193 us, backward 237 (5.6 and 5.7 TB/s of what they
+// cannot do without; a copy of 0.5 GB reaches 5.3); 8192 rows to codes 14 us (4.3);
+// dropout alone 79 us (6.8).  A row's elements stay in registers between the sums
+// and the results.  Narrow rows share a wave (2 to 32 lanes each), a row of up to
+// 1024 columns has a wave, longer ones a block.  Lanes hold groups of eight
+// neighbouring columns (the generator's and the codes' unit); waves walk the rows in
+// steps of the grid with the gains (and the gains' gradient) in registers, and the
+// next row's loads go out before a row's sums.
 //
 // Sums are fp32; the residual sum is rounded to the storage type before the norm,
 // so that the backward differentiates what the forward computed.
@@ -319,8 +321,14 @@ __global__ __launch_bounds__(1024) void norm_dgain_kernel(const float* __restric
   if (y == 0 && c < cols) dgain[c] = sum[0][x];
 }
 
-// Calls f(RowCfg) with the narrowest configuration that holds `cols`.
-template <typename F>
+// Calls f(RowCfg) with the narrowest configuration that holds `cols`: lanes a row as
+// few as its groups fill (1M rows of 16, bf16: forward 22 us with two, 112 with 16), two
+// groups a lane and more waves a row from there on (four groups left two waves a
+// SIMD: 2048 rows of 8192, bf16, backward 68 us, so 32).  The longest rows' backward, with four
+// sets of values a group, does not fit the 128 registers of a block of 16 waves: 2048
+// rows of 16384, bf16 / fp32, 72 / 126 us so, 132 / 373 with 16 waves, whose
+// forward is the faster one (53 and 55).
+template <bool BWD, typename F>
 static auto with_cfg(int cols, F f) {
   const int g = cdiv(cols, 8);
   if (g <= 2) return f(RowCfg<2, 1, 1>());
@@ -333,10 +341,14 @@ static auto with_cfg(int cols, F f) {
   if (g <= 256) return f(RowCfg<64, 2, 2>());
   if (g <= 512) return f(RowCfg<64, 2, 4>());
   if (g <= 1024) return f(RowCfg<64, 2, 8>());
-  return f(RowCfg<64, 4, 8>());
+  return f(std::conditional_t<BWD, RowCfg<64, 4, 8>, RowCfg<64, 2, 16>>());
 }
 
-// Blocks of a launch: rows in steps of the grid, at most `most` waves in all.
+// Blocks of a launch: rows in steps of the grid, at most `most` waves in all: few
+// enough that a wave's gains serve several rows and its next loads are out before a
+// row's sums.  131072 / 8192 rows of 1024, bf16: forward 194 / 13.6 us with 4096 waves, 195 /
+// 14.0 with 8192; backward (and 2048 rows of 8192) 257 / 32 us with 2048, 263 / 38 with 4096,
+// 259 / 43 with 1024.
 template <typename C>
 static int norm_blocks(int64_t rows, int most) {
   const int64_t n = cdiv(rows, C::RPB), cap = most / (C::THREADS / 64);
@@ -369,7 +381,7 @@ static NormK norm_k(const NormArgs& a) {
 hipError_t add_rmsnorm_fwd(const NormArgs& a, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
   const NormK A = norm_k(a);
-  with_cfg(a.cols, [&](auto cfg) {
+  with_cfg<false>(a.cols, [&](auto cfg) {
     using C = decltype(cfg);
     const int n = norm_blocks<C>(a.rows, NORM_FWD_WAVES);
     const bool tail = a.cols % 8 != 0;
@@ -387,7 +399,7 @@ hipError_t add_rmsnorm_fwd(const NormArgs& a, hipStream_t s) {
 }
 
 static int norm_bwd_blocks(int64_t rows, int cols) {
-  return with_cfg(cols, [&](auto cfg) { return norm_blocks<decltype(cfg)>(rows, NORM_BWD_WAVES); });
+  return with_cfg<true>(cols, [&](auto cfg) { return norm_blocks<decltype(cfg)>(rows, NORM_BWD_WAVES); });
 }
 
 size_t add_rmsnorm_bwd_workspace(int64_t rows, int cols) {
@@ -400,7 +412,7 @@ hipError_t add_rmsnorm_bwd(const NormArgs& a, void* ws, hipStream_t s) {
   const int n = a.rows > 0 ? norm_bwd_blocks(a.rows, a.cols) : 0;
   const int tensors = 2 + !!a.dh.p + !!a.dr.p + !!a.dx.p;
   if (n > 0) {
-    with_cfg(a.cols, [&](auto cfg) {
+    with_cfg<true>(a.cols, [&](auto cfg) {
       using C = decltype(cfg);
       auto launch = [&](auto kern) { kern<<<n, C::THREADS, 0, s>>>(A); };
       const bool tail = a.cols % 8 != 0, nt = (double)a.rows * a.cols * (a.dt == DT_BF16 ? 2 : 4) * tensors > CACHED_BYTES;
