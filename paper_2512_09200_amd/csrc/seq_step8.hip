@@ -485,7 +485,8 @@ hipError_t seq_step8(const SeqStepArgs& a, const SeqCache8Args& c, const RopeTur
 }
 
 // ---------------------------------------------------------------------------
-// Fill.  A wave takes a block of 16 slots of k or v of a key head.  The slots that
+// Fill.  A wave takes a block of 16 slots of a key head, keys and values (bf16 heads
+// above 64: one of them).  The slots that
 // a sequence's rows go to are at most three ranges (sinks, and the window's, which
 // may wrap); their blocks are numbered through, each once.  Reads and writes the
 // kept rows once.
@@ -524,46 +525,66 @@ struct SlotRanges {
   }
 };
 
+// Keys and values of a block by one wave, both loads out together, or by two.  Two:
+// bf16 heads of 128, whose registers would leave four waves a SIMD instead of five
+// (153600 kept rows, 2 heads: 44 us, by one 46).  One: 100000 histories of 5, a head of
+// 32, 70 us, by two 144; fp32, 8000 of 20, 2 heads of 128, 84 and 101.
+template <typename T, int DP> struct Fill8Cfg { static constexpr int SIDES = sizeof(T) == 2 && DP == 128 ? 1 : 2; };
+
 template <typename T, int DP>
 __global__ __launch_bounds__(256) void seq_fill8_kernel(SeqCache8Args C, int rows, const int32_t* __restrict__ off, int S,
                                                         const int32_t* __restrict__ first, SeqTensor k, SeqTensor v,
-                                                        int ld, int nb) {
+                                                        int ld, int nb, int per_seq) {
   using B8 = Block8<T, DP>;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), cap = C.sinks + C.window;
-  for (int s = blockIdx.y; s < S; s += gridDim.y) {
+  constexpr int SIDES = Fill8Cfg<T, DP>::SIDES;
+  const int cap = C.sinks + C.window;
+  const int wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+  // groups of per_seq waves take sequences in turn; waves that make no whole group are left out
+  const int group = wave / per_seq, groups = (int)(gridDim.x * 4) / per_seq;
+  if (group >= groups) return;
+  for (int s = group; s < S; s += groups) {
     const int ci = __builtin_amdgcn_readfirstlane(C.index ? C.index[s] : s);
-    if (ci < 0 || ci >= C.num_caches) continue;
     const int a = max(__builtin_amdgcn_readfirstlane(off[s]), 0), e = min(__builtin_amdgcn_readfirstlane(off[s + 1]), rows);
     const int f = first ? __builtin_amdgcn_readfirstlane(first[s]) : 0;
-    if (e <= a || f < 0) continue;
+    if (ci < 0 || ci >= C.num_caches || e <= a || f < 0) continue;
     const uint32_t total = (uint32_t)f + (uint32_t)(e - a);
     const SlotRanges R((uint32_t)f, total, C.sinks, C.window);
-    const int64_t items = (int64_t)R.count * C.kv_heads * 2;
-    for (int64_t it = blockIdx.x * 4 + w; it < items; it += (int64_t)gridDim.x * 4) {
-      const int vside = (int)(it & 1), h = (int)((it >> 1) % C.kv_heads), blk = R.block((int)((it >> 1) / C.kv_heads));
-      const SeqTensor& t = vside ? v : k;
+    const int sides = 2 / SIDES;                 // items of a block and head
+    const int64_t items = (int64_t)R.count * C.kv_heads * sides;
+    for (int64_t it = wave % per_seq; it < items; it += per_seq) {
+      const int side = (int)(it % sides), h = (int)(it / sides % C.kv_heads);
+      const int blk = R.block((int)(it / sides / C.kv_heads));
       const int64_t head = (int64_t)ci * C.kv_heads + h;
-      uint8_t* const codes = (vside ? C.vc : C.kc) + head * cap * ld;
-      float* const sp = (vside ? C.vs : C.ks) + head * nb + blk;
       // the last position that is in the lane's slot, and whether this call brings it
       const int slot = blk * CACHE8_BLOCK + B8::slot();
       const bool reached = slot < cap && (uint32_t)slot < total;
       uint32_t p = (uint32_t)slot;
       if (reached && slot >= C.sinks) p = total - 1 - (total - 1 - (uint32_t)slot) % (uint32_t)C.window;
-      const bool fresh = reached && p >= (uint32_t)f;
-      B8 x;
-      x.load_row((const T*)t.p + (a + (int64_t)(fresh ? p - (uint32_t)f : 0u)) * t.ld + h * C.dim, C.dim, fresh);
-      x.old = reached && !fresh;
-      float s1;
-      if (!wave_any(x.old) && x.fresh_scale(&s1)) {
-        x.encode_fresh(s1, codes + (int64_t)slot * ld, ld);
-      } else {
-        x.s0 = *sp;
-        x.load_codes(codes + (int64_t)(x.old ? slot : blk * CACHE8_BLOCK) * ld, ld);
-        s1 = x.scale(C.dim);
-        x.encode(s1, C.dim, codes + (int64_t)slot * ld, ld, fresh || (x.old && s1 != x.s0), nullptr);
+      const bool fresh = reached && p >= (uint32_t)f, old = reached && !fresh, any_old = wave_any(old);
+      const int64_t row = a + (int64_t)(fresh ? p - (uint32_t)f : 0u);
+      B8 x[SIDES];                               // keys, values; or what `side` says
+#pragma unroll
+      for (int i = 0; i < SIDES; ++i) {
+        const SeqTensor& t = side + i ? v : k;
+        x[i].load_row((const T*)t.p + row * t.ld + h * C.dim, C.dim, fresh);
       }
-      if ((threadIdx.x & 63) == 0) *sp = s1;
+#pragma unroll
+      for (int i = 0; i < SIDES; ++i) {
+        uint8_t* const base = (side + i ? C.vc : C.kc) + head * cap * ld;
+        uint8_t* const codes = base + (int64_t)slot * ld;
+        float* const sp = (side + i ? C.vs : C.ks) + head * nb + blk;
+        x[i].old = old;
+        float s1;
+        if (!any_old && x[i].fresh_scale(&s1)) {
+          x[i].encode_fresh(s1, codes, ld);
+        } else {
+          x[i].s0 = *sp;
+          x[i].load_codes(old ? codes : base + (int64_t)blk * CACHE8_BLOCK * ld, ld);
+          s1 = x[i].scale(C.dim);
+          x[i].encode(s1, C.dim, codes, ld, fresh || (old && s1 != x[i].s0), nullptr);
+        }
+        if ((threadIdx.x & 63) == 0) *sp = s1;
+      }
     }
   }
 }
@@ -571,15 +592,20 @@ __global__ __launch_bounds__(256) void seq_fill8_kernel(SeqCache8Args C, int row
 hipError_t seq_cache8_fill(const SeqCache8Args& c, int64_t rows, const int32_t* offsets, int num_seqs,
                            const int32_t* first, SeqTensor k, SeqTensor v, hipStream_t s) {
   if (rows == 0 || num_seqs == 0) return hipSuccess;
+  const int D = c.dim;
   // a wave an item where the sequences have the mean length
   const int64_t mean = cdiv(rows, num_seqs), cap = (int64_t)c.sinks + c.window;
   const int64_t blocks = (mean < cap ? mean : cap) / CACHE8_BLOCK + 1;
-  int bx = cdiv(blocks * c.kv_heads * 2, 4);
-  if (bx > 1024) bx = 1024;
-  const int by = num_seqs < 65535 ? num_seqs : 65535;
+  int64_t per_seq = blocks * c.kv_heads * (c.dt == DT_BF16 && D > 64 ? 2 : 1);
+  if (per_seq > 4096) per_seq = 4096;
+  int64_t n = cdiv(per_seq * num_seqs, 4);
+  const int64_t most = (int64_t)1 << 20;
+  if (n > most) n = most;
+  if (n * 4 < per_seq) n = cdiv(per_seq, 4);
   const int ld = cache8_ld(c.dim), nb = cdiv(cap, CACHE8_BLOCK);
-  auto launch = [&](auto kern) { kern<<<dim3(bx, by), 256, 0, s>>>(c, (int)rows, offsets, num_seqs, first, k, v, ld, nb); };
-  const int D = c.dim;
+  auto launch = [&](auto kern) {
+    kern<<<(int)n, 256, 0, s>>>(c, (int)rows, offsets, num_seqs, first, k, v, ld, nb, (int)per_seq);
+  };
   if (c.dt == DT_BF16) {
     if (D <= 32) launch(seq_fill8_kernel<bf16_t, 32>);
     else if (D <= 64) launch(seq_fill8_kernel<bf16_t, 64>);

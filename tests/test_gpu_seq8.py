@@ -346,6 +346,41 @@ def test_caches_beyond_4_gib():
     assert not k[:C - 1].any()
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_millions_of_sequences(dt):
+    """More sequences than a launch has waves for: the same as from calls of a few
+    hundred thousand, and blocks that hold older events are made anew once."""
+    from paper_2512_09200_amd import api
+    S, J, D, W = 1_500_000, 3, 8, 5
+    k, v = (torch.randn(2 * S, J, D, device=DEV, dtype=TT[dt]) for _ in "kv")
+    k[1::2] *= 100
+    whole = [torch.zeros(S, J, W, 16, dtype=torch.uint8, device=DEV) for _ in "kv"] + [
+        torch.ones(S, J, 1, device=DEV) for _ in "kv"]
+    parts = [t.clone() for t in whole]
+    index = torch.randperm(S, device=DEV).int()
+
+    def fill(caches, a, b, at, first):
+        n = b - a
+        s = api.lattice_seq_plan(torch.arange(n + 1, device=DEV, dtype=torch.int32), n)
+        x, y = k[at::2][a:b], v[at::2][a:b]
+        api.lattice_seq_cache8_fill(s, x.contiguous(), y.contiguous(), *caches, W, cache_index=index[a:b].contiguous(),
+                                    first=torch.full((n,), first, dtype=torch.int32, device=DEV))
+
+    for at in (0, 1):
+        fill(whole, 0, S, at, at)
+        for a in range(0, S, 250_000):
+            fill(parts, a, a + 250_000, at, at)
+    for a, b in zip(whole, parts):
+        assert torch.equal(a, b)
+    host = dict(k=np.zeros((3, J, W, 16), np.uint8), v=np.zeros((3, J, W, 16), np.uint8), ks=np.ones((3, J, 1), np.float32),
+                vs=np.ones((3, J, 1), np.float32))
+    for i, s in enumerate((0, 777_777, S - 1)):
+        for at in (0, 1):
+            c8.put(host, i, {at: (f64(k[2 * s + at]), f64(v[2 * s + at]))}, at + 1)
+    pick = index[[0, 777_777, S - 1]].long()
+    same([t[pick] for t in whole], host)
+
+
 @pytest.mark.parametrize("long", [False, True])
 def test_a_step_in_a_graph_that_advances_by_itself(long):
     from paper_2512_09200_amd import api
