@@ -95,7 +95,7 @@ struct SeqCache8Args {
 };
 inline int cache8_ld(int dim) { return (dim + 15) / 16 * 16; }   // bytes of a slot's codes
 hipError_t seq_cache8_fill(const SeqCache8Args& c, int64_t rows, const int32_t* offsets, int num_seqs,
-                           const int32_t* first, SeqTensor k, SeqTensor v, hipStream_t s);
+                           int64_t max_len, const int32_t* first, SeqTensor k, SeqTensor v, hipStream_t s);
 size_t seq_step8_workspace(int batch, int heads, int kv_heads, int dim, int cap);
 // a.c is not read
 hipError_t seq_step8(const SeqStepArgs& a, const SeqCache8Args& c, const RopeTurns& t, void* ws, hipStream_t s);

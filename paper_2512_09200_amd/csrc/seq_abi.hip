@@ -393,7 +393,8 @@ lattice_status lattice_seq_cache8_fill(const lattice_seq_attn_desc* d, const lat
   REQUIRE(seqs->offsets, "null offsets");
   TRY(check_tensor("k", k, k_stride, d->kv_heads, d->head_dim));
   TRY(check_tensor("v", v, v_stride, d->kv_heads, d->head_dim));
-  HIPRET(seq_cache8_fill(cache8_args(d, cache, cache_index), seqs->rows, seqs->offsets, seqs->num_seqs, first,
+  HIPRET(seq_cache8_fill(cache8_args(d, cache, cache_index), seqs->rows, seqs->offsets, seqs->num_seqs,
+                         seqs->max_len < seqs->rows ? seqs->max_len : seqs->rows, first,
                          tensor(k, k_stride), tensor(v, v_stride), strm(stream)));
   return LATTICE_OK;
 }

@@ -105,6 +105,31 @@ def test_fill(dt, J, D, W, N, spread):
     same(kc, host, "second fill")
 
 
+@pytest.mark.parametrize("dt,J,D,W,N", [("bf16", 2, 64, 500, 3), ("f32", 1, 40, 2000, 0), ("bf16", 3, 128, 90, 17)])
+@pytest.mark.parametrize("max_len", [0, 900, 5])
+def test_long_histories_among_many_short_ones(dt, J, D, W, N, max_len):
+    """Long ones are spread over waves of their own (max_len 5: a wrong bound costs
+    time, not results); empty ones, and rows behind the last, in between."""
+    from paper_2512_09200_amd import api
+    rng = np.random.default_rng(W)
+    lens = np.array([3, 0, 1, 5] * 60)
+    lens[[0, 101, 239]] = 900, 333, 128
+    S, cap = len(lens), W + N
+    off = np.concatenate([[0], np.cumsum(lens)])
+    rows = int(off[-1]) + 70
+    host = new_caches(S, J, cap, D)
+    kc = to_gpu(host)
+    k, v = (rows_of(rng, dt, rows, J, D, 1) for _ in "kv")
+    index = rng.permutation(S)
+    s = api.lattice_seq_plan(i32(off), rows, max_len=max_len)
+    api.lattice_seq_cache8_fill(s, k, v, *kc, W, N, cache_index=i32(index))
+    c8.fill(host, f64(k), f64(v), off, W, N, index, np.zeros(S, int))
+    same(kc, host, "fill")
+    api.lattice_seq_cache8_fill(s, v, k, *kc, W, N, cache_index=i32(index), first=i32(lens))
+    c8.fill(host, f64(v), f64(k), off, W, N, index, lens)
+    same(kc, host, "second fill")
+
+
 def test_fill_of_positions_next_to_the_end_of_int32():
     from paper_2512_09200_amd import api
     rng = np.random.default_rng(0)
