@@ -302,7 +302,8 @@ __global__ __launch_bounds__(C::THREADS) void add_rmsnorm_bwd_kernel(NormK A) {
 }
 
 // dgain from the blocks' sums: 16 columns a block, 64 strands of rows of `part`,
-// joined in strand order.
+// joined in a fixed order.  512 rows of 1024 columns: 4.5 us, of which a launch that
+// has nothing to do would take 2.
 __global__ __launch_bounds__(1024) void norm_dgain_kernel(const float* __restrict__ part, int n, int cols,
                                                           float* __restrict__ dgain) {
   __shared__ float sum[64][17];
@@ -434,7 +435,9 @@ hipError_t add_rmsnorm_bwd(const NormArgs& a, void* ws, hipStream_t s) {
 
 // ---------------------------------------------------------------------------
 // Dropout alone.  A block takes DROP_GROUPS neighbouring groups of eight columns
-// of the whole matrix, each thread every 256th.  Memory: one read, one write.
+// of the whole matrix, each thread every 256th.  One read and one write of memory:
+// 131072 x 1024, bf16, 79 to 91 us (6.8 to 5.9 TB/s), the generator's ten rounds and the
+// selection issuing in 73% of the cycles.
 constexpr int DROP_PER = 4, DROP_GROUPS = 256 * DROP_PER;
 
 template <typename T, bool TAIL, bool NT>
