@@ -4,7 +4,7 @@
 //
 // Memory bound: every visible slot's two rows of codes are read once, half the
 // bytes of bf16.  Work is split as in the bf16 step: a block is a user, a key head
-// and a split of the slots, its four waves take tiles of 32 slots in turn with
+// and a split of the slots (short windows of many users: a wave is), its four waves take tiles of 32 slots in turn with
 // their own running maximum, sum and output.  Codes become bf16 in registers
 // (exactly: three bits of fraction) and go to 16x16x32 matrix instructions; a
 // block's scale multiplies the 16 scores of its slots and their probabilities.
@@ -43,6 +43,7 @@ struct Step8K {
   SeqCache8Args c;
   int heads, group, cap, ld, nb;             // bytes of a slot, blocks of a cache and head
   int work;                                  // bytes of LDS for tiles and join
+  int items;                                 // users x key heads x groups of heads (one wave each)
   int hg0, hgs, append;                      // this launch's groups of 16 query heads; whether it brings the events
   float eps, inv_dim;
   int rope, rotary, inter;
@@ -96,28 +97,41 @@ template <int DP> struct Tile8 {
 // LDS: the waves' value tiles, over them the join of the waves (`heads` of 16 head
 // columns); the query's fragments; the new k and v; the block's codes, k then v,
 // and its scales.
-template <typename T, int DP> struct Step8Cfg {
+template <typename T, int DP, int WPI> struct Step8Cfg {
   static constexpr int PARTS = sizeof(T) == 2 ? 2 : 3;
-  static constexpr int JROW = DP + 4, VT = 4 * Tile8<DP>::BYTES;
+  static constexpr int JROW = DP + 4, VT = WPI * Tile8<DP>::BYTES;
   static constexpr int QF = DP / 32 * PARTS * 1024;
   static constexpr int KN = QF, COPY = KN + 2 * DP * 4, SC = COPY + 2 * CACHE8_BLOCK * DP, REST = SC + 16;
   __host__ __device__ static constexpr int work(int heads) {
-    return 16 * heads * JROW > VT ? 16 * heads * JROW : VT;
+    return ((4 * WPI * heads * JROW > VT ? 4 * WPI * heads * JROW : VT) + 15) & ~15;
   }
 };
 
-template <typename T, int DP>
+template <typename T, int DP, int WPI>
 __global__ __launch_bounds__(256, 3) void seq_step8_kernel(Step8K A, RopeTurns turns) {
-  using Cfg = Step8Cfg<T, DP>;
+#pragma clang fp contract(off)                       // the same roundings whichever kernel a batch gets
+  using Cfg = Step8Cfg<T, DP, WPI>;
   using TL = Tile8<DP>;
   using B8 = Block8<float, DP>;
   constexpr int NP = Cfg::PARTS, KS = DP / 32, OB = DP / 16, KV = DP == 128 ? 2 : 1, UPR = TL::UPR;
   constexpr int R = STEP8_TILE / CACHE8_BLOCK, VL = R * UPR / 4;     // scale blocks of a tile, value loads of a lane
   typedef typename std::conditional<DP == 32, u32x2, u32x4>::type KVec;
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  extern __shared__ __attribute__((aligned(1024))) char smem_all[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int w = WPI == 1 ? 0 : wave;                 // of the item's waves
   const int g16 = lane >> 4, l16 = lane & 15, D = A.c.dim, ns = A.j.ns;
-  int blk = blockIdx.x;
+  int blk = WPI == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
+  if (WPI == 1 && blk >= A.items) return;
+  char* const smem = smem_all + (WPI == 1 ? wave * (A.work + Cfg::REST) : 0);
+  // what the item's waves have written to LDS is there for them
+  auto item_sync = [&]() {
+    if constexpr (WPI == 1) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_wave_barrier();
+    } else {
+      __syncthreads();
+    }
+  };
   const int u = blk % ns; blk /= ns;
   const int hg = A.hg0 + blk % A.hgs; blk /= A.hgs;
   const int kv = blk % A.c.kv_heads, b = blk / A.c.kv_heads;
@@ -137,17 +151,22 @@ __global__ __launch_bounds__(256, 3) void seq_step8_kernel(Step8K A, RopeTurns t
   float* const kn = reinterpret_cast<float*>(rest + Cfg::KN);         // k, v
   char* const copy = rest + Cfg::COPY;
   float* const sc = reinterpret_cast<float*>(rest + Cfg::SC);
-  char* const VS = smem + w * TL::BYTES;
+  char* const VS = smem + w * TL::BYTES;             // the wave's value tile
 
-  // The event's block: made anew by waves 0 (keys) and 1 (values) of the split that
-  // holds the slot (in a launch for further query heads it has been)
+  // The event's block: made anew by waves 0 (keys) and 1 (values; or by the only wave
+  // both) of the split that holds the slot (in a launch for further query heads it
+  // has been)
   const bool owner = A.append && slot >= a0 && slot < a1;
   const int sb = slot & ~(CACHE8_BLOCK - 1);
+  constexpr int SIDES = WPI == 1 ? 2 : 1;
   const bool remake = owner && w < 2;
-  B8 x8;
+  B8 x8[SIDES];
   if (remake) {
-    x8.load_codes((w == 0 ? kc : vc) + (int64_t)min(sb + B8::slot(), n - 1) * A.ld, A.ld);
-    x8.s0 = (w == 0 ? ks : vs)[sb / CACHE8_BLOCK];
+#pragma unroll
+    for (int i = 0; i < SIDES; ++i) {
+      x8[i].load_codes((w + i == 0 ? kc : vc) + (int64_t)min(sb + B8::slot(), n - 1) * A.ld, A.ld);
+      x8[i].s0 = (w + i == 0 ? ks : vs)[sb / CACHE8_BLOCK];
+    }
   }
   // the event's own vectors, a row a wave: pairs (x0, y0) of dimensions
   const int np = A.rotary >> 1, nh = min(STEP_HEADS, A.group - hg * STEP_HEADS), h0 = kv * A.group + hg * STEP_HEADS;
@@ -161,10 +180,12 @@ __global__ __launch_bounds__(256, 3) void seq_step8_kernel(Step8K A, RopeTurns t
     x = ld(src + xl);
     y = ld(src + yl);
   };
-  const int first_q = (w + 2) & 3;                   // query rows: waves 2 and 3 first
-  float qx, qy, ex = 0.f, ey = 0.f, gqx = 1.f, gqy = 1.f, gkx = 1.f, gky = 1.f;
+  const int first_q = WPI == 1 ? 0 : (w + 2) & 3;    // query rows: waves 2 and 3 first
+  float qx, qy, ex[SIDES], ey[SIDES], gqx = 1.f, gqy = 1.f, gkx = 1.f, gky = 1.f;
   row_of(A.q, h0 + min(first_q, nh - 1), qx, qy);
-  if (remake) row_of(w == 0 ? A.k : A.v, kv, ex, ey);
+  if (remake)
+#pragma unroll
+    for (int i = 0; i < SIDES; ++i) row_of(w + i == 0 ? A.k : A.v, kv, ex[i], ey[i]);
   if (A.gq) { gqx = A.gq[xl]; gqy = A.gq[yl]; }
   if (A.gk) { gkx = A.gk[xl]; gky = A.gk[yl]; }
   const int pos = A.pos ? A.pos[b] : p;
@@ -214,46 +235,55 @@ __global__ __launch_bounds__(256, 3) void seq_step8_kernel(Step8K A, RopeTurns t
     zy = ty;
   };
   if (remake) {
-    if (!on) ex = ey = 0.f;
-    if (A.rope && w == 0) {
-      if constexpr (sizeof(T) == 4) {
-        // An fp32 key is rounded to eight bits next; its norm and rotation are
-        // taken in 64, so that which code it gets does not hang on the order of
-        // a sum (one row a user).
-        const double dx = ex, dy = ey, rr = 1.0 / sqrt(wave_sum(dx * dx + dy * dy) / D + (double)A.eps);
-        const double ux = dx * rr * gkx, uy = dy * rr * gky;
-        double c = 1.0, s = 0.0;
-        if (rot) {
-          const double t = (double)pos * turns.f[lane];
-          sincospi(2.0 * (t - rint(t)), &s, &c);
+#pragma unroll
+    for (int i = 0; i < SIDES; ++i) {
+      const int side = w + i;                        // 0: k, 1: v
+      float zx = on ? ex[i] : 0.f, zy = on ? ey[i] : 0.f;
+      if (A.rope && side == 0) {
+        if constexpr (sizeof(T) == 4) {
+          // An fp32 key is rounded to eight bits next; its norm and rotation are
+          // taken in 64, so that which code it gets does not hang on the order of
+          // a sum (one row a user).
+          const double dx = zx, dy = zy, rr = 1.0 / sqrt(wave_sum(dx * dx + dy * dy) / D + (double)A.eps);
+          const double ux = dx * rr * gkx, uy = dy * rr * gky;
+          double c = 1.0, s = 0.0;
+          if (rot) {
+            const double t = (double)pos * turns.f[lane];
+            sincospi(2.0 * (t - rint(t)), &s, &c);
+          }
+          zx = (float)(ux * c - uy * s);
+          zy = (float)(ux * s + uy * c);
+        } else {
+          norm_rope(zx, zy, gkx, gky);
         }
-        ex = (float)(ux * c - uy * s);
-        ey = (float)(ux * s + uy * c);
-      } else {
-        norm_rope(ex, ey, gkx, gky);
       }
-    }
-    if (x0 < DP) {
-      kn[w * DP + x0] = on ? ld_round<T>(ex) : 0.f;
-      kn[w * DP + y0] = on ? ld_round<T>(ey) : 0.f;
-    }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the wave reads what its other lanes have just written
-    const int row = sb + B8::slot();
-    x8.load_row(kn + w * DP, DP, row == slot);
-    x8.old = row != slot && row < n;
-    const float s1 = x8.scale(D);
-    x8.encode(s1, D, (w == 0 ? kc : vc) + (int64_t)row * A.ld, A.ld, x8.fresh || (x8.old && s1 != x8.s0),
-              reinterpret_cast<uint8_t*>(copy) + (w * CACHE8_BLOCK + B8::slot()) * DP);
-    if (lane == 0) {
-      (w == 0 ? ks : vs)[sb / CACHE8_BLOCK] = s1;
-      sc[w] = s1;
+      if (x0 < DP) {
+        kn[side * DP + x0] = on ? ld_round<T>(zx) : 0.f;
+        kn[side * DP + y0] = on ? ld_round<T>(zy) : 0.f;
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the wave reads what its other lanes have just written
+      const int row = sb + B8::slot();
+      B8& x = x8[i];
+      x.load_row(kn + side * DP, DP, row == slot);
+      x.old = row != slot && row < n;
+      const float s1 = x.scale(D);
+      x.encode(s1, D, (side == 0 ? kc : vc) + (int64_t)row * A.ld, A.ld, x.fresh || (x.old && s1 != x.s0),
+               reinterpret_cast<uint8_t*>(copy) + (side * CACHE8_BLOCK + B8::slot()) * DP);
+      if (lane == 0) {
+        (side == 0 ? ks : vs)[sb / CACHE8_BLOCK] = s1;
+        sc[side] = s1;
+      }
     }
   }
   // The query's parts: those of element d of row r are element e of lane 16 g + r in
   // the fragment of step i, (i, g, e) as the keys' loads have them.
-  for (int r = first_q; r < STEP_HEADS; r += 4) {
+  if constexpr (WPI == 1) {                          // rows past the heads: zeros at once
+#pragma unroll
+    for (int i = 0; i < KS * NP; ++i) *reinterpret_cast<u32x4*>(rest + (i * 64 + lane) * 16) = u32x4{0u, 0u, 0u, 0u};
+  }
+  for (int r = first_q; r < (WPI == 1 ? nh : STEP_HEADS); r += WPI) {
     float zx = qx, zy = qy;
-    if (r + 4 < nh) row_of(A.q, h0 + r + 4, qx, qy);
+    if (r + WPI < nh) row_of(A.q, h0 + r + WPI, qx, qy);
     if (!on || r >= nh) zx = zy = 0.f;
     if (A.rope && r < nh) norm_rope(zx, zy, gqx, gqy);
     auto put = [&](int d, float z) {
@@ -270,7 +300,7 @@ __global__ __launch_bounds__(256, 3) void seq_step8_kernel(Step8K A, RopeTurns t
       put(y0, zy);
     }
   }
-  __syncthreads();
+  item_sync();
 
   const float c = A.j.scale * STEP_LOG2E;
   f32x4 o[OB];
@@ -278,7 +308,7 @@ __global__ __launch_bounds__(256, 3) void seq_step8_kernel(Step8K A, RopeTurns t
   for (int i = 0; i < OB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
 #pragma unroll 1
-  for (int t = w; t < tiles; t += 4) {
+  for (int t = w; t < tiles; t += WPI) {
     const int j0 = a0 + t * STEP8_TILE, nk = min(STEP8_TILE, a1 - j0);
     const int nr = owner && sb >= j0 && sb < j0 + STEP8_TILE ? (sb - j0) / CACHE8_BLOCK : -1;   // the event's block here
     // values to the wave's LDS rows; slots that are not there are zeros
@@ -300,7 +330,7 @@ __global__ __launch_bounds__(256, 3) void seq_step8_kernel(Step8K A, RopeTurns t
           for (int i = 0; i < KV; ++i)
             lk[r * KV + i] = *reinterpret_cast<const KVec*>(copy + l16 * DP + (DP == 32 ? 8 * g16 : 64 * i + 16 * g16));
     }
-    if (t + 4 < tiles) issue_v(t + 4);                   // into the registers that are free now
+    if (t + WPI < tiles) issue_v(t + WPI);               // into the registers that are free now
     f32x4 s[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) s[r] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -336,7 +366,7 @@ __global__ __launch_bounds__(256, 3) void seq_step8_kernel(Step8K A, RopeTurns t
         tm = fmaxf(tm, x[4 * r + i]);
       }
     }
-    if (t + 4 < tiles) issue_k(t + 4);
+    if (t + WPI < tiles) issue_k(t + WPI);
     tm = fmaxf(tm, __shfl_xor(tm, 16, 64));
     tm = max32(tm);
     const bool up = (tm - m) * c > 8.f;                  // as in the batch's forward
@@ -375,7 +405,7 @@ __global__ __launch_bounds__(256, 3) void seq_step8_kernel(Step8K A, RopeTurns t
   l = add32(l);
   // join of the waves: O[w][head][DP], then m and l
   float* const J = reinterpret_cast<float*>(smem);
-  __syncthreads();
+  item_sync();
   if (l16 < nh) {
     float* const Jw = J + (w * nh + l16) * Cfg::JROW;
 #pragma unroll
@@ -385,18 +415,18 @@ __global__ __launch_bounds__(256, 3) void seq_step8_kernel(Step8K A, RopeTurns t
       Jw[DP + 1] = l;
     }
   }
-  __syncthreads();
-  for (int x = threadIdx.x; x < nh * D; x += 256) {
+  item_sync();
+  for (int x = WPI == 1 ? lane : threadIdx.x; x < nh * D; x += 64 * WPI) {
     const int h = x / D, d = x - h * D;
-    float mm[4], M = -INFINITY;
+    float mm[WPI], M = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < WPI; ++i) {
       mm[i] = J[(i * nh + h) * Cfg::JROW + DP];
       M = fmaxf(M, mm[i]);
     }
     float S = 0.f, O = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < WPI; ++i) {
       const float* P = J + (i * nh + h) * Cfg::JROW;
       const float f = mm[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mm[i] - M) * c);
       S += P[DP + 1] * f;
@@ -437,28 +467,41 @@ size_t seq_step8_workspace(int batch, int heads, int kv_heads, int dim, int cap)
   return ns > 1 ? (size_t)batch * heads * ns * (dim + 2) * sizeof(float) : 0;
 }
 
-template <typename T, int DP>
+template <typename T, int DP, int WPI>
 static hipError_t step8_launch(Step8K A, const RopeTurns& t, int batch, hipStream_t s) {
-  using Cfg = Step8Cfg<T, DP>;
+  using Cfg = Step8Cfg<T, DP, WPI>;
   A.work = Cfg::work(A.group < STEP_HEADS ? A.group : STEP_HEADS);
-  const size_t lds = (size_t)A.work + Cfg::REST;      // at most 64 KB: no limit to raise
-  static_assert(Cfg::work(STEP_HEADS) + Cfg::REST <= 65536, "LDS");
-  A.hg0 = 0;
-  A.hgs = A.append = 1;
-  seq_step8_kernel<T, DP><<<batch * A.c.kv_heads * A.j.ns, 256, lds, s>>>(A, t);
-  LAT_LAUNCH_CHECK();
-  if (A.group > STEP_HEADS) {
-    A.hg0 = 1;
-    A.hgs = cdiv(A.group, STEP_HEADS) - 1;
-    A.append = 0;
-    seq_step8_kernel<T, DP><<<batch * A.c.kv_heads * A.hgs * A.j.ns, 256, lds, s>>>(A, t);
+  const size_t lds = (size_t)(A.work + Cfg::REST) * (4 / WPI);
+  static LdsLimit lim;
+  LAT_HIP_CHECK(lds_limit(seq_step8_kernel<T, DP, WPI>, (Cfg::work(STEP_HEADS) + Cfg::REST) * (4 / WPI), lim));
+  auto launch = [&](int hg0, int hgs, int append) -> hipError_t {
+    A.hg0 = hg0;
+    A.hgs = hgs;
+    A.append = append;
+    A.items = batch * A.c.kv_heads * hgs * A.j.ns;
+    seq_step8_kernel<T, DP, WPI><<<WPI == 1 ? cdiv(A.items, 4) : A.items, 256, lds, s>>>(A, t);
     LAT_LAUNCH_CHECK();
-  }
+    return hipSuccess;
+  };
+  LAT_HIP_CHECK(launch(0, 1, 1));
+  if (A.group > STEP_HEADS) LAT_HIP_CHECK(launch(1, cdiv(A.group, STEP_HEADS) - 1, 0));
   if (A.j.ns > 1) {
     seq_step_join_kernel<T, DP><<<batch * A.heads, 256, 0, s>>>(A.j);
     LAT_LAUNCH_CHECK();
   }
   return hipSuccess;
+}
+
+// Short windows of many users: a wave an item (a user's key head) instead of four, whose
+// start and join would be most of a block's time.  The more items, the longer the windows
+// it pays for.  bf16, 2 key heads of 64, 16384 items of 30 / 128 / 500 slots 102 / 118 / 226 us
+// with four waves, 50 / 76 / 201 with one; 1024 items 10.1 / 11.5 / 18.2 and 9.8 / 12.5 / 24.9.
+// fp32 heads above 64 leave one block a unit so: 180 us of 16384 items of 30 slots, 184.
+template <typename T, int DP>
+static hipError_t step8_pick(const Step8K& A, const RopeTurns& t, int batch, hipStream_t s) {
+  if constexpr (sizeof(T) == 2 || DP < 128)
+    if (A.cap <= 512 && A.cap <= (int64_t)batch * A.c.kv_heads / 16) return step8_launch<T, DP, 1>(A, t, batch, s);
+  return step8_launch<T, DP, 4>(A, t, batch, s);
 }
 
 hipError_t seq_step8(const SeqStepArgs& a, const SeqCache8Args& c, const RopeTurns& t, void* ws, hipStream_t s) {
@@ -483,10 +526,10 @@ hipError_t seq_step8(const SeqStepArgs& a, const SeqCache8Args& c, const RopeTur
   A.j = {a.lens, c.index, c.num_caches, a.heads, c.dim, step8_splits(a.batch, c.kv_heads, A.cap), a.scale, A.part, a.out};
   const int D = c.dim;
   if (c.dt == DT_BF16)
-    return D <= 32 ? step8_launch<bf16_t, 32>(A, t, a.batch, s) : D <= 64 ? step8_launch<bf16_t, 64>(A, t, a.batch, s)
-                                                                         : step8_launch<bf16_t, 128>(A, t, a.batch, s);
-  return D <= 32 ? step8_launch<float, 32>(A, t, a.batch, s) : D <= 64 ? step8_launch<float, 64>(A, t, a.batch, s)
-                                                                      : step8_launch<float, 128>(A, t, a.batch, s);
+    return D <= 32 ? step8_pick<bf16_t, 32>(A, t, a.batch, s) : D <= 64 ? step8_pick<bf16_t, 64>(A, t, a.batch, s)
+                                                                         : step8_pick<bf16_t, 128>(A, t, a.batch, s);
+  return D <= 32 ? step8_pick<float, 32>(A, t, a.batch, s) : D <= 64 ? step8_pick<float, 64>(A, t, a.batch, s)
+                                                                      : step8_pick<float, 128>(A, t, a.batch, s);
 }
 
 // ---------------------------------------------------------------------------

@@ -268,6 +268,57 @@ def test_step_against_the_definition(dt, H, J, D, W, N, rope):
             within(out[b, h], want, (r + 2 * np.expm1(es)) * mass + u * np.abs(want) * (1 + r), f"out {b} {h}")
 
 
+@pytest.mark.parametrize("dt,H,J,D,W,N,S", [("bf16", 4, 2, 64, 30, 3, 300), ("f32", 2, 2, 32, 60, 5, 700),
+                                            ("bf16", 20, 1, 128, 17, 0, 300), ("f32", 3, 1, 40, 1, 1, 40),
+                                            ("bf16", 6, 2, 104, 20, 64, 700), ("f32", 34, 2, 64, 9, 16, 200)])
+@pytest.mark.parametrize("rope", [True, False])
+def test_short_windows_of_many_users(dt, H, J, D, W, N, S, rope):
+    """A wave each: the definition's outputs, and where a window is one tile those that
+    each user gets in a batch of few, bit for bit; the same caches always."""
+    from paper_2512_09200_amd import api
+    rng = np.random.default_rng(S + D)
+    cap = W + N
+    assert cap <= S * J // 16
+    lens = rng.integers(-1, 3 * cap, S)
+    index = rng.permutation(S + 3)[:S]
+    index[7] = S + 3
+    host = used_caches(rng, dt, S + 3, J, cap, D, lens, index)
+    kc, kf = to_gpu(host), to_gpu(host)
+    q, k, v = (randn(rng, S, h, D).to(TT[dt]).to(DEV) for h in (H, J, J))
+    kw = dict(gain_q=(1 + 0.1 * randn(rng, D)).to(DEV), gain_k=(1 + 0.1 * randn(rng, D)).to(DEV)) if rope else dict(rope=False)
+    out = api.lattice_seq_step8(q, k, v, i32(lens), *kc, W, N, cache_index=i32(index), **kw)
+    for a in range(0, S, 4):
+        b = slice(a, min(a + 4, S))
+        ref = api.lattice_seq_step8(q[b], k[b], v[b], i32(lens[b]), *kf, W, N, cache_index=i32(index[b]), **kw)
+        live = [i for i in range(*b.indices(S)) if lens[i] >= 0 and index[i] < S + 3]
+        if not live:
+            continue
+        got, want = out[live], ref[[i - a for i in live]]
+        if cap <= 32:
+            assert torch.equal(got, want)
+    # Longer windows: two evaluations of one row, each as far from the definition as
+    # test_step_against_the_definition allows.  (Events here differ by 10^4 in size, so scores
+    # reach hundreds, and an exponent's fp32 argument is off by 2^-24 of that: no bound
+    # relative to out alone holds.)
+    Q = f64(q)
+    if rope:
+        Q, _ = o.qk_rope(Q, f64(kw["gain_q"]), np.maximum(lens, 0), D, 1e4, 1e-6, False)
+    c = {x: t.cpu().numpy() for x, t in zip(("k", "v", "ks", "vs"), kc)}
+    r, u = 2.0 ** -16 if dt == "bf16" else 2.0 ** -23, o.HALF_STEP[dt]
+    for b in range(0, S, 9):
+        at, n = index[b], int(min(lens[b] + 1, cap))
+        if lens[b] < 0 or at >= S + 3:
+            continue
+        KC, VC = c8.value(c["k"][at], c["ks"][at], D), c8.value(c["v"][at], c["vs"][at], D)
+        for h in range(H):
+            j = h // (H // J)
+            want, mass, size = c8.attend(KC[j], VC[j], Q[b, h], n, D ** -0.5)
+            es = r * size + (2 * D + 48) * o.U32 * size * 1.5 + (n + 16) * o.U32
+            within(out[b, h], want, (r + 2 * np.expm1(es)) * mass + u * np.abs(want) * (1 + r), f"out {b} {h}")
+    for x, y in zip(kc, kf):
+        assert ((x == y) | ((x != x) & (y != y))).all()
+
+
 # (the last: more rounds of slots than a join has places for splits)
 @pytest.mark.parametrize("dt,H,J,D,W,N,S", [("bf16", 16, 2, 128, 70000, 36, 2), ("f32", 2, 1, 64, 20000, 0, 1),
                                             ("bf16", 3, 1, 32, 150001, 7, 1)])
