@@ -4,10 +4,11 @@
 //
 // Memory bound: every visible slot's two rows of codes are read once, half the
 // bytes of bf16.  Work is split as in the bf16 step: a block is a user, a key head
-// and a split of the slots (short windows of many users: a wave is), its four waves take tiles of 32 slots in turn with
-// their own running maximum, sum and output.  Codes become bf16 in registers
-// (exactly: three bits of fraction) and go to 16x16x32 matrix instructions; a
-// block's scale multiplies the 16 scores of its slots and their probabilities.
+// and a split of the slots, its four waves (one, for short windows of many users) take
+// tiles of 32 slots in turn with their own running maximum, sum and output.  Codes
+// become bf16 in registers (exactly: three bits of fraction) and go to 16x16x32
+// matrix instructions; a block's scale multiplies the 16 scores of its slots and their
+// probabilities.
 // What the step computes itself (query, probabilities) enters as two bf16 parts,
 // three where the storage type is fp32, so that out is rounded once.
 //
@@ -15,7 +16,7 @@
 // through the wave's own LDS rows and come back transposed, eight codes of one
 // dimension a lane: a direct load to LDS would have the compiler wait for the
 // next tile's loads before the first transposed read.  The query's parts lie in LDS
-// as fragments, one read of each a tile, so that sixteen waves fit a compute unit.
+// as fragments, one read of each a tile, so that twelve waves fit a compute unit.
 //
 // The new event may change its block's scale, and with it the codes of the block's
 // other slots.  The split that holds the slot makes the block anew before its
@@ -43,7 +44,6 @@ struct Step8K {
   SeqCache8Args c;
   int heads, group, cap, ld, nb;             // bytes of a slot, blocks of a cache and head
   int work;                                  // bytes of LDS for tiles and join
-  int items;                                 // users x key heads x groups of heads (one wave each)
   int hg0, hgs, append;                      // this launch's groups of 16 query heads; whether it brings the events
   float eps, inv_dim;
   int rope, rotary, inter;
@@ -108,7 +108,7 @@ template <typename T, int DP, int WPI> struct Step8Cfg {
 };
 
 template <typename T, int DP, int WPI>
-__global__ __launch_bounds__(256, 3) void seq_step8_kernel(Step8K A, RopeTurns turns) {
+__global__ __launch_bounds__(64 * WPI, 3) void seq_step8_kernel(Step8K A, RopeTurns turns) {
 #pragma clang fp contract(off)                       // the same roundings whichever kernel a batch gets
   using Cfg = Step8Cfg<T, DP, WPI>;
   using TL = Tile8<DP>;
@@ -116,22 +116,10 @@ __global__ __launch_bounds__(256, 3) void seq_step8_kernel(Step8K A, RopeTurns t
   constexpr int NP = Cfg::PARTS, KS = DP / 32, OB = DP / 16, KV = DP == 128 ? 2 : 1, UPR = TL::UPR;
   constexpr int R = STEP8_TILE / CACHE8_BLOCK, VL = R * UPR / 4;     // scale blocks of a tile, value loads of a lane
   typedef typename std::conditional<DP == 32, u32x2, u32x4>::type KVec;
-  extern __shared__ __attribute__((aligned(1024))) char smem_all[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int w = WPI == 1 ? 0 : wave;                 // of the item's waves
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g16 = lane >> 4, l16 = lane & 15, D = A.c.dim, ns = A.j.ns;
-  int blk = WPI == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
-  if (WPI == 1 && blk >= A.items) return;
-  char* const smem = smem_all + (WPI == 1 ? wave * (A.work + Cfg::REST) : 0);
-  // what the item's waves have written to LDS is there for them
-  auto item_sync = [&]() {
-    if constexpr (WPI == 1) {
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      __builtin_amdgcn_wave_barrier();
-    } else {
-      __syncthreads();
-    }
-  };
+  int blk = blockIdx.x;
   const int u = blk % ns; blk /= ns;
   const int hg = A.hg0 + blk % A.hgs; blk /= A.hgs;
   const int kv = blk % A.c.kv_heads, b = blk / A.c.kv_heads;
@@ -300,7 +288,7 @@ __global__ __launch_bounds__(256, 3) void seq_step8_kernel(Step8K A, RopeTurns t
       put(y0, zy);
     }
   }
-  item_sync();
+  __syncthreads();
 
   const float c = A.j.scale * STEP_LOG2E;
   f32x4 o[OB];
@@ -405,7 +393,7 @@ __global__ __launch_bounds__(256, 3) void seq_step8_kernel(Step8K A, RopeTurns t
   l = add32(l);
   // join of the waves: O[w][head][DP], then m and l
   float* const J = reinterpret_cast<float*>(smem);
-  item_sync();
+  __syncthreads();
   if (l16 < nh) {
     float* const Jw = J + (w * nh + l16) * Cfg::JROW;
 #pragma unroll
@@ -415,8 +403,8 @@ __global__ __launch_bounds__(256, 3) void seq_step8_kernel(Step8K A, RopeTurns t
       Jw[DP + 1] = l;
     }
   }
-  item_sync();
-  for (int x = WPI == 1 ? lane : threadIdx.x; x < nh * D; x += 64 * WPI) {
+  __syncthreads();
+  for (int x = threadIdx.x; x < nh * D; x += 64 * WPI) {
     const int h = x / D, d = x - h * D;
     float mm[WPI], M = -INFINITY;
 #pragma unroll
@@ -471,15 +459,13 @@ template <typename T, int DP, int WPI>
 static hipError_t step8_launch(Step8K A, const RopeTurns& t, int batch, hipStream_t s) {
   using Cfg = Step8Cfg<T, DP, WPI>;
   A.work = Cfg::work(A.group < STEP_HEADS ? A.group : STEP_HEADS);
-  const size_t lds = (size_t)(A.work + Cfg::REST) * (4 / WPI);
-  static LdsLimit lim;
-  LAT_HIP_CHECK(lds_limit(seq_step8_kernel<T, DP, WPI>, (Cfg::work(STEP_HEADS) + Cfg::REST) * (4 / WPI), lim));
+  const size_t lds = (size_t)A.work + Cfg::REST;      // at most 64 KB: no limit to raise
+  static_assert(Cfg::work(STEP_HEADS) + Cfg::REST <= 65536, "LDS");
   auto launch = [&](int hg0, int hgs, int append) -> hipError_t {
     A.hg0 = hg0;
     A.hgs = hgs;
     A.append = append;
-    A.items = batch * A.c.kv_heads * hgs * A.j.ns;
-    seq_step8_kernel<T, DP, WPI><<<WPI == 1 ? cdiv(A.items, 4) : A.items, 256, lds, s>>>(A, t);
+    seq_step8_kernel<T, DP, WPI><<<batch * A.c.kv_heads * hgs * A.j.ns, 64 * WPI, lds, s>>>(A, t);
     LAT_LAUNCH_CHECK();
     return hipSuccess;
   };
@@ -495,12 +481,11 @@ static hipError_t step8_launch(Step8K A, const RopeTurns& t, int batch, hipStrea
 // Short windows of many users: a wave an item (a user's key head) instead of four, whose
 // start and join would be most of a block's time.  The more items, the longer the windows
 // it pays for.  bf16, 2 key heads of 64, 16384 items of 30 / 128 / 500 slots 102 / 118 / 226 us
-// with four waves, 50 / 76 / 201 with one; 1024 items 10.1 / 11.5 / 18.2 and 9.8 / 12.5 / 24.9.
-// fp32 heads above 64 leave one block a unit so: 180 us of 16384 items of 30 slots, 184.
+// with four waves, 53 / 78 / 198 with one; 1024 items 10.1 / 11.5 / 18.2 and 9.9 / 12.6 / 25.3.
+// fp32, heads of 128, 16384 items of 30 / 500 slots: 180 / 461 and 127 / 451.
 template <typename T, int DP>
 static hipError_t step8_pick(const Step8K& A, const RopeTurns& t, int batch, hipStream_t s) {
-  if constexpr (sizeof(T) == 2 || DP < 128)
-    if (A.cap <= 512 && A.cap <= (int64_t)batch * A.c.kv_heads / 16) return step8_launch<T, DP, 1>(A, t, batch, s);
+  if (A.cap <= 512 && A.cap <= (int64_t)batch * A.c.kv_heads / 16) return step8_launch<T, DP, 1>(A, t, batch, s);
   return step8_launch<T, DP, 4>(A, t, batch, s);
 }
 

@@ -270,7 +270,8 @@ def test_step_against_the_definition(dt, H, J, D, W, N, rope):
 
 @pytest.mark.parametrize("dt,H,J,D,W,N,S", [("bf16", 4, 2, 64, 30, 3, 300), ("f32", 2, 2, 32, 60, 5, 700),
                                             ("bf16", 20, 1, 128, 17, 0, 300), ("f32", 3, 1, 40, 1, 1, 40),
-                                            ("bf16", 6, 2, 104, 20, 64, 700), ("f32", 34, 2, 64, 9, 16, 200)])
+                                            ("bf16", 6, 2, 104, 20, 64, 700), ("f32", 34, 2, 64, 9, 16, 200),
+                                            ("f32", 8, 2, 128, 28, 4, 300), ("f32", 5, 1, 120, 40, 0, 700)])
 @pytest.mark.parametrize("rope", [True, False])
 def test_short_windows_of_many_users(dt, H, J, D, W, N, S, rope):
     """A wave each: the definition's outputs, and where a window is one tile those that
