@@ -592,8 +592,9 @@ lattice_status lattice_seq_step(const lattice_seq_attn_desc* desc, const lattice
  * and key head.  A scale is the smallest power of two s >= 2^-117 with |x| <= 448 s
  * for every finite x of its block's reached slots (1 where all are 0): an event
  * that changes it has the block's codes rounded anew, exactly but for codes
- * that become subnormal.  A value that is not finite is kept as NaN (0x7f).  Half the memory and
- * the memory time of bf16; codes are off by 2^-4 of themselves at most.
+ * that become subnormal.  A value that is not finite is kept as NaN (0x7f).  Half
+ * the memory and the memory time of bf16; a code is off by 2^-4 of its value at
+ * most, a subnormal one by 2^-10 scales.
  * Slots that no position has reached have no value: their codes and, where a
  * block has none that is reached, its scales are never used. */
 #define LATTICE_SEQ_CACHE8_BLOCK 16
@@ -658,8 +659,9 @@ lattice_status lattice_dropout(const lattice_dropout_desc* desc, lattice_dtype d
  * layer adds to and what the backward needs), arithmetic in fp32.  The norm
  * leaves as y in the storage type, as e4m3 codes with a scale for each row (the
  * format of lattice_fp8_quantize, row-wise, from the fp32 norm: the operand of
- * lattice_linear_fp8_fwd), or both.  A row whose sum of squares or whose norm is not finite
- * gets NaN as its scale and in its codes. */
+ * lattice_linear_fp8_fwd; no scale is below 2^-126), or both.  A row whose sum of
+ * squares or whose norm is not finite gets NaN as its scale and in its codes; its y
+ * is what the formula gives in fp32 (0 where h is finite and its squares' sum is not). */
 #define LATTICE_NORM_MAX_COLS 16384
 typedef struct {
   lattice_dtype dtype;

@@ -99,7 +99,7 @@ def dgain_bound(h, eps, dy):
 
 def scale_of(y):
     top = np.abs(y).max(-1)
-    return np.where(top > 0, top / E4M3_MAX, 1.0)
+    return np.where(top > 0, np.maximum(top / E4M3_MAX, 2.0 ** -126), 1.0)
 
 
 def code_bound(y, scale):

@@ -167,10 +167,11 @@ __global__ __launch_bounds__(C::THREADS) void add_rmsnorm_fwd_kernel(NormK A) {
     }
     if (!A.q) continue;
     row_join<C>(top, Max(), red_top, turn_top);
-    // a row that is not finite says so: NaN scale and codes
+    // a row that is not finite says so: NaN scale and codes.  A scale is a normal number, as
+    // the reciprocal of a smaller one is infinite
     const float amax = __uint_as_float(top[0]);
     const bool bad = !(s[0] < INFINITY) || !(amax < INFINITY);
-    const float sc = bad ? NAN : amax > 0.f ? amax / E4M3_MAX : 1.f, inv = 1.f / sc;
+    const float sc = bad ? NAN : amax > 0.f ? fmaxf(amax / E4M3_MAX, 0x1p-126f) : 1.f, inv = 1.f / sc;
     if (!live) continue;
     if (at.lane == 0) A.scales[row] = sc;
     uint8_t* const q = A.q + row * A.ldq;

@@ -239,6 +239,24 @@ def test_rows_of_zeros():
     assert torch.isnan(y).all() and torch.isnan(s).all()
 
 
+def test_rows_of_the_smallest_and_the_largest_numbers():
+    from paper_2512_09200_amd import api
+    from oracle import fp8
+    r = np.random.default_rng(11)
+    x = randn(r, "f32", 6, 100)
+    x *= torch.tensor([2.0 ** -149, 2.0 ** -140, 2.0 ** -130, 2.0 ** -122, 2.0 ** -117, 2.0 ** -110], device=DEV)[:, None]
+    _, y, q, s = api.lattice_add_rmsnorm_fwd(x, None, eps=1.0, out="both")      # the square root is 1
+    assert torch.equal(y, x) and (s >= 2.0 ** -126).all()
+    got = fp8.e4m3_value(q.cpu().numpy()[:, :100]).astype(np.float64) * f64(s)[:, None]
+    # half a step of a code, normal or not; the reciprocal, its product and the scale are off by 2^-24 each
+    want, S = f64(x), f64(s)[:, None]
+    step = np.maximum(2.0 ** -4 * np.abs(want), 2.0 ** -10 * S)
+    assert (np.abs(got - want) <= step * (1 + 2.0 ** -20) + 2.0 ** -22 * np.abs(want)).all()
+    big = torch.full((3, 70), 2.0 ** 70, device=DEV)                            # squares past fp32
+    h, y, q, s = api.lattice_add_rmsnorm_fwd(big, None, out="both")
+    assert torch.equal(h, big) and (y == 0).all() and torch.isnan(s).all() and (q[:, :70] == 0x7f).all()
+
+
 def test_norm_beyond_4_gib():
     from paper_2512_09200_amd import api
     r = np.random.default_rng(5)
