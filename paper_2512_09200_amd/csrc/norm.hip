@@ -245,7 +245,9 @@ __global__ __launch_bounds__(C::THREADS) void add_rmsnorm_bwd_kernel(NormK A) {
     if (C::AHEAD && base + step < A.rows) fetch(base + step);
     row_join<C>(s, Add(), red, turn);
     const float rho = 1.f / sqrtf(s[0] * A.inv_cols + A.eps);
-    const float c = rho * rho * s[1] * A.inv_cols;             // mean(dn n) rho
+    // mean(dn n) rho; not from rho^2, which is infinite where a row's root mean square is
+    // below 2^-64 (eps 0)
+    const float c = rho * (rho * s[1] * A.inv_cols);
 #pragma unroll
     for (int i = 0; i < C::CH; ++i) {
       float r[8];

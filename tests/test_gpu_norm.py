@@ -257,6 +257,26 @@ def test_rows_of_the_smallest_and_the_largest_numbers():
     assert torch.equal(h, big) and (y == 0).all() and torch.isnan(s).all() and (q[:, :70] == 0x7f).all()
 
 
+@pytest.mark.parametrize("dt,cols", [("f32", 100), ("bf16", 24), ("bf16", 1500)])
+def test_gradients_of_rows_whose_scale_has_an_infinite_square(dt, cols):
+    """eps 0 and values around 2^-65: 1 / rms is 2^65, its square past fp32."""
+    from paper_2512_09200_amd import api
+    r = np.random.default_rng(13)
+    h = torch.ldexp(randn(r, "f32", 9, cols).clamp(0.25, 4.0), torch.tensor(-65, device=DEV)).to(TT[dt])
+    dy = randn(r, dt, 9, cols)
+    gain = torch.from_numpy(1 + 0.3 * r.standard_normal(cols)).float().to(DEV)
+    d, _, dg = api.lattice_add_rmsnorm_bwd(h, dy, None, gain, eps=0.0)
+    H, Y, G = f64(h), f64(dy), f64(gain)
+    want, wg = o.rmsnorm_bwd(H, G, 0.0, Y)
+    # Besides the ordinary roundings: a square is at least 2^-134 and off by 2^-150, as is the
+    # mean, which is above it, so 1 / rms is off by 2^-16 of itself
+    n = H / np.sqrt((H ** 2).mean(-1, keepdims=True))
+    rho, e = n / H, 2.0 ** -16
+    terms = np.abs(rho * Y * G) + 3 * np.abs(n * rho) * np.abs(Y * G * n).mean(-1, keepdims=True)
+    within(d, want, o.dr_bound(H, G, 0.0, Y, None, dt) + e * (1 + 2 * o.HALF_STEP[dt]) * terms, "d_residual")
+    within(dg, wg, o.dgain_bound(H, 0.0, Y) + e * np.abs(Y * n).sum(0) * 1.001, "dgain")
+
+
 def test_norm_beyond_4_gib():
     from paper_2512_09200_amd import api
     r = np.random.default_rng(5)
