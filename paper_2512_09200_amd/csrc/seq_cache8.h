@@ -10,11 +10,10 @@
 #pragma once
 #include "e4m3.h"
 #include "lanes.h"
+#include "seq_fill8.h"
 #include "seq_tile.h"
 
 namespace lat {
-
-constexpr int CACHE8_BLOCK = 16;
 
 // The smallest power of two s >= 2^-117 with top <= 448 s (448 = 1.75 2^8); 1 for 0.
 __host__ __device__ inline float cache8_scale(float top) {

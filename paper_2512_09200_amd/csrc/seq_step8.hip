@@ -564,16 +564,7 @@ struct SlotRanges {
 // 32, 70 us, by two 144; fp32, 8000 of 20, 2 heads of 128, 84 and 101.
 template <typename T, int DP> struct Fill8Cfg { static constexpr int SIDES = sizeof(T) == 2 && DP == 128 ? 1 : 2; };
 
-// Which waves take a sequence's items: per_seq of a group of waves that goes through
-// the sequences, or, where it has `large` rows or more, those waves behind the groups
-// (from wave `behind` on) whose row it holds: `per_tile` waves for each row that is a
-// multiple of `tile`.  The batch's mean length sets per_seq and tile, so one long
-// history among thousands of short ones is not a few waves' work: one of 32000 events
-// among 3000 of 20, bf16, 2 heads of 64 and 4100 slots: 17 us, 194 by the groups alone.
-// Where lengths are even the waves behind find nothing (8000 of 20: 37 us, 33 without);
-// with a bound of the lengths that says so they are not launched.
-struct Fill8Plan { int per_seq, groups, behind, tile, per_tile, large; };
-
+// A sequence's items are shared out by seq_fill8.h's plan.
 template <typename T, int DP>
 __global__ __launch_bounds__(256) void seq_fill8_kernel(SeqCache8Args C, int rows, const int32_t* __restrict__ off, int S,
                                                         const int32_t* __restrict__ first, SeqTensor k, SeqTensor v,
@@ -582,36 +573,18 @@ __global__ __launch_bounds__(256) void seq_fill8_kernel(SeqCache8Args C, int row
   constexpr int SIDES = Fill8Cfg<T, DP>::SIDES;
   const int cap = C.sinks + C.window;
   const int wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-  int64_t s = wave / P.per_seq, ds = P.groups;       // sequences s, s + ds, ..
-  int64_t it0 = wave % P.per_seq, dit = P.per_seq;   // items it0, it0 + dit, ..
-  const bool behind = wave >= P.behind;
-  if (!behind && s >= P.groups) return;              // no whole group
-  if (behind) {
-    const int64_t row = (int64_t)((wave - P.behind) / P.per_tile) * P.tile;
-    if (row >= rows) return;
-    int lo = 0, hi = S - 1;                          // the last sequence that starts at or before the row
-    while (lo < hi) {
-      const int m = lo + (hi - lo + 1) / 2;
-      if (__builtin_amdgcn_readfirstlane(off[m]) <= row) lo = m; else hi = m - 1;
-    }
-    const int a = __builtin_amdgcn_readfirstlane(off[lo]), e = min(__builtin_amdgcn_readfirstlane(off[lo + 1]), rows);
-    if (a < 0 || row < a || row >= e) return;
-    const int64_t t0 = ((int64_t)a + P.tile - 1) / P.tile;               // the sequence's first such row
-    it0 = (row / P.tile - t0) * P.per_tile + (wave - P.behind) % P.per_tile;
-    dit = ((e - 1) / P.tile - t0 + 1) * P.per_tile;
-    s = lo;
-    ds = S;
-  }
-  for (; s < S; s += ds) {
+  Fill8Share w;
+  if (!fill8_share(P, wave, rows, S, [&](int i) { return __builtin_amdgcn_readfirstlane(off[i]); }, &w)) return;
+  for (int64_t s = w.s; s < S; s += w.ds) {
     const int ci = __builtin_amdgcn_readfirstlane(C.index ? C.index[s] : (int)s);
     const int a = max(__builtin_amdgcn_readfirstlane(off[s]), 0), e = min(__builtin_amdgcn_readfirstlane(off[s + 1]), rows);
     const int f = first ? __builtin_amdgcn_readfirstlane(first[s]) : 0;
-    if (ci < 0 || ci >= C.num_caches || e <= a || f < 0 || (e - a >= P.large) != behind) continue;
+    if (ci < 0 || ci >= C.num_caches || e <= a || f < 0 || (e - a >= P.large) != w.behind) continue;
     const uint32_t total = (uint32_t)f + (uint32_t)(e - a);
     const SlotRanges R((uint32_t)f, total, C.sinks, C.window);
     const int sides = 2 / SIDES;                 // items of a block and head
     const int64_t items = (int64_t)R.count * C.kv_heads * sides;
-    for (int64_t it = it0; it < items; it += dit) {
+    for (int64_t it = w.it0; it < items; it += w.dit) {
       const int side = (int)(it % sides), h = (int)(it / sides % C.kv_heads);
       const int blk = R.block((int)(it / sides / C.kv_heads));
       const int64_t head = (int64_t)ci * C.kv_heads + h;
@@ -652,32 +625,11 @@ __global__ __launch_bounds__(256) void seq_fill8_kernel(SeqCache8Args C, int row
 hipError_t seq_cache8_fill(const SeqCache8Args& c, int64_t rows, const int32_t* offsets, int num_seqs, int64_t max_len,
                            const int32_t* first, SeqTensor k, SeqTensor v, hipStream_t s) {
   if (rows == 0 || num_seqs == 0) return hipSuccess;
-  const int D = c.dim, sides = c.kv_heads * (c.dt == DT_BF16 && D > 64 ? 2 : 1);
-  const int64_t mean = cdiv(rows, num_seqs), cap = (int64_t)c.sinks + c.window, most = (int64_t)1 << 22;
-  Fill8Plan P;
-  // a wave an item where the sequences have the mean length
-  const int64_t per_seq = ((mean < cap ? mean : cap) / CACHE8_BLOCK + 1) * sides;
-  P.per_seq = (int)(per_seq < 4096 ? per_seq : 4096);
-  int64_t n = (int64_t)P.per_seq * num_seqs;
-  if (n > most) n = most;
-  P.groups = (int)(n / P.per_seq);
-  P.behind = (int)((n + 3) & ~(int64_t)3);
-  P.tile = (int)(mean < 16 ? 64 : mean < rows / 4 ? 4 * mean : rows);
-  P.large = 2 * (int64_t)P.tile < rows ? 2 * P.tile : 0x7fffffff;
-  P.per_tile = sides;
-  int64_t all = P.behind;
-  if (P.large <= (max_len ? max_len : rows)) {
-    // (at most as many again: longer tiles where that is not enough)
-    const int64_t tiles = (most - 4) / P.per_tile > 1 ? (most - 4) / P.per_tile : 1;
-    if (cdiv(rows, P.tile) > tiles) P.tile = cdiv(rows, tiles);
-    P.large = 2 * P.tile;
-    all += (int64_t)cdiv(rows, P.tile) * P.per_tile;
-  } else {
-    P.large = 0x7fffffff;
-  }
+  const int D = c.dim, cap = c.sinks + c.window;
+  const Fill8Plan P = fill8_plan(rows, num_seqs, max_len, cap, c.kv_heads * (c.dt == DT_BF16 && D > 64 ? 2 : 1));
   const int ld = cache8_ld(c.dim), nb = cdiv(cap, CACHE8_BLOCK);
   auto launch = [&](auto kern) {
-    kern<<<cdiv(all, 4), 256, 0, s>>>(c, (int)rows, offsets, num_seqs, first, k, v, ld, nb, P);
+    kern<<<cdiv(P.waves, 4), 256, 0, s>>>(c, (int)rows, offsets, num_seqs, first, k, v, ld, nb, P);
   };
   if (c.dt == DT_BF16) {
     if (D <= 32) launch(seq_fill8_kernel<bf16_t, 32>);

@@ -130,6 +130,33 @@ def test_long_histories_among_many_short_ones(dt, J, D, W, N, max_len):
     same(kc, host, "second fill")
 
 
+@pytest.mark.parametrize("dt,J,D,W,N", [("bf16", 2, 64, 700, 3), ("bf16", 1, 128, 1200, 0), ("f32", 3, 24, 660, 20)])
+def test_long_histories_among_middling_ones(dt, J, D, W, N):
+    """The longest are 8 and more times as many blocks as a history of the mean length,
+    which one just misses; another order of the sequences in the call that goes on."""
+    from paper_2512_09200_amd import api
+    rng = np.random.default_rng(W)
+    lens = np.tile([40, 0, 61, 17, 70], 24)
+    lens[[3, 50, 77, 100]] = 1300, 640, 639, 657
+    S, cap = len(lens), W + N
+    off = np.concatenate([[0], np.cumsum(lens)])
+    rows = int(off[-1])
+    assert -(-rows // S) // 16 + 1 == 5 and cap >= 8 * 5 * 16
+    host = new_caches(S, J, cap, D)
+    kc = to_gpu(host)
+    k, v = (rows_of(rng, dt, rows, J, D, 1) for _ in "kv")
+    index = rng.permutation(S)
+    api.lattice_seq_cache8_fill(plan(off, rows), k, v, *kc, W, N, cache_index=i32(index))
+    c8.fill(host, f64(k), f64(v), off, W, N, index, np.zeros(S, int))
+    same(kc, host, "fill")
+    order = np.concatenate([np.arange(78, S), np.arange(78)])
+    off = np.concatenate([[0], np.cumsum(lens[order])])
+    api.lattice_seq_cache8_fill(plan(off, rows), v, k, *kc, W, N, cache_index=i32(index[order]),
+                                first=i32(lens[order]))
+    c8.fill(host, f64(v), f64(k), off, W, N, index[order], lens[order])
+    same(kc, host, "second fill")
+
+
 def test_fill_of_positions_next_to_the_end_of_int32():
     from paper_2512_09200_amd import api
     rng = np.random.default_rng(0)
