@@ -8,9 +8,9 @@
 // the backward needs no statistic of the forward.
 //
 // Bound by memory: every tensor is read or written once.  131072 rows of 1024, bf16,
-// residual and dropout: forward 193 us, backward 237 (5.6 and 5.7 TB/s of what they
+// residual and dropout: forward 193 us, backward 243 (5.6 and 5.5 TB/s of what they
 // cannot do without; a copy of 0.5 GB reaches 5.3); 8192 rows to codes 14 us (4.3);
-// dropout alone 79 us (6.8).  A row's elements stay in registers between the sums
+// dropout alone 83 us (6.5).  A row's elements stay in registers between the sums
 // and the results.  Narrow rows share a wave (2 to 32 lanes each), a row of up to
 // 1024 columns has a wave, longer ones a block.  Lanes hold groups of eight
 // neighbouring columns (the generator's and the codes' unit); waves walk the rows in
@@ -359,10 +359,17 @@ static int norm_blocks(int64_t rows, int most) {
   return (int)(n < cap ? n : cap);
 }
 // Data of more bytes than the 256 MB that memory's own cache holds goes past the
-// caches: it would find nothing there.  131072 rows of 1024, bf16: backward with
-// dropout 255 -> 235 us, dropout alone 91 -> 79; the forward was the same (193, 195) and
-// does without.  Below, what the operator before has just written is still there: 8192
-// rows of 1024, forward 13.5 us, past the caches 15.4.
+// caches, where that was found to pay: bf16, and for the backward, which also writes so,
+// whole 128-byte lines at once (a part of a line costs a read of the rest).  us past the
+// caches / through them:
+//   backward with dropout, 131072 rows of 1024, bf16 243 / 257, 16 bytes off a line 273 / 273,
+//   of 1001 289 / 271, 400000 of 520 472 / 428, 4M of 16 106 / 122; fp32, whose lanes' two
+//   words of 16 bytes are 32 apart, 131072 of 1024 534 / 499, 16384 of 8192 505 / 528
+//   dropout alone, 131072 rows of 1024, bf16 83 / 96, of 1001 85 / 95, in its input's place
+//   82 / 79 and 95 / 81; fp32 203 / 192
+//   forward the same either way (193, 195)
+// Below 256 MB, what the operator before has just written is still there: 8192 rows of 1024,
+// forward 13.5 us, past the caches 15.4.
 constexpr double CACHED_BYTES = 256 << 20;
 constexpr int NORM_FWD_WAVES = 4096, NORM_BWD_WAVES = 2048;
 
@@ -410,6 +417,18 @@ size_t add_rmsnorm_bwd_workspace(int64_t rows, int cols) {
   return (size_t)norm_bwd_blocks(rows, cols) * cols * sizeof(float);
 }
 
+// Whether what a wave reads or writes at once is whole 128-byte lines (bf16): rows of
+// whole lines, or rows that follow each other.
+template <typename C>
+static bool whole_lines(const NormArgs& a) {
+  for (const RowTensor& t : {a.h, a.dy, a.dh, a.dr, a.dx}) {
+    if (!t.p) continue;
+    if ((uintptr_t)t.p % 128) return false;
+    if (!(a.cols % 64 == 0 && t.ld % 64 == 0) && !(t.ld == a.cols && C::RPW * a.cols % 64 == 0)) return false;
+  }
+  return true;
+}
+
 hipError_t add_rmsnorm_bwd(const NormArgs& a, void* ws, hipStream_t s) {
   NormK A = norm_k(a);
   A.part = a.dgain ? (float*)ws : nullptr;
@@ -419,12 +438,16 @@ hipError_t add_rmsnorm_bwd(const NormArgs& a, void* ws, hipStream_t s) {
     with_cfg<true>(a.cols, [&](auto cfg) {
       using C = decltype(cfg);
       auto launch = [&](auto kern) { kern<<<n, C::THREADS, 0, s>>>(A); };
-      const bool tail = a.cols % 8 != 0, nt = (double)a.rows * a.cols * (a.dt == DT_BF16 ? 2 : 4) * tensors > CACHED_BYTES;
-#define NORM_PICK(T) \
-  (tail ? nt ? launch(add_rmsnorm_bwd_kernel<T, true, true, C>) : launch(add_rmsnorm_bwd_kernel<T, true, false, C>) \
-        : nt ? launch(add_rmsnorm_bwd_kernel<T, false, true, C>) : launch(add_rmsnorm_bwd_kernel<T, false, false, C>))
-      if (a.dt == DT_BF16) NORM_PICK(bf16_t); else NORM_PICK(float);
-#undef NORM_PICK
+      const bool tail = a.cols % 8 != 0;
+      const bool nt = (double)a.rows * a.cols * 2 * tensors > CACHED_BYTES && whole_lines<C>(a);
+      if (a.dt == DT_BF16) {
+        if (tail) launch(add_rmsnorm_bwd_kernel<bf16_t, true, false, C>);
+        else if (nt) launch(add_rmsnorm_bwd_kernel<bf16_t, false, true, C>);
+        else launch(add_rmsnorm_bwd_kernel<bf16_t, false, false, C>);
+      } else {
+        if (tail) launch(add_rmsnorm_bwd_kernel<float, true, false, C>);
+        else launch(add_rmsnorm_bwd_kernel<float, false, false, C>);
+      }
       return 0;
     });
     LAT_LAUNCH_CHECK();
@@ -439,7 +462,7 @@ hipError_t add_rmsnorm_bwd(const NormArgs& a, void* ws, hipStream_t s) {
 // ---------------------------------------------------------------------------
 // Dropout alone.  A block takes DROP_GROUPS neighbouring groups of eight columns
 // of the whole matrix, each thread every 256th.  One read and one write of memory:
-// 131072 x 1024, bf16, 79 to 91 us (6.8 to 5.9 TB/s), the generator's ten rounds and the
+// 131072 x 1024, bf16, 83 to 93 us (6.5 to 5.8 TB/s), the generator's ten rounds and the
 // selection issuing in 73% of the cycles.
 constexpr int DROP_PER = 4, DROP_GROUPS = 256 * DROP_PER;
 
@@ -478,12 +501,13 @@ hipError_t dropout(DType dt, int64_t rows, int cols, const DropArgs& d, RowTenso
   const FastDiv div(groups);
   const int n = cdiv(total, DROP_GROUPS);
   auto launch = [&](auto kern) { kern<<<n, 256, 0, s>>>(total, cols, groups, div, d, x, out); };
-  const bool tail = cols % 8 != 0, nt = (double)rows * cols * (dt == DT_BF16 ? 2 : 4) * 2 > CACHED_BYTES;
-#define DROP_PICK(T) \
-  (tail ? nt ? launch(dropout_kernel<T, true, true>) : launch(dropout_kernel<T, true, false>) \
-        : nt ? launch(dropout_kernel<T, false, true>) : launch(dropout_kernel<T, false, false>))
-  if (dt == DT_BF16) DROP_PICK(bf16_t); else DROP_PICK(float);
-#undef DROP_PICK
+  const bool tail = cols % 8 != 0, nt = (double)rows * cols * 2 * 2 > CACHED_BYTES && x.p != out.p;
+  if (dt == DT_BF16) {
+    if (tail) nt ? launch(dropout_kernel<bf16_t, true, true>) : launch(dropout_kernel<bf16_t, true, false>);
+    else nt ? launch(dropout_kernel<bf16_t, false, true>) : launch(dropout_kernel<bf16_t, false, false>);
+  } else {
+    tail ? launch(dropout_kernel<float, true, false>) : launch(dropout_kernel<float, false, false>);
+  }
   LAT_LAUNCH_CHECK();
   return hipSuccess;
 }

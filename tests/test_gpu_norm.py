@@ -294,6 +294,66 @@ def test_norm_beyond_4_gib():
     assert torch.equal(api.lattice_dropout(wide, 0.5, rng_state(), out=wide), api.lattice_dropout(dr, 0.5, rng_state()))
 
 
+@pytest.mark.parametrize("dt,cols", [("bf16", c) for c in (16, 64, 200, 256, 512, 1001, 1024, 2048, 4096, 8192, 16384)]
+                         + [("f32", 1024), ("f32", 1001)])
+def test_backward_of_data_beyond_the_caches(dt, cols):
+    """More than 256 MB in five tensors.  Every row's gradient is that of a call of fewer
+    rows, bit for bit; some rows' and the gain's are the definition's."""
+    from paper_2512_09200_amd import api
+    rows = (1 << 28) // (5 * cols * (2 if dt == "bf16" else 4)) + 1 + 30
+    rows += -rows % 2 + 1
+    h, dy, dh = (torch.randn(rows, cols, device=DEV).to(TT[dt]) for _ in range(3))
+    gain, drop = 1 + 0.3 * torch.randn(cols, device=DEV), (0.2, rng_state(), SITE)
+    dr, dx, dg = api.lattice_add_rmsnorm_bwd(h, dy, dh, gain, dropout=drop)
+    for a in range(0, rows, -(-rows // 4)):
+        b = slice(a, a + -(-rows // 4))
+        assert torch.equal(dr[b], api.lattice_add_rmsnorm_bwd(h[b], dy[b], dh[b], gain)[0]), a
+    pick = [0, 1, rows // 3, rows - 2, rows - 1]
+    H, Y, R, G, u = f64(h[pick]), f64(dy[pick]), f64(dh[pick]), f64(gain), o.HALF_STEP[dt]
+    want, _ = o.rmsnorm_bwd(H, G, 1e-6, Y, R)
+    f, b = o.factor(np.array(pick), cols, 0.2, SEED, STEP, SITE), o.dr_bound(H, G, 1e-6, Y, R, dt)
+    within(dr[pick], want, b, "d_residual")
+    within(dx[pick], want * f, (b + 2 * (o.U32 + u * (dt == "bf16")) * np.abs(want)) * f, "dx")
+    n = h.double() / (h.double().square().mean(-1, keepdim=True) + 1e-6).sqrt()
+    terms = dy.double() * n
+    within(dg, f64(terms.sum(0)), (o.RHO + (3 + rows) * o.U32) * f64(terms.abs().sum(0)), "dgain")
+    d = dh.clone()                                           # in an input's place
+    dr2, dx2, dg2 = api.lattice_add_rmsnorm_bwd(h, dy, d, gain, dropout=drop, d_residual=d)
+    assert dr2 is d and torch.equal(dr2, dr) and torch.equal(dx2, dx) and torch.equal(dg2, dg)
+
+
+def test_backward_of_strided_rows_beyond_the_caches():
+    """Rows that are not whole lines of memory: other kernels, the same bits."""
+    from paper_2512_09200_amd import api
+    rows, cols = 60000, 512
+    h, dy, dh = (torch.randn(rows, cols, device=DEV).bfloat16() for _ in range(3))
+    gain = torch.rand(cols, device=DEV)
+    want = api.lattice_add_rmsnorm_bwd(h, dy, dh, gain)
+    for ld, at in ((520, 0), (576, 0), (576, 3)):
+        x, y, z, out = (torch.zeros(rows, ld, dtype=torch.bfloat16, device=DEV)[:, at:at + cols] for _ in range(4))
+        for a, b in ((x, h), (y, dy), (z, dh)):
+            a.copy_(b)
+        got = api.lattice_add_rmsnorm_bwd(x, y, z, gain, d_residual=out)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2]), (ld, at)
+        base = out._base
+        assert not base[:, :at].any() and not base[:, at + cols:].any()
+
+
+@pytest.mark.parametrize("dt,cols", [("bf16", 1024), ("bf16", 1001), ("bf16", 24), ("f32", 1024), ("f32", 1001)])
+def test_dropout_of_data_beyond_the_caches(dt, cols):
+    from paper_2512_09200_amd import api
+    rows = (1 << 28) // (2 * cols * (2 if dt == "bf16" else 4)) + 33
+    x = torch.randn(rows, cols, device=DEV).to(TT[dt])
+    out = api.lattice_dropout(x, 0.3, rng_state(), site=SITE)
+    pick = [0, 1, rows // 3, rows - 2, rows - 1]
+    f, X = o.factor(np.array(pick), cols, 0.3, SEED, STEP, SITE), f64(x[pick])
+    within(out[pick], X * f, np.abs(X * f) * (2 * o.U32 + o.HALF_STEP[dt]) * 1.001, "out")
+    # the first rows are those of a smaller call, and in its input's place nothing changes
+    assert torch.equal(out[:rows // 3], api.lattice_dropout(x[:rows // 3], 0.3, rng_state(), site=SITE))
+    api.lattice_dropout(x, 0.3, rng_state(), site=SITE, out=x)
+    assert torch.equal(out, x)
+
+
 # ---------------------------------------------------------------------------
 def test_a_captured_step_draws_anew_and_repeats_the_eager_bits():
     """Two graphs that share a pool, replayed in turn with eager work between."""
