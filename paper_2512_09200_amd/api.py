@@ -993,6 +993,8 @@ def lattice_add_rmsnorm_fwd(x, residual=None, gain=None, eps=1e-6, dropout=None,
         return _on(stream, x, lattice_add_rmsnorm_fwd, x, residual, gain, eps, dropout, out, h, y)
     if out not in ("y", "fp8", "both"):
         raise ValueError(f"out: expected 'y', 'fp8' or 'both', got {out!r}")
+    if y is not None and out == "fp8":
+        raise ValueError("y: out='fp8' writes none")
     shape, dev = _rows2(x, "x"), _gpu(x)
     rows, cols = shape
     desc, like = _norm_desc(x, cols, gain, eps, dropout, dev), (shape, x.dtype, dev)

@@ -189,3 +189,9 @@ int main() {
     subprocess.run(["g++", "-O1", "-o", str(tmp_path / "div"), str(src)], check=True)
     r = subprocess.run([str(tmp_path / "div")], capture_output=True, text=True)
     assert r.returncode == 0, r.stdout
+
+
+def test_a_buffer_that_nothing_would_be_written_to():
+    x = torch.zeros(2, 16)
+    with pytest.raises(ValueError, match="out='fp8' writes none"):
+        api.lattice_add_rmsnorm_fwd(x, out="fp8", y=torch.zeros(2, 16))
