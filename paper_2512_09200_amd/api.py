@@ -927,8 +927,10 @@ def _drop_desc(dropout, dev):
     p, rng, site = dropout
     if rng is not None and rng.dtype not in (torch.int64, torch.uint64):
         raise ValueError("rng: expected two elements of int64 or uint64")
-    return A.lattice_dropout_desc(float(p), _vec(rng, rng.dtype, 2, "rng", dev) if rng is not None else None,
-                                  int(site) & 0xffffffff)
+    site = int(site)
+    if not 0 <= site < 1 << 32:
+        raise ValueError(f"site: expected 0 .. 2^32 - 1, got {site}")
+    return A.lattice_dropout_desc(float(p), _vec(rng, rng.dtype, 2, "rng", dev) if rng is not None else None, site)
 
 
 def _row_ptr(t, like, name):
@@ -961,8 +963,8 @@ def _rows2(t, name):
 def lattice_dropout(x, p, rng, site=0, out=None, stream=None):
     """Dropout of x [rows, cols] with probability p (a multiple of 2^-16 is
     taken); rng: int64 [2] on the GPU, the seed and the step's number, read when
-    the kernel runs; site: which dropout of the model.  The gradient of x is the
-    same call on the gradient of the result.  out may be x."""
+    the kernel runs; site: which dropout of the model, 0 .. 2^32 - 1.  The gradient of
+    x is the same call on the gradient of the result.  out may be x."""
     if stream is not None:
         return _on(stream, x, lattice_dropout, x, p, rng, site, out)
     shape, dev = _rows2(x, "x"), _gpu(x)

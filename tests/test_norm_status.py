@@ -195,3 +195,10 @@ def test_a_buffer_that_nothing_would_be_written_to():
     x = torch.zeros(2, 16)
     with pytest.raises(ValueError, match="out='fp8' writes none"):
         api.lattice_add_rmsnorm_fwd(x, out="fp8", y=torch.zeros(2, 16))
+
+
+@pytest.mark.parametrize("site", [-1, 1 << 32, -(1 << 32)])
+def test_sites_that_would_be_another_one(site):
+    with pytest.raises(ValueError, match="site"):
+        api._drop_desc((0.5, None, site), 0)
+    assert api._drop_desc((0.5, None, (1 << 32) - 1), 0).site == (1 << 32) - 1
