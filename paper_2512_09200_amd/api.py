@@ -573,7 +573,7 @@ def _memory(xs):
             yield from (x.offsets, x.span)
         elif isinstance(x, SeqAttnSaved):
             yield from _memory((x.lse, x.out_lo))
-        elif isinstance(x, tuple):
+        elif isinstance(x, (tuple, list)):
             yield from _memory(x)
         elif isinstance(x, torch.Tensor):
             yield x

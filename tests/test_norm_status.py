@@ -202,3 +202,11 @@ def test_sites_that_would_be_another_one(site):
     with pytest.raises(ValueError, match="site"):
         api._drop_desc((0.5, None, site), 0)
     assert api._drop_desc((0.5, None, (1 << 32) - 1), 0).site == (1 << 32) - 1
+
+
+def test_the_memory_of_a_call_on_another_stream():
+    """What a call on another stream keeps until that stream has passed it: the
+    generator's state too, in a tuple or a list."""
+    rng, x = torch.zeros(2, dtype=torch.int64), torch.zeros(2, 16)
+    for drop in ((0.5, rng, 1), [0.5, rng, 1]):
+        assert [t.data_ptr() for t in api._memory((x, None, drop, 0.1))] == [x.data_ptr(), rng.data_ptr()]
