@@ -615,9 +615,12 @@ lattice_status lattice_seq_cache8_fill(const lattice_seq_attn_desc* desc, const 
                                        const int32_t* first, const int32_t* cache_index,
                                        const lattice_seq_cache8* cache, void* stream);
 
-/* lattice_seq_step over 8-bit caches: the event's k is rounded to desc's dtype
- * (as lattice_qk_rope_fwd gives it), then k and v to codes, and out_b is the
- * attention over the codes, the event's own included.  A non-finite k or v
+/* lattice_seq_step over 8-bit caches: the event's normalised and rotated k is
+ * rounded to desc's dtype, then k and v to codes, and out_b is the attention
+ * over the codes, the event's own included.  k is computed in fp32 for bf16 and
+ * in 64 bits for fp32, not with lattice_qk_rope_fwd's instructions: where it lies
+ * next to a border, the code (or, of a block's largest key, the scale) can be the
+ * neighbour of what the fill gives for lattice_qk_rope_fwd's k.  A non-finite k or v
  * reaches what sees it as NaN.  Two users of a call must not share a cache.
  * Other arguments and errors as for lattice_seq_step. */
 size_t lattice_seq_step8_workspace(const lattice_seq_attn_desc* desc, int32_t batch);

@@ -397,6 +397,49 @@ def test_events_one_by_one(dt, H, J, D, W, N):
             same(kc, host, f"step {t}")
 
 
+@pytest.mark.parametrize("dt,interleaved", [("bf16", False), ("bf16", True), ("f32", False), ("f32", True)])
+def test_rotated_events_stepped_and_filled(dt, interleaved):
+    """lattice_qk_rope_fwd and the fill against the step's own norm and rotation: a key's
+    code is that of the definition's key rounded to the type, either way, but for keys that
+    lie nearer to a border than the fp32 operator's roundings reach; values are the same."""
+    from paper_2512_09200_amd import api
+    rng = np.random.default_rng(21)
+    B, H, J, D, W, N, n = 3, 4, 2, 64, 20, 3, 70
+    q, k, v = (randn(rng, B * n, h, D).to(TT[dt]).to(DEV) for h in (H, J, J))
+    gain = (1 + 0.1 * randn(rng, D)).to(DEV)
+    kw = dict(gain_k=gain, rotary=48, interleaved=interleaved)
+    s = plan(np.arange(B + 1) * n, B * n)
+    filled, stepped = (to_gpu(new_caches(B, J, W + N, D)) for _ in "fs")
+    _, kr = api.lattice_qk_rope_fwd(s, q, k, **kw)
+    api.lattice_seq_cache8_fill(s, kr, v, *filled, W, N)
+    rows = [x.view(B, n, -1, D) for x in (q, k, v)]
+    for t in range(n):
+        api.lattice_seq_step8(*(x[:, t] for x in rows), i32([t] * B), *stepped, W, N, **kw)
+    pos = np.tile(np.arange(n), B)
+    K, _ = o.qk_rope(f64(k), f64(gain), pos, 48, 1e4, 1e-6, interleaved)
+    at = [t for t in range(n) if t < N or t >= n - W]
+    slots = [o.slot_of(t, W, N) for t in at]
+    u = o.HALF_STEP[dt]
+
+    def typed(x):
+        return torch.from_numpy(x.astype(np.float32)).to(TT[dt]).double().numpy()
+
+    for side, x, e in (("k", K, (D + 40) * o.U32 * 1.5 * np.abs(K).max(-1, keepdims=True)), ("v", f64(v), 0.0)):
+        S = c8.block_scale(np.abs(x).max())                  # no block had a larger one
+        x, e = (np.broadcast_to(y, x.shape).reshape(B, n, J, D)[:, at].transpose(0, 2, 1, 3) for y in (x, e))
+        # the code's value does not depend on the scale while it is normal
+        lo, hi = (fp8.e4m3_value(fp8.e4m3_code(typed(y) / S)) * S for y in (x - e, x + e))
+        normal = np.abs(x) - e >= 2.0 ** -6 * S
+        assert normal.mean() > 0.9 and (lo == hi)[normal].mean() > 0.99
+        for c in (filled, stepped):
+            codes, scales = (c[0], c[2]) if side == "k" else (c[1], c[3])
+            got = np.stack([c8.value(a, b, D) for a, b in zip(codes.cpu().numpy(), scales.cpu().numpy())])[:, :, slots]
+            assert ((lo <= got) & (got <= hi))[normal].all(), side       # both roundings are monotonic
+            # a subnormal one is off by half a step of each scale it was written under,
+            # which double: twice the largest's at most
+            assert (np.abs(got - x) <= (2.0 ** -4 + 2 * u) * np.abs(x) + 3 * 2.0 ** -10 * S + 2 * e).all(), side
+
+
 def test_8_bit_caches_answer_nearly_as_bf16_ones():
     """The same histories served from both: the outputs differ by what the
     codes lose (at most 2^-4 of each key and value)."""
