@@ -66,9 +66,10 @@ def rmsnorm_bwd(h, gain, eps, dy, dh=None):
     return dr, (dy * n).sum(0)
 
 
-# Relative error of rho: a lane adds up at most 32 squares, a row's lanes and
-# waves are joined in at most 6 + 7 sums; half of that, and the mean's two
-# products, eps, the root and the division.
+# Relative error of rho: a lane adds up at most 16 squares or 32, its wave's lanes are joined in
+# 6 sums, and a row's waves one after another, at most 16 where lanes have 16 squares and 8
+# where they have 32: 16 + 6 + 15 or 32 + 6 + 7 = 45 sums and the squares' own
+# rounding; half of that, and the mean's two products, eps, the root and the division.
 RHO = (32 + 13 + 2) / 2 * U32 + 5 * U32
 
 

@@ -103,6 +103,7 @@ __device__ inline const T* row_of(const RowTensor& t, int64_t row) { return (con
 template <typename T, bool TAIL, typename C>
 __global__ __launch_bounds__(C::THREADS) void add_rmsnorm_fwd_kernel(NormK A) {
 #pragma clang fp contract(off)
+  static_assert(C::AHEAD, "the forward's configurations");
   __shared__ float red[2 * C::WPR];
   __shared__ uint32_t red_top[2 * C::WPR];
   int turn = 0, turn_top = 0;
@@ -121,9 +122,8 @@ __global__ __launch_bounds__(C::THREADS) void add_rmsnorm_fwd_kernel(NormK A) {
 #pragma unroll
       for (int i = 0; i < C::CH; ++i) rr[i] = load8<T, TAIL>(row_of<T>(A.r, row), at.lane + i * C::STEP, A.cols);
   };
-  if (C::AHEAD && at.first < A.rows) fetch(at.first);
+  if (at.first < A.rows) fetch(at.first);
   for (int64_t base = at.first; base < A.rows; base += step) {
-    if (!C::AHEAD) fetch(base);
     const int64_t row = base + at.sub;
     const bool live = row < A.rows;
     float h[C::CH][8], s[1] = {0.f};
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(C::THREADS) void add_rmsnorm_fwd_kernel(NormK A) {
       if (A.h.p && live) store8<T, TAIL>((T*)A.h.p + row * A.h.ld, at.lane + i * C::STEP, A.cols, o);
       o.get(h[i]);
     }
-    if (C::AHEAD && base + step < A.rows) fetch(base + step);
+    if (base + step < A.rows) fetch(base + step);
 #pragma unroll
     for (int i = 0; i < C::CH; ++i)
 #pragma unroll
