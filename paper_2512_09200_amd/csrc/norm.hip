@@ -8,9 +8,9 @@
 // the backward needs no statistic of the forward.
 //
 // Bound by memory: every tensor is read or written once.  131072 rows of 1024, bf16,
-// residual and dropout: forward 193 us, backward 243 (5.6 and 5.5 TB/s of what they
-// cannot do without; a copy of 0.5 GB reaches 5.3); 8192 rows to codes 14 us (4.3);
-// dropout alone 83 us (6.5).  A row's elements stay in registers between the sums
+// residual and dropout: forward 193 us at best and 200 on average, backward 245 and 251
+// (5.4 and 5.3 TB/s of what they cannot do without; a copy of 0.5 GB reaches 5.3); 8192
+// rows to codes 14 us (4.2); dropout alone 83 and 91 us (5.9).  A row's elements stay in registers between the sums
 // and the results.  Narrow rows share a wave (2 to 32 lanes each), a row of up to
 // 1024 columns has a wave, longer ones a block.  Lanes hold groups of eight
 // neighbouring columns (the generator's and the codes' unit); waves walk the rows in

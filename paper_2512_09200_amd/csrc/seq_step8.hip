@@ -25,9 +25,9 @@
 // slots.  Query heads above 16 on a key head are taken by a second launch, which
 // finds the block as it is now, for the same reason.
 //
-// 1024 users, windows of 1024 slots of 128, 2 key heads of 4 query heads, bf16: 86 us,
-// 5.5 TB/s of the bytes it cannot do without (a copy of 0.5 GB reaches 5.3); 94 without
-// the hint that a code is read once.  Matrix cores 15% busy, 51% of the cycles issue
+// 1024 users, windows of 1024 slots of 128, 2 key heads of 4 query heads, bf16: 88 us at
+// best and 90 on average, 5.2 TB/s of the bytes it cannot do without (a copy of 0.5 GB
+// reaches 5.3); 94 without the hint that a code is read once.  Matrix cores 15% busy, 51% of the cycles issue
 // vector instructions (half of them conversions), LDS 15%.
 #include "kernels.h"
 #include "lanes.h"
@@ -435,8 +435,10 @@ __global__ __launch_bounds__(64 * WPI, 3) void seq_step8_kernel(Step8K A, RopeTu
 
 // Splits of the slots: as many as leave all blocks of the launch on the chip at once
 // (three a compute unit), of 128 slots (a round of a block's waves) or more, and
-// no more than the join holds.  Three users, 131049 slots of 128, 2 key heads: 32 us with
+// no more than the join holds.  Three users, 131049 slots of 128, 2 key heads: 33 us with
 // 768 blocks in all, 38 with 512, 36 with 1024 (whose join takes 8 us instead of 5).
+// With hundreds of users the rounding down leaves places empty: 200 users of 2 key heads,
+// 20000 slots, 392 us in 400 blocks, 402 in 800, 358 in 1200; 1020 slots 28, 33 and 35.
 // One user, 1020 / 4000 / 16000 slots: 12.4 / 13.5 / 15.3 us a step, with splits of 256
 // or more 13.1 / 14.4 / 16.2, of 1024 16.0 / 22.3 / 21.3.  Up to four rounds of slots
 // a block alone is faster than its parts and their join: 500 slots 11.1 and 11.8 us.
@@ -481,7 +483,7 @@ static hipError_t step8_launch(Step8K A, const RopeTurns& t, int batch, hipStrea
 // Short windows of many users: a wave an item (a user's key head) instead of four, whose
 // start and join would be most of a block's time.  The more items, the longer the windows
 // it pays for.  bf16, 2 key heads of 64, 16384 items of 30 / 128 / 500 slots 102 / 118 / 226 us
-// with four waves, 53 / 78 / 198 with one; 1024 items 10.1 / 11.5 / 18.2 and 9.9 / 12.6 / 25.3.
+// with four waves, 50 / 74 / 198 with one (16, 55 and 203 at the copy's rate); 1024 items 10.1 / 11.5 / 18.2 and 9.9 / 12.6 / 25.3.
 // fp32, heads of 128, 16384 items of 30 / 500 slots: 180 / 461 and 127 / 451.
 template <typename T, int DP>
 static hipError_t step8_pick(const Step8K& A, const RopeTurns& t, int batch, hipStream_t s) {
@@ -522,7 +524,8 @@ hipError_t seq_step8(const SeqStepArgs& a, const SeqCache8Args& c, const RopeTur
 // above 64: one of them).  The slots that
 // a sequence's rows go to are at most three ranges (sinks, and the window's, which
 // may wrap); their blocks are numbered through, each once.  Reads and writes the
-// kept rows once: 153600 rows of 2 heads of 128, bf16, 44 us (5.0 TB/s).
+// kept rows once: 153600 rows of 2 heads of 128, bf16, 43 us at best, 46
+// on average (4.8 TB/s).
 struct SlotRanges {
   int lo[3], hi[3];                          // blocks, ascending, no block twice
   int count;
@@ -561,7 +564,7 @@ struct SlotRanges {
 // Keys and values of a block by one wave, both loads out together, or by two.  Two:
 // bf16 heads of 128, whose registers would leave four waves a SIMD instead of five
 // (153600 kept rows, 2 heads: 44 us, by one 46).  One: 100000 histories of 5, a head of
-// 32, 70 us, by two 144; fp32, 8000 of 20, 2 heads of 128, 84 and 101.
+// 32, 67 us, by two 144; fp32, 8000 of 20, 2 heads of 128, 84 and 101.
 template <typename T, int DP> struct Fill8Cfg { static constexpr int SIDES = sizeof(T) == 2 && DP == 128 ? 1 : 2; };
 
 // A sequence's items are shared out by seq_fill8.h's plan.
