@@ -691,8 +691,9 @@ lattice_status lattice_add_rmsnorm_fwd(const lattice_add_rmsnorm_desc* desc, int
  * identity) and dh = what reaches h by the residual stream (or NULL): writes
  * d_residual and dx (storage dtype, each may be NULL; without dropout they are
  * equal) and, where not NULL, dgain [cols] (fp32, overwritten, summed over rows
- * in a fixed order; needs a workspace).  rng must hold what it held in the
- * forward.  d_residual and dx may be h, dy or dh (same stride), not each other.
+ * in a fixed order; needs a workspace).  A row's sums of h^2 and of dy gain h are fp32:
+ * where one leaves its range, the row's gradients are what that gives.  rng must
+ * hold what it held in the forward.  d_residual and dx may be h, dy or dh (same stride), not each other.
  * Errors: as the forward, WORKSPACE. */
 size_t lattice_add_rmsnorm_bwd_workspace(const lattice_add_rmsnorm_desc* desc, int64_t rows);
 lattice_status lattice_add_rmsnorm_bwd(const lattice_add_rmsnorm_desc* desc, int64_t rows,
